@@ -43,10 +43,10 @@ def listed():
         dict(name="linear_single", kind="linear", M=1, N=32000, K=1024, epilogue=LOGITS, bias=False),
         # an odd few dozen users: the MLP's up projection with its activation
         dict(name="linear_dozens", kind="linear", M=37, N=4096, K=1024, epilogue=GELU, bias=True),
-        # sizes that no tile divides
-        dict(name="linear_odd", kind="linear", M=3001, N=4001, K=1000, epilogue=STORE, bias=True),
-        # the down projection of the large benchmark batch, added into the residual stream
-        dict(name="linear_down", kind="linear", M=16384, N=1024, K=4096, epilogue=RESIDUAL, bias=True),
+        # sizes that no tile divides, added into an fp32 residual stream
+        dict(name="linear_odd", kind="linear", M=3001, N=4001, K=1000, epilogue=RESIDUAL, bias=True),
+        # the down projection of the large benchmark batch, left in bf16 for the next norm to add
+        dict(name="linear_down", kind="linear", M=16384, N=1024, K=4096, epilogue=STORE, bias=True),
         # a wide model's projection over a long prefill: the largest product
         dict(name="linear_large", kind="linear", M=8192, N=8192, K=8192, epilogue=STORE, bias=False),
         # one user: one row of logits, all filters on
