@@ -593,6 +593,67 @@ int srm_linear_argmax_noalloc(int32_t dtype, const void *d_A, const void *d_W, c
 size_t srm_linear_argmax_noalloc_max_bytes(void);
 
 /*
+ * Rows in 8 bits ("fp8 matrices"), their products and sampling by request: operators that need no model, for the projections and
+ * the end of a decode step.
+ *
+ * An fp8 matrix of `rows` x K holds e4m3 values (OCP: 448 largest, no infinities) with one E8M0 scale (a byte s: 2^(s - 127)) for
+ * every block of 128 consecutive elements of a row:
+ *   q       [rows][Kp], Kp = srm_fp8_row_bytes(K) = K rounded up to 128; zeros behind K; at a multiple of 16 bytes
+ *   scales  [ceil(K / 512)][rows][4], srm_fp8_scale_bytes(rows, K) bytes: scales[b / 4][r][b % 4] belongs to
+ *           q[r][128 b .. 128 b + 127]; 127 behind the last block; at a multiple of 4 bytes
+ * A block's scale is the smallest power of two, 2^-126 at least, that brings its largest finite magnitude to 448 or less (1 for a
+ * block of zeros); q is the quotient, rounded to the nearest, ties to even.  An infinity or a NaN does not count for the scale and
+ * becomes a NaN.  Buffers of a call must not overlap unless said otherwise.  All calls may be made under stream capture.
+ *
+ * srm_quantize_fp8: d_x [rows][K] of type dtype (SRM_FP32 | SRM_BF16), row stride ldx elements, at any multiple of an element ->
+ * q, scales.  For weights once, and for activations between two products.
+ * Errors: SRM_EINVAL (null pointer, rows or K <= 0, rows >= 2^31, K > 2^22, ldx < K, unknown dtype, misaligned q or scales).
+ *
+ * srm_rmsnorm_fp8: the residual addition and root-mean-square norm in front of a product:
+ *   x <- x + add  (d_add may be NULL: x is only read then)      y = x / sqrt(mean(x^2) + eps) * gain      y -> q, scales
+ * d_x [rows][d] of type dtype, row stride ldx; d_add [rows][d] of type add_dtype, row stride ld_add (ignored if NULL); d_gain [d]
+ * fp32.  The sum is formed in fp32 and rounded to x's type; the norm is that of the row as it is stored, its mean of squares in
+ * fp32, in an order that depends on d alone.
+ * Errors: SRM_EINVAL (null pointer, rows or d <= 0, rows >= 2^31, d > 32768, a row stride < d, eps < 0 or NaN, unknown dtype,
+ * misaligned q or scales).
+ *
+ * srm_linear_fp8: out = epilogue(A W^T + bias) of fp8 matrices A [M][K] and W [N][K], accumulated in fp32.  With a bf16 output the
+ * matrix cores' 8-bit products are taken, which add eight neighbouring products within some 14 bits of the largest (1e-5 of a
+ * result's size, where its rounding is 2e-3); with an fp32 output the operands are widened to bf16, with scales from 2^-117 to 2^119
+ * exactly (a block of smaller or larger ones may flush to 0 or overflow), and nothing is lost but the roundings of fp32 sums, at
+ * half the rate.  d_bias [N] fp32 or NULL.  Epilogues as in srm_linear: 0 = store bf16, 1 = exact GELU then store bf16, 2 = add into fp32 d_out (residual), 4 = store
+ * fp32 (3, the fused argmax, does not exist here: srm_sample_rows with temperature 0 chooses from stored logits).  d_out is
+ * [M][N], dense.  Any M, N and K.
+ * Errors: SRM_EINVAL (null operand, scales or output, sizes <= 0, M >= 2^31, K > 2^22, misaligned operands, output or bias,
+ * unknown epilogue).
+ *
+ * srm_sample_rows: one token for each row of d_logits [rows][vocab] (dtype SRM_FP32 | SRM_BF16, row stride ld elements), with
+ * parameters of its own; each parameter array is device memory of `rows` elements or NULL for "off".  With
+ * w_v = exp((l_v - max l) / temperature), in the order of the logits from the largest down, equal ones by their index, the tokens
+ * that may be drawn are the longest prefix that has
+ *   at most top_k[r] tokens (top_k <= 0: no limit), no token with w < min_p[r] (min_p <= 0 or NaN: no limit; above 1: as 1), and of
+ *   the tokens that these two leave the fewest whose w reach top_p[r] of their sum (top_p >= 1 or NaN: all; <= 0: one).
+ * d_tok_out[r] is the first of them, by index, whose running sum of w over them exceeds uniform[r] times the sum of all of them
+ * (uniform in [0, 1): below 0 or NaN counts as 0, 1 and above draw the last one).  temperature NULL: 1; <= 0 or NaN: greedy (the
+ * lowest index of the largest logit).  A logit that is NaN counts as -infinity and is never drawn; logits of +infinity share the
+ * draw equally; a row that holds nothing else than -infinity gets token -1.  d_logprob[rows] (fp32, may be NULL): the logarithm of
+ * the probability with which the token was drawn, 0 for a greedy row, -infinity with token -1.  Weights are held as whole numbers
+ * of 2^-43 of the largest one, so that sums are exact and a result depends on its row alone; smaller weights are never drawn.
+ * Errors: SRM_EINVAL (null logits, uniform or output, rows or vocab <= 0, rows >= 2^31, vocab > 2^20, ld < vocab, unknown dtype).
+ */
+size_t srm_fp8_row_bytes(int32_t K);
+size_t srm_fp8_scale_bytes(int64_t rows, int32_t K);
+int srm_quantize_fp8(int32_t dtype, const void *d_x, int64_t ldx, int64_t rows, int32_t K, void *d_q, void *d_scales,
+                     void *hip_stream);
+int srm_rmsnorm_fp8(int32_t dtype, void *d_x, int64_t ldx, int32_t add_dtype, const void *d_add, int64_t ld_add,
+                    const float *d_gain, float eps, int64_t rows, int32_t d, void *d_q, void *d_scales, void *hip_stream);
+int srm_linear_fp8(int32_t epilogue, const void *d_a, const void *d_a_scales, const void *d_w, const void *d_w_scales,
+                   const float *d_bias, int64_t M, int32_t N, int32_t K, void *d_out, void *hip_stream);
+int srm_sample_rows(int32_t dtype, const void *d_logits, int64_t ld, int64_t rows, int32_t vocab, const float *d_temperature,
+                    const int32_t *d_top_k, const float *d_top_p, const float *d_min_p, const float *d_uniform,
+                    int32_t *d_tok_out, float *d_logprob, void *hip_stream);
+
+/*
  * Work-groups of the one-kernel path that srm_generate / srm_generate_topp take
  * for a batch of B samples, or 0 if such a call runs the ordinary step kernels.
  * The one-kernel path ("MAX model details": per-call overhead dominates small

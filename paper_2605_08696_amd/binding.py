@@ -127,6 +127,18 @@ def lib():
         L.srm_probe_copy.argtypes = [vp, vp, sz, i32, vp]
         L.srm_probe_mfma.restype = C.c_int
         L.srm_probe_mfma.argtypes = [vp, i32, i32, i32, C.POINTER(C.c_double), vp]
+        L.srm_fp8_row_bytes.restype = sz
+        L.srm_fp8_row_bytes.argtypes = [i32]
+        L.srm_fp8_scale_bytes.restype = sz
+        L.srm_fp8_scale_bytes.argtypes = [i64, i32]
+        L.srm_quantize_fp8.restype = C.c_int
+        L.srm_quantize_fp8.argtypes = [i32, vp, i64, i64, i32, vp, vp, vp]
+        L.srm_rmsnorm_fp8.restype = C.c_int
+        L.srm_rmsnorm_fp8.argtypes = [i32, vp, i64, i32, vp, i64, vp, C.c_float, i64, i32, vp, vp, vp]
+        L.srm_linear_fp8.restype = C.c_int
+        L.srm_linear_fp8.argtypes = [i32, vp, vp, vp, vp, vp, i64, i32, i32, vp, vp]
+        L.srm_sample_rows.restype = C.c_int
+        L.srm_sample_rows.argtypes = [i32, vp, i64, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp]
         L.srm_last_error.restype = C.c_char_p
         L.srm_last_error.argtypes = []
         _lib = L
@@ -510,3 +522,140 @@ def linear(dtype, epilogue, A, W, bias, out=None, argmax=None, scratch=None, str
         p_sc = _dev(scratch, torch.uint8, linear_scratch_bytes(M, N), "scratch")
     code = epilogue if tile is None else (tile + 1) * 100 + epi
     _check(lib().srm_linear(dtype, code, p_a, p_w, p_b, M, N, K, p_o, p_am, p_sc, _stream(stream)))
+
+
+# ---- rows in 8 bits, their products, sampling by request ------------------------------------------------------------
+def _row_dtype(t, name: str) -> int:
+    torch = _torch()
+    if t.dtype is torch.float32:
+        return SRM_FP32
+    if t.dtype is torch.bfloat16:
+        return SRM_BF16
+    raise ValueError(f"{name}: dtype {t.dtype}, expected float32 or bfloat16")
+
+
+def _rows_of(t, name: str):
+    """(rows, columns, row stride) of a matrix whose rows are contiguous."""
+    if t.dim() != 2:
+        raise ValueError(f"{name}: must be a matrix")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: rows must be contiguous")
+    ld = t.stride(0)
+    if rows > 1 and ld < cols:
+        raise ValueError(f"{name}: rows overlap")
+    return rows, cols, max(ld, cols)
+
+
+def _launch(first, others, stream, fn, *args):
+    """fn(*args, stream) on the device of the tensors, which is that of `first`."""
+    device = first.device
+    if device.type != "cuda":
+        raise ValueError("operands must be CUDA tensors")
+    for t in others:
+        if t is not None and t.device != device:
+            raise ValueError(f"operands on {device} and {t.device}")
+    torch = _torch()
+    if stream is None:
+        raw = torch.cuda.current_stream(device).cuda_stream
+    elif stream.device != device:
+        raise ValueError(f"operands on {device}, stream on {stream.device}")
+    else:
+        raw = stream.cuda_stream
+    if device.index == torch.cuda.current_device():
+        rc = fn(*args, raw)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, raw)
+    if rc != 0:
+        raise SrmError(rc, lib().srm_last_error().decode())
+
+
+def _fp8(q, scales, name: str, rows=None, K=None):
+    """(rows, Kp) of an fp8 matrix after the checks of its two tensors."""
+    torch = _torch()
+    if q.dtype is not torch.float8_e4m3fn or scales.dtype is not torch.float8_e8m0fnu:
+        raise ValueError(f"{name}: dtypes {q.dtype}, {scales.dtype}, expected float8_e4m3fn, float8_e8m0fnu")
+    if q.dim() != 2 or not q.is_contiguous() or not scales.is_contiguous():
+        raise ValueError(f"{name}: must be a contiguous matrix with contiguous scales")
+    n, kp = q.shape
+    if rows is not None and (n != rows or kp != (K + 127) // 128 * 128):
+        raise ValueError(f"{name}: shape {tuple(q.shape)}, expected {(rows, (K + 127) // 128 * 128)}")
+    if kp % 128 or scales.numel() != (kp + 511) // 512 * n * 4:
+        raise ValueError(f"{name}: {kp} columns with {scales.numel()} scales")
+    return n, kp
+
+
+def fp8_row_bytes(K: int) -> int:
+    return lib().srm_fp8_row_bytes(K)
+
+
+def fp8_scale_bytes(rows: int, K: int) -> int:
+    return lib().srm_fp8_scale_bytes(rows, K)
+
+
+def fp8_empty(rows: int, K: int, device="cuda"):
+    """Tensors (q, scales) for an fp8 matrix of rows x K."""
+    torch = _torch()
+    q = torch.empty((rows, (K + 127) // 128 * 128), dtype=torch.float8_e4m3fn, device=device)
+    return q, torch.empty(((K + 511) // 512, rows, 4), dtype=torch.float8_e8m0fnu, device=device)
+
+
+def quantize_fp8(x, q, scales, stream=None):
+    """srm_quantize_fp8: rows of x (float32 or bfloat16, any row stride) -> q, scales (fp8_empty)."""
+    rows, K, ld = _rows_of(x, "x")
+    _fp8(q, scales, "q", rows, K)
+    _launch(x, (q, scales), stream, lib().srm_quantize_fp8, _row_dtype(x, "x"), x.data_ptr(), ld, rows, K, q.data_ptr(),
+            scales.data_ptr())
+
+
+def rmsnorm_fp8(x, gain, eps, q, scales, add=None, stream=None):
+    """srm_rmsnorm_fp8: x += add (if given, in place), the root-mean-square norm of its rows times gain -> q, scales."""
+    torch = _torch()
+    rows, d, ld = _rows_of(x, "x")
+    _fp8(q, scales, "q", rows, d)
+    if gain.dtype is not torch.float32 or gain.numel() != d or not gain.is_contiguous():
+        raise ValueError(f"gain: must be {d} contiguous float32 values")
+    kind, p_add, ld_add = 0, None, 0
+    if add is not None:
+        n, c, ld_add = _rows_of(add, "add")
+        if (n, c) != (rows, d):
+            raise ValueError(f"add: shape {(n, c)}, expected {(rows, d)}")
+        kind, p_add = _row_dtype(add, "add"), add.data_ptr()
+    _launch(x, (gain, q, scales, add), stream, lib().srm_rmsnorm_fp8, _row_dtype(x, "x"), x.data_ptr(), ld, kind, p_add, ld_add,
+            gain.data_ptr(), eps, rows, d, q.data_ptr(), scales.data_ptr())
+
+
+def linear_fp8(epilogue, a, a_scales, w, w_scales, bias, out, stream=None):
+    """srm_linear_fp8 on fp8 matrices a [M][K], w [N][K] -> out [M][N]: bfloat16 for epilogues 0 and 1, float32 for 2 and 4."""
+    torch = _torch()
+    M, K = _fp8(a, a_scales, "a")
+    N, K2 = _fp8(w, w_scales, "w")
+    if K != K2:
+        raise ValueError("a and w disagree on K")
+    if bias is not None and (bias.dtype is not torch.float32 or bias.numel() != N or not bias.is_contiguous()):
+        raise ValueError(f"bias: must be {N} contiguous float32 values")
+    want = torch.float32 if epilogue in (2, 4) else torch.bfloat16
+    if out.dtype is not want or tuple(out.shape) != (M, N) or not out.is_contiguous():
+        raise ValueError(f"out: must be a contiguous {want} matrix of {M} x {N}")
+    _launch(a, (a_scales, w, w_scales, bias, out), stream, lib().srm_linear_fp8, epilogue, a.data_ptr(), a_scales.data_ptr(),
+            w.data_ptr(), w_scales.data_ptr(), None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr())
+
+
+def sample_rows(logits, uniform, tok_out, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, stream=None):
+    """srm_sample_rows: logits [rows][vocab] (float32 or bfloat16, any row stride) -> tok_out [rows] int32; each parameter
+    a tensor of one value per row (float32, top_k int32), or None."""
+    torch = _torch()
+    rows, vocab, ld = _rows_of(logits, "logits")
+    ptr = []
+    for name, t, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
+                           ("min_p", min_p, torch.float32), ("uniform", uniform, torch.float32), ("tok_out", tok_out, torch.int32),
+                           ("logprob", logprob, torch.float32)):
+        if t is None:
+            ptr.append(None)
+            continue
+        if t.dtype is not dtype or t.numel() != rows or not t.is_contiguous():
+            raise ValueError(f"{name}: must be {rows} contiguous {dtype} values")
+        ptr.append(t.data_ptr())
+    _launch(logits, (uniform, tok_out, temperature, top_k, top_p, min_p, logprob), stream, lib().srm_sample_rows,
+            _row_dtype(logits, "logits"), logits.data_ptr(), ld, rows, vocab, *ptr)

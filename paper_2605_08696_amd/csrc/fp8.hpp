@@ -1,0 +1,186 @@
+// Rows in 8 bits: e4m3 values (OCP: 448 largest, no infinities) with one E8M0 scale, a power of two, for each block of 128 along
+// a row.  A block's scale is the smallest power of two that brings its largest finite magnitude to 448 or less, so that it lands in
+// (224, 448]; e4m3 is a floating-point type, so a scale between the powers of two would win at most part of a bit for values near the
+// type's subnormals, and the matrix cores multiply by an E8M0 scale at no cost (v_mfma_scale), which a factor in fp32 is not.
+//
+// A wavefront takes 512 elements of a row at a time, four blocks: sixteen lanes (a DPP row) with eight consecutive elements each hold a
+// block, whose largest magnitude is four DPP steps away, and the four scales are one 32-bit word of the scales' array
+// [ceil(d / 512)][rows].  What bounds both kernels is the memory's rate, or for few rows the launch and one trip to memory.
+#pragma once
+#include "common.hpp"
+
+constexpr int kFp8Block = 128, kFp8Group = 512;      // elements of a block, of a word of scales
+
+__device__ __forceinline__ uint32_t row16_max_u32(uint32_t v)
+{
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));   // quad_perm [1,0,3,2]
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));   // quad_perm [2,3,0,1]
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true));  // row_half_mirror
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, true));  // row_mirror
+    return v;
+}
+
+// Eight consecutive elements from any address of whole elements (gfx950 loads 16 bytes from unaligned ones); n of them exist.
+__device__ __forceinline__ void load8(const float *p, int n, float (&v)[8])
+{
+    if (n >= 8) {
+        f32x4_t a, b;
+        __builtin_memcpy(&a, p, 16);
+        __builtin_memcpy(&b, p + 4, 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.0f;
+    }
+}
+__device__ __forceinline__ void load8(const bf16 *p, int n, float (&v)[8])
+{
+    if (n >= 8) {
+        bf16x8_t a;
+        __builtin_memcpy(&a, p, 16);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? (float)p[i] : 0.0f;
+    }
+}
+// v as it is stored at p, rounded to p's type
+__device__ __forceinline__ void store8(float *p, int n, float (&v)[8])
+{
+    if (n >= 8) {
+        const f32x4_t a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
+        __builtin_memcpy(p, &a, 16);
+        __builtin_memcpy(p + 4, &b, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = v[i];
+    }
+}
+__device__ __forceinline__ void store8(bf16 *p, int n, float (&v)[8])
+{
+    bf16x8_t a;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { a[i] = (bf16)v[i]; v[i] = (float)a[i]; }
+    if (n >= 8) {
+        __builtin_memcpy(p, &a, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = a[i];
+    }
+}
+
+// This lane's eight values of the group's block lane / 16 -> their e4m3 codes; the group's four scales in every lane.  Infinities and
+// NaN do not count for the scale and become NaN.  Absent elements are zeros.
+__device__ __forceinline__ uint2 fp8_of_8(const float (&v)[8], uint32_t &scales)
+{
+    constexpr uint32_t kInf = 0x7f800000u;
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t a = __float_as_uint(v[i]) & 0x7fffffffu;
+        top = max(top, a < kInf ? a : 0u);
+    }
+    top = row16_max_u32(top);
+    // top / 448 rounded up to a power of two: 448 = 1.75 2^8.  Biased exponents; 1 (2^-126) at least, 127 for zeros
+    int s = (int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
+    s = top == 0 ? 127 : max(s, 1);
+    const float inv = __uint_as_float((uint32_t)(254 - s) << 23);
+    float q[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        q[i] = (__float_as_uint(v[i]) & 0x7fffffffu) < kInf ? v[i] * inv : __uint_as_float(0x7fc00000u);
+    int lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false), hi = __builtin_amdgcn_cvt_pk_fp8_f32(q[4], q[5], 0, false);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], lo, true);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(q[6], q[7], hi, true);
+    scales = (uint32_t)__builtin_amdgcn_readlane(s, 0) | (uint32_t)__builtin_amdgcn_readlane(s, 16) << 8 |
+             (uint32_t)__builtin_amdgcn_readlane(s, 32) << 16 | (uint32_t)__builtin_amdgcn_readlane(s, 48) << 24;
+    return make_uint2((uint32_t)lo, (uint32_t)hi);
+}
+
+// x [rows][d], row stride ldx -> q [rows][dp], dp = d rounded up to 128, and scales [groups][rows].  One wavefront per row and group.
+template <typename T>
+__global__ void __launch_bounds__(256)
+quantize_fp8_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int d, unsigned char *__restrict__ q, uint32_t *__restrict__ scales)
+{
+    const int groups = (d + kFp8Group - 1) / kFp8Group, dp = (d + kFp8Block - 1) / kFp8Block * kFp8Block;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t row = unit / groups;
+    const int g = (int)(unit - row * groups), lane = threadIdx.x & 63;
+    if (row >= rows) return;
+    const int col = g * kFp8Group + lane * 8;
+    float v[8];
+    load8(x + row * ldx + col, d - col, v);
+    uint32_t s;
+    const uint2 codes = fp8_of_8(v, s);
+    if (col < dp) *reinterpret_cast<uint2 *>(q + row * dp + col) = codes;
+    if (lane == 0) scales[(int64_t)g * rows + row] = s;
+}
+
+// x += add (if there is one), then y = x / sqrt(mean(x^2) + eps) * gain of the row as it is stored -> q, scales.  NW wavefronts hold a
+// row in registers, wavefront w its groups w, w + NW, ..., G of them at most.
+template <typename T, typename TAdd, int NW, int G>
+__global__ void __launch_bounds__(NW > 4 ? NW * 64 : 256)
+rmsnorm_fp8_kernel(T *__restrict__ x, int64_t ldx, const TAdd *__restrict__ add, int64_t ld_add, const float *__restrict__ gain, float eps,
+                   int64_t rows, int d, unsigned char *__restrict__ q, uint32_t *__restrict__ scales)
+{
+    constexpr int ROWS = NW > 4 ? 1 : 4 / NW;        // rows of a work-group
+    __shared__ float part[ROWS * NW];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, w = wave % NW;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + wave / NW;
+    const int groups = (d + kFp8Group - 1) / kFp8Group, dp = (d + kFp8Block - 1) / kFp8Block * kFp8Block;
+    const bool in = row < rows;
+    float v[G][8], sum = 0.0f;
+    if (in) {
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            const int col = (w + i * NW) * kFp8Group + lane * 8;
+            load8(x + row * ldx + col, d - col, v[i]);
+        }
+        if (add) {
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                const int col = (w + i * NW) * kFp8Group + lane * 8;
+                float t[8];
+                load8(add + row * ld_add + col, d - col, t);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[i][k] += t[k];
+            }
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                const int col = (w + i * NW) * kFp8Group + lane * 8;
+                store8(x + row * ldx + col, d - col, v[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum = fmaf(v[i][k], v[i][k], sum);
+    }
+    sum = wave_sum(sum);
+    if constexpr (NW > 1) {
+        if (lane == 0) part[wave] = sum;
+        __syncthreads();
+        sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NW; ++k) sum += part[wave / NW * NW + k];
+    }
+    if (!in) return;
+    const float r = 1.0f / sqrtf(sum / (float)d + eps);
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+        const int g = w + i * NW, col = g * kFp8Group + lane * 8;
+        if (g >= groups) break;                      // wave-uniform
+        float t[8];
+        load8(gain + col, d - col, t);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[i][k] = col + k < d ? v[i][k] * r * t[k] : 0.0f;          // (r may be a NaN)
+        uint32_t s;
+        const uint2 codes = fp8_of_8(v[i], s);
+        if (col < dp) *reinterpret_cast<uint2 *>(q + row * dp + col) = codes;
+        if (lane == 0) scales[(int64_t)g * rows + row] = s;
+    }
+}

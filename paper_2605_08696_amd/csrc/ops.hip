@@ -1,0 +1,207 @@
+// The operators of libsrm that need no model: rows in 8 bits with scales, their products, and sampling by request.
+// (A translation unit of its own, so that the code object of the generation kernels stays as it is.)
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "srm.h"
+#include "fp8.hpp"
+#include "gemm_fp8.hpp"
+#include "sample_rows.hpp"
+#include "status.hpp"
+
+static hipStream_t as_stream(void *s) { return static_cast<hipStream_t>(s); }
+static bool misaligned(const void *p, unsigned to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
+
+// ------------------------------------------------------------------ 8-bit rows
+extern "C" size_t srm_fp8_row_bytes(int32_t K) { return K > 0 ? align_up((size_t)K, kFp8Block) : 0; }
+extern "C" size_t srm_fp8_scale_bytes(int64_t rows, int32_t K)
+{
+    return rows > 0 && K > 0 ? (size_t)cdiv(K, kFp8Group) * (size_t)rows * 4 : 0;
+}
+
+static int check_fp8(const char *who, const void *d_q, const void *d_scales)
+{
+    if (!d_q || !d_scales) return fail(SRM_EINVAL, "%s: null argument", who);
+    if (misaligned(d_q, 16) || misaligned(d_scales, 4))
+        return fail(SRM_EINVAL, "%s: 8-bit rows must lie at multiples of 16 bytes, their scales at multiples of 4", who);
+    return SRM_OK;
+}
+constexpr int64_t kMaxRows = 1ll << 31;
+constexpr int32_t kMaxWidth = 1 << 22;                // (256 rows of a tile are addressed by 32 bits)
+
+template <typename T>
+static int quantize(const void *d_x, int64_t ldx, int64_t rows, int32_t K, void *d_q, void *d_scales, hipStream_t st)
+{
+    const int64_t blocks = cdiv(rows * cdiv(K, kFp8Group), 4);
+    if (blocks >= (1ll << 31)) return fail(SRM_EINVAL, "srm_quantize_fp8: sizes out of range");
+    hipLaunchKernelGGL(quantize_fp8_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, st, static_cast<const T *>(d_x), ldx, rows, K,
+                       static_cast<unsigned char *>(d_q), static_cast<uint32_t *>(d_scales));
+    HIP_TRY(hipGetLastError());
+    return SRM_OK;
+}
+
+extern "C" int srm_quantize_fp8(int32_t dtype, const void *d_x, int64_t ldx, int64_t rows, int32_t K, void *d_q, void *d_scales,
+                                void *hip_stream)
+{
+    const char *who = "srm_quantize_fp8";
+    if (!d_x) return fail(SRM_EINVAL, "%s: null argument", who);
+    SRM_TRY(check_fp8(who, d_q, d_scales));
+    if (rows <= 0 || rows >= kMaxRows || K <= 0 || K > kMaxWidth) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    if (ldx < K) return fail(SRM_EINVAL, "%s: row stride %lld is less than %d", who, (long long)ldx, K);
+    if (dtype == SRM_FP32) return quantize<float>(d_x, ldx, rows, K, d_q, d_scales, as_stream(hip_stream));
+    if (dtype == SRM_BF16) return quantize<bf16>(d_x, ldx, rows, K, d_q, d_scales, as_stream(hip_stream));
+    return fail(SRM_EINVAL, "%s: unknown dtype %d", who, dtype);
+}
+
+template <typename T, typename TAdd, int NW, int G>
+static int launch_rmsnorm(void *d_x, int64_t ldx, const void *d_add, int64_t ld_add, const float *d_gain, float eps, int64_t rows, int32_t d,
+                          void *d_q, void *d_scales, hipStream_t st)
+{
+    constexpr int ROWS = NW > 4 ? 1 : 4 / NW;
+    hipLaunchKernelGGL((rmsnorm_fp8_kernel<T, TAdd, NW, G>), dim3((unsigned)cdiv(rows, ROWS)), dim3(NW > 4 ? NW * 64 : 256), 0, st,
+                       static_cast<T *>(d_x), ldx, static_cast<const TAdd *>(d_add), ld_add, d_gain, eps, rows, d,
+                       static_cast<unsigned char *>(d_q), static_cast<uint32_t *>(d_scales));
+    HIP_TRY(hipGetLastError());
+    return SRM_OK;
+}
+constexpr int32_t kMaxNorm = 32768;
+// (by the width alone: a row's sum is formed in the same order whatever the number of rows)
+template <typename T, typename TAdd>
+static int rmsnorm(void *d_x, int64_t ldx, const void *d_add, int64_t ld_add, const float *d_gain, float eps, int64_t rows, int32_t d,
+                   void *d_q, void *d_scales, hipStream_t st)
+{
+    const int groups = (int)cdiv(d, kFp8Group);
+#define RMS_CASE(NW, G) return launch_rmsnorm<T, TAdd, NW, G>(d_x, ldx, d_add, ld_add, d_gain, eps, rows, d, d_q, d_scales, st)
+    if (groups <= 1) RMS_CASE(1, 1);
+    if (groups <= 2) RMS_CASE(1, 2);
+    if (groups <= 4) RMS_CASE(2, 2);
+    if (groups <= 8) RMS_CASE(4, 2);
+    if (groups <= 16) RMS_CASE(8, 2);
+    if (groups <= 32) RMS_CASE(16, 2);
+    RMS_CASE(16, 4);
+#undef RMS_CASE
+}
+
+extern "C" int srm_rmsnorm_fp8(int32_t dtype, void *d_x, int64_t ldx, int32_t add_dtype, const void *d_add, int64_t ld_add,
+                               const float *d_gain, float eps, int64_t rows, int32_t d, void *d_q, void *d_scales, void *hip_stream)
+{
+    const char *who = "srm_rmsnorm_fp8";
+    if (!d_x || !d_gain) return fail(SRM_EINVAL, "%s: null argument", who);
+    SRM_TRY(check_fp8(who, d_q, d_scales));
+    if (rows <= 0 || rows >= kMaxRows || d <= 0 || d > kMaxNorm) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    if (ldx < d || (d_add && ld_add < d)) return fail(SRM_EINVAL, "%s: a row stride is less than %d", who, d);
+    if (!(eps >= 0.0f)) return fail(SRM_EINVAL, "%s: eps must not be negative", who);
+    if (!d_add) add_dtype = dtype;
+    if ((dtype != SRM_FP32 && dtype != SRM_BF16) || (add_dtype != SRM_FP32 && add_dtype != SRM_BF16))
+        return fail(SRM_EINVAL, "%s: unknown dtype %d, %d", who, dtype, add_dtype);
+    hipStream_t st = as_stream(hip_stream);
+    if (dtype == SRM_FP32)
+        return add_dtype == SRM_FP32 ? rmsnorm<float, float>(d_x, ldx, d_add, ld_add, d_gain, eps, rows, d, d_q, d_scales, st)
+                                     : rmsnorm<float, bf16>(d_x, ldx, d_add, ld_add, d_gain, eps, rows, d, d_q, d_scales, st);
+    return add_dtype == SRM_FP32 ? rmsnorm<bf16, float>(d_x, ldx, d_add, ld_add, d_gain, eps, rows, d, d_q, d_scales, st)
+                                 : rmsnorm<bf16, bf16>(d_x, ldx, d_add, ld_add, d_gain, eps, rows, d, d_q, d_scales, st);
+}
+
+// ------------------------------------------------------------------ their products
+struct Fp8Call {
+    const unsigned char *a;
+    const uint32_t *sa;
+    const unsigned char *w;
+    const uint32_t *sw;
+    int64_t M;
+    int N, Kp;
+    Fp8Epi ep;
+    hipStream_t st;
+};
+static int device_cus()
+{
+    static thread_local int dev_of = -1, cus_of = 0;
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess) return 0;
+    if (dev != dev_of) {
+        int cus = 0;
+        if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return 0;
+        dev_of = dev;
+        cus_of = cus;
+    }
+    return cus_of;
+}
+
+template <auto KERN>
+static int launch_fp8(int64_t blocks, int threads, int lds, const Fp8Call &c)
+{
+    if (blocks >= (1 << 30)) return fail(SRM_EINVAL, "srm_linear_fp8: sizes out of range");
+    static bool attr_set = false;
+    if (!attr_set) {
+        HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(KERN), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+        attr_set = true;
+    }
+    hipLaunchKernelGGL(KERN, dim3((unsigned)blocks), dim3(threads), lds, c.st, c.a, c.sa, c.w, c.sw, c.M, c.N, c.Kp, c.ep);
+    HIP_TRY(hipGetLastError());
+    return SRM_OK;
+}
+template <int BM, int BN, int WM, int WN, int NS, int EPI>
+static int launch_fp8_tile(const Fp8Call &c)
+{
+    return launch_fp8<gemm_fp8_tile_kernel<BM, BN, WM, WN, NS, EPI>>(cdiv(c.M, BM) * cdiv(c.N, BN), WM * WN * 64, NS * fp8_stage_bytes<BM, BN>(), c);
+}
+template <int RT, int CT, int NS, int EPI>
+static int launch_fp8_slices(const Fp8Call &c)
+{
+    return launch_fp8<gemm_fp8_slices_kernel<RT, CT, NS, EPI>>(cdiv(c.M, 16 * RT) * cdiv(c.N, 16 * CT), kFp8SliceWaves * 64,
+                                                              kFp8SliceWaves * fp8_slice_lds<RT, CT, NS>(), c);
+}
+template <int EPI>
+static int linear_fp8(const Fp8Call &c)
+{
+    const int cus = device_cus();
+    if (cus <= 0) return fail(SRM_EHIP, "cannot read the number of compute units");
+    auto fits = [&](int rt, int ct) { return cdiv(c.M, 16 * rt) * cdiv(c.N, 16 * ct) <= 2 * cus; };
+    if (fits(1, 1)) return launch_fp8_slices<1, 1, 2, EPI>(c);
+    if (fits(2, 2)) return launch_fp8_slices<2, 2, 1, EPI>(c);
+    return launch_fp8_tile<128, 128, 2, 2, 2, EPI>(c);
+}
+
+extern "C" int srm_linear_fp8(int32_t epilogue, const void *d_a, const void *d_a_scales, const void *d_w, const void *d_w_scales,
+                              const float *d_bias, int64_t M, int32_t N, int32_t K, void *d_out, void *hip_stream)
+{
+    const char *who = "srm_linear_fp8";
+    SRM_TRY(check_fp8(who, d_a, d_a_scales));
+    SRM_TRY(check_fp8(who, d_w, d_w_scales));
+    if (!d_out) return fail(SRM_EINVAL, "%s: null output", who);
+    if (M <= 0 || M >= kMaxRows || N <= 0 || K <= 0 || K > kMaxWidth) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    if (misaligned(d_out, epilogue == 0 || epilogue == 1 ? 2 : 4) || misaligned(d_bias, 4))
+        return fail(SRM_EINVAL, "%s: output or bias does not lie at a whole element", who);
+    const Fp8Call c{static_cast<const unsigned char *>(d_a), static_cast<const uint32_t *>(d_a_scales), static_cast<const unsigned char *>(d_w),
+                    static_cast<const uint32_t *>(d_w_scales), M, N, (int)align_up(K, kFp8Block), Fp8Epi{d_bias, d_out, N},
+                    as_stream(hip_stream)};
+    switch (epilogue) {
+    case 0: return linear_fp8<EPI_STORE>(c);
+    case 1: return linear_fp8<EPI_GELU>(c);
+    case 2: return linear_fp8<EPI_RESID>(c);
+    case 4: return linear_fp8<EPI_F32>(c);
+    default: return fail(SRM_EINVAL, "%s: unknown epilogue %d", who, epilogue);
+    }
+}
+
+// ------------------------------------------------------------------ sampling by request
+extern "C" int srm_sample_rows(int32_t dtype, const void *d_logits, int64_t ld, int64_t rows, int32_t vocab, const float *d_temperature,
+                               const int32_t *d_top_k, const float *d_top_p, const float *d_min_p, const float *d_uniform,
+                               int32_t *d_tok_out, float *d_logprob, void *hip_stream)
+{
+    const char *who = "srm_sample_rows";
+    if (!d_logits || !d_uniform || !d_tok_out) return fail(SRM_EINVAL, "%s: null argument", who);
+    if (rows <= 0 || rows >= kMaxRows || vocab <= 0 || vocab > kSampleVocab) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    if (ld < vocab) return fail(SRM_EINVAL, "%s: row stride %lld is less than %d", who, (long long)ld, vocab);
+    const SampleRows p{ld, vocab, d_temperature, d_top_p, d_min_p, d_uniform, d_top_k, d_tok_out, d_logprob};
+    hipStream_t st = as_stream(hip_stream);
+    if (dtype == SRM_FP32)
+        hipLaunchKernelGGL(sample_rows_kernel<float>, dim3((unsigned)rows), dim3(kSampleThreads), 0, st, static_cast<const float *>(d_logits), p);
+    else if (dtype == SRM_BF16)
+        hipLaunchKernelGGL(sample_rows_kernel<bf16>, dim3((unsigned)rows), dim3(kSampleThreads), 0, st, static_cast<const bf16 *>(d_logits), p);
+    else
+        return fail(SRM_EINVAL, "%s: unknown dtype %d", who, dtype);
+    HIP_TRY(hipGetLastError());
+    return SRM_OK;
+}

@@ -24,12 +24,13 @@
 #include "norm.hpp"
 #include "probe.hpp"
 #include "sample.hpp"
+#include "status.hpp"
 #include "tokmix.hpp"
 
 // ------------------------------------------------------------------ errors
 static thread_local std::string g_err;
 
-static int fail(int code, const char *fmt, ...)
+int fail(int code, const char *fmt, ...)
 {
     char buf[512];
     va_list ap;
@@ -39,23 +40,6 @@ static int fail(int code, const char *fmt, ...)
     g_err = buf;
     return code;
 }
-
-#define HIP_TRY(expr)                                                                       \
-    do {                                                                                    \
-        hipError_t e_ = (expr);                                                             \
-        if (e_ != hipSuccess)                                                               \
-            return fail(SRM_EHIP, "%s failed: %s (%s:%d)", #expr, hipGetErrorString(e_),    \
-                        __FILE__, __LINE__);                                                \
-    } while (0)
-
-#define SRM_TRY(expr)                 \
-    do {                              \
-        int rc_ = (expr);             \
-        if (rc_ != SRM_OK) return rc_; \
-    } while (0)
-
-static inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 // ------------------------------------------------------------------ model
 struct LayerDev {
