@@ -197,9 +197,9 @@ extern "C" int srm_sample_rows(int32_t dtype, const void *d_logits, int64_t ld, 
     const SampleRows p{ld, vocab, d_temperature, d_top_p, d_min_p, d_uniform, d_top_k, d_tok_out, d_logprob};
     hipStream_t st = as_stream(hip_stream);
     if (dtype == SRM_FP32)
-        hipLaunchKernelGGL(sample_rows_kernel<float>, dim3((unsigned)rows), dim3(kSampleThreads), 0, st, static_cast<const float *>(d_logits), p);
+        hipLaunchKernelGGL((sample_rows_kernel<float, 512>), dim3((unsigned)rows), dim3(512), 0, st, static_cast<const float *>(d_logits), p);
     else if (dtype == SRM_BF16)
-        hipLaunchKernelGGL(sample_rows_kernel<bf16>, dim3((unsigned)rows), dim3(kSampleThreads), 0, st, static_cast<const bf16 *>(d_logits), p);
+        hipLaunchKernelGGL((sample_rows_kernel<bf16, 512>), dim3((unsigned)rows), dim3(512), 0, st, static_cast<const bf16 *>(d_logits), p);
     else
         return fail(SRM_EINVAL, "%s: unknown dtype %d", who, dtype);
     HIP_TRY(hipGetLastError());

@@ -9,17 +9,24 @@
 // depend on their order, LDS atomics included.  (V <= 2^20 of them fit 64 bits.)  Tokens whose weight rounds to zero are never drawn and
 // may be left out of every list: they come last in the order.
 //
-// A work-group of 1024 threads takes a row; a thread reads eight consecutive logits, a wavefront 512, a segment.  Passes over the row:
-//   the largest logit;
-//   for top-k a histogram of counts, for top-p one of weights, over 1024 equal steps of logit value; the step in which the limit is
-//   reached is divided again by key until it holds a few members, which are compared with each other (or one value: its first ones);
+// A work-group takes a row; a thread reads eight consecutive logits, a wavefront 512, a segment.  Passes over the row:
+//   the largest logit, and each thread's own largest: the top_k-th largest of those is a lower bound of the row's;
+//   top-k: the logits above that bound are listed; top-p: a histogram of weights over 2048 equal steps of logit value, and a list of the
+//   step in which the limit is reached;
+//   the list (LDS) is divided by key until a few members are left, which are compared with each other, or one value, of which the
+//   first ones by index are kept;
 //   sums of the kept weights by segment, one of which holds the token.
-// Later passes evaluate only vectors that hold a logit at or above the smallest that may still be drawn.
+// A list that is too long (nearly equal logits) and a top_k above 512 take the histogram again, of the step's keys or of counts.
+// What bounds it: the instructions of the weights, some 30 per logit and pass that forms them (one, two with top-p), eight independent
+// chains at a time; below that the row's passes through the last-level cache.
 #pragma once
 #include "fp8.hpp"
+#include <type_traits>
 
 typedef unsigned long long sr_mass;
-constexpr int kSampleThreads = 1024, kSampleVocab = 1 << 20, kSampleSegment = 512, kSampleSteps = 1024, kSampleMembers = 256;
+constexpr int kSampleVocab = 1 << 20, kSampleSegment = 512, kSampleSteps = kSampleVocab / kSampleSegment;
+constexpr int kSampleList = 2048, kSampleFew = 64, kSampleBound = 512;
+#define SR_INLINE __attribute__((always_inline))
 constexpr double kSampleUnit = 8796093022208.0;      // 2^43
 
 struct SampleRows {
@@ -64,47 +71,98 @@ __device__ __forceinline__ sr_mass sample_mass(double y)
     return __builtin_bit_cast(unsigned long long, __builtin_bit_cast(double, bits) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kSampleThreads)
+
+// Lane exchanges by DPP: through the LDS crossbar a scan or sum of 64 bits is a chain of twelve trips of some hundred clocks.
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ sr_mass sample_moved(sr_mass x)              // 0 where no lane is the source
+{
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, ROWS, 0xF, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), CTRL, ROWS, 0xF, false);
+    return (sr_mass)hi << 32 | lo;
+}
+__device__ __forceinline__ sr_mass sample_lane(sr_mass x, int lane)
+{
+    return (sr_mass)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane);
+}
+// Running sum over the wavefront's lanes, this one's included.
+__device__ __forceinline__ sr_mass sample_wave_scan(sr_mass v)
+{
+    v += sample_moved<0x111>(v);                     // row_shr:1, 2, 4, 8
+    v += sample_moved<0x112>(v);
+    v += sample_moved<0x114>(v);
+    v += sample_moved<0x118>(v);
+    v += sample_moved<0x142, 0xA>(v);                // row_bcast:15 into rows 1 and 3
+    v += sample_moved<0x143, 0xC>(v);                // row_bcast:31 into rows 2 and 3
+    return v;
+}
+// Sum over the wavefront, in every lane.
+__device__ __forceinline__ sr_mass sample_wave_sum(sr_mass v)
+{
+    v += sample_moved<0xB1>(v);                      // quad_perm [1,0,3,2], [2,3,0,1], row_half_mirror, row_mirror
+    v += sample_moved<0x4E>(v);
+    v += sample_moved<0x141>(v);
+    v += sample_moved<0x140>(v);
+    return (sample_lane(v, 0) + sample_lane(v, 16)) + (sample_lane(v, 32) + sample_lane(v, 48));
+}
+__device__ __forceinline__ uint32_t sample_wave_max(uint32_t v)
+{
+    const int r = (int)row16_max_u32(v);
+    return max(max((uint32_t)__builtin_amdgcn_readlane(r, 0), (uint32_t)__builtin_amdgcn_readlane(r, 16)),
+               max((uint32_t)__builtin_amdgcn_readlane(r, 32), (uint32_t)__builtin_amdgcn_readlane(r, 48)));
+}
+
+template <typename T, int NT>
+__global__ void __launch_bounds__(NT)
 sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
 {
-    constexpr int NT = kSampleThreads, NW = NT / 64, PER = kSampleVocab / kSampleSegment / NT;
+    constexpr int NW = NT / 64, PER = kSampleSteps / NT;
+    static_assert(NW * kSampleSegment * 4 >= kSampleList * 8, "a second list fits where the segments' kept logits lie");
     __shared__ sr_mass red[NW];
-    __shared__ sr_mass mass_of[kSampleSteps];
-    __shared__ uint32_t count_of[kSampleSteps];
-    __shared__ sr_mass segment[PER * NT];
-    __shared__ uint32_t member_key[kSampleMembers];
-    __shared__ int member_at[kSampleMembers];
-    __shared__ sr_mass member_mass[kSampleMembers];
+    __shared__ sr_mass table[kSampleSteps];          // sums by step or by segment
+    __shared__ uint32_t list_key[kSampleList];
+    __shared__ int list_at[kSampleList];
+    __shared__ __align__(8) float dense[NW][kSampleSegment];            // also: the second list; the weights of a segment
+    __shared__ sr_mass few_rank[kSampleFew], few_mass[kSampleFew], few_sum[kSampleFew];
     __shared__ sr_mass found_before;
-    __shared__ uint32_t found, low_s, high_s, n_members;
+    __shared__ uint32_t found, low_s, high_s, n_list, n_all;
     const int64_t row = blockIdx.x;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = p.V;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = p.V;
     const T *L = logits + row * p.ld;
+    auto uniform = [](bool x) SR_INLINE { return __builtin_amdgcn_readfirstlane((int)x) != 0; };
+    bool hot = false;                                // an infinite logit leaves all others without weight: see below
 
-    // fn(values, index of the first, how many exist); the next vector is on its way meanwhile
-    auto pass = [&](auto &&fn) {
-        int at = wave * kSampleSegment + lane * 8;
-        float v[8];
-        load8(L + at, V - at, v);
-        while (at - lane * 8 < V) {                  // wave-uniform
-            const int next = at + NW * kSampleSegment;
-            float w[8];
-            load8(L + next, V - next, w);
-            fn(v, at, V - at);
+    // eight logits from `at` on, -infinity behind the row
+    auto read = [&](int at, float (&v)[8]) SR_INLINE { load8(L + at, V - at, v); };
+    auto complete = [&](int at, float (&v)[8]) SR_INLINE {
+        if (__ballot(at + 8 > V)) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = w[i];
-            at = next;
+            for (int i = 0; i < 8; ++i) v[i] = at + i < V ? v[i] : -INFINITY;
+        }
+        if (hot) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = v[i] == INFINITY ? 0.0f : -INFINITY;
+        }
+    };
+    // fn(values, index of the first); the next two vectors are on their way meanwhile
+    auto pass = [&](auto &&fn) SR_INLINE {
+        constexpr int STEP = NW * kSampleSegment;
+        int at = wave * kSampleSegment + lane * 8;
+        float v[8], w[8];
+        read(at, v);
+        read(at + STEP, w);
+        for (int first = wave * kSampleSegment; first < V; first += STEP) {
+            float next[8];
+            read(at + 2 * STEP, next);
+            complete(at, v);
+            fn(v, at);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { v[i] = w[i]; w[i] = next[i]; }
+            at += STEP;
         }
     };
     // exclusive prefix sum over the threads; total: of all
-    auto scan = [&](sr_mass v, sr_mass &total) {
-        sr_mass s = v;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const sr_mass o = __shfl_up(s, off, kWave);
-            if (lane >= off) s += o;
-        }
+    auto scan = [&](sr_mass v, sr_mass &total) SR_INLINE {
+        const sr_mass s = sample_wave_scan(v);
         __syncthreads();
         if (lane == 63) red[wave] = s;
         __syncthreads();
@@ -118,17 +176,52 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         }
         return before + s - v;
     };
+    auto clear = [&]() SR_INLINE {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PER; ++i) table[i * NT + tid] = 0;
+        if (tid == 0) { found = ~0u; n_list = n_all = 0; low_s = ~0u; high_s = 0; }
+        __syncthreads();
+    };
+    // The entry of the table in which before + its running sum reaches limit_of(sum of all): its number, and `before` becomes the sum in
+    // front of it.  ~0u if none does.
+    auto reached = [&](sr_mass &before, auto &&limit_of, sr_mass &total) SR_INLINE {
+        __syncthreads();
+        sr_mass own = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) own += table[tid * PER + i];
+        sr_mass up = before + scan(own, total);
+        const sr_mass limit = limit_of(total);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const sr_mass s = table[tid * PER + i];
+            if (up < limit && limit - up <= s) { found = tid * PER + i; found_before = up; }
+            up += s;
+        }
+        __syncthreads();
+        before = found_before;
+        return (uint32_t)__builtin_amdgcn_readfirstlane((int)found);
+    };
+    // low_s and high_s: the smallest and the largest of the threads' keys.  (A wavefront's first: the compiler turns an atomic of 64
+    // lanes on one word into a loop over the lanes.)
+    auto range = [&](uint32_t lo, uint32_t hi) SR_INLINE {
+        lo = ~sample_wave_max(~lo);
+        hi = sample_wave_max(hi);
+        if (lane == 0 && lo <= hi) { atomicMin(&low_s, lo); atomicMax(&high_s, hi); }
+    };
 
-    float most = -INFINITY;
-    pass([&](const float (&v)[8], int, int n) {
+    float own_most = -INFINITY;
+    pass([&](const float (&v)[8], int) SR_INLINE {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) most = fmaxf(most, i < n ? v[i] : -INFINITY);
+        for (int i = 0; i < 8; ++i) own_most = fmaxf(own_most, v[i]);
     });
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, kWave));
-    if (lane == 0) red[wave] = __float_as_uint(most);
+    const uint32_t wave_most = sample_wave_max(sample_key(own_most));
+    if (lane == 0) red[wave] = wave_most;
     __syncthreads();
-    for (int i = 0; i < NW; ++i) most = fmaxf(most, __uint_as_float((uint32_t)red[i]));
+    uint32_t most_key = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) most_key = max(most_key, (uint32_t)red[i]);
+    float most = sample_value((uint32_t)__builtin_amdgcn_readfirstlane((int)most_key));
     if (most == -INFINITY) {                         // nothing to draw from
         if (tid == 0) {
             p.tok[row] = -1;
@@ -142,16 +235,19 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     const int top_k = p.top_k ? p.top_k[row] : 0;
     if (!(temp > 0.0f) || top_k == 1 || top_p <= 0.0f) {                // one token: the first of the largest
         int first = V;
-        pass([&](const float (&v)[8], int at, int n) {
+        if (own_most == most)
+            for (int at = wave * kSampleSegment + lane * 8; at < V && first == V; at += NW * kSampleSegment) {
+                float v[8];
+                read(at, v);
 #pragma unroll
-            for (int i = 7; i >= 0; --i)
-                if (i < n && v[i] == most) first = min(first, at + i);
-        });
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) first = min(first, __shfl_xor(first, off, kWave));
+                for (int i = 7; i >= 0; --i)
+                    if (at + i < V && v[i] == most) first = at + i;
+            }
+        first = ~(int)sample_wave_max(~(uint32_t)first);
         __syncthreads();
         if (lane == 0) red[wave] = (sr_mass)first;
         __syncthreads();
+#pragma unroll
         for (int i = 0; i < NW; ++i) first = min(first, (int)red[i]);
         if (tid == 0) {
             p.tok[row] = first;
@@ -160,95 +256,105 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         return;
     }
 
-    // an infinite logit leaves all others without weight: the row is read as 0 where it is infinite and -infinity elsewhere
-    const bool hot = most == INFINITY;
-    if (hot) most = 0.0f;
-    auto seen = [&](float x) { return hot ? (x == INFINITY ? 0.0f : -INFINITY) : x; };
+    // (a row with an infinite logit is read as 0 where it is infinite and -infinity elsewhere)
+    hot = uniform(most == INFINITY);
+    if (hot) { own_most = own_most == INFINITY ? 0.0f : -INFINITY; most = 0.0f; }
     const double c = 1.4426950408889634 / (double)temp;
     const float min_p = p.min_p && p.min_p[row] > 0.0f ? fminf(p.min_p[row], 1.0f) : 0.0f;
-    const sr_mass least = max((sr_mass)1, min_p > 0.0f ? (sr_mass)ceil((double)min_p * kSampleUnit) : (sr_mass)0);
-    auto mass = [&](float x) {
+    const sr_mass least = min_p > 0.0f ? max((sr_mass)1, (sr_mass)ceil((double)min_p * kSampleUnit)) : 1;
+    const bool has_least = uniform(least > 1);
+    auto mass = [&](float x) SR_INLINE {
         const sr_mass m = sample_mass(((double)x - (double)most) * c);
         return m >= least ? m : 0;
     };
-    // The smallest logit that may be drawn: below `floor_v` nothing has weight (a little too low: weights decide); of value
-    // `cut_v` only indices up to cut_at are kept.
-    double lowest = (double)most + (fmax(-44.0, log2((double)least / kSampleUnit)) - 0.001) / c;
+    // Nothing below floor_v has weight (it lies a little too low: weights decide); of value cut_v only indices up to cut_at are kept.
+    const double lowest = (double)most + (has_least ? log2((double)least / kSampleUnit) - 0.001 : -44.001) / c;
     float floor_v = (float)(lowest - fabs(lowest) * 1e-6);
     float cut_v = -INFINITY;
     int cut_at = V;
-    auto kept = [&](float x, int at) { return x > cut_v || (x == cut_v && at <= cut_at); };
-    // fn(value, index) for the logits that may still be kept
-    auto each = [&](auto &&fn) {
-        pass([&](const float (&v)[8], int at, int n) {
-            float top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, i < n ? seen(v[i]) : -INFINITY);
-            if (__ballot(top >= floor_v) == 0) return;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float x = seen(v[i]);
-                if (i < n && x >= floor_v && kept(x, at + i)) fn(x, at + i);
-            }
-        });
+    bool cut = false, in_list = false;               // in_list: the list holds all kept logits (and others, which kept() tells)
+    uint32_t n = 0;                                  // of the list
+    auto kept = [&](float x, int at) SR_INLINE { return x > cut_v || (x == cut_v && at <= cut_at); };
+    auto kept_lanes = [&](float x, int at) SR_INLINE {
+        unsigned long long who = __ballot(x > cut_v);
+        if (__ballot(x == cut_v)) who |= __ballot(x == cut_v && at <= cut_at);
+        return who;
     };
-    // The first index at which the running sum of weight(value, index) exceeds target(sum of all); the sum of all in `total`.
-    auto index_of = [&](auto &&weight, auto &&target, sr_mass &total) {
-        const int segments = (V + kSampleSegment - 1) / kSampleSegment;
-        for (int i = tid; i < PER * NT; i += NT) segment[i] = 0;
-        __syncthreads();
-        pass([&](const float (&v)[8], int at, int n) {
-            float top = -INFINITY;
+    auto slot = [&](unsigned long long who) SR_INLINE {                 // of this lane among those of `who`
+        return __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+    };
+    // vectors that hold a logit from floor_v up
+    auto live = [&](const float (&v)[8]) SR_INLINE {
+        float top = v[0];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, i < n ? seen(v[i]) : -INFINITY);
-            if (__ballot(top >= floor_v) == 0) return;
-            sr_mass s = 0;
+        for (int i = 1; i < 8; ++i) top = fmaxf(top, v[i]);
+        return __ballot(top >= floor_v) != 0;
+    };
+    // the weights of a vector's kept logits, in chains that do not wait for each other
+    auto masses = [&](const float (&v)[8], int at, sr_mass (&m)[8]) SR_INLINE {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float x = seen(v[i]);
-                if (i < n && x >= floor_v) s += weight(x, at + i);
+        for (int i = 0; i < 8; ++i) m[i] = sample_mass(((double)v[i] - (double)most) * c);
+        if (has_least) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m[i] = m[i] >= least ? m[i] : 0;
+        }
+        if (cut) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m[i] = kept(v[i], at + i) ? m[i] : 0;
+        }
+    };
+    // The first index at which the running sum of weights exceeds target(sum of all): one_of(value, index) gives a kept logit's,
+    // of(values, index, weights) those of a vector, and sum_of(values, index) the sum of the wavefront's vectors.
+    auto index_of = [&](auto &&one_of, auto &&of, auto &&sum_of, auto &&target, sr_mass &total) SR_INLINE {
+        clear();
+        if (in_list) {
+            for (uint32_t i = tid; i < n; i += NT) {
+                const float x = sample_value(list_key[i]);
+                const int at = list_at[i];
+                if (kept(x, at)) atomicAdd(&table[at / kSampleSegment], one_of(x, at));
             }
-#pragma unroll
-            for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off, kWave);
-            if (lane == 0) segment[at / kSampleSegment] = s;
-        });
-        __syncthreads();
-        sr_mass own = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) own += segment[tid * PER + i];
-        sr_mass before = scan(own, total);
-        const sr_mass t = target(total);
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const sr_mass s = segment[tid * PER + i];
-            if (t >= before && t - before < s) { found = tid * PER + i; found_before = before; }
-            before += s;
+        } else {
+            pass([&](const float (&v)[8], int at) SR_INLINE {
+                if (!live(v)) return;
+                const sr_mass s = sum_of(v, at);
+                if (lane == 0) table[at / kSampleSegment] = s;
+            });
+        }
+        sr_mass before = 0, goal = 0;
+        const uint32_t seg = min(reached(before, [&](sr_mass sum) SR_INLINE { goal = target(sum); return goal + 1; }, total),
+                                 (uint32_t)(V - 1) / kSampleSegment);
+        sr_mass *weights = reinterpret_cast<sr_mass *>(&dense[0][0]);
+        if (in_list) {
+            for (int i = tid; i < kSampleSegment; i += NT) weights[i] = 0;
+            __syncthreads();
+            for (uint32_t i = tid; i < n; i += NT) {
+                const float x = sample_value(list_key[i]);
+                const int at = list_at[i];
+                if ((uint32_t)at / kSampleSegment == seg && kept(x, at)) weights[at % kSampleSegment] = one_of(x, at);
+            }
         }
         __syncthreads();
-        const int at = min((int)found, segments - 1) * kSampleSegment + lane * 8;
         if (wave == 0) {
-            float v[8];
-            load8(L + at, V - at, v);
-            sr_mass w[8], s = 0;
+            const int at = (int)seg * kSampleSegment + lane * 8;
+            sr_mass m[8], s = 0;
+            if (in_list) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float x = seen(v[i]);
-                w[i] = at + i < V && x >= floor_v ? weight(x, at + i) : 0;
-                s += w[i];
+                for (int i = 0; i < 8; ++i) m[i] = weights[lane * 8 + i];
+            } else {
+                float v[8];
+                read(at, v);
+                complete(at, v);
+                of(v, at, m);
             }
-            sr_mass upto = s;
 #pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const sr_mass o = __shfl_up(upto, off, kWave);
-                if (lane >= off) upto += o;
-            }
-            sr_mass run = found_before + upto - s;
-            if (t >= run && t - run < s) {
+            for (int i = 0; i < 8; ++i) s += m[i];
+            sr_mass run = before + sample_wave_scan(s) - s;
+            if (goal >= run && goal - run < s) {
                 int k = 0;
 #pragma unroll
                 for (int i = 0; i < 7; ++i) {
-                    run += w[i];
-                    if (k == i && t >= run) k = i + 1;
+                    run += m[i];
+                    if (k == i && goal >= run) k = i + 1;
                 }
                 found = at + k;
             }
@@ -256,118 +362,290 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         __syncthreads();
         return (int)found;
     };
-
-    // Cuts the kept tokens at the first one with which their number or their mass reaches a limit.
-    auto cut = [&](bool by_mass, auto &&limit_of) {
-        uint32_t key_low = 0, key_high = 0;          // of the step being divided, once it is one of keys
-        int shift = -1;                              // -1: steps of value
-        const float scale = (float)kSampleSteps / (most - floor_v);
-        auto step_of = [&](float x) -> uint32_t {
-            if (shift < 0) return (uint32_t)fminf((most - x) * scale, (float)(kSampleSteps - 1));
-            return (key_high - sample_key(x)) >> shift;
-        };
-        sr_mass limit = 0, before = 0;
-        uint32_t step = 0;
-        int value_step = -1;
-        auto inside = [&](float x) {                 // of the step being divided
-            if (value_step < 0) return true;
-            const uint32_t key = sample_key(x);
-            return shift < 0 || (key >= key_low && key <= key_high);
-        };
-        for (int round = 0;; ++round) {
-            __syncthreads();
-            mass_of[tid] = 0;
-            count_of[tid] = 0;
-            if (tid == 0) { found = ~0u; n_members = 0; low_s = ~0u; high_s = 0; }
-            __syncthreads();
-            each([&](float x, int) {
-                if (!inside(x)) return;
-                const uint32_t s = step_of(x);
-                if (by_mass) {
-                    const sr_mass m = mass(x);
-                    if (m == 0) return;
-                    atomicAdd(&mass_of[s], m);
-                }
-                atomicAdd(&count_of[s], 1u);
-            });
-            __syncthreads();
-            const sr_mass own = by_mass ? mass_of[tid] : count_of[tid];
-            sr_mass total;
-            const sr_mass up = before + scan(own, total);
-            if (round == 0) {
-                limit = limit_of(total);
-                if (limit > total) return;           // never reached
+    // Lists the logits from `from` to `to`: how many there are.  `above`: the larger ones too, in the second list.
+    auto gather = [&](float from, float to, bool above, uint32_t &larger) SR_INLINE {
+        uint32_t *second_key = reinterpret_cast<uint32_t *>(&dense[0][0]);
+        int *second_at = reinterpret_cast<int *>(second_key + kSampleList);
+        __syncthreads();
+        if (tid == 0) n_list = n_all = 0;
+        __syncthreads();
+        from = fmaxf(from, floor_v);
+        pass([&](const float (&v)[8], int at) SR_INLINE {
+            float top = v[0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top = fmaxf(top, v[i]);
+            if (__ballot(top >= from) == 0) return;
+            unsigned long long up[8], who[8];
+            uint32_t ups = 0, ins = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                up[i] = __ballot(v[i] >= from);
+                who[i] = up[i] & __ballot(v[i] <= to);
+                ups += (uint32_t)__popcll(up[i]);
+                ins += (uint32_t)__popcll(who[i]);
             }
-            if (up < limit && limit - up <= own) { found = tid; found_before = up; }
-            __syncthreads();
-            step = found;
-            before = found_before;
-            const uint32_t n = count_of[step];
-            if (n <= kSampleMembers) break;
-            // the keys of this step's members
-            uint32_t lo = ~0u, hi = 0;
-            each([&](float x, int) {
-                if (inside(x) && step_of(x) == step) {
-                    const uint32_t key = sample_key(x);
-                    lo = min(lo, key);
-                    hi = max(hi, key);
-                }
-            });
-            if (lo <= hi) { atomicMin(&low_s, lo); atomicMax(&high_s, hi); }
-            __syncthreads();
-            key_low = low_s;
-            key_high = high_s;
-            value_step = 0;
-            if (key_low == key_high) {               // one value: its first ones, by index
-                const float x0 = sample_value(key_low);
-                const sr_mass one = by_mass ? mass(x0) : 1;
-                const sr_mass n_kept = (limit - before + one - 1) / one;
-                sr_mass all;
-                const int at = index_of([&](float x, int i) -> sr_mass { return x == x0 && kept(x, i) ? 1 : 0; },
-                                        [&](sr_mass) { return n_kept - 1; }, all);
-                cut_v = floor_v = x0;
-                cut_at = at;
-                return;
+            uint32_t k = 0, a = 0;
+            if (lane == 0) {
+                if (ins) k = atomicAdd(&n_list, ins);
+                if (above) a = atomicAdd(&n_all, ups);
             }
-            shift = 0;
-            while (((key_high - key_low) >> shift) >= (uint32_t)kSampleSteps) ++shift;
-        }
-        each([&](float x, int at) {
-            if (!inside(x) || step_of(x) != step) return;
-            const sr_mass m = by_mass ? mass(x) : 1;
-            if (m == 0) return;
-            const uint32_t i = atomicAdd(&n_members, 1u);
-            member_key[i] = sample_key(x);
-            member_at[i] = at;
-            member_mass[i] = m;
+            k = (uint32_t)__builtin_amdgcn_readfirstlane((int)k);
+            a = (uint32_t)__builtin_amdgcn_readfirstlane((int)a);
+            if (ins && k < (uint32_t)kSampleList) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t mine = k + slot(who[i]);
+                    if ((who[i] >> lane & 1) && mine < (uint32_t)kSampleList) { list_key[mine] = sample_key(v[i]); list_at[mine] = at + i; }
+                    k += (uint32_t)__popcll(who[i]);
+                }
+            }
+            if (above && a < (uint32_t)kSampleList) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t mine = a + slot(up[i]);
+                    if ((up[i] >> lane & 1) && mine < (uint32_t)kSampleList) { second_key[mine] = sample_key(v[i]); second_at[mine] = at + i; }
+                    a += (uint32_t)__popcll(up[i]);
+                }
+            }
         });
         __syncthreads();
-        const int n = (int)n_members;
-        if (tid < n) {
-            const uint32_t key = member_key[tid];
-            const int at = member_at[tid];
-            sr_mass up = before;
-            for (int j = 0; j < n; ++j) {
-                const uint32_t k = member_key[j];
-                up += k > key || (k == key && member_at[j] < at) ? member_mass[j] : 0;
-            }
-            if (up < limit && limit - up <= member_mass[tid]) { low_s = key; high_s = (uint32_t)at; }
+        larger = (uint32_t)__builtin_amdgcn_readfirstlane((int)n_all);
+        const uint32_t found_n = (uint32_t)__builtin_amdgcn_readfirstlane((int)n_list);
+        if (above && larger <= (uint32_t)kSampleList) {
+            for (uint32_t i = tid; i < larger; i += NT) { list_key[i] = second_key[i]; list_at[i] = second_at[i]; }
+            __syncthreads();
         }
-        __syncthreads();
-        cut_v = floor_v = sample_value(low_s);
-        cut_at = (int)high_s;
+        return found_n;
     };
-    if (top_k > 0 && top_k < V) cut(false, [&](sr_mass) { return (sr_mass)top_k; });
-    if (top_p < 1.0f) cut(true, [&](sr_mass total) { return max((sr_mass)ceil((double)top_p * (double)total), (sr_mass)1); });
+
+    // top-k (their number), then top-p (their mass): the kept tokens end at the first one with which a limit is reached
+    for (int by_mass = 0; by_mass < 2; ++by_mass) {
+        if (uniform(by_mass ? !(top_p < 1.0f) : top_k <= 0 || top_k >= V)) continue;
+        auto limit_of = [&](sr_mass sum) SR_INLINE {
+            return by_mass ? max((sr_mass)ceil((double)top_p * (double)sum), (sr_mass)1) : (sr_mass)top_k;
+        };
+        const float scale = (float)kSampleSteps / (most - floor_v);
+        auto value_step = [&](float x) SR_INLINE { return (uint32_t)fminf((most - x) * scale, (float)(kSampleSteps - 1)); };
+        uint32_t low = 0, high = ~0u, step = 0;      // the keys that are left; the step of the table, of value while shift < 0
+        int shift = -1;
+        sr_mass before = 0, limit = 0, total;
+        auto step_of = [&](float x) SR_INLINE { return shift < 0 ? value_step(x) : (high - sample_key(x)) >> shift; };
+        auto in_keys = [&](uint32_t key) SR_INLINE { return key >= low && key <= high; };
+        bool listed = false, all = false, whole = false;     // whole: all of the list is divided, not a step
+        if (!by_mass && top_k <= kSampleBound) {
+            // top_k threads whose largest logit is at least a bound hold top_k logits that are: those above it are listed
+            clear();
+            uint32_t mine = ~0u;
+            if (own_most >= floor_v) {
+                mine = value_step(own_most);
+                atomicAdd(&table[mine], (sr_mass)1);
+            }
+            const uint32_t last = reached(before, limit_of, total);
+            before = 0;
+            if (last != ~0u) {
+                const uint32_t own_key = sample_key(own_most);
+                range(mine <= last ? own_key : ~0u, mine <= last ? own_key : 0);
+                __syncthreads();
+                const float bound = fmaxf(floor_v, sample_value((uint32_t)__builtin_amdgcn_readfirstlane((int)low_s)));
+                uint32_t larger;
+                n = gather(bound, INFINITY, false, larger);
+                listed = in_list = whole = n <= (uint32_t)kSampleList;
+                limit = (sr_mass)top_k;
+                if (listed) floor_v = bound;
+            }
+        } else if (by_mass && in_list) {
+            clear();
+            for (uint32_t i = tid; i < n; i += NT) {
+                const float x = sample_value(list_key[i]);
+                if (kept(x, list_at[i])) atomicAdd(&table[value_step(x)], mass(x));
+            }
+            step = reached(before, [&](sr_mass sum) SR_INLINE { return limit = limit_of(sum); }, total);
+            all = step == ~0u;
+            listed = true;
+        }
+        while (!listed) {
+            clear();
+            pass([&](const float (&v)[8], int at) SR_INLINE {
+                if (!live(v)) return;
+                sr_mass m[8];
+                if (by_mass) {
+                    masses(v, at, m);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) m[i] = kept(v[i], at + i) ? 1 : 0;
+                }
+                if (shift < 0) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (v[i] >= floor_v) atomicAdd(&table[value_step(v[i])], m[i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint32_t key = sample_key(v[i]);
+                        if (v[i] >= floor_v && in_keys(key)) atomicAdd(&table[(high - key) >> shift], m[i]);
+                    }
+                }
+            });
+            step = reached(before, [&](sr_mass sum) SR_INLINE { return shift < 0 ? limit = limit_of(sum) : limit; }, total);
+            all = step == ~0u;                       // never reached
+            if (all) break;
+            // about where the step lies (no bound where the scale is not finite)
+            float from = -INFINITY, to = INFINITY;
+            if (shift < 0) {
+                const float width = 1.0f / scale, slack = fabsf(most) * 1e-6f;
+                if (step + 1 < (uint32_t)kSampleSteps && width < 1e30f) from = most - ((float)step + 1.01f) * width - slack;
+                if (width < 1e30f) to = most - ((float)step - 0.01f) * width + slack;
+            } else {
+                from = sample_value(low);
+                to = sample_value(high);
+            }
+            uint32_t larger;
+            n = gather(from, to, true, larger);
+            in_list = larger <= (uint32_t)kSampleList;
+            listed = in_list || n <= (uint32_t)kSampleList;
+            if (in_list) n = larger;
+            if (listed) break;
+            // the step is divided by the keys of its members
+            uint32_t lo = ~0u, hi = 0;
+            pass([&](const float (&v)[8], int at) SR_INLINE {
+                if (!live(v)) return;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t key = sample_key(v[i]);
+                    if (v[i] >= from && v[i] <= to && v[i] >= floor_v && in_keys(key) && step_of(v[i]) == step) { lo = min(lo, key); hi = max(hi, key); }
+                }
+            });
+            range(lo, hi);
+            __syncthreads();
+            low = (uint32_t)__builtin_amdgcn_readfirstlane((int)low_s);
+            high = (uint32_t)__builtin_amdgcn_readfirstlane((int)high_s);
+            if (low == high) break;
+            shift = 0;
+            while (((high - low) >> shift) >= (uint32_t)kSampleSteps) ++shift;
+        }
+        if (all) continue;
+        // the step's members in the list, by key, until a few or one value is left
+        bool few = false;
+        auto member = [&](uint32_t i) SR_INLINE {
+            const uint32_t key = list_key[i];
+            const float x = sample_value(key);
+            return in_keys(key) && (whole || step_of(x) == step) && kept(x, list_at[i]);
+        };
+        while (listed) {
+            __syncthreads();
+            if (tid == 0) { n_list = 0; low_s = ~0u; high_s = 0; }
+            __syncthreads();
+            uint32_t lo = ~0u, hi = 0, in = 0;
+            for (uint32_t i = tid; i < n; i += NT)
+                if (member(i)) { lo = min(lo, list_key[i]); hi = max(hi, list_key[i]); ++in; }
+            range(lo, hi);
+            in = (uint32_t)sample_wave_sum(in);
+            if (lane == 0 && in) atomicAdd(&n_list, in);
+            __syncthreads();
+            low = (uint32_t)__builtin_amdgcn_readfirstlane((int)low_s);
+            high = (uint32_t)__builtin_amdgcn_readfirstlane((int)high_s);
+            whole = true;
+            few = uniform(n_list <= (uint32_t)kSampleFew);
+            if (few || low == high) break;
+            clear();
+            shift = 0;
+            while (((high - low) >> shift) >= (uint32_t)kSampleSteps) ++shift;
+            for (uint32_t i = tid; i < n; i += NT)
+                if (member(i)) {
+                    const uint32_t key = list_key[i];
+                    atomicAdd(&table[(high - key) >> shift], by_mass ? mass(sample_value(key)) : (sr_mass)1);
+                }
+            step = reached(before, [&](sr_mass) SR_INLINE { return limit; }, total);
+            const uint32_t top = high - (step << shift), size = (1u << shift) - 1;
+            low = top - low > size ? top - size : low;
+            high = top;
+        }
+        if (few) {
+            __syncthreads();
+            if (tid == 0) n_list = 0;
+            if (tid < kSampleFew) few_sum[tid] = 0;
+            __syncthreads();
+            for (uint32_t i = tid; i < n; i += NT)
+                if (member(i)) {
+                    const uint32_t k = atomicAdd(&n_list, 1u), key = list_key[i];
+                    few_rank[k] = (sr_mass)key << 32 | (uint32_t)~list_at[i];            // larger: earlier in the order
+                    few_mass[k] = by_mass ? mass(sample_value(key)) : (sr_mass)1;
+                }
+            __syncthreads();
+            // lane: a member; wavefront w compares it with members w, w + NW, ...
+            const int m = (int)n_list;
+            const sr_mass rank = few_rank[min(lane, m - 1)], own = few_mass[min(lane, m - 1)];
+            sr_mass sum = 0;
+            for (int j = wave; j < m; j += NW) sum += few_rank[j] > rank ? few_mass[j] : 0;
+            atomicAdd(&few_sum[lane], sum);
+            __syncthreads();
+            if (wave == 0 && lane < m) {
+                const sr_mass up = before + few_sum[lane];
+                if (up < limit && limit - up <= own) { low_s = (uint32_t)(rank >> 32); high_s = ~(uint32_t)rank; }
+            }
+            __syncthreads();
+            cut_v = sample_value((uint32_t)__builtin_amdgcn_readfirstlane((int)low_s));
+            cut_at = __builtin_amdgcn_readfirstlane((int)high_s);
+        } else {
+            // of one value the first ones, by index
+            const float x0 = sample_value(low);
+            const sr_mass one = by_mass ? mass(x0) : 1, n_kept = (limit - before + one - 1) / one;
+            const int last = x0 > cut_v ? V : cut_at;
+            floor_v = fmaxf(floor_v, x0);
+            const int at = index_of([&](float x, int) SR_INLINE { return (sr_mass)(x == x0); },
+                                    [&](const float (&v)[8], int at, sr_mass (&m)[8]) SR_INLINE {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) m[i] = v[i] == x0 && at + i <= last ? 1 : 0;
+            }, [&](const float (&v)[8], int at) SR_INLINE {
+                uint32_t s = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s += (uint32_t)__popcll(__ballot(v[i] == x0 && at + i <= last));
+                return (sr_mass)s;
+            }, [&](sr_mass) SR_INLINE { return n_kept - 1; }, total);
+            cut_v = x0;
+            cut_at = __builtin_amdgcn_readfirstlane(at);
+        }
+        cut = true;
+        floor_v = fmaxf(floor_v, cut_v);
+    }
 
     const float u = p.uniform[row];
     sr_mass total;
-    const int tok = index_of([&](float x, int at) -> sr_mass { return kept(x, at) ? mass(x) : 0; },
-                             [&](sr_mass sum) { return min((sr_mass)((double)(u > 0.0f ? fminf(u, 1.0f) : 0.0f) * (double)sum), sum - 1); }, total);
+    const int tok = index_of([&](float x, int) SR_INLINE { return mass(x); }, masses, [&](const float (&v)[8], int at) SR_INLINE {
+        sr_mass s = 0;
+        uint32_t k = kSampleSegment;
+        unsigned long long who[8];
+        if (cut) {
+            k = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                who[i] = kept_lanes(v[i], at + i);
+                k += (uint32_t)__popcll(who[i]);
+            }
+        }
+        if (k > (uint32_t)kSampleSegment / 2) {
+            sr_mass m[8];
+            masses(v, at, m);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += m[i];
+        } else {                                     // few of the segment's logits are kept: side by side they take fewer evaluations
+            const uint32_t some = k;
+            k = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (who[i] >> lane & 1) dense[wave][k + slot(who[i])] = v[i];
+                k += (uint32_t)__popcll(who[i]);
+            }
+            __builtin_amdgcn_wave_barrier();
+            for (uint32_t j = lane; j < some; j += 64) s += mass(dense[wave][j]);
+            __builtin_amdgcn_wave_barrier();
+        }
+        return sample_wave_sum(s);
+    }, [&](sr_mass sum) SR_INLINE { return min((sr_mass)((double)(u > 0.0f ? fminf(u, 1.0f) : 0.0f) * (double)sum), sum - 1); }, total);
     if (tid == 0) {
         p.tok[row] = tok;
         if (p.logprob) {
-            const float x = seen((float)L[tok]);
+            const float x = hot ? 0.0f : (float)L[tok];
             p.logprob[row] = (float)(((double)x - (double)most) / (double)temp - log((double)total / kSampleUnit));
         }
     }
