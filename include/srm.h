@@ -635,7 +635,7 @@ size_t srm_linear_argmax_noalloc_max_bytes(void);
  *   the tokens that these two leave the fewest whose w reach top_p[r] of their sum (top_p >= 1 or NaN: all; <= 0: one).
  * d_tok_out[r] is the first of them, by index, whose running sum of w over them exceeds uniform[r] times the sum of all of them
  * (uniform in [0, 1): below 0 or NaN counts as 0, 1 and above draw the last one).  temperature NULL: 1; <= 0 or NaN: greedy (the
- * lowest index of the largest logit).  A logit that is NaN counts as -infinity and is never drawn; logits of +infinity share the
+ * lowest index of the largest logit); above 1e30: 1e30.  A logit that is NaN counts as -infinity and is never drawn; logits of +infinity share the
  * draw equally; a row that holds nothing else than -infinity gets token -1.  d_logprob[rows] (fp32, may be NULL): the logarithm of
  * the probability with which the token was drawn, 0 for a greedy row, -infinity with token -1.  Weights are held as whole numbers
  * of 2^-43 of the largest one, so that sums are exact and a result depends on its row alone; smaller weights are never drawn.

@@ -25,7 +25,7 @@
 
 typedef unsigned long long sr_mass;
 constexpr int kSampleVocab = 1 << 20, kSampleSegment = 512, kSampleSteps = kSampleVocab / kSampleSegment;
-constexpr int kSampleList = 2048, kSampleFew = 64, kSampleBound = 512;
+constexpr int kSampleList = 1024, kSampleFew = 64, kSampleBound = 512, kSampleDense = 256;
 #define SR_INLINE __attribute__((always_inline))
 constexpr double kSampleUnit = 8796093022208.0;      // 2^43
 
@@ -46,31 +46,44 @@ __device__ __forceinline__ uint32_t sample_key(float f)
 }
 __device__ __forceinline__ float sample_value(uint32_t key) { return __uint_as_float((key & 0x80000000u) ? key & 0x7fffffffu : ~key); }
 
-// round(2^43 2^y) for y <= 0, 0 for y <= -44 and for a NaN.  2^f on [-1/2, 1/2] by the polynomial that interpolates it at Chebyshev's
-// points, of degree 10 (below 1e-15 of the value), its constant term 1 so that y = 0 gives the unit.
-__device__ __forceinline__ sr_mass sample_mass(double y)
+// round(2^43 2^(d c)) for d c from -900 to 0 (0 below -44).  2^f on [-1/2, 1/2] by the polynomial of degree 9 with the constant term 1
+// (so that d = 0 gives the unit) whose other part interpolates (2^f - 1) / f at Chebyshev's points: below 2^-44 of the value.
+// (N at a time, stage by stage: a chain of dependent fp64 instructions takes twice the clocks that issuing them does, and left alone the
+// compiler forms one chain behind the other.)
+template <int N>
+__device__ __forceinline__ void sample_mass(const double (&d)[N], double c, sr_mass (&m)[N])
 {
-    y = __builtin_fmax(y, -44.0);
-    const double magic = 6755399441055744.0;         // 1.5 2^52: its sum with y holds y's nearest integer in the low bits
-    const double t = y + magic;
-    const double f = y - (t - magic);
-    double p = 7.070977866508138e-09;
-    p = __builtin_fma(p, f, 1.0205905413765595e-07);
-    p = __builtin_fma(p, f, 1.3215451633221434e-06);
-    p = __builtin_fma(p, f, 1.5252672924850737e-05);
-    p = __builtin_fma(p, f, 0.00015403530424776529);
-    p = __builtin_fma(p, f, 0.0013333558200794592);
-    p = __builtin_fma(p, f, 0.009618129107618665);
-    p = __builtin_fma(p, f, 0.05550410866465167);
-    p = __builtin_fma(p, f, 0.24022650695910075);
-    p = __builtin_fma(p, f, 0.6931471805599462);
-    p = __builtin_fma(p, f, 1.0);
-    // p 2^(43 + n), then its nearest integer in the mantissa of 2^52 + it
-    const int n = (int)(uint32_t)__builtin_bit_cast(unsigned long long, t);
-    const unsigned long long bits = __builtin_bit_cast(unsigned long long, p) + ((unsigned long long)(unsigned)(n + 43) << 52);
-    return __builtin_bit_cast(unsigned long long, __builtin_bit_cast(double, bits) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
+    constexpr double magic = 6755399441055744.0 + 43.0;                // 1.5 2^52 + 43: a sum with it holds 43 + the nearest integer n in the low bits
+    constexpr double coef[9] = {1.0203121063391729e-07, 1.3255224878668817e-06, 1.525268684626772e-05, 0.00015403455852453838, 0.0013333558179043112, 0.009618129159402558, 0.055504108664760424, 0.2402265069581299, 0.6931471805599453};
+    double t[N], f[N], p[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) t[i] = __builtin_fma(d[i], c, magic);
+    if constexpr (N > 1) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = t[i] - magic;
+    if constexpr (N > 1) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = __builtin_fma(d[i], c, -f[i]);
+    if constexpr (N > 1) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) p[i] = coef[0];
+#pragma unroll
+    for (int k = 1; k < 10; ++k) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] = __builtin_fma(p[i], f[i], k < 9 ? coef[k] : 1.0);
+        if constexpr (N > 1) __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {                    // p 2^(43 + n), then its nearest integer in the mantissa of 2^52 + it
+        const unsigned long long bits = __builtin_bit_cast(unsigned long long, p[i]);
+        uint32_t high = (uint32_t)(bits >> 32) + ((uint32_t)__builtin_bit_cast(unsigned long long, t[i]) << 20);
+        asm("" : "+v"(high));                        // (one 32-bit instruction; a 64-bit sum otherwise)
+        p[i] = __builtin_bit_cast(double, (unsigned long long)high << 32 | (uint32_t)bits) + 4503599627370496.0;
+    }
+    if constexpr (N > 1) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) m[i] = __builtin_bit_cast(unsigned long long, p[i]) & 0xFFFFFFFFFFFFFull;
 }
-
 
 // Lane exchanges by DPP: through the LDS crossbar a scan or sum of 64 bits is a chain of twelve trips of some hundred clocks.
 template <int CTRL, int ROWS = 0xF>
@@ -95,6 +108,16 @@ __device__ __forceinline__ sr_mass sample_wave_scan(sr_mass v)
     v += sample_moved<0x143, 0xC>(v);                // row_bcast:31 into rows 2 and 3
     return v;
 }
+__device__ __forceinline__ uint32_t sample_wave_scan32(uint32_t v)
+{
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xA, 0xF, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xC, 0xF, false);
+    return v;
+}
 // Sum over the wavefront, in every lane.
 __device__ __forceinline__ sr_mass sample_wave_sum(sr_mass v)
 {
@@ -112,19 +135,19 @@ __device__ __forceinline__ uint32_t sample_wave_max(uint32_t v)
 }
 
 template <typename T, int NT>
-__global__ void __launch_bounds__(NT)
+__global__ void __launch_bounds__(NT, 4)
 sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
 {
     constexpr int NW = NT / 64, PER = kSampleSteps / NT;
-    static_assert(NW * kSampleSegment * 4 >= kSampleList * 8, "a second list fits where the segments' kept logits lie");
+    static_assert(NW * kSampleDense >= 2 * kSampleSegment, "the weights of a segment fit");
     __shared__ sr_mass red[NW];
     __shared__ sr_mass table[kSampleSteps];          // sums by step or by segment
     __shared__ uint32_t list_key[kSampleList];
     __shared__ int list_at[kSampleList];
-    __shared__ __align__(8) float dense[NW][kSampleSegment];            // also: the second list; the weights of a segment
+    __shared__ __align__(8) float dense[NW * kSampleDense];             // kept logits of the wavefronts' segments; the weights of a segment
     __shared__ sr_mass few_rank[kSampleFew], few_mass[kSampleFew], few_sum[kSampleFew];
     __shared__ sr_mass found_before;
-    __shared__ uint32_t found, low_s, high_s, n_list, n_all;
+    __shared__ uint32_t found, low_s, high_s, n_list;
     const int64_t row = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = p.V;
     const T *L = logits + row * p.ld;
@@ -143,20 +166,19 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
             for (int i = 0; i < 8; ++i) v[i] = v[i] == INFINITY ? 0.0f : -INFINITY;
         }
     };
-    // fn(values, index of the first); the next two vectors are on their way meanwhile
+    // fn(values, index of the first); the next vector is on its way meanwhile
     auto pass = [&](auto &&fn) SR_INLINE {
         constexpr int STEP = NW * kSampleSegment;
         int at = wave * kSampleSegment + lane * 8;
-        float v[8], w[8];
+        float v[8];
         read(at, v);
-        read(at + STEP, w);
         for (int first = wave * kSampleSegment; first < V; first += STEP) {
             float next[8];
-            read(at + 2 * STEP, next);
+            read(at + STEP, next);
             complete(at, v);
             fn(v, at);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { v[i] = w[i]; w[i] = next[i]; }
+            for (int i = 0; i < 8; ++i) v[i] = next[i];
             at += STEP;
         }
     };
@@ -180,7 +202,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < PER; ++i) table[i * NT + tid] = 0;
-        if (tid == 0) { found = ~0u; n_list = n_all = 0; low_s = ~0u; high_s = 0; }
+        if (tid == 0) { found = ~0u; n_list = 0; low_s = ~0u; high_s = 0; }
         __syncthreads();
     };
     // The entry of the table in which before + its running sum reaches limit_of(sum of all): its number, and `before` becomes the sum in
@@ -259,30 +281,26 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     // (a row with an infinite logit is read as 0 where it is infinite and -infinity elsewhere)
     hot = uniform(most == INFINITY);
     if (hot) { own_most = own_most == INFINITY ? 0.0f : -INFINITY; most = 0.0f; }
-    const double c = 1.4426950408889634 / (double)temp;
+    const double most_d = (double)most, per_bit = (double)fminf(temp, 1e30f) * 0.6931471805599453, c = 1.0 / per_bit;
+    // (2^-900 and less are alike; also what a NaN counts as)
+    const double clamp_d = -900.0 * per_bit;
     const float min_p = p.min_p && p.min_p[row] > 0.0f ? fminf(p.min_p[row], 1.0f) : 0.0f;
     const sr_mass least = min_p > 0.0f ? max((sr_mass)1, (sr_mass)ceil((double)min_p * kSampleUnit)) : 1;
     const bool has_least = uniform(least > 1);
     auto mass = [&](float x) SR_INLINE {
-        const sr_mass m = sample_mass(((double)x - (double)most) * c);
-        return m >= least ? m : 0;
+        const double d[1] = {fmax((double)x - most_d, clamp_d)};
+        sr_mass m[1];
+        sample_mass(d, c, m);
+        return m[0] >= least ? m[0] : 0;
     };
     // Nothing below floor_v has weight (it lies a little too low: weights decide); of value cut_v only indices up to cut_at are kept.
-    const double lowest = (double)most + (has_least ? log2((double)least / kSampleUnit) - 0.001 : -44.001) / c;
+    const double lowest = (double)most + (has_least ? log2((double)least / kSampleUnit) - 0.001 : -44.001) * per_bit;
     float floor_v = (float)(lowest - fabs(lowest) * 1e-6);
     float cut_v = -INFINITY;
     int cut_at = V;
     bool cut = false, in_list = false;               // in_list: the list holds all kept logits (and others, which kept() tells)
     uint32_t n = 0;                                  // of the list
     auto kept = [&](float x, int at) SR_INLINE { return x > cut_v || (x == cut_v && at <= cut_at); };
-    auto kept_lanes = [&](float x, int at) SR_INLINE {
-        unsigned long long who = __ballot(x > cut_v);
-        if (__ballot(x == cut_v)) who |= __ballot(x == cut_v && at <= cut_at);
-        return who;
-    };
-    auto slot = [&](unsigned long long who) SR_INLINE {                 // of this lane among those of `who`
-        return __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
-    };
     // vectors that hold a logit from floor_v up
     auto live = [&](const float (&v)[8]) SR_INLINE {
         float top = v[0];
@@ -292,8 +310,12 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     };
     // the weights of a vector's kept logits, in chains that do not wait for each other
     auto masses = [&](const float (&v)[8], int at, sr_mass (&m)[8]) SR_INLINE {
+        double d[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m[i] = sample_mass(((double)v[i] - (double)most) * c);
+        for (int i = 0; i < 8; ++i) d[i] = (double)v[i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] = fmax(d[i] - most_d, clamp_d);
+        sample_mass(d, c, m);
         if (has_least) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) m[i] = m[i] >= least ? m[i] : 0;
@@ -323,7 +345,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         sr_mass before = 0, goal = 0;
         const uint32_t seg = min(reached(before, [&](sr_mass sum) SR_INLINE { goal = target(sum); return goal + 1; }, total),
                                  (uint32_t)(V - 1) / kSampleSegment);
-        sr_mass *weights = reinterpret_cast<sr_mass *>(&dense[0][0]);
+        sr_mass *weights = reinterpret_cast<sr_mass *>(dense);
         if (in_list) {
             for (int i = tid; i < kSampleSegment; i += NT) weights[i] = 0;
             __syncthreads();
@@ -362,60 +384,32 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         __syncthreads();
         return (int)found;
     };
-    // Lists the logits from `from` to `to`: how many there are.  `above`: the larger ones too, in the second list.
-    auto gather = [&](float from, float to, bool above, uint32_t &larger) SR_INLINE {
-        uint32_t *second_key = reinterpret_cast<uint32_t *>(&dense[0][0]);
-        int *second_at = reinterpret_cast<int *>(second_key + kSampleList);
+    // Lists the logits from `from` to `to`: how many there are, or more than kSampleList if they do not fit (what is listed is no use then).
+    auto gather = [&](float from, float to) SR_INLINE {
         __syncthreads();
-        if (tid == 0) n_list = n_all = 0;
+        if (tid == 0) n_list = 0;
         __syncthreads();
         from = fmaxf(from, floor_v);
+        bool full = false;
         pass([&](const float (&v)[8], int at) SR_INLINE {
-            float top = v[0];
+            if (full) return;
+            uint32_t own = 0;
 #pragma unroll
-            for (int i = 1; i < 8; ++i) top = fmaxf(top, v[i]);
-            if (__ballot(top >= from) == 0) return;
-            unsigned long long up[8], who[8];
-            uint32_t ups = 0, ins = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                up[i] = __ballot(v[i] >= from);
-                who[i] = up[i] & __ballot(v[i] <= to);
-                ups += (uint32_t)__popcll(up[i]);
-                ins += (uint32_t)__popcll(who[i]);
-            }
-            uint32_t k = 0, a = 0;
-            if (lane == 0) {
-                if (ins) k = atomicAdd(&n_list, ins);
-                if (above) a = atomicAdd(&n_all, ups);
-            }
+            for (int i = 0; i < 8; ++i) own += v[i] >= from && v[i] <= to ? 1u : 0u;
+            if (__ballot(own != 0) == 0) return;
+            const uint32_t upto = sample_wave_scan32(own), sum = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+            uint32_t k = 0;
+            if (lane == 0) k = atomicAdd(&n_list, sum);
             k = (uint32_t)__builtin_amdgcn_readfirstlane((int)k);
-            a = (uint32_t)__builtin_amdgcn_readfirstlane((int)a);
-            if (ins && k < (uint32_t)kSampleList) {
+            full = k + sum > (uint32_t)kSampleList;
+            if (full) return;
+            k += upto - own;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t mine = k + slot(who[i]);
-                    if ((who[i] >> lane & 1) && mine < (uint32_t)kSampleList) { list_key[mine] = sample_key(v[i]); list_at[mine] = at + i; }
-                    k += (uint32_t)__popcll(who[i]);
-                }
-            }
-            if (above && a < (uint32_t)kSampleList) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t mine = a + slot(up[i]);
-                    if ((up[i] >> lane & 1) && mine < (uint32_t)kSampleList) { second_key[mine] = sample_key(v[i]); second_at[mine] = at + i; }
-                    a += (uint32_t)__popcll(up[i]);
-                }
-            }
+            for (int i = 0; i < 8; ++i)
+                if (v[i] >= from && v[i] <= to) { list_key[k] = sample_key(v[i]); list_at[k] = at + i; ++k; }
         });
         __syncthreads();
-        larger = (uint32_t)__builtin_amdgcn_readfirstlane((int)n_all);
-        const uint32_t found_n = (uint32_t)__builtin_amdgcn_readfirstlane((int)n_list);
-        if (above && larger <= (uint32_t)kSampleList) {
-            for (uint32_t i = tid; i < larger; i += NT) { list_key[i] = second_key[i]; list_at[i] = second_at[i]; }
-            __syncthreads();
-        }
-        return found_n;
+        return (uint32_t)__builtin_amdgcn_readfirstlane((int)n_list);
     };
 
     // top-k (their number), then top-p (their mass): the kept tokens end at the first one with which a limit is reached
@@ -447,8 +441,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
                 range(mine <= last ? own_key : ~0u, mine <= last ? own_key : 0);
                 __syncthreads();
                 const float bound = fmaxf(floor_v, sample_value((uint32_t)__builtin_amdgcn_readfirstlane((int)low_s)));
-                uint32_t larger;
-                n = gather(bound, INFINITY, false, larger);
+                n = gather(bound, INFINITY);
                 listed = in_list = whole = n <= (uint32_t)kSampleList;
                 limit = (sr_mass)top_k;
                 if (listed) floor_v = bound;
@@ -499,11 +492,11 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
                 from = sample_value(low);
                 to = sample_value(high);
             }
-            uint32_t larger;
-            n = gather(from, to, true, larger);
-            in_list = larger <= (uint32_t)kSampleList;
-            listed = in_list || n <= (uint32_t)kSampleList;
-            if (in_list) n = larger;
+            for (int narrow = 0; narrow < 2 && !listed; ++narrow) {          // everything from there up, else the step alone
+                n = gather(from, narrow ? to : INFINITY);
+                listed = n <= (uint32_t)kSampleList;
+                in_list = listed && narrow == 0;
+            }
             if (listed) break;
             // the step is divided by the keys of its members
             uint32_t lo = ~0u, hi = 0;
@@ -613,31 +606,33 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     sr_mass total;
     const int tok = index_of([&](float x, int) SR_INLINE { return mass(x); }, masses, [&](const float (&v)[8], int at) SR_INLINE {
         sr_mass s = 0;
-        uint32_t k = kSampleSegment;
-        unsigned long long who[8];
+        uint32_t own = 8, upto = 8, some = kSampleSegment;
         if (cut) {
-            k = 0;
+            own = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                who[i] = kept_lanes(v[i], at + i);
-                k += (uint32_t)__popcll(who[i]);
-            }
+            for (int i = 0; i < 8; ++i) own += kept(v[i], at + i) ? 1u : 0u;
+            upto = sample_wave_scan32(own);
+            some = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
         }
-        if (k > (uint32_t)kSampleSegment / 2) {
+        if (some > (uint32_t)kSampleDense) {
             sr_mass m[8];
             masses(v, at, m);
 #pragma unroll
             for (int i = 0; i < 8; ++i) s += m[i];
         } else {                                     // few of the segment's logits are kept: side by side they take fewer evaluations
-            const uint32_t some = k;
-            k = 0;
+            float *to = dense + wave * kSampleDense + (upto - own);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (who[i] >> lane & 1) dense[wave][k + slot(who[i])] = v[i];
-                k += (uint32_t)__popcll(who[i]);
-            }
+            for (int i = 0; i < 8; ++i)
+                if (kept(v[i], at + i)) *to++ = v[i];
             __builtin_amdgcn_wave_barrier();
-            for (uint32_t j = lane; j < some; j += 64) s += mass(dense[wave][j]);
+            for (uint32_t j = lane; j < some + lane; j += 128) {
+                const float *at2 = dense + wave * kSampleDense;
+                const double d[2] = {j < some ? fmax((double)at2[j] - most_d, clamp_d) : clamp_d,
+                                     j + 64 < some ? fmax((double)at2[j + 64] - most_d, clamp_d) : clamp_d};
+                sr_mass m[2];
+                sample_mass(d, c, m);
+                s += (m[0] >= least ? m[0] : 0) + (m[1] >= least ? m[1] : 0);
+            }
             __builtin_amdgcn_wave_barrier();
         }
         return sample_wave_sum(s);
