@@ -525,49 +525,59 @@ def linear(dtype, epilogue, A, W, bias, out=None, argmax=None, scratch=None, str
 
 
 # ---- rows in 8 bits, their products, sampling by request ------------------------------------------------------------
+# (These calls take a few microseconds on the device, so the checks in front of them are kept short: one reading of a tensor's
+# shape and strides, and the current stream's handle without a Stream object around it.)
+_row_types: dict = {}
+
+
 def _row_dtype(t, name: str) -> int:
-    torch = _torch()
-    if t.dtype is torch.float32:
-        return SRM_FP32
-    if t.dtype is torch.bfloat16:
-        return SRM_BF16
-    raise ValueError(f"{name}: dtype {t.dtype}, expected float32 or bfloat16")
+    if not _row_types:
+        torch = _torch()
+        _row_types.update({torch.float32: SRM_FP32, torch.bfloat16: SRM_BF16})
+    code = _row_types.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name}: dtype {t.dtype}, expected float32 or bfloat16")
+    return code
 
 
 def _rows_of(t, name: str):
     """(rows, columns, row stride) of a matrix whose rows are contiguous."""
-    if t.dim() != 2:
+    shape = t.shape
+    if len(shape) != 2:
         raise ValueError(f"{name}: must be a matrix")
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+    rows, cols = shape
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
         raise ValueError(f"{name}: rows must be contiguous")
-    ld = t.stride(0)
-    if rows > 1 and ld < cols:
-        raise ValueError(f"{name}: rows overlap")
-    return rows, cols, max(ld, cols)
+    if ld < cols:
+        if rows > 1:
+            raise ValueError(f"{name}: rows overlap")
+        ld = cols
+    return rows, cols, ld
 
 
-def _launch(first, others, stream, fn, *args):
+def _launch(fn, args, first, others, stream):
     """fn(*args, stream) on the device of the tensors, which is that of `first`."""
+    torch = _torch()
     device = first.device
     if device.type != "cuda":
         raise ValueError("operands must be CUDA tensors")
     for t in others:
         if t is not None and t.device != device:
             raise ValueError(f"operands on {device} and {t.device}")
-    torch = _torch()
+    index = device.index
     if stream is None:
-        raw = torch.cuda.current_stream(device).cuda_stream
+        raw = torch._C._cuda_getCurrentRawStream(index)
     elif stream.device != device:
         raise ValueError(f"operands on {device}, stream on {stream.device}")
     else:
         raw = stream.cuda_stream
-    if device.index == torch.cuda.current_device():
+    if index == torch._C._cuda_getDevice():
         rc = fn(*args, raw)
     else:
         with torch.cuda.device(device):
             rc = fn(*args, raw)
-    if rc != 0:
+    if rc:
         raise SrmError(rc, lib().srm_last_error().decode())
 
 
@@ -576,11 +586,12 @@ def _fp8(q, scales, name: str, rows=None, K=None):
     torch = _torch()
     if q.dtype is not torch.float8_e4m3fn or scales.dtype is not torch.float8_e8m0fnu:
         raise ValueError(f"{name}: dtypes {q.dtype}, {scales.dtype}, expected float8_e4m3fn, float8_e8m0fnu")
-    if q.dim() != 2 or not q.is_contiguous() or not scales.is_contiguous():
+    shape = q.shape
+    if len(shape) != 2 or not q.is_contiguous() or not scales.is_contiguous():
         raise ValueError(f"{name}: must be a contiguous matrix with contiguous scales")
-    n, kp = q.shape
+    n, kp = shape
     if rows is not None and (n != rows or kp != (K + 127) // 128 * 128):
-        raise ValueError(f"{name}: shape {tuple(q.shape)}, expected {(rows, (K + 127) // 128 * 128)}")
+        raise ValueError(f"{name}: shape {tuple(shape)}, expected {(rows, (K + 127) // 128 * 128)}")
     if kp % 128 or scales.numel() != (kp + 511) // 512 * n * 4:
         raise ValueError(f"{name}: {kp} columns with {scales.numel()} scales")
     return n, kp
@@ -605,8 +616,8 @@ def quantize_fp8(x, q, scales, stream=None):
     """srm_quantize_fp8: rows of x (float32 or bfloat16, any row stride) -> q, scales (fp8_empty)."""
     rows, K, ld = _rows_of(x, "x")
     _fp8(q, scales, "q", rows, K)
-    _launch(x, (q, scales), stream, lib().srm_quantize_fp8, _row_dtype(x, "x"), x.data_ptr(), ld, rows, K, q.data_ptr(),
-            scales.data_ptr())
+    _launch(lib().srm_quantize_fp8, (_row_dtype(x, "x"), x.data_ptr(), ld, rows, K, q.data_ptr(), scales.data_ptr()), x, (q, scales),
+            stream)
 
 
 def rmsnorm_fp8(x, gain, eps, q, scales, add=None, stream=None):
@@ -622,8 +633,8 @@ def rmsnorm_fp8(x, gain, eps, q, scales, add=None, stream=None):
         if (n, c) != (rows, d):
             raise ValueError(f"add: shape {(n, c)}, expected {(rows, d)}")
         kind, p_add = _row_dtype(add, "add"), add.data_ptr()
-    _launch(x, (gain, q, scales, add), stream, lib().srm_rmsnorm_fp8, _row_dtype(x, "x"), x.data_ptr(), ld, kind, p_add, ld_add,
-            gain.data_ptr(), eps, rows, d, q.data_ptr(), scales.data_ptr())
+    _launch(lib().srm_rmsnorm_fp8, (_row_dtype(x, "x"), x.data_ptr(), ld, kind, p_add, ld_add, gain.data_ptr(), eps, rows, d,
+                                    q.data_ptr(), scales.data_ptr()), x, (gain, q, scales, add), stream)
 
 
 def linear_fp8(epilogue, a, a_scales, w, w_scales, bias, out, stream=None):
@@ -636,10 +647,11 @@ def linear_fp8(epilogue, a, a_scales, w, w_scales, bias, out, stream=None):
     if bias is not None and (bias.dtype is not torch.float32 or bias.numel() != N or not bias.is_contiguous()):
         raise ValueError(f"bias: must be {N} contiguous float32 values")
     want = torch.float32 if epilogue in (2, 4) else torch.bfloat16
-    if out.dtype is not want or tuple(out.shape) != (M, N) or not out.is_contiguous():
+    if out.dtype is not want or out.shape != (M, N) or not out.is_contiguous():
         raise ValueError(f"out: must be a contiguous {want} matrix of {M} x {N}")
-    _launch(a, (a_scales, w, w_scales, bias, out), stream, lib().srm_linear_fp8, epilogue, a.data_ptr(), a_scales.data_ptr(),
-            w.data_ptr(), w_scales.data_ptr(), None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr())
+    _launch(lib().srm_linear_fp8, (epilogue, a.data_ptr(), a_scales.data_ptr(), w.data_ptr(), w_scales.data_ptr(),
+                                   None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr()),
+            a, (a_scales, w, w_scales, bias, out), stream)
 
 
 def sample_rows(logits, uniform, tok_out, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, stream=None):
@@ -647,15 +659,16 @@ def sample_rows(logits, uniform, tok_out, temperature=None, top_k=None, top_p=No
     a tensor of one value per row (float32, top_k int32), or None."""
     torch = _torch()
     rows, vocab, ld = _rows_of(logits, "logits")
-    ptr = []
-    for name, t, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
-                           ("min_p", min_p, torch.float32), ("uniform", uniform, torch.float32), ("tok_out", tok_out, torch.int32),
-                           ("logprob", logprob, torch.float32)):
-        if t is None:
-            ptr.append(None)
-            continue
-        if t.dtype is not dtype or t.numel() != rows or not t.is_contiguous():
-            raise ValueError(f"{name}: must be {rows} contiguous {dtype} values")
-        ptr.append(t.data_ptr())
-    _launch(logits, (uniform, tok_out, temperature, top_k, top_p, min_p, logprob), stream, lib().srm_sample_rows,
-            _row_dtype(logits, "logits"), logits.data_ptr(), ld, rows, vocab, *ptr)
+    single = (temperature, top_p, min_p, uniform, logprob)
+    for t in single:
+        if t is not None and (t.dtype is not torch.float32 or t.numel() != rows or not t.is_contiguous()):
+            name = ("temperature", "top_p", "min_p", "uniform", "logprob")[[t is o for o in single].index(True)]
+            raise ValueError(f"{name}: must be {rows} contiguous float32 values")
+    for t in (top_k, tok_out):
+        if t is not None and (t.dtype is not torch.int32 or t.numel() != rows or not t.is_contiguous()):
+            raise ValueError(f"{'top_k' if t is top_k else 'tok_out'}: must be {rows} contiguous int32 values")
+    _launch(lib().srm_sample_rows, (_row_dtype(logits, "logits"), logits.data_ptr(), ld, rows, vocab,
+                                    None if temperature is None else temperature.data_ptr(), None if top_k is None else top_k.data_ptr(),
+                                    None if top_p is None else top_p.data_ptr(), None if min_p is None else min_p.data_ptr(),
+                                    uniform.data_ptr(), tok_out.data_ptr(), None if logprob is None else logprob.data_ptr()),
+            logits, (uniform, tok_out, temperature, top_k, top_p, min_p, logprob), stream)
