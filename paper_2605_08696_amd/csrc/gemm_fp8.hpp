@@ -24,26 +24,39 @@ struct Fp8Epi {
 template <int EPI>
 constexpr bool kFp8Exact = EPI == EPI_RESID || EPI == EPI_F32;
 
-// Columns col .. col + 3 of a row, those that exist; at any multiple of an element.
+// Columns col .. col + 3 of a row, those that exist; at any multiple of an element.  What a store adds to is requested apart from it,
+// so that several requests travel together.
 template <int EPI>
-__device__ __forceinline__ void fp8_store4(const Fp8Epi &ep, int64_t row, int col, f32x4_t v)
+__device__ __forceinline__ f32x4_t fp8_old4(const Fp8Epi &ep, int64_t row, int col)
 {
-    if (col >= ep.N) return;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (EPI == EPI_RESID) {
+        const float *p = static_cast<const float *>(ep.out) + row * ep.N + col;
+        if (col + 4 <= ep.N) {
+            __builtin_memcpy(&o, p, 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (col + i < ep.N) o[i] = p[i];
+        }
+    }
+    return o;
+}
+template <int EPI>
+__device__ __forceinline__ void fp8_store4(const Fp8Epi &ep, int64_t row, int col, f32x4_t v, f32x4_t old)
+{
     const int64_t at = row * ep.N + col;
+    if constexpr (EPI == EPI_RESID) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += old[i];
+    }
     if constexpr (EPI == EPI_GELU) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = gelu_bf16out(v[i]);
     }
     if (col + 4 <= ep.N) {
         if constexpr (kFp8Exact<EPI>) {
-            float *p = static_cast<float *>(ep.out) + at;
-            if constexpr (EPI == EPI_RESID) {
-                f32x4_t o;
-                __builtin_memcpy(&o, p, 16);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] += o[i];
-            }
-            __builtin_memcpy(p, &v, 16);
+            __builtin_memcpy(static_cast<float *>(ep.out) + at, &v, 16);
         } else {
             const bf16x4_t o = {(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
             __builtin_memcpy(static_cast<bf16 *>(ep.out) + at, &o, 8);
@@ -53,8 +66,7 @@ __device__ __forceinline__ void fp8_store4(const Fp8Epi &ep, int64_t row, int co
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
         if (col + i >= ep.N) break;
-        if constexpr (EPI == EPI_RESID) static_cast<float *>(ep.out)[at + i] += v[i];
-        else if constexpr (EPI == EPI_F32) static_cast<float *>(ep.out)[at + i] = v[i];
+        if constexpr (kFp8Exact<EPI>) static_cast<float *>(ep.out)[at + i] = v[i];
         else static_cast<bf16 *>(ep.out)[at + i] = (bf16)v[i];
     }
 }
@@ -161,9 +173,10 @@ gemm_fp8_tile_kernel(const unsigned char *__restrict__ A, const uint32_t *__rest
                      const uint32_t *__restrict__ sw, int64_t M, int N, int Kp, Fp8Epi ep)
 {
     constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
-    constexpr int LOADS = (BM + BN) / 8 / NW, WORDS = (BM + BN) / 64;            // tile loads of a wavefront, scale loads of the work-group
-    static_assert((BM + BN) % (8 * NW) == 0 && BM % 64 == 0 && BN % 64 == 0 && WORDS % NW == 0 && BM % (8 * NW) == 0, "whole loads");
-    constexpr int PER_STAGE = LOADS + WORDS / NW;
+    // tile loads of a wavefront; scale loads of the work-group and of a wavefront (where there are fewer than wavefronts, several of them
+    // make the same one: every wavefront counts the same loads)
+    constexpr int LOADS = (BM + BN) / 8 / NW, WORDS = (BM + BN) / 64, WORD_LOADS = (WORDS + NW - 1) / NW, PER_STAGE = LOADS + WORD_LOADS;
+    static_assert((BM + BN) % (8 * NW) == 0 && BM % 64 == 0 && BN % 64 == 0 && BM % (8 * NW) == 0, "whole loads");
     extern __shared__ __align__(16) unsigned char fp8_smem[];
     const unsigned lds = fp8_lds_address(fp8_smem);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -186,8 +199,8 @@ gemm_fp8_tile_kernel(const unsigned char *__restrict__ A, const uint32_t *__rest
             fp8_dma16(stage + r0 * 128, is_a ? ra : rw, row * Kp + ((ld_c ^ swz_of_row(r)) << 4), kt * 128);
         }
 #pragma unroll
-        for (int i = 0; i < WORDS / NW; ++i) {
-            const int g0 = (i * NW + wave) * 64;
+        for (int i = 0; i < WORD_LOADS; ++i) {
+            const int g0 = (i * NW + wave) % WORDS * 64;
             const bool is_a = g0 < BM;
             const int64_t at = is_a ? (int64_t)(kt >> 2) * M + m0 : (int64_t)(kt >> 2) * N + n0;
             fp8_dma4(stage + (BM + BN) * 128 + g0 * 4, fp8_descriptor((is_a ? sa : sw) + at, (is_a ? rows : cols) * 4),
@@ -224,12 +237,34 @@ gemm_fp8_tile_kernel(const unsigned char *__restrict__ A, const uint32_t *__rest
         for (int i = 0; i < TM; ++i) read(wm * (BM / WM) + i * 16 + lr, fa[i], va[i]);
         fp8_products<kFp8Exact<EPI>>(acc, fa, fw, va, vw);
     }
+    // Sixteen rows at a time pass through a wave-private stage in LDS, 16-byte chunk c of row r at chunk c ^ r, so that a row's columns
+    // are read and written side by side.
+    constexpr int CHUNKS = TN * 4, AT_ONCE = 64 / CHUNKS;
+    static_assert(NW * 16 * CHUNKS * 16 <= NS * fp8_stage_bytes<BM, BN>(), "the stages fit the ring");
+    __syncthreads();                                 // the ring has been read
+    f32x4_t *out_stage = reinterpret_cast<f32x4_t *>(fp8_smem) + wave * 16 * CHUNKS;
+    const int o_row = lane / CHUNKS, o_chunk = lane % CHUNKS;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-        const int64_t row = m0 + wm * (BM / WM) + i * 16 + lr;
-        if (row >= M) continue;
 #pragma unroll
-        for (int j = 0; j < TN; ++j) fp8_store4<EPI>(ep, row, n0 + wn * (BN / WN) + j * 16 + 4 * lq, acc[i][j]);
+        for (int j = 0; j < TN; ++j) out_stage[lr * CHUNKS + ((4 * j + lq) ^ (lr & (CHUNKS - 1)))] = acc[i][j];
+        __builtin_amdgcn_wave_barrier();
+        f32x4_t v[16 / AT_ONCE], old[16 / AT_ONCE];
+        const int col = n0 + wn * (BN / WN) + o_chunk * 4;
+#pragma unroll
+        for (int it = 0; it < 16 / AT_ONCE; ++it)
+            old[it] = fp8_old4<EPI>(ep, min(m0 + wm * (BM / WM) + i * 16 + it * AT_ONCE + o_row, M - 1), min(col, N - 1));
+#pragma unroll
+        for (int it = 0; it < 16 / AT_ONCE; ++it) {
+            const int r = it * AT_ONCE + o_row;
+            v[it] = out_stage[r * CHUNKS + (o_chunk ^ (r & (CHUNKS - 1)))];
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int it = 0; it < 16 / AT_ONCE; ++it) {
+            const int64_t row = m0 + wm * (BM / WM) + i * 16 + it * AT_ONCE + o_row;
+            if (row < M && col < N) fp8_store4<EPI>(ep, row, col, v[it], old[it]);
+        }
     }
 }
 
@@ -317,8 +352,217 @@ gemm_fp8_slices_kernel(const unsigned char *__restrict__ A, const uint32_t *__re
         const int r = g / (BN / 4), c = g % (BN / 4) * 4;
         if (m0 + r >= M || n0 + c >= N) continue;
         f32x4_t v = fp8_bias4(ep, n0 + c);
+        const f32x4_t old = fp8_old4<EPI>(ep, m0 + r, n0 + c);
 #pragma unroll
         for (int w = 0; w < NW; ++w) v += *reinterpret_cast<const f32x4_t *>(part + w * (WAVE / 4) + r * RS + c);
-        fp8_store4<EPI>(ep, m0 + r, n0 + c, v);
+        fp8_store4<EPI>(ep, m0 + r, n0 + c, v, old);
     }
+}
+
+// ------------------------------------------------------------------ large products with a bf16 output
+// A 256 x 256 tile by eight wavefronts (2 x 4, 128 x 64 each, v_mfma_scale_f32_32x32x64_f8f6f4), persistent: one work-group per CU walks
+// its tiles, and the LDS ring runs from one tile into the next.  The bytes move as in gemm_bf16_persist_kernel (gemm_persist.hpp): LDS is a
+// ring of five units of 32 KB, each 256 rows x 128 bytes of A or W in the swizzled layout; block T has A in unit 2T mod 5 and W in unit
+// 2T + 1 mod 5:
+//     half 0 of T: products of its first 64 k | operands of its second half | loads of A of T+2 (unit 2T+4: W of T-1 is done)
+//     half 1 of T, its first two products; barrier: T+1 has landed, T has been read by all
+//     the others of the second 64 k | operands of T+1's first half | loads of W of T+2 (unit 2T: A of T is done)
+// An operand of A is read for the next half behind the two products that use it in this one, into the same registers.  The ring is all of the LDS, so the scales are in registers: the words of four blocks for this lane's rows, the lowest byte in use, and
+// those of the next four, requested when the last ones begin to be used.
+constexpr int kFp8PersistLds = 160 * 1024;
+template <int EPI>
+__global__ void __launch_bounds__(512)
+gemm_fp8_persist_kernel(const unsigned char *__restrict__ A, const uint32_t *__restrict__ sa, const unsigned char *__restrict__ W,
+                        const uint32_t *__restrict__ sw, int64_t M, int N, int Kp, Fp8Epi ep)
+{
+    static_assert(!kFp8Exact<EPI>, "bf16 outputs");
+    constexpr int BM = 256, BN = 256, WN = 4, WTM = 128, WTN = 64, TM = 4, TN = 2;
+    constexpr int UNITS = 5, UNIT = 256 * 128, LD_IT = UNIT / 16 / 512;
+    static_assert(UNITS * UNIT <= kFp8PersistLds, "the ring is the LDS");
+    extern __shared__ __align__(16) unsigned char fp8_smem[];
+    const unsigned ring = fp8_lds_address(fp8_smem);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WN, wn = wave % WN, l32 = lane & 31, lq = lane >> 5;
+    const int nbm = (int)((M + BM - 1) / BM), nbn = (N + BN - 1) / BN, nblk = nbm * nbn;
+    const int KT = Kp / 128, KG = (KT + 3) / 4;      // KT >= 2 (the launcher checks)
+
+    // one wavefront's load: 8 rows x 128 bytes, lane (r = l >> 3, slot = l & 7) fetches chunk slot ^ swz(r) of its row
+    const int ld_r = tid >> 3, ld_voff = ld_r * Kp + (((tid & 7) ^ swz_of_row(ld_r)) << 4);
+    auto dma_one = [&](int i, const u32x4_t &rs, int kt, unsigned unit) {
+        fp8_dma16(ring + unit + (i * 64 + wave * 8) * 128, rs, ld_voff, i * 64 * Kp + kt * 128);
+    };
+    struct Tile {
+        int64_t m0;
+        int n0;
+        u32x4_t ra, rw;
+    };
+    auto tile_at = [&](int v) {
+        Tile t;
+        const bool exists = v < nblk;
+        int bm, bn;
+        tile_of_pid(exists ? v : 0, nbm, nbn, bm, bn);
+        t.m0 = (int64_t)bm * BM;
+        t.n0 = bn * BN;
+        t.ra = fp8_descriptor(A + t.m0 * Kp, exists ? (int)min((int64_t)BM, M - t.m0) * Kp : 0);
+        t.rw = fp8_descriptor(W + (int64_t)t.n0 * Kp, exists ? min(BN, N - t.n0) * Kp : 0);
+        return t;
+    };
+#define FP8_WAIT_VM(n) __builtin_amdgcn_s_waitcnt(0x0F70 | ((n) & 15) | (((n) >> 4) << 14))
+    auto lds_barrier = [] {                          // orders LDS accesses only
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    };
+    // the scales of group g: rows that do not exist take those of the last one (their results are not stored)
+    uint32_t ca[TM], cw[TN], na[TM], nw[TN];
+    auto request_scales = [&](const Tile &t, int g) {
+        const uint32_t *pa = sa + (int64_t)g * M, *pw = sw + (int64_t)g * N;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) na[i] = pa[min(t.m0 + wm * WTM + i * 32 + l32, M - 1)];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) nw[j] = pw[min(t.n0 + wn * WTN + j * 32 + l32, N - 1)];
+    };
+    auto take_scales = [&] {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) ca[i] = na[i];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) cw[j] = nw[j];
+    };
+
+    // LDS byte offsets of this lane's first chunk of half 0; its second lies at ^ 16, those of half 1 at ^ 64
+    typedef const __attribute__((address_space(3))) u32x4_t lds_frag;
+    const unsigned a_lds = ring + (wm * WTM + l32) * 128 + (((2 * lq) ^ swz_of_row(l32)) << 4);
+    const unsigned w_lds = ring + (wn * WTN + l32) * 128 + (((2 * lq) ^ swz_of_row(l32)) << 4);
+    i32x8_t fa[TM], fw[2][TN];
+    f32x16_t acc[TM][TN];
+    auto fragment = [](unsigned at) {
+        const u32x4_t x = *(lds_frag *)(unsigned long long)at, y = *(lds_frag *)(unsigned long long)(at ^ 16);
+        return i32x8_t{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+    };
+    auto read_a = [&](int i, int h, unsigned ua) { fa[i] = fragment((a_lds ^ (h * 64)) + ua + i * (32 * 128)); };
+    auto read_w = [&](int j, int h, unsigned uw) { fw[h][j] = fragment((w_lds ^ (h * 64)) + uw + j * (32 * 128)); };
+    // products of half h; behind them the operands of the other half from units ua, uw, and a unit's loads
+    auto half = [&](auto h_, auto &&before_reads, unsigned ua, unsigned uw, const u32x4_t &rs, int kt, unsigned unit) {
+        constexpr int h = decltype(h_)::value;
+        static_for<0, TM>([&](auto i_) {
+            constexpr int i = decltype(i_)::value;
+            static_for<0, TN>([&](auto j_) {
+                constexpr int j = decltype(j_)::value;
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[h][j], fa[i], acc[i][j], 0, 0, 0, (int)cw[j], 0, (int)ca[i]);
+            });
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (i == 0) before_reads();
+            read_a(i, 1 - h, ua);
+            if constexpr (i < TN) read_w(i, 1 - h, uw);
+            dma_one(i, rs, kt, unit);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    static_assert(LD_IT == TM, "a load behind the products of each operand");
+    constexpr std::integral_constant<int, 0> h0{};
+    constexpr std::integral_constant<int, 1> h1{};
+
+    int v = blockIdx.x;                              // gridDim.x <= nblk: every work-group has a first tile
+    Tile cur = tile_at(v);
+    request_scales(cur, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    static_for<0, LD_IT>([&](auto i_) { dma_one(decltype(i_)::value, cur.ra, 0, 0); });
+    static_for<0, LD_IT>([&](auto i_) { dma_one(decltype(i_)::value, cur.rw, 0, UNIT); });
+    static_for<0, LD_IT>([&](auto i_) { dma_one(decltype(i_)::value, cur.ra, 1, 2 * UNIT); });
+    static_for<0, LD_IT>([&](auto i_) { dma_one(decltype(i_)::value, cur.rw, 1, 3 * UNIT); });
+    FP8_WAIT_VM(0);                                  // the scales and blocks 0 and 1 are there
+    lds_barrier();
+    take_scales();
+    unsigned u = 0;                                  // unit of A of this block; the five units from there on:
+    auto at = [&](unsigned k) { const unsigned x = u + k; return (x >= UNITS ? x - UNITS : x) * UNIT; };
+    for (;;) {
+        const int vn = v + (int)gridDim.x;
+        const Tile nxt = tile_at(vn);                // of zero size behind the last tile
+        // (the last block's half 1 has read these too, but they are not held across the epilogue, which has no registers for them)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) read_w(j, 0, at(1));
+#pragma unroll
+        for (int i = 0; i < TM; ++i) read_a(i, 0, at(0));
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.0f;
+        for (int kt = 0; kt < KT; ++kt) {
+            if ((kt & 3) == 0) {
+                if (kt) {                            // the next scales have landed (and what else is on its way, requested most of a half ago)
+                    FP8_WAIT_VM(0);
+                    take_scales();
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                const bool last = kt + 4 >= KT;
+                request_scales(last ? nxt : cur, last ? 0 : (kt >> 2) + 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            const bool ahead = kt + 2 >= KT;
+            const u32x4_t ra = ahead ? nxt.ra : cur.ra, rw = ahead ? nxt.rw : cur.rw;
+            const int kq = ahead ? kt + 2 - KT : kt + 2;
+            half(h0, [] {}, at(0), at(1), ra, kq, at(4));
+            half(h1, [&] {
+                if (kt) FP8_WAIT_VM(LD_IT);          // block T+1 has landed
+                lds_barrier();                       // ... for everyone, and T's units are free
+            }, at(2), at(3), rw, kq, at(0));
+            u = u + 2 >= UNITS ? u + 2 - UNITS : u + 2;
+#pragma unroll
+            for (int i = 0; i < TM; ++i) ca[i] >>= 8;
+#pragma unroll
+            for (int j = 0; j < TN; ++j) cw[j] >>= 8;
+        }
+        // The next tile's first scales and its blocks 0 and 1, waited for in front of the stores: stores count as loads do, and a wait
+        // behind them would be one for them.
+        FP8_WAIT_VM(0);
+        take_scales();
+        // The epilogue: acc[i][j][4 g + k] of lane (lq, l32) is row 32 i + l32, column 32 j + 8 g + 4 lq + k of the wave tile.  32 rows at a
+        // time pass through a wave-private stage of 32 x 64 bf16 in the unit of the last block's W, free since that block's barrier: 16-byte
+        // chunk c of row r at chunk c ^ (r & 7).
+        int tid_e = threadIdx.x;                     // (an opaque copy: addresses formed here are not held across the k loop)
+        asm volatile("" : "+v"(tid_e));
+        const int le = tid_e & 63, row_e = le & 31, half_e = le >> 5, n_wave = cur.n0 + wn * WTN;
+        unsigned char *stage = fp8_smem + at(4) + wave * 4096;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    f32x4_t x = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+                    if (ep.bias) x += fp8_bias4(ep, n_wave + 32 * j + 8 * g + 4 * half_e);
+                    if constexpr (EPI == EPI_GELU) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) x[k] = gelu_bf16out(x[k]);
+                    }
+                    const bf16x4_t o = {(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
+                    *reinterpret_cast<bf16x4_t *>(stage + row_e * 128 + (((4 * j + g) ^ (row_e & 7)) << 4) + half_e * 8) = o;
+                }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                const int r = it * 8 + (le >> 3), c = le & 7, col = n_wave + c * 8;
+                const bf16x8_t o = *reinterpret_cast<const bf16x8_t *>(stage + r * 128 + ((c ^ (r & 7)) << 4));
+                const int64_t row = cur.m0 + wm * WTM + i * 32 + r;
+                if (row >= M || col >= N) continue;
+                bf16 *to = static_cast<bf16 *>(ep.out) + row * N + col;
+                if (col + 8 <= N) {
+                    __builtin_memcpy(to, &o, 16);
+                } else {
+                    const bf16 *from = reinterpret_cast<const bf16 *>(stage + r * 128 + ((c ^ (r & 7)) << 4));
+#pragma unroll 1
+                    for (int k = 0; col + k < N; ++k) to[k] = from[k];
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+        if (vn >= nblk) break;                       // (block-uniform)
+        v = vn;
+        cur = nxt;
+        lds_barrier();                               // every wave has read its stage back: the unit can be filled
+    }
+    FP8_WAIT_VM(0);                                  // (the loads behind the last tile, of zero size)
+#undef FP8_WAIT_VM
 }

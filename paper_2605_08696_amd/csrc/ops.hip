@@ -146,21 +146,50 @@ static int launch_fp8_tile(const Fp8Call &c)
 {
     return launch_fp8<gemm_fp8_tile_kernel<BM, BN, WM, WN, NS, EPI>>(cdiv(c.M, BM) * cdiv(c.N, BN), WM * WN * 64, NS * fp8_stage_bytes<BM, BN>(), c);
 }
+template <int EPI>
+static int launch_fp8_persist(const Fp8Call &c, int64_t cus)
+{
+    if (cdiv(c.M, 256) * cdiv(c.N, 256) >= (1 << 30)) return fail(SRM_EINVAL, "srm_linear_fp8: sizes out of range");
+    return launch_fp8<gemm_fp8_persist_kernel<EPI>>(std::min(cdiv(c.M, 256) * cdiv(c.N, 256), cus), 512, kFp8PersistLds, c);
+}
 template <int RT, int CT, int NS, int EPI>
 static int launch_fp8_slices(const Fp8Call &c)
 {
     return launch_fp8<gemm_fp8_slices_kernel<RT, CT, NS, EPI>>(cdiv(c.M, 16 * RT) * cdiv(c.N, 16 * CT), kFp8SliceWaves * 64,
                                                               kFp8SliceWaves * fp8_slice_lds<RT, CT, NS>(), c);
 }
+// Which kernel.  Measured (graphs of launches over matrices in turn, us, rows x columns x K):
+//   K cut over the wavefronts while a launch is one round of the chip: 16x16 | 32x32 | 64x64 | 64x64 tile of four wavefronts:
+//     64 x 1024 x 4096 4.2 | 5.4 | 9.0 | 14.0; 37 x 4096 x 1024 4.9 | 3.6 | 5.2 | 5.3; 700 x 1024 x 4096 21 | 11.7 | 9.6 | 14.3;
+//     300 x 4096 x 1024 20 | 9.4 | 9.3 | 6.7 (two rounds of the 64x64 form)
+//   up to 16 rows of many columns are bound by reading W: 16x32 | 16x16 | 32x32: 16 x 32000 x 4096 28.3 | 30.0 | 29.5, 1 x 32000 x 1024
+//     8.4 | 11.4 | 9.2 (W at 3.9 to 5.9 TB/s)
+//   64x64 with a ring of two | four | 128x128: 300 x 4096 x 1024 6.7 | 6.9 | 8.6, 2048 x 1024 x 4096 18.1 | 17.5 | 23.8, 700 x 4096 x 1024
+//     9.0 | 11.1 | 9.4, 1024 x 4096 x 4096 33.0 | 36.6 | 30.4
+//   256x256 persistent | 128x128 by eight wavefronts: 8192^3 412 | 582, 4096^3 55.5 | 85, 3001 x 4001 x 1024 18.2 | 19.7, but 2048 x 4096 x 4096
+//     (128 tiles for 256 CUs) 47.5 | 39.7: a tile of 256x256 takes 0.7 of the time of four tiles of 128x128, two of which a CU holds
+//   fp32 outputs, 128x128 by four | eight wavefronts: 8192^3 892 | 1010, 16384 x 1024 x 4096 (+=) 133 | 143, 3001 x 4001 x 1024 (+=) 39.9 | 35.4
 template <int EPI>
 static int linear_fp8(const Fp8Call &c)
 {
-    const int cus = device_cus();
+    const int64_t cus = device_cus();
     if (cus <= 0) return fail(SRM_EHIP, "cannot read the number of compute units");
-    auto fits = [&](int rt, int ct) { return cdiv(c.M, 16 * rt) * cdiv(c.N, 16 * ct) <= 2 * cus; };
-    if (fits(1, 1)) return launch_fp8_slices<1, 1, 2, EPI>(c);
-    if (fits(2, 2)) return launch_fp8_slices<2, 2, 1, EPI>(c);
-    return launch_fp8_tile<128, 128, 2, 2, 2, EPI>(c);
+    auto tiles = [&](int bm, int bn) { return cdiv(c.M, bm) * cdiv(c.N, bn); };
+    if (tiles(16, 16) <= cus) return launch_fp8_slices<1, 1, 2, EPI>(c);
+    if (c.M <= 16) return launch_fp8_slices<1, 2, 1, EPI>(c);
+    if (tiles(32, 32) <= 2 * cus) return launch_fp8_slices<2, 2, 1, EPI>(c);
+    if (tiles(64, 64) <= cus) return launch_fp8_slices<4, 4, 1, EPI>(c);
+    const int64_t rounds = cdiv(tiles(128, 128), 2 * cus);
+    if constexpr (!kFp8Exact<EPI>) {
+        if (c.Kp >= 256 && 10 * cdiv(tiles(256, 256), cus) <= 7 * rounds) return launch_fp8_persist<EPI>(c, cus);
+    }
+    if (tiles(128, 128) >= cus) {
+        if constexpr (kFp8Exact<EPI>) {
+            if (tiles(128, 128) >= 2 * cus && (EPI == EPI_F32 || c.Kp >= 2048)) return launch_fp8_tile<128, 128, 2, 2, 2, EPI>(c);
+        }
+        return launch_fp8_tile<128, 128, 2, 4, 2, EPI>(c);
+    }
+    return tiles(64, 64) <= 2 * cus ? launch_fp8_tile<64, 64, 2, 2, 4, EPI>(c) : launch_fp8_tile<64, 64, 2, 2, 2, EPI>(c);
 }
 
 extern "C" int srm_linear_fp8(int32_t epilogue, const void *d_a, const void *d_a_scales, const void *d_w, const void *d_w_scales,
