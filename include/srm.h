@@ -607,7 +607,8 @@ size_t srm_linear_argmax_noalloc_max_bytes(void);
  *
  * srm_quantize_fp8: d_x [rows][K] of type dtype (SRM_FP32 | SRM_BF16), row stride ldx elements, at any multiple of an element ->
  * q, scales.  For weights once, and for activations between two products.
- * Errors: SRM_EINVAL (null pointer, rows or K <= 0, rows >= 2^31, K > 2^22, ldx < K, unknown dtype, misaligned q or scales).
+ * Errors: SRM_EINVAL (null pointer, rows or K <= 0, rows times ceil(K / 512) >= 2^31 - 4, K > 2^22, ldx < K, unknown dtype,
+ * misaligned q or scales).
  *
  * srm_rmsnorm_fp8: the residual addition and root-mean-square norm in front of a product:
  *   x <- x + add  (d_add may be NULL: x is only read then)      y = x / sqrt(mean(x^2) + eps) * gain      y -> q, scales

@@ -20,30 +20,81 @@ __device__ __forceinline__ uint32_t row16_max_u32(uint32_t v)
     return v;
 }
 
-// Eight consecutive elements from any address of whole elements (gfx950 loads 16 bytes from unaligned ones); n of them exist.
-__device__ __forceinline__ void load8(const float *p, int n, float (&v)[8])
+// Eight consecutive elements of a row from index `col` on, in two steps, so that several requests travel together: a load without a
+// branch (16 bytes from any address of whole elements, which gfx950 allows; the row's last eight where it ends before), and behind it
+// their values, zeros behind the row.  (With a branch around each load, the compiler waits for every load at its end: 16384 x 1024
+// fp32 rows + bf16 40.6 us, 35 without.)  ONCE: what nothing reads again soon, with the streaming hint.
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<float> {
+    f32x4_t a, b;
+};
+template <>
+struct Raw8<bf16> {
+    bf16x8_t a;
+};
+template <bool ONCE = false>
+__device__ __forceinline__ Raw8<float> raw8(const float *row, int col, int d)
 {
-    if (n >= 8) {
-        f32x4_t a, b;
-        __builtin_memcpy(&a, p, 16);
-        __builtin_memcpy(&b, p + 4, 16);
+    typedef f32x4_t __attribute__((aligned(4))) unaligned;
+    Raw8<float> r;
+    if (d < 8) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.0f;
+        for (int i = 0; i < 8; ++i) {
+            const float x = col + i < d ? row[col + i] : 0.0f;
+            if (i < 4) r.a[i] = x; else r.b[i - 4] = x;
+        }
+        return r;
     }
-}
-__device__ __forceinline__ void load8(const bf16 *p, int n, float (&v)[8])
-{
-    if (n >= 8) {
-        bf16x8_t a;
-        __builtin_memcpy(&a, p, 16);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
+    const unaligned *q = reinterpret_cast<const unaligned *>(row + min(col, d - 8));
+    if constexpr (ONCE) {
+        r.a = __builtin_nontemporal_load(q);
+        r.b = __builtin_nontemporal_load(q + 1);
     } else {
+        r.a = q[0];
+        r.b = q[1];
+    }
+    return r;
+}
+template <bool ONCE = false>
+__device__ __forceinline__ Raw8<bf16> raw8(const bf16 *row, int col, int d)
+{
+    typedef bf16x8_t __attribute__((aligned(2))) unaligned;
+    Raw8<bf16> r;
+    if (d < 8) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? (float)p[i] : 0.0f;
+        for (int i = 0; i < 8; ++i) r.a[i] = col + i < d ? row[col + i] : (bf16)0.0f;
+        return r;
+    }
+    const unaligned *q = reinterpret_cast<const unaligned *>(row + min(col, d - 8));
+    if constexpr (ONCE) r.a = __builtin_nontemporal_load(q);
+    else r.a = *q;
+    return r;
+}
+__device__ __forceinline__ void raw8_values(const Raw8<float> &r, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[i] = r.a[i]; v[4 + i] = r.b[i]; }
+}
+__device__ __forceinline__ void raw8_values(const Raw8<bf16> &r, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)r.a[i];
+}
+template <typename T>
+__device__ __forceinline__ void widen8(const Raw8<T> &r, int col, int d, float (&v)[8])
+{
+    raw8_values(r, v);
+    if (d >= 8 && __ballot(col + 8 > d)) {           // some lane's eight are the row's last: moved to their places
+        const int late = col + 8 - d;                // by which they lie too high
+#pragma unroll
+        for (int s = 4; s >= 1; s >>= 1)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (late > 0 && (late & s)) v[i] = i + s < 8 ? v[i + s] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = col + i < d ? v[i] : 0.0f;
     }
 }
 // v as it is stored at p, rounded to p's type
@@ -101,22 +152,22 @@ __device__ __forceinline__ uint2 fp8_of_8(const float (&v)[8], uint32_t &scales)
     return make_uint2((uint32_t)lo, (uint32_t)hi);
 }
 
-// x [rows][d], row stride ldx -> q [rows][dp], dp = d rounded up to 128, and scales [groups][rows].  One wavefront per row and group.
+// x [rows][d], row stride ldx -> q [rows][dp], dp = d rounded up to 128, and scales [groups][rows].  A wavefront takes a group of a row,
+// those of a row side by side.  (16384 x 1024 fp32: 16.0 us, 5.2 TB/s; with the groups of a column of rows side by side 17.5, with two or
+// four rows a wavefront 16.9 and 17.7.)
 template <typename T>
 __global__ void __launch_bounds__(256)
-quantize_fp8_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int d, unsigned char *__restrict__ q, uint32_t *__restrict__ scales)
+quantize_fp8_kernel(const T *__restrict__ x, int64_t ldx, uint32_t rows, int d, unsigned char *__restrict__ q, uint32_t *__restrict__ scales)
 {
-    const int groups = (d + kFp8Group - 1) / kFp8Group, dp = (d + kFp8Block - 1) / kFp8Block * kFp8Block;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int64_t row = unit / groups;
-    const int g = (int)(unit - row * groups), lane = threadIdx.x & 63;
-    if (row >= rows) return;
-    const int col = g * kFp8Group + lane * 8;
+    const uint32_t groups = (uint32_t)(d + kFp8Group - 1) / kFp8Group, unit = blockIdx.x * 4 + (threadIdx.x >> 6);      // < 2^31
+    const uint32_t row = unit / groups, g = unit - row * groups;
+    if (row >= rows) return;                         // wave-uniform
+    const int dp = (d + kFp8Block - 1) / kFp8Block * kFp8Block, lane = threadIdx.x & 63, col = (int)g * kFp8Group + lane * 8;
     float v[8];
-    load8(x + row * ldx + col, d - col, v);
+    widen8(raw8<true>(x + row * ldx, col, d), col, d, v);
     uint32_t s;
     const uint2 codes = fp8_of_8(v, s);
-    if (col < dp) *reinterpret_cast<uint2 *>(q + row * dp + col) = codes;
+    if (col < dp) *reinterpret_cast<uint2 *>(q + (int64_t)row * dp + col) = codes;
     if (lane == 0) scales[(int64_t)g * rows + row] = s;
 }
 
@@ -133,33 +184,40 @@ rmsnorm_fp8_kernel(T *__restrict__ x, int64_t ldx, const TAdd *__restrict__ add,
     const int64_t row = (int64_t)blockIdx.x * ROWS + wave / NW;
     const int groups = (d + kFp8Group - 1) / kFp8Group, dp = (d + kFp8Block - 1) / kFp8Block * kFp8Block;
     const bool in = row < rows;
+    const int64_t at = in ? row : rows - 1;
     float v[G][8], sum = 0.0f;
-    if (in) {
+    Raw8<T> rx[G];
+    Raw8<TAdd> ra[G];
+    // up to 1024 elements a wavefront the gain is requested with the row, so that its latency does not follow the sum
+    constexpr bool EARLY = G <= 2;
+    Raw8<float> rg[G];
+#pragma unroll
+    for (int i = 0; i < G; ++i) rx[i] = raw8(x + at * ldx, (w + i * NW) * kFp8Group + lane * 8, d);
+    if (add) {
+#pragma unroll
+        for (int i = 0; i < G; ++i) ra[i] = raw8<true>(add + at * ld_add, (w + i * NW) * kFp8Group + lane * 8, d);
+    }
+    if constexpr (EARLY) {
+#pragma unroll
+        for (int i = 0; i < G; ++i) rg[i] = raw8(gain, (w + i * NW) * kFp8Group + lane * 8, d);
+    }
+#pragma unroll
+    for (int i = 0; i < G; ++i) widen8(rx[i], (w + i * NW) * kFp8Group + lane * 8, d, v[i]);
+    if (add) {
 #pragma unroll
         for (int i = 0; i < G; ++i) {
             const int col = (w + i * NW) * kFp8Group + lane * 8;
-            load8(x + row * ldx + col, d - col, v[i]);
+            float t[8];
+            widen8(ra[i], col, d, t);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[i][k] += t[k];
+            store8(x + at * ldx + col, in ? d - col : 0, v[i]);
         }
-        if (add) {
-#pragma unroll
-            for (int i = 0; i < G; ++i) {
-                const int col = (w + i * NW) * kFp8Group + lane * 8;
-                float t[8];
-                load8(add + row * ld_add + col, d - col, t);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[i][k] += t[k];
-            }
-#pragma unroll
-            for (int i = 0; i < G; ++i) {
-                const int col = (w + i * NW) * kFp8Group + lane * 8;
-                store8(x + row * ldx + col, d - col, v[i]);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < G; ++i)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) sum = fmaf(v[i][k], v[i][k], sum);
     }
+#pragma unroll
+    for (int i = 0; i < G; ++i)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum = fmaf(v[i][k], v[i][k], sum);
     sum = wave_sum(sum);
     if constexpr (NW > 1) {
         if (lane == 0) part[wave] = sum;
@@ -175,7 +233,8 @@ rmsnorm_fp8_kernel(T *__restrict__ x, int64_t ldx, const TAdd *__restrict__ add,
         const int g = w + i * NW, col = g * kFp8Group + lane * 8;
         if (g >= groups) break;                      // wave-uniform
         float t[8];
-        load8(gain + col, d - col, t);
+        if constexpr (!EARLY) rg[i] = raw8(gain, col, d);
+        widen8(rg[i], col, d, t);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[i][k] = col + k < d ? v[i][k] * r * t[k] : 0.0f;          // (r may be a NaN)
         uint32_t s;

@@ -33,9 +33,9 @@ constexpr int32_t kMaxWidth = 1 << 22;                // (256 rows of a tile are
 template <typename T>
 static int quantize(const void *d_x, int64_t ldx, int64_t rows, int32_t K, void *d_q, void *d_scales, hipStream_t st)
 {
-    const int64_t blocks = cdiv(rows * cdiv(K, kFp8Group), 4);
-    if (blocks >= (1ll << 31)) return fail(SRM_EINVAL, "srm_quantize_fp8: sizes out of range");
-    hipLaunchKernelGGL(quantize_fp8_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, st, static_cast<const T *>(d_x), ldx, rows, K,
+    const int64_t units = rows * cdiv(K, kFp8Group);
+    if (units >= (1ll << 31) - 4) return fail(SRM_EINVAL, "srm_quantize_fp8: sizes out of range");
+    hipLaunchKernelGGL(quantize_fp8_kernel<T>, dim3((unsigned)cdiv(units, 4)), dim3(256), 0, st, static_cast<const T *>(d_x), ldx, (uint32_t)rows, K,
                        static_cast<unsigned char *>(d_q), static_cast<uint32_t *>(d_scales));
     HIP_TRY(hipGetLastError());
     return SRM_OK;

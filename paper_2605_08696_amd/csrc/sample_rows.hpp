@@ -155,8 +155,8 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     bool hot = false;                                // an infinite logit leaves all others without weight: see below
 
     // eight logits from `at` on, -infinity behind the row
-    auto read = [&](int at, float (&v)[8]) SR_INLINE { load8(L + at, V - at, v); };
-    auto complete = [&](int at, float (&v)[8]) SR_INLINE {
+    auto complete = [&](const Raw8<T> &raw, int at, float (&v)[8]) SR_INLINE {
+        widen8(raw, at, V, v);
         if (__ballot(at + 8 > V)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = at + i < V ? v[i] : -INFINITY;
@@ -170,15 +170,13 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     auto pass = [&](auto &&fn) SR_INLINE {
         constexpr int STEP = NW * kSampleSegment;
         int at = wave * kSampleSegment + lane * 8;
-        float v[8];
-        read(at, v);
+        Raw8<T> raw = raw8(L, at, V);
         for (int first = wave * kSampleSegment; first < V; first += STEP) {
-            float next[8];
-            read(at + STEP, next);
-            complete(at, v);
+            const Raw8<T> next = raw8(L, at + STEP, V);
+            float v[8];
+            complete(raw, at, v);
             fn(v, at);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = next[i];
+            raw = next;
             at += STEP;
         }
     };
@@ -260,10 +258,10 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         if (own_most == most)
             for (int at = wave * kSampleSegment + lane * 8; at < V && first == V; at += NW * kSampleSegment) {
                 float v[8];
-                read(at, v);
+                complete(raw8(L, at, V), at, v);
 #pragma unroll
                 for (int i = 7; i >= 0; --i)
-                    if (at + i < V && v[i] == most) first = at + i;
+                    if (v[i] == most) first = at + i;
             }
         first = ~(int)sample_wave_max(~(uint32_t)first);
         __syncthreads();
@@ -364,8 +362,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
                 for (int i = 0; i < 8; ++i) m[i] = weights[lane * 8 + i];
             } else {
                 float v[8];
-                read(at, v);
-                complete(at, v);
+                complete(raw8(L, at, V), at, v);
                 of(v, at, m);
             }
 #pragma unroll
