@@ -215,6 +215,14 @@ extern "C" int srm_linear_fp8(int32_t epilogue, const void *d_a, const void *d_a
 }
 
 // ------------------------------------------------------------------ sampling by request
+// Work-groups of 1024 threads while each row has a CU of its own, behind that of 512, of which a CU holds two to four.
+template <typename T>
+static void launch_sample(const void *d_logits, int64_t rows, const SampleRows &p, bool wide, hipStream_t st)
+{
+    if (wide) hipLaunchKernelGGL((sample_rows_kernel<T, 1024>), dim3((unsigned)rows), dim3(1024), 0, st, static_cast<const T *>(d_logits), p);
+    else hipLaunchKernelGGL((sample_rows_kernel<T, 512>), dim3((unsigned)rows), dim3(512), 0, st, static_cast<const T *>(d_logits), p);
+}
+
 extern "C" int srm_sample_rows(int32_t dtype, const void *d_logits, int64_t ld, int64_t rows, int32_t vocab, const float *d_temperature,
                                const int32_t *d_top_k, const float *d_top_p, const float *d_min_p, const float *d_uniform,
                                int32_t *d_tok_out, float *d_logprob, void *hip_stream)
@@ -225,12 +233,10 @@ extern "C" int srm_sample_rows(int32_t dtype, const void *d_logits, int64_t ld, 
     if (ld < vocab) return fail(SRM_EINVAL, "%s: row stride %lld is less than %d", who, (long long)ld, vocab);
     const SampleRows p{ld, vocab, d_temperature, d_top_p, d_min_p, d_uniform, d_top_k, d_tok_out, d_logprob};
     hipStream_t st = as_stream(hip_stream);
-    if (dtype == SRM_FP32)
-        hipLaunchKernelGGL((sample_rows_kernel<float, 512>), dim3((unsigned)rows), dim3(512), 0, st, static_cast<const float *>(d_logits), p);
-    else if (dtype == SRM_BF16)
-        hipLaunchKernelGGL((sample_rows_kernel<bf16, 512>), dim3((unsigned)rows), dim3(512), 0, st, static_cast<const bf16 *>(d_logits), p);
-    else
-        return fail(SRM_EINVAL, "%s: unknown dtype %d", who, dtype);
+    const bool wide = rows <= device_cus();
+    if (dtype == SRM_FP32) launch_sample<float>(d_logits, rows, p, wide, st);
+    else if (dtype == SRM_BF16) launch_sample<bf16>(d_logits, rows, p, wide, st);
+    else return fail(SRM_EINVAL, "%s: unknown dtype %d", who, dtype);
     HIP_TRY(hipGetLastError());
     return SRM_OK;
 }

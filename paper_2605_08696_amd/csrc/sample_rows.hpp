@@ -409,21 +409,37 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         return (uint32_t)__builtin_amdgcn_readfirstlane((int)n_list);
     };
 
+    if (has_least) {                                 // min-p leaves few of most rows: those are listed
+        n = gather(floor_v, INFINITY);
+        in_list = n <= (uint32_t)kSampleList;
+    }
     // top-k (their number), then top-p (their mass): the kept tokens end at the first one with which a limit is reached
     for (int by_mass = 0; by_mass < 2; ++by_mass) {
         if (uniform(by_mass ? !(top_p < 1.0f) : top_k <= 0 || top_k >= V)) continue;
         auto limit_of = [&](sr_mass sum) SR_INLINE {
             return by_mass ? max((sr_mass)ceil((double)top_p * (double)sum), (sr_mass)1) : (sr_mass)top_k;
         };
-        const float scale = (float)kSampleSteps / (most - floor_v);
-        auto value_step = [&](float x) SR_INLINE { return (uint32_t)fminf((most - x) * scale, (float)(kSampleSteps - 1)); };
+        const float scale = (float)kSampleSteps / (most - floor_v), scaled = most * scale;
+        auto value_step = [&](float x) SR_INLINE { return (uint32_t)fminf(fmaf(x, -scale, scaled), (float)(kSampleSteps - 1)); };
         uint32_t low = 0, high = ~0u, step = 0;      // the keys that are left; the step of the table, of value while shift < 0
         int shift = -1;
         sr_mass before = 0, limit = 0, total;
         auto step_of = [&](float x) SR_INLINE { return shift < 0 ? value_step(x) : (high - sample_key(x)) >> shift; };
         auto in_keys = [&](uint32_t key) SR_INLINE { return key >= low && key <= high; };
         bool listed = false, all = false, whole = false;     // whole: all of the list is divided, not a step
-        if (!by_mass && top_k <= kSampleBound) {
+        if (in_list) {
+            clear();
+            for (uint32_t i = tid; i < n; i += NT) {
+                const float x = sample_value(list_key[i]);
+                if (kept(x, list_at[i])) {
+                    const sr_mass m = mass(x);
+                    if (m) atomicAdd(&table[value_step(x)], by_mass ? m : (sr_mass)1);
+                }
+            }
+            step = reached(before, [&](sr_mass sum) SR_INLINE { return limit = limit_of(sum); }, total);
+            all = step == ~0u;
+            listed = true;
+        } else if (!by_mass && top_k <= kSampleBound) {
             // top_k threads whose largest logit is at least a bound hold top_k logits that are: those above it are listed
             clear();
             uint32_t mine = ~0u;
@@ -443,15 +459,6 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
                 limit = (sr_mass)top_k;
                 if (listed) floor_v = bound;
             }
-        } else if (by_mass && in_list) {
-            clear();
-            for (uint32_t i = tid; i < n; i += NT) {
-                const float x = sample_value(list_key[i]);
-                if (kept(x, list_at[i])) atomicAdd(&table[value_step(x)], mass(x));
-            }
-            step = reached(before, [&](sr_mass sum) SR_INLINE { return limit = limit_of(sum); }, total);
-            all = step == ~0u;
-            listed = true;
         }
         while (!listed) {
             clear();
@@ -604,10 +611,20 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     const int tok = index_of([&](float x, int) SR_INLINE { return mass(x); }, masses, [&](const float (&v)[8], int at) SR_INLINE {
         sr_mass s = 0;
         uint32_t own = 8, upto = 8, some = kSampleSegment;
+        bool equal = false;                          // some logit of the vector equals cut_v
         if (cut) {
             own = 0;
+            unsigned long long eq = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) own += kept(v[i], at + i) ? 1u : 0u;
+            for (int i = 0; i < 8; ++i) {
+                own += v[i] > cut_v ? 1u : 0u;
+                eq |= __ballot(v[i] == cut_v);
+            }
+            equal = eq != 0;
+            if (equal) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) own += v[i] == cut_v && at + i <= cut_at ? 1u : 0u;
+            }
             upto = sample_wave_scan32(own);
             some = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
         }
@@ -620,7 +637,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
             float *to = dense + wave * kSampleDense + (upto - own);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (kept(v[i], at + i)) *to++ = v[i];
+                if (v[i] > cut_v || (equal && v[i] == cut_v && at + i <= cut_at)) *to++ = v[i];
             __builtin_amdgcn_wave_barrier();
             for (uint32_t j = lane; j < some + lane; j += 128) {
                 const float *at2 = dense + wave * kSampleDense;
