@@ -559,23 +559,22 @@ def _rows_of(t, name: str):
 def _launch(fn, args, first, others, stream):
     """fn(*args, stream) on the device of the tensors, which is that of `first`."""
     torch = _torch()
-    device = first.device
-    if device.type != "cuda":
+    index = first.get_device()
+    if index < 0:
         raise ValueError("operands must be CUDA tensors")
     for t in others:
-        if t is not None and t.device != device:
-            raise ValueError(f"operands on {device} and {t.device}")
-    index = device.index
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"operands on {first.device} and {t.device}")
     if stream is None:
         raw = torch._C._cuda_getCurrentRawStream(index)
-    elif stream.device != device:
-        raise ValueError(f"operands on {device}, stream on {stream.device}")
+    elif stream.device.index != index:
+        raise ValueError(f"operands on {first.device}, stream on {stream.device}")
     else:
         raw = stream.cuda_stream
     if index == torch._C._cuda_getDevice():
         rc = fn(*args, raw)
     else:
-        with torch.cuda.device(device):
+        with torch.cuda.device(index):
             rc = fn(*args, raw)
     if rc:
         raise SrmError(rc, lib().srm_last_error().decode())
