@@ -152,23 +152,31 @@ __device__ __forceinline__ uint2 fp8_of_8(const float (&v)[8], uint32_t &scales)
     return make_uint2((uint32_t)lo, (uint32_t)hi);
 }
 
-// x [rows][d], row stride ldx -> q [rows][dp], dp = d rounded up to 128, and scales [groups][rows].  A wavefront takes a group of a row,
-// those of a row side by side.  (16384 x 1024 fp32: 16.0 us, 5.2 TB/s; with the groups of a column of rows side by side 17.5, with two or
-// four rows a wavefront 16.9 and 17.7.)
-template <typename T>
+// x [rows][d], row stride ldx -> q [rows][dp], dp = d rounded up to 128, and scales [groups][rows].  A wavefront takes a group of R rows,
+// requested together; the groups of a row lie side by side.  (us, R = 1 | 2 | 4: 16384 x 1024 fp32 16.6 | 17 | 17.7, with the groups of a
+// column of rows side by side instead 18.2; 16384 x 4096 bf16 40.4 | 36.9 | 36.9 (5.5 TB/s), 3001 x 4001 bf16 8.9 | 8.4 | 9.4, 300 x 4096 bf16
+// 2.6 | 2.9 | 3.6.  With the streaming hint what the caches hold is read from memory: 3001 x 4001 9.5.)
+template <typename T, int R>
 __global__ void __launch_bounds__(256)
 quantize_fp8_kernel(const T *__restrict__ x, int64_t ldx, uint32_t rows, int d, unsigned char *__restrict__ q, uint32_t *__restrict__ scales)
 {
     const uint32_t groups = (uint32_t)(d + kFp8Group - 1) / kFp8Group, unit = blockIdx.x * 4 + (threadIdx.x >> 6);      // < 2^31
-    const uint32_t row = unit / groups, g = unit - row * groups;
-    if (row >= rows) return;                         // wave-uniform
+    const uint32_t row0 = unit / groups * R, g = unit % groups;
     const int dp = (d + kFp8Block - 1) / kFp8Block * kFp8Block, lane = threadIdx.x & 63, col = (int)g * kFp8Group + lane * 8;
-    float v[8];
-    widen8(raw8<true>(x + row * ldx, col, d), col, d, v);
-    uint32_t s;
-    const uint2 codes = fp8_of_8(v, s);
-    if (col < dp) *reinterpret_cast<uint2 *>(q + (int64_t)row * dp + col) = codes;
-    if (lane == 0) scales[(int64_t)g * rows + row] = s;
+    Raw8<T> raw[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) raw[r] = raw8(x + (int64_t)min(row0 + r, rows - 1) * ldx, col, d);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        float v[8];
+        widen8(raw[r], col, d, v);
+        uint32_t s;
+        const uint2 codes = fp8_of_8(v, s);
+        const uint32_t row = row0 + r;
+        if (row >= rows) return;                     // wave-uniform
+        if (col < dp) *reinterpret_cast<uint2 *>(q + (int64_t)row * dp + col) = codes;
+        if (lane == 0) scales[(int64_t)g * rows + row] = s;
+    }
 }
 
 // x += add (if there is one), then y = x / sqrt(mean(x^2) + eps) * gain of the row as it is stored -> q, scales.  NW wavefronts hold a

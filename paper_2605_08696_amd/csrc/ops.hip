@@ -30,15 +30,25 @@ static int check_fp8(const char *who, const void *d_q, const void *d_scales)
 constexpr int64_t kMaxRows = 1ll << 31;
 constexpr int32_t kMaxWidth = 1 << 22;                // (256 rows of a tile are addressed by 32 bits)
 
+template <typename T, int R>
+static int launch_quantize(const void *d_x, int64_t ldx, int64_t rows, int32_t K, void *d_q, void *d_scales, hipStream_t st)
+{
+    const int64_t blocks = cdiv(cdiv(rows, R) * cdiv(K, kFp8Group), 4);
+    hipLaunchKernelGGL((quantize_fp8_kernel<T, R>), dim3((unsigned)blocks), dim3(256), 0, st, static_cast<const T *>(d_x), ldx, (uint32_t)rows, K,
+                       static_cast<unsigned char *>(d_q), static_cast<uint32_t *>(d_scales));
+    HIP_TRY(hipGetLastError());
+    return SRM_OK;
+}
+// (two bf16 rows a wavefront, whose eight elements are half the bytes of fp32 ones, once there are some tens of wavefronts a CU)
 template <typename T>
 static int quantize(const void *d_x, int64_t ldx, int64_t rows, int32_t K, void *d_q, void *d_scales, hipStream_t st)
 {
     const int64_t units = rows * cdiv(K, kFp8Group);
     if (units >= (1ll << 31) - 4) return fail(SRM_EINVAL, "srm_quantize_fp8: sizes out of range");
-    hipLaunchKernelGGL(quantize_fp8_kernel<T>, dim3((unsigned)cdiv(units, 4)), dim3(256), 0, st, static_cast<const T *>(d_x), ldx, (uint32_t)rows, K,
-                       static_cast<unsigned char *>(d_q), static_cast<uint32_t *>(d_scales));
-    HIP_TRY(hipGetLastError());
-    return SRM_OK;
+    if constexpr (sizeof(T) == 2) {
+        if (units >= 8192) return launch_quantize<T, 2>(d_x, ldx, rows, K, d_q, d_scales, st);
+    }
+    return launch_quantize<T, 1>(d_x, ldx, rows, K, d_q, d_scales, st);
 }
 
 extern "C" int srm_quantize_fp8(int32_t dtype, const void *d_x, int64_t ldx, int64_t rows, int32_t K, void *d_q, void *d_scales,

@@ -54,7 +54,7 @@ def _words(s):
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("rows,d,pad,offset", [
     (1, 1, 0, 0), (3, 2, 0, 1), (1, 127, 0, 0), (2, 128, 0, 0), (5, 129, 3, 0), (4, 511, 1, 1), (7, 512, 0, 0), (3, 513, 0, 3), (64, 1000, 8, 0),
-    (1, 4096, 0, 0), (37, 4096, 0, 0), (33, 4097, 2, 5), (260, 640, 0, 0), (2, 70000, 0, 0)])
+    (1, 4096, 0, 0), (37, 4096, 0, 0), (33, 4097, 2, 5), (260, 640, 0, 0), (2, 70000, 0, 0), (4099, 1030, 0, 1)])
 def test_quantize_has_the_bits_of_the_format(srm, dtype, rows, d, pad, offset):
     rng = np.random.default_rng(rows * 1000 + d)
     x = _wide(rng, rows, d, pad, TYPES[dtype], offset)
