@@ -607,26 +607,26 @@ size_t srm_linear_argmax_noalloc_max_bytes(void);
  *
  * srm_quantize_fp8: d_x [rows][K] of type dtype (SRM_FP32 | SRM_BF16), row stride ldx elements, at any multiple of an element ->
  * q, scales.  For weights once, and for activations between two products.
- * Errors: SRM_EINVAL (null pointer, rows or K <= 0, rows times ceil(K / 512) >= 2^31 - 4, K > 2^22, ldx < K, unknown dtype,
- * misaligned q or scales).
+ * Errors: SRM_EINVAL (null pointer, rows or K <= 0, rows >= 2^30, rows times ceil(K / 512) >= 2^31, K > 2^22, ldx < K,
+ * unknown dtype, d_x not at a multiple of an element, misaligned q or scales).
  *
  * srm_rmsnorm_fp8: the residual addition and root-mean-square norm in front of a product:
  *   x <- x + add  (d_add may be NULL: x is only read then)      y = x / sqrt(mean(x^2) + eps) * gain      y -> q, scales
  * d_x [rows][d] of type dtype, row stride ldx; d_add [rows][d] of type add_dtype, row stride ld_add (ignored if NULL); d_gain [d]
  * fp32.  The sum is formed in fp32 and rounded to x's type; the norm is that of the row as it is stored, its mean of squares in
  * fp32, in an order that depends on d alone.
- * Errors: SRM_EINVAL (null pointer, rows or d <= 0, rows >= 2^31, d > 32768, a row stride < d, eps < 0 or NaN, unknown dtype,
- * misaligned q or scales).
+ * Errors: SRM_EINVAL (null pointer, rows or d <= 0, rows >= 2^30, d > 32768, a row stride < d, eps < 0 or NaN, unknown dtype,
+ * an operand not at a multiple of its element, misaligned q or scales).
  *
  * srm_linear_fp8: out = epilogue(A W^T + bias) of fp8 matrices A [M][K] and W [N][K], accumulated in fp32.  With a bf16 output the
  * matrix cores' 8-bit products are taken, which add eight neighbouring products within some 14 bits of the largest (1e-5 of a
  * result's size, where its rounding is 2e-3); with an fp32 output the operands are widened to bf16, with scales from 2^-117 to 2^119
  * exactly (a block of smaller or larger ones may flush to 0 or overflow), and nothing is lost but the roundings of fp32 sums, at
- * half the rate.  d_bias [N] fp32 or NULL.  Epilogues as in srm_linear: 0 = store bf16, 1 = exact GELU then store bf16, 2 = add into fp32 d_out (residual), 4 = store
- * fp32 (3, the fused argmax, does not exist here: srm_sample_rows with temperature 0 chooses from stored logits).  d_out is
+ * half the rate.  d_bias [N] fp32 or NULL.  Epilogues as in srm_linear: 0 = store bf16, 1 = exact GELU then store bf16, 2 = add into
+ * fp32 d_out (residual), 4 = store fp32 (3, the fused argmax, does not exist here: srm_sample_rows with temperature 0 chooses from stored logits).  d_out is
  * [M][N], dense.  Any M, N and K.
- * Errors: SRM_EINVAL (null operand, scales or output, sizes <= 0, M >= 2^31, K > 2^22, misaligned operands, output or bias,
- * unknown epilogue).
+ * Errors: SRM_EINVAL (null operand, scales or output, sizes <= 0, M or N >= 2^30, 2^30 tiles, K > 2^22, misaligned operands,
+ * output or bias, unknown epilogue).
  *
  * srm_sample_rows: one token for each row of d_logits [rows][vocab] (dtype SRM_FP32 | SRM_BF16, row stride ld elements), with
  * parameters of its own; each parameter array is device memory of `rows` elements or NULL for "off".  With
@@ -640,7 +640,8 @@ size_t srm_linear_argmax_noalloc_max_bytes(void);
  * draw equally; a row that holds nothing else than -infinity gets token -1.  d_logprob[rows] (fp32, may be NULL): the logarithm of
  * the probability with which the token was drawn, 0 for a greedy row, -infinity with token -1.  Weights are held as whole numbers
  * of 2^-43 of the largest one, so that sums are exact and a result depends on its row alone; smaller weights are never drawn.
- * Errors: SRM_EINVAL (null logits, uniform or output, rows or vocab <= 0, rows >= 2^31, vocab > 2^20, ld < vocab, unknown dtype).
+ * Errors: SRM_EINVAL (null logits, uniform or output, rows or vocab <= 0, rows >= 2^30, vocab > 2^20, ld < vocab, unknown dtype,
+ * an operand not at a multiple of its element).
  */
 size_t srm_fp8_row_bytes(int32_t K);
 size_t srm_fp8_scale_bytes(int64_t rows, int32_t K);

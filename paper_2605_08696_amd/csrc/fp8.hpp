@@ -11,6 +11,11 @@
 
 constexpr int kFp8Block = 128, kFp8Group = 512;      // elements of a block, of a word of scales
 
+// A dimension of a grid holds less than 2^32 threads, which tens of millions of rows exceed: work-groups behind the first 2^21 are further
+// rows of the grid, the last of which may have more than there is work for.
+constexpr uint32_t kGridRow = 1u << 21;
+__device__ __forceinline__ uint32_t work_group() { return blockIdx.y * kGridRow + blockIdx.x; }
+
 __device__ __forceinline__ uint32_t row16_max_u32(uint32_t v)
 {
     v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));   // quad_perm [1,0,3,2]
@@ -160,7 +165,7 @@ template <typename T, int R>
 __global__ void __launch_bounds__(256)
 quantize_fp8_kernel(const T *__restrict__ x, int64_t ldx, uint32_t rows, int d, unsigned char *__restrict__ q, uint32_t *__restrict__ scales)
 {
-    const uint32_t groups = (uint32_t)(d + kFp8Group - 1) / kFp8Group, unit = blockIdx.x * 4 + (threadIdx.x >> 6);      // < 2^31
+    const uint32_t groups = (uint32_t)(d + kFp8Group - 1) / kFp8Group, unit = work_group() * 4 + (threadIdx.x >> 6);    // < 2^32
     const uint32_t row0 = unit / groups * R, g = unit % groups;
     const int dp = (d + kFp8Block - 1) / kFp8Block * kFp8Block, lane = threadIdx.x & 63, col = (int)g * kFp8Group + lane * 8;
     Raw8<T> raw[R];
@@ -189,7 +194,7 @@ rmsnorm_fp8_kernel(T *__restrict__ x, int64_t ldx, const TAdd *__restrict__ add,
     constexpr int ROWS = NW > 4 ? 1 : 4 / NW;        // rows of a work-group
     __shared__ float part[ROWS * NW];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, w = wave % NW;
-    const int64_t row = (int64_t)blockIdx.x * ROWS + wave / NW;
+    const int64_t row = (int64_t)work_group() * ROWS + wave / NW;
     const int groups = (d + kFp8Group - 1) / kFp8Group, dp = (d + kFp8Block - 1) / kFp8Block * kFp8Block;
     const bool in = row < rows;
     const int64_t at = in ? row : rows - 1;

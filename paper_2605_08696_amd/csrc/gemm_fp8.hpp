@@ -182,7 +182,9 @@ gemm_fp8_tile_kernel(const unsigned char *__restrict__ A, const uint32_t *__rest
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN, lr = lane & 15, lq = lane >> 4;
     int bm, bn;
-    tile_of_pid(blockIdx.x, (int)((M + BM - 1) / BM), (N + BN - 1) / BN, bm, bn);
+    const int nbm = (int)((M + BM - 1) / BM), nbn = (N + BN - 1) / BN, pid = (int)work_group();                       // < 2^30 + 2^21
+    if (pid >= nbm * nbn) return;
+    tile_of_pid(pid, nbm, nbn, bm, bn);
     const int64_t m0 = (int64_t)bm * BM;
     const int n0 = bn * BN, rows = (int)min((int64_t)BM, M - m0), cols = min(BN, N - n0), KT = Kp / 128;
     const u32x4_t ra = fp8_descriptor(A + m0 * Kp, rows * Kp), rw = fp8_descriptor(W + (int64_t)n0 * Kp, cols * Kp);
@@ -291,7 +293,9 @@ gemm_fp8_slices_kernel(const unsigned char *__restrict__ A, const uint32_t *__re
     extern __shared__ __align__(16) unsigned char fp8_smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lq = lane >> 4;
     int bm, bn;
-    tile_of_pid(blockIdx.x, (int)((M + BM - 1) / BM), (N + BN - 1) / BN, bm, bn);
+    const int nbm = (int)((M + BM - 1) / BM), nbn = (N + BN - 1) / BN, pid = (int)work_group();                       // < 2^30 + 2^21
+    if (pid >= nbm * nbn) return;
+    tile_of_pid(pid, nbm, nbn, bm, bn);
     const int64_t m0 = (int64_t)bm * BM;
     const int n0 = bn * BN, rows = (int)min((int64_t)BM, M - m0), cols = min(BN, N - n0), KT = Kp / 128;
     const u32x4_t ra = fp8_descriptor(A + m0 * Kp, rows * Kp), rw = fp8_descriptor(W + (int64_t)n0 * Kp, cols * Kp);

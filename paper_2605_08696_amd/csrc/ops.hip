@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "srm.h"
 #include "fp8.hpp"
@@ -11,6 +12,8 @@
 #include "status.hpp"
 
 static hipStream_t as_stream(void *s) { return static_cast<hipStream_t>(s); }
+// blocks < 2^30
+static dim3 grid_of(int64_t blocks) { return dim3((unsigned)std::min<int64_t>(blocks, kGridRow), (unsigned)cdiv(blocks, kGridRow)); }
 static bool misaligned(const void *p, unsigned to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
 
 // ------------------------------------------------------------------ 8-bit rows
@@ -27,14 +30,16 @@ static int check_fp8(const char *who, const void *d_q, const void *d_scales)
         return fail(SRM_EINVAL, "%s: 8-bit rows must lie at multiples of 16 bytes, their scales at multiples of 4", who);
     return SRM_OK;
 }
-constexpr int64_t kMaxRows = 1ll << 31;
+static unsigned size_of(int32_t dtype) { return dtype == SRM_BF16 ? 2 : 4; }
+static const char *const kNotWhole = "an operand does not lie at a whole element";
+constexpr int64_t kMaxRows = 1ll << 30;
 constexpr int32_t kMaxWidth = 1 << 22;                // (256 rows of a tile are addressed by 32 bits)
 
 template <typename T, int R>
 static int launch_quantize(const void *d_x, int64_t ldx, int64_t rows, int32_t K, void *d_q, void *d_scales, hipStream_t st)
 {
     const int64_t blocks = cdiv(cdiv(rows, R) * cdiv(K, kFp8Group), 4);
-    hipLaunchKernelGGL((quantize_fp8_kernel<T, R>), dim3((unsigned)blocks), dim3(256), 0, st, static_cast<const T *>(d_x), ldx, (uint32_t)rows, K,
+    hipLaunchKernelGGL((quantize_fp8_kernel<T, R>), grid_of(blocks), dim3(256), 0, st, static_cast<const T *>(d_x), ldx, (uint32_t)rows, K,
                        static_cast<unsigned char *>(d_q), static_cast<uint32_t *>(d_scales));
     HIP_TRY(hipGetLastError());
     return SRM_OK;
@@ -44,7 +49,7 @@ template <typename T>
 static int quantize(const void *d_x, int64_t ldx, int64_t rows, int32_t K, void *d_q, void *d_scales, hipStream_t st)
 {
     const int64_t units = rows * cdiv(K, kFp8Group);
-    if (units >= (1ll << 31) - 4) return fail(SRM_EINVAL, "srm_quantize_fp8: sizes out of range");
+    if (units >= 1ll << 31) return fail(SRM_EINVAL, "srm_quantize_fp8: sizes out of range");
     if constexpr (sizeof(T) == 2) {
         if (units >= 8192) return launch_quantize<T, 2>(d_x, ldx, rows, K, d_q, d_scales, st);
     }
@@ -59,6 +64,7 @@ extern "C" int srm_quantize_fp8(int32_t dtype, const void *d_x, int64_t ldx, int
     SRM_TRY(check_fp8(who, d_q, d_scales));
     if (rows <= 0 || rows >= kMaxRows || K <= 0 || K > kMaxWidth) return fail(SRM_EINVAL, "%s: sizes out of range", who);
     if (ldx < K) return fail(SRM_EINVAL, "%s: row stride %lld is less than %d", who, (long long)ldx, K);
+    if (misaligned(d_x, size_of(dtype))) return fail(SRM_EINVAL, "%s: %s", who, kNotWhole);
     if (dtype == SRM_FP32) return quantize<float>(d_x, ldx, rows, K, d_q, d_scales, as_stream(hip_stream));
     if (dtype == SRM_BF16) return quantize<bf16>(d_x, ldx, rows, K, d_q, d_scales, as_stream(hip_stream));
     return fail(SRM_EINVAL, "%s: unknown dtype %d", who, dtype);
@@ -69,7 +75,7 @@ static int launch_rmsnorm(void *d_x, int64_t ldx, const void *d_add, int64_t ld_
                           void *d_q, void *d_scales, hipStream_t st)
 {
     constexpr int ROWS = NW > 4 ? 1 : 4 / NW;
-    hipLaunchKernelGGL((rmsnorm_fp8_kernel<T, TAdd, NW, G>), dim3((unsigned)cdiv(rows, ROWS)), dim3(NW > 4 ? NW * 64 : 256), 0, st,
+    hipLaunchKernelGGL((rmsnorm_fp8_kernel<T, TAdd, NW, G>), grid_of(cdiv(rows, ROWS)), dim3(NW > 4 ? NW * 64 : 256), 0, st,
                        static_cast<T *>(d_x), ldx, static_cast<const TAdd *>(d_add), ld_add, d_gain, eps, rows, d,
                        static_cast<unsigned char *>(d_q), static_cast<uint32_t *>(d_scales));
     HIP_TRY(hipGetLastError());
@@ -105,6 +111,7 @@ extern "C" int srm_rmsnorm_fp8(int32_t dtype, void *d_x, int64_t ldx, int32_t ad
     if (!d_add) add_dtype = dtype;
     if ((dtype != SRM_FP32 && dtype != SRM_BF16) || (add_dtype != SRM_FP32 && add_dtype != SRM_BF16))
         return fail(SRM_EINVAL, "%s: unknown dtype %d, %d", who, dtype, add_dtype);
+    if (misaligned(d_x, size_of(dtype)) || misaligned(d_add, size_of(add_dtype)) || misaligned(d_gain, 4)) return fail(SRM_EINVAL, "%s: %s", who, kNotWhole);
     hipStream_t st = as_stream(hip_stream);
     if (dtype == SRM_FP32)
         return add_dtype == SRM_FP32 ? rmsnorm<float, float>(d_x, ldx, d_add, ld_add, d_gain, eps, rows, d, d_q, d_scales, st)
@@ -142,12 +149,14 @@ template <auto KERN>
 static int launch_fp8(int64_t blocks, int threads, int lds, const Fp8Call &c)
 {
     if (blocks >= (1 << 30)) return fail(SRM_EINVAL, "srm_linear_fp8: sizes out of range");
-    static bool attr_set = false;
-    if (!attr_set) {
+    static std::atomic<uint64_t> set_on{0};          // devices, by number
+    int dev = 0;
+    HIP_TRY(hipGetDevice(&dev));
+    if (!(set_on.load(std::memory_order_acquire) >> (dev & 63) & 1)) {
         HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(KERN), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
-        attr_set = true;
+        set_on.fetch_or(1ull << (dev & 63), std::memory_order_release);
     }
-    hipLaunchKernelGGL(KERN, dim3((unsigned)blocks), dim3(threads), lds, c.st, c.a, c.sa, c.w, c.sw, c.M, c.N, c.Kp, c.ep);
+    hipLaunchKernelGGL(KERN, grid_of(blocks), dim3(threads), lds, c.st, c.a, c.sa, c.w, c.sw, c.M, c.N, c.Kp, c.ep);
     HIP_TRY(hipGetLastError());
     return SRM_OK;
 }
@@ -209,9 +218,9 @@ extern "C" int srm_linear_fp8(int32_t epilogue, const void *d_a, const void *d_a
     SRM_TRY(check_fp8(who, d_a, d_a_scales));
     SRM_TRY(check_fp8(who, d_w, d_w_scales));
     if (!d_out) return fail(SRM_EINVAL, "%s: null output", who);
-    if (M <= 0 || M >= kMaxRows || N <= 0 || K <= 0 || K > kMaxWidth) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    if (M <= 0 || M >= kMaxRows || N <= 0 || N >= kMaxRows || K <= 0 || K > kMaxWidth) return fail(SRM_EINVAL, "%s: sizes out of range", who);
     if (misaligned(d_out, epilogue == 0 || epilogue == 1 ? 2 : 4) || misaligned(d_bias, 4))
-        return fail(SRM_EINVAL, "%s: output or bias does not lie at a whole element", who);
+        return fail(SRM_EINVAL, "%s: %s", who, kNotWhole);
     const Fp8Call c{static_cast<const unsigned char *>(d_a), static_cast<const uint32_t *>(d_a_scales), static_cast<const unsigned char *>(d_w),
                     static_cast<const uint32_t *>(d_w_scales), M, N, (int)align_up(K, kFp8Block), Fp8Epi{d_bias, d_out, N},
                     as_stream(hip_stream)};
@@ -229,8 +238,8 @@ extern "C" int srm_linear_fp8(int32_t epilogue, const void *d_a, const void *d_a
 template <typename T>
 static void launch_sample(const void *d_logits, int64_t rows, const SampleRows &p, bool wide, hipStream_t st)
 {
-    if (wide) hipLaunchKernelGGL((sample_rows_kernel<T, 1024>), dim3((unsigned)rows), dim3(1024), 0, st, static_cast<const T *>(d_logits), p);
-    else hipLaunchKernelGGL((sample_rows_kernel<T, 512>), dim3((unsigned)rows), dim3(512), 0, st, static_cast<const T *>(d_logits), p);
+    if (wide) hipLaunchKernelGGL((sample_rows_kernel<T, 1024>), grid_of(rows), dim3(1024), 0, st, static_cast<const T *>(d_logits), p);
+    else hipLaunchKernelGGL((sample_rows_kernel<T, 512>), grid_of(rows), dim3(512), 0, st, static_cast<const T *>(d_logits), p);
 }
 
 extern "C" int srm_sample_rows(int32_t dtype, const void *d_logits, int64_t ld, int64_t rows, int32_t vocab, const float *d_temperature,
@@ -241,7 +250,11 @@ extern "C" int srm_sample_rows(int32_t dtype, const void *d_logits, int64_t ld, 
     if (!d_logits || !d_uniform || !d_tok_out) return fail(SRM_EINVAL, "%s: null argument", who);
     if (rows <= 0 || rows >= kMaxRows || vocab <= 0 || vocab > kSampleVocab) return fail(SRM_EINVAL, "%s: sizes out of range", who);
     if (ld < vocab) return fail(SRM_EINVAL, "%s: row stride %lld is less than %d", who, (long long)ld, vocab);
-    const SampleRows p{ld, vocab, d_temperature, d_top_p, d_min_p, d_uniform, d_top_k, d_tok_out, d_logprob};
+    const void *const words[] = {d_temperature, d_top_k, d_top_p, d_min_p, d_uniform, d_tok_out, d_logprob};
+    bool whole = !misaligned(d_logits, size_of(dtype));
+    for (const void *w : words) whole = whole && !misaligned(w, 4);
+    if (!whole) return fail(SRM_EINVAL, "%s: %s", who, kNotWhole);
+    const SampleRows p{rows, ld, vocab, d_temperature, d_top_p, d_min_p, d_uniform, d_top_k, d_tok_out, d_logprob};
     hipStream_t st = as_stream(hip_stream);
     const bool wide = rows <= device_cus();
     if (dtype == SRM_FP32) launch_sample<float>(d_logits, rows, p, wide, st);

@@ -30,7 +30,7 @@ constexpr int kSampleList = 1024, kSampleFew = 64, kSampleBound = 512, kSampleDe
 constexpr double kSampleUnit = 8796093022208.0;      // 2^43
 
 struct SampleRows {
-    int64_t ld;
+    int64_t rows, ld;
     int V;
     const float *temperature, *top_p, *min_p, *uniform;
     const int32_t *top_k;
@@ -148,7 +148,8 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     __shared__ sr_mass few_rank[kSampleFew], few_mass[kSampleFew], few_sum[kSampleFew];
     __shared__ sr_mass found_before;
     __shared__ uint32_t found, low_s, high_s, n_list;
-    const int64_t row = blockIdx.x;
+    const int64_t row = work_group();
+    if (row >= p.rows) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = p.V;
     const T *L = logits + row * p.ld;
     auto uniform = [](bool x) SR_INLINE { return __builtin_amdgcn_readfirstlane((int)x) != 0; };
@@ -279,7 +280,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     // (a row with an infinite logit is read as 0 where it is infinite and -infinity elsewhere)
     hot = uniform(most == INFINITY);
     if (hot) { own_most = own_most == INFINITY ? 0.0f : -INFINITY; most = 0.0f; }
-    const double most_d = (double)most, per_bit = (double)fminf(temp, 1e30f) * 0.6931471805599453, c = 1.0 / per_bit;
+    const double most_d = (double)most, temp_d = (double)fminf(temp, 1e30f), per_bit = temp_d * 0.6931471805599453, c = 1.0 / per_bit;
     // (2^-900 and less are alike; also what a NaN counts as)
     const double clamp_d = -900.0 * per_bit;
     const float min_p = p.min_p && p.min_p[row] > 0.0f ? fminf(p.min_p[row], 1.0f) : 0.0f;
@@ -655,7 +656,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         p.tok[row] = tok;
         if (p.logprob) {
             const float x = hot ? 0.0f : (float)L[tok];
-            p.logprob[row] = (float)(((double)x - (double)most) / (double)temp - log((double)total / kSampleUnit));
+            p.logprob[row] = (float)(((double)x - most_d) / temp_d - log((double)total / kSampleUnit));
         }
     }
 }

@@ -311,6 +311,50 @@ def test_linear_of_more_than_two_gigabytes(srm):
         assert ((got.double() - ref).abs() <= (K + 3) * 2.0 ** -23 * size).all()
 
 
+def test_more_rows_than_a_dimension_of_a_grid_has_threads_for(srm):
+    """2^26 + 5 rows of 8 (a wavefront each) in 2^24 work-groups: the same codes as in a small call."""
+    rows, d = (1 << 26) + 5, 8
+    x = torch.zeros(rows, d, device="cuda")
+    some = torch.tensor([0, 1, 12345, (1 << 23) + 1, (1 << 25) - 1, 1 << 25, (1 << 26) - 1, 1 << 26, rows - 1], device="cuda")
+    few = torch.randn(len(some), d, device="cuda")
+    x[some] = few
+    (q, s), (qf, sf) = srm.fp8_empty(rows, d), srm.fp8_empty(len(some), d)
+    gain = torch.rand(d, device="cuda") + 0.5
+    for call in (lambda x, q, s: srm.quantize_fp8(x, q, s), lambda x, q, s: srm.rmsnorm_fp8(x, gain, 1e-5, q, s)):
+        q.view(torch.uint8).fill_(0x5A)
+        s.view(torch.uint8).fill_(0x5A)
+        call(x, q, s)
+        call(few, qf, sf)
+        assert torch.equal(q.view(torch.uint8)[some], qf.view(torch.uint8)) and torch.equal(s.view(torch.uint8)[:, some], sf.view(torch.uint8))
+        q.view(torch.uint8)[some] = 0
+        s.view(torch.uint8)[:, some] = 127
+        assert int(q.view(torch.int64).amax()) == 0 == int(q.view(torch.int64).amin()) and (s.view(torch.int32) == 0x7F7F7F7F).all()
+
+
+def test_a_single_row_of_more_columns_than_a_dimension_of_a_grid_has_threads_for(srm):
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("less than 60 GiB of free memory")
+    N, K = (1 << 28) + 37, 128
+    a, sa = srm.fp8_empty(1, K)
+    srm.quantize_fp8(torch.randn(1, K, device="cuda"), a, sa)
+    w, sw = srm.fp8_empty(N, K)
+    w.view(torch.uint8).zero_()
+    sw.view(torch.uint8).fill_(127)
+    some = torch.tensor([0, 17, (1 << 26) + 3, (1 << 27) - 1, 1 << 27, (1 << 28) - 1, 1 << 28, N - 1], device="cuda")
+    wf, swf = srm.fp8_empty(len(some), K)
+    srm.quantize_fp8(torch.randn(len(some), K, device="cuda"), wf, swf)
+    w.view(torch.uint8)[some] = wf.view(torch.uint8)
+    sw.view(torch.uint8)[:, some] = swf.view(torch.uint8)
+    out, few = torch.full((1, N), 7.0, device="cuda"), torch.empty(1, len(some), device="cuda")
+    srm.linear_fp8(4, a, sa, w, sw, None, out)
+    srm.linear_fp8(4, a, sa, wf, swf, None, few)
+    # (another kernel, which adds K's parts in another order)
+    size = _values(a, sa).abs() @ _values(wf, swf).abs().t().contiguous()
+    assert ((out[:, some] - few).double().abs() <= (K + 3) * 2.0 ** -22 * size).all()
+    out[:, some] = 0
+    assert (out == 0).all()
+
+
 # ------------------------------------------------------------------ together
 def _block(srm, M, d, ff, rng):
     """A channel mixer in 8 bits: norm, up projection with GELU, quantize, down projection into the residual stream."""

@@ -174,6 +174,32 @@ def test_extreme_temperatures(srm, t):
     check(srm, logits, rng.random(8), temperature=[t] * 8, top_p=[0.9, 1.0] * 4)
 
 
+def test_an_infinite_temperature_is_the_largest(srm):
+    """Of logits that far apart, the probabilities are those of 1e30."""
+    x = torch.tensor([[0.0, -2e30], [3e38, -3e38]], device="cuda")
+    tok, lp = torch.empty(2, dtype=torch.int32, device="cuda"), torch.empty(2, device="cuda")
+    srm.sample_rows(x, _column([0.99, 0.99], torch.float32), tok, temperature=_column([INF, 1e35], torch.float32), logprob=lp)
+    want = [float(x[0, 1].double()) / float(np.float32(1e30)), 0.0]
+    want[0] -= math.log1p(math.exp(want[0]))
+    assert tok.tolist() == [1, 0]
+    assert [abs(a - b) <= 2.0 ** -24 * abs(b) + 1e-9 for a, b in zip(lp.double().tolist(), want)] == [True, True]
+
+
+def test_more_rows_than_a_dimension_of_a_grid_has_threads_for(srm):
+    rows, V = (1 << 23) + 3, 5
+    logits = torch.randn(rows, V, device="cuda")
+    u = torch.rand(rows, device="cuda")
+    tok = torch.full((rows + 1,), -7, dtype=torch.int32, device="cuda")
+    srm.sample_rows(logits, u, tok[:-1])
+    w = torch.exp(logits.double() - logits.double().amax(1, keepdim=True))
+    run = w.cumsum(1)
+    goal = u.double() * run[:, -1]
+    want = (run <= goal[:, None]).sum(1)
+    near = ((run - goal[:, None]).abs() < 1e-9).any(1)        # (8 million draws: a few may lie that near)
+    assert near.sum() < 10 and tok[-1] == -7
+    assert ((tok[:-1] == want) | near).all()
+
+
 def test_the_ends_of_the_draw(srm):
     """u = 0 draws the first kept token, the largest u below 1 the last one that has weight."""
     rng = np.random.default_rng(12)

@@ -80,6 +80,29 @@ def test_sample_rows_refuses(srm, at, value, word):
     refused(srm, srm.lib().srm_sample_rows(*args), word)
 
 
+@pytest.mark.parametrize("call,args,at", [
+    ("srm_quantize_fp8", (0, P, 100, 4, 100, P, P, None), {1: 2}), ("srm_quantize_fp8", (1, P, 100, 4, 100, P, P, None), {1: 1}),
+    ("srm_rmsnorm_fp8", (0, P, 100, 1, P, 100, P, 1e-5, 4, 100, P, P, None), {1: 2, 4: 1, 6: 2}),
+    ("srm_rmsnorm_fp8", (1, P, 100, 0, P, 100, P, 1e-5, 4, 100, P, P, None), {1: 1, 4: 2, 6: 1}),
+    ("srm_sample_rows", (0, P, 100, 4, 100, P, P, P, P, P, P, P, None), {1: 2, 5: 1, 6: 2, 7: 3, 8: 2, 9: 2, 10: 1, 11: 2}),
+    ("srm_sample_rows", (1, P, 100, 4, 100, None, None, None, None, P, P, None, None), {1: 1})])
+def test_operands_lie_at_whole_elements(srm, call, args, at):
+    for i, off in at.items():
+        bad = list(args)
+        bad[i] = P + off
+        refused(srm, getattr(srm.lib(), call)(*bad), b"whole element")
+
+
+def test_sizes_whose_grids_or_indexes_do_not_fit_are_refused(srm):
+    lib, big = srm.lib(), 1 << 30
+    refused(srm, lib.srm_quantize_fp8(0, P, 2000, big - 1, 2000, P, P, None), b"sizes")        # 2^32 groups
+    refused(srm, lib.srm_quantize_fp8(0, P, 8, big, 8, P, P, None), b"sizes")
+    refused(srm, lib.srm_rmsnorm_fp8(0, P, 8, 0, None, 0, P, 0.0, big, 8, P, P, None), b"sizes")
+    refused(srm, lib.srm_linear_fp8(0, P, P, P, P, None, big, 1, 1, P, None), b"sizes")
+    refused(srm, lib.srm_linear_fp8(0, P, P, P, P, None, 1, big, 1, P, None), b"sizes")
+    refused(srm, lib.srm_sample_rows(0, P, 8, big, 8, None, None, None, None, P, P, None, None), b"sizes")
+
+
 def test_binding_refuses_before_the_library(srm):
     x, add, gain = torch.zeros(3, 200), torch.zeros(3, 200), torch.zeros(200)
     q, s = srm.fp8_empty(3, 200, device="cpu")
