@@ -234,7 +234,7 @@ extern "C" int srm_linear_fp8(int32_t epilogue, const void *d_a, const void *d_a
 }
 
 // ------------------------------------------------------------------ sampling by request
-// Work-groups of 1024 threads while each row has a CU of its own, behind that of 512, of which a CU holds two to four.
+// Work-groups of 1024 threads while each row has a CU of its own, behind that of 512, of which a CU holds two.
 template <typename T>
 static void launch_sample(const void *d_logits, int64_t rows, const SampleRows &p, bool wide, hipStream_t st)
 {

@@ -280,7 +280,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     // (a row with an infinite logit is read as 0 where it is infinite and -infinity elsewhere)
     hot = uniform(most == INFINITY);
     if (hot) { own_most = own_most == INFINITY ? 0.0f : -INFINITY; most = 0.0f; }
-    const double most_d = (double)most, temp_d = (double)fminf(temp, 1e30f), per_bit = temp_d * 0.6931471805599453, c = 1.0 / per_bit;
+    const double most_d = (double)most, per_bit = (double)fminf(temp, 1e30f) * 0.6931471805599453, c = 1.0 / per_bit;
     // (2^-900 and less are alike; also what a NaN counts as)
     const double clamp_d = -900.0 * per_bit;
     const float min_p = p.min_p && p.min_p[row] > 0.0f ? fminf(p.min_p[row], 1.0f) : 0.0f;
@@ -655,8 +655,8 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     if (tid == 0) {
         p.tok[row] = tok;
         if (p.logprob) {
-            const float x = hot ? 0.0f : (float)L[tok];
-            p.logprob[row] = (float)(((double)x - most_d) / temp_d - log((double)total / kSampleUnit));
+            const float x = hot ? 0.0f : (float)L[tok], t = fminf(p.temperature ? p.temperature[row] : 1.0f, 1e30f);
+            p.logprob[row] = (float)(((double)x - most_d) / (double)t - log((double)total / kSampleUnit));
         }
     }
 }
