@@ -25,6 +25,7 @@
 
 typedef unsigned long long sr_mass;
 constexpr int kSampleVocab = 1 << 20, kSampleSegment = 512, kSampleSteps = kSampleVocab / kSampleSegment;
+constexpr int kSampleCodes = 5120, kSampleTabled = 16384;                   // entries of the table of bf16 weights
 constexpr int kSampleList = 1024, kSampleFew = 64, kSampleBound = 512, kSampleDense = 256;
 #define SR_INLINE __attribute__((always_inline))
 constexpr double kSampleUnit = 8796093022208.0;      // 2^43
@@ -141,17 +142,25 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     constexpr int NW = NT / 64, PER = kSampleSteps / NT;
     static_assert(NW * kSampleDense >= 2 * kSampleSegment, "the weights of a segment fit");
     __shared__ sr_mass red[NW];
-    __shared__ sr_mass table[kSampleSteps];          // sums by step or by segment
-    __shared__ uint32_t list_key[kSampleList];
-    __shared__ int list_at[kSampleList];
+    __shared__ struct {
+        sr_mass table[kSampleSteps];                 // sums by step or by segment
+        uint32_t list_key[kSampleList];
+        int list_at[kSampleList];
+    } lds;
+    sr_mass *const table = lds.table;
+    uint32_t *const list_key = lds.list_key;
+    int *const list_at = lds.list_at;
     __shared__ __align__(8) float dense[NW * kSampleDense];             // kept logits of the wavefronts' segments; the weights of a segment
     __shared__ sr_mass few_rank[kSampleFew], few_mass[kSampleFew], few_sum[kSampleFew];
+    constexpr bool CODES = sizeof(T) == 2;
+    __shared__ sr_mass by_code[CODES ? kSampleCodes + 1 : 1];
     __shared__ sr_mass found_before;
     __shared__ uint32_t found, low_s, high_s, n_list;
     const int64_t row = work_group();
     if (row >= p.rows) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = p.V;
     const T *L = logits + row * p.ld;
+    auto scalar = [](float x) SR_INLINE { return __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(x))); };
     auto uniform = [](bool x) SR_INLINE { return __builtin_amdgcn_readfirstlane((int)x) != 0; };
     bool hot = false;                                // an infinite logit leaves all others without weight: see below
 
@@ -294,10 +303,10 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     };
     // Nothing below floor_v has weight (it lies a little too low: weights decide); of value cut_v only indices up to cut_at are kept.
     const double lowest = (double)most + (has_least ? log2((double)least / kSampleUnit) - 0.001 : -44.001) * per_bit;
-    float floor_v = (float)(lowest - fabs(lowest) * 1e-6);
+    float floor_v = scalar((float)(lowest - fabs(lowest) * 1e-6));
     float cut_v = -INFINITY;
     int cut_at = V;
-    bool cut = false, in_list = false;               // in_list: the list holds all kept logits (and others, which kept() tells)
+    bool cut = false, summed = false, in_list = false;                  // summed: the table holds the segments' sums; in_list: the list holds all kept logits (and others, which kept() tells)
     uint32_t n = 0;                                  // of the list
     auto kept = [&](float x, int at) SR_INLINE { return x > cut_v || (x == cut_v && at <= cut_at); };
     // vectors that hold a logit from floor_v up
@@ -307,19 +316,93 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         for (int i = 1; i < 8; ++i) top = fmaxf(top, v[i]);
         return __ballot(top >= floor_v) != 0;
     };
+    // bf16 logits have few values: from most down to floor_v, those of a magnitude below tiny_v apart (there are as many of them in each
+    // octave towards 0), they fit a table of their weights.  A logit's code times 8, minus the first code of its sign's part, is its place.
+    bool tabled = false, cut_in_table = false;       // cut_in_table: logits from cut_v down have no weight there
+    int pos_n = 0;
+    float tiny_v = 0.0f;
+    uint32_t pos8 = 0, neg8 = 0, end8 = 0;
+    auto tabulate = [&]() SR_INLINE {
+        if constexpr (CODES) {
+            if (tabled || hot || V < kSampleTabled) return;
+            auto code = [](float x) SR_INLINE { return (int)(__float_as_uint(x) >> 16 & 0x7fff); };
+            const int first = code(most), last = code(floor_v);
+            if (max(first, last) >= 0x6000) return;  // (2^65: so that no NaN's code falls into the table)
+            int neg_n = 0, from;                     // entries of each sign; the smallest magnitude
+            if (most > 0.0f && floor_v < 0.0f) {
+                from = max(0x1800, (first + last + 3 - kSampleCodes) / 2);          // (2^-79, for the same reason)
+                pos_n = max(0, first - from + 1);
+                neg_n = max(0, last - from + 1);
+                tiny_v = __uint_as_float((uint32_t)from << 16);
+            } else {
+                const int least_code = max(1, min(first, last));
+                from = max(least_code, max(first, last) - kSampleCodes + 1);
+                (most > 0.0f ? pos_n : neg_n) = max(0, max(first, last) - from + 1);
+                tiny_v = from > min(first, last) ? __uint_as_float((uint32_t)from << 16) : 0.0f;
+            }
+            if (pos_n + neg_n > kSampleCodes) return;
+            pos8 = (uint32_t)(pos_n ? from : 0x8000 + from) * 8;
+            neg8 = neg_n ? (uint32_t)(0x8000 + from - pos_n) * 8 : pos8;
+            end8 = (uint32_t)(pos_n + neg_n) * 8;
+            const int end = pos_n + neg_n;
+            for (int i0 = tid; i0 <= end; i0 += 8 * NT) {
+                double d[8];
+                sr_mass m[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int i = i0 + k * NT;
+                    const uint32_t bits = (uint32_t)(i < pos_n ? from + i : 0x8000 + from + i - pos_n) << 16;
+                    d[k] = fmax((double)__uint_as_float(bits) - most_d, clamp_d);
+                    d[k] = fmin(d[k], 0.0);          // (codes behind the last one)
+                }
+                sample_mass(d, c, m);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (i0 + k * NT <= end) by_code[i0 + k * NT] = i0 + k * NT < end && m[k] >= least ? m[k] : 0;
+            }
+            tiny_v = scalar(tiny_v);
+            tabled = true;
+            __syncthreads();
+        }
+    };
+    auto place8 = [&](float x) SR_INLINE {
+        const uint32_t at8 = __float_as_uint(x) >> 13;
+        return min(min(at8 - pos8, at8 - neg8), end8);
+    };
+    auto tiny = [&](const auto &v) SR_INLINE {       // some logit of the wavefront's vectors is not in the table
+        float small = fabsf(v[0]);
+#pragma unroll
+        for (unsigned i = 1; i < sizeof(v) / sizeof(v[0]); ++i) small = fminf(small, fabsf(v[i]));
+        return __ballot(small < tiny_v) != 0;
+    };
+    // the weights of N logits from the table; false if one of the wavefront's is not in it
+    auto looked_up = [&](auto &v, auto &m) SR_INLINE {
+        if constexpr (CODES) {
+            constexpr int N = sizeof(v) / sizeof(v[0]);
+            if (!tabled) return false;
+            if (tiny(v)) return false;
+#pragma unroll
+            for (int i = 0; i < N; ++i) m[i] = *reinterpret_cast<const sr_mass *>(reinterpret_cast<const char *>(by_code) + place8(v[i]));
+            return true;
+        }
+        return false;
+    };
     // the weights of a vector's kept logits, in chains that do not wait for each other
     auto masses = [&](const float (&v)[8], int at, sr_mass (&m)[8]) SR_INLINE {
-        double d[8];
+        const bool from_table = looked_up(v, m);
+        if (!from_table) {
+            double d[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] = (double)v[i];
+            for (int i = 0; i < 8; ++i) d[i] = (double)v[i];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] = fmax(d[i] - most_d, clamp_d);
-        sample_mass(d, c, m);
-        if (has_least) {
+            for (int i = 0; i < 8; ++i) d[i] = fmax(d[i] - most_d, clamp_d);
+            sample_mass(d, c, m);
+            if (has_least) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m[i] = m[i] >= least ? m[i] : 0;
+                for (int i = 0; i < 8; ++i) m[i] = m[i] >= least ? m[i] : 0;
+            }
         }
-        if (cut) {
+        if (cut && !(from_table && cut_in_table)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) m[i] = kept(v[i], at + i) ? m[i] : 0;
         }
@@ -327,8 +410,9 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     // The first index at which the running sum of weights exceeds target(sum of all): one_of(value, index) gives a kept logit's,
     // of(values, index, weights) those of a vector, and sum_of(values, index) the sum of the wavefront's vectors.
     auto index_of = [&](auto &&one_of, auto &&of, auto &&sum_of, auto &&target, sr_mass &total) SR_INLINE {
-        clear();
-        if (in_list) {
+        if (!summed) clear();
+        if (summed) {
+        } else if (in_list) {
             for (uint32_t i = tid; i < n; i += NT) {
                 const float x = sample_value(list_key[i]);
                 const int at = list_at[i];
@@ -414,11 +498,139 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         n = gather(floor_v, INFINITY);
         in_list = n <= (uint32_t)kSampleList;
     }
+    auto top_p_limit = [&](sr_mass sum) SR_INLINE { return max((sr_mass)ceil((double)top_p * (double)sum), (sr_mass)1); };
+    // top-p of bf16 logits: how many there are of each code, from which follow the last kept value and how many of it are kept; then the
+    // segments' sums and their numbers of that value, in one pass.  false if the limit is reached among the tiny ones.
+    auto top_p_by_code = [&]() SR_INLINE {
+        if constexpr (CODES) {
+            constexpr int PERC = kSampleCodes / NT;
+            static_assert(sizeof(lds) >= kSampleCodes * 4 && kSampleCodes % NT == 0, "the counts fit");
+            uint32_t *const count = reinterpret_cast<uint32_t *>(&lds);
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < PERC; ++i) count[i * NT + tid] = 0;
+            if (tid == 0) { few_sum[0] = 0; found = ~0u; }
+            __syncthreads();
+            pass([&](const float (&v)[8], int) SR_INLINE {
+                if (!live(v)) return;
+                const bool some_tiny = tiny(v);
+                if (some_tiny) {
+#pragma unroll 1
+                    for (int i = 0; i < 8; ++i) {
+                        float x = v[0];
+#pragma unroll
+                        for (int k = 1; k < 8; ++k) x = i == k ? v[k] : x;
+                        if (fabsf(x) < tiny_v) atomicAdd(&few_sum[0], mass(x));
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t at8 = place8(v[i]);
+                    if (at8 < end8 && !(some_tiny && fabsf(v[i]) < tiny_v)) atomicAdd(&count[at8 >> 3], 1u);
+                }
+            });
+            __syncthreads();
+            const sr_mass tiny_sum = few_sum[0];
+            // the k-th code from the largest down: positive ones lie the other way round
+            auto place = [&](int k) SR_INLINE { return k < pos_n ? pos_n - 1 - k : k; };
+            const int end = (int)(end8 >> 3);
+            sr_mass own = 0, total;
+#pragma unroll
+            for (int i = 0; i < PERC; ++i) {
+                const int k = tid * PERC + i;
+                if (k < end) own += (sr_mass)count[place(k)] * by_code[place(k)];
+            }
+            sr_mass up = scan(own, total);
+            const sr_mass limit = top_p_limit(total + tiny_sum);
+#pragma unroll
+            for (int i = 0; i < PERC; ++i) {
+                const int k = tid * PERC + i;
+                if (k >= end) break;
+                const sr_mass one = by_code[place(k)], all_of = (sr_mass)count[place(k)] * one, before = up + (k >= pos_n ? tiny_sum : 0);
+                if (before < limit && limit - before <= all_of) {
+                    found = (uint32_t)k;
+                    low_s = (uint32_t)((limit - before + one - 1) / one);
+                    high_s = count[place(k)];
+                }
+                up += all_of;
+            }
+            __syncthreads();
+            const int last = __builtin_amdgcn_readfirstlane((int)found), last_at = place(last);
+            if (last < 0) return false;
+            const uint32_t n_kept = (uint32_t)__builtin_amdgcn_readfirstlane((int)low_s);
+            const bool some = uniform(n_kept < high_s);          // not all of the value
+            cut_v = __uint_as_float(((last < pos_n ? pos8 : neg8) / 8 + (uint32_t)last_at) << 16);
+            cut_at = some ? -1 : V;
+            cut = cut_in_table = true;
+            floor_v = scalar(fmaxf(floor_v, cut_v));
+            const sr_mass one = by_code[last_at];
+            __syncthreads();
+            for (int k = last + (some ? 0 : 1) + tid; k < end; k += NT) by_code[place(k)] = 0;
+            clear();
+            pass([&](const float (&v)[8], int at) SR_INLINE {
+                if (!live(v)) return;
+                sr_mass m[8], s = 0;
+                masses(v, at, m);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s += m[i];
+                s = sample_wave_sum(s);
+                uint32_t ties = 0;
+                if (some) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) ties += (uint32_t)__popcll(__ballot(v[i] == cut_v));
+                }
+                if (lane == 0) table[at / kSampleSegment] = s | (sr_mass)ties << 53;         // (512 2^43 < 2^53)
+            });
+            if (some) {
+                __syncthreads();
+                sr_mass ties = 0;
+#pragma unroll
+                for (int i = 0; i < PER; ++i) ties += table[tid * PER + i] >> 53;
+                sr_mass before = scan(ties, total);
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const sr_mass s = table[tid * PER + i], here = s >> 53;
+                    const sr_mass kept_here = before < n_kept ? min(here, n_kept - before) : 0;
+                    table[tid * PER + i] = (s & ((1ull << 53) - 1)) + kept_here * one;
+                    if (before < n_kept && n_kept - before <= here) { found = (uint32_t)(tid * PER + i); low_s = n_kept - (uint32_t)before; }
+                    before += here;
+                }
+                __syncthreads();
+                if (wave == 0) {                     // of this segment the low_s first ones
+                    const int first = (int)found * kSampleSegment + lane * 8;
+                    float v[8];
+                    complete(raw8(L, first, V), first, v);
+                    uint32_t own_ties = 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) own_ties += v[i] == cut_v ? 1u : 0u;
+                    uint32_t rank = low_s - (sample_wave_scan32(own_ties) - own_ties);         // of this lane's
+                    if (rank - 1 < own_ties) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (v[i] == cut_v && --rank == 0) high_s = (uint32_t)(first + i);
+                    }
+                    if (lane == 0) by_code[last_at] = one;
+                }
+                __syncthreads();
+                cut_at = __builtin_amdgcn_readfirstlane((int)high_s);
+                cut_in_table = false;
+            }
+            __syncthreads();
+            if (tid == 0) found = ~0u;
+            return true;
+        }
+        return false;
+    };
     // top-k (their number), then top-p (their mass): the kept tokens end at the first one with which a limit is reached
-    for (int by_mass = 0; by_mass < 2; ++by_mass) {
-        if (uniform(by_mass ? !(top_p < 1.0f) : top_k <= 0 || top_k >= V)) continue;
+    const bool by_count = uniform(top_k > 0 && top_k < V), by_sum = uniform(top_p < 1.0f);
+    if (by_sum && !by_count && !in_list) {
+        tabulate();
+        summed = tabled && top_p_by_code();
+    }
+    for (int by_mass = summed ? 2 : 0; by_mass < 2; ++by_mass) {
+        if (by_mass ? !by_sum : !by_count) continue;
         auto limit_of = [&](sr_mass sum) SR_INLINE {
-            return by_mass ? max((sr_mass)ceil((double)top_p * (double)sum), (sr_mass)1) : (sr_mass)top_k;
+            return by_mass ? top_p_limit(sum) : (sr_mass)top_k;
         };
         const float scale = (float)kSampleSteps / (most - floor_v), scaled = most * scale;
         auto value_step = [&](float x) SR_INLINE { return (uint32_t)fminf(fmaf(x, -scale, scaled), (float)(kSampleSteps - 1)); };
@@ -461,6 +673,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
                 if (listed) floor_v = bound;
             }
         }
+        if (by_mass && !listed) tabulate();
         while (!listed) {
             clear();
             pass([&](const float (&v)[8], int at) SR_INLINE {
@@ -582,7 +795,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
                 if (up < limit && limit - up <= own) { low_s = (uint32_t)(rank >> 32); high_s = ~(uint32_t)rank; }
             }
             __syncthreads();
-            cut_v = sample_value((uint32_t)__builtin_amdgcn_readfirstlane((int)low_s));
+            cut_v = scalar(sample_value((uint32_t)__builtin_amdgcn_readfirstlane((int)low_s)));
             cut_at = __builtin_amdgcn_readfirstlane((int)high_s);
         } else {
             // of one value the first ones, by index
@@ -604,9 +817,10 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
             cut_at = __builtin_amdgcn_readfirstlane(at);
         }
         cut = true;
-        floor_v = fmaxf(floor_v, cut_v);
+        floor_v = scalar(fmaxf(floor_v, cut_v));
     }
 
+    if (!in_list && !cut) tabulate();
     const float u = p.uniform[row];
     sr_mass total;
     const int tok = index_of([&](float x, int) SR_INLINE { return mass(x); }, masses, [&](const float (&v)[8], int at) SR_INLINE {
@@ -642,11 +856,15 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
             __builtin_amdgcn_wave_barrier();
             for (uint32_t j = lane; j < some + lane; j += 128) {
                 const float *at2 = dense + wave * kSampleDense;
-                const double d[2] = {j < some ? fmax((double)at2[j] - most_d, clamp_d) : clamp_d,
-                                     j + 64 < some ? fmax((double)at2[j + 64] - most_d, clamp_d) : clamp_d};
+                const float x[2] = {j < some ? at2[j] : -INFINITY, j + 64 < some ? at2[j + 64] : -INFINITY};
                 sr_mass m[2];
-                sample_mass(d, c, m);
-                s += (m[0] >= least ? m[0] : 0) + (m[1] >= least ? m[1] : 0);
+                if (!looked_up(x, m)) {
+                    const double d[2] = {fmax((double)x[0] - most_d, clamp_d), fmax((double)x[1] - most_d, clamp_d)};
+                    sample_mass(d, c, m);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) m[i] = m[i] >= least ? m[i] : 0;
+                }
+                s += m[0] + m[1];
             }
             __builtin_amdgcn_wave_barrier();
         }
