@@ -24,6 +24,7 @@
 #include <type_traits>
 
 typedef unsigned long long sr_mass;
+typedef __attribute__((ext_vector_type(2))) uint16_t sr_codes;
 constexpr int kSampleVocab = 1 << 20, kSampleSegment = 512, kSampleSteps = kSampleVocab / kSampleSegment;
 constexpr int kSampleCodes = 5120, kSampleTabled = 16384;                   // entries of the table of bf16 weights
 constexpr int kSampleList = 1024, kSampleFew = 64, kSampleBound = 512, kSampleDense = 256;
@@ -127,6 +128,19 @@ __device__ __forceinline__ sr_mass sample_wave_sum(sr_mass v)
     v += sample_moved<0x141>(v);
     v += sample_moved<0x140>(v);
     return (sample_lane(v, 0) + sample_lane(v, 16)) + (sample_lane(v, 32) + sample_lane(v, 48));
+}
+// The same of values below 2^46, whose low 26 and high 20 bits do not leave 32 bits: half the instructions.
+__device__ __forceinline__ sr_mass sample_wave_sum46(sr_mass v)
+{
+    auto sum = [](uint32_t x) {
+        x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true);
+        x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, true);
+        x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xF, 0xF, true);
+        x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xF, 0xF, true);
+        return ((uint32_t)__builtin_amdgcn_readlane((int)x, 0) + (uint32_t)__builtin_amdgcn_readlane((int)x, 16)) +
+               ((uint32_t)__builtin_amdgcn_readlane((int)x, 32) + (uint32_t)__builtin_amdgcn_readlane((int)x, 48));
+    };
+    return (sr_mass)sum((uint32_t)v & 0x3ffffffu) + ((sr_mass)sum((uint32_t)(v >> 26)) << 26);
 }
 __device__ __forceinline__ uint32_t sample_wave_max(uint32_t v)
 {
@@ -317,11 +331,11 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         return __ballot(top >= floor_v) != 0;
     };
     // bf16 logits have few values: from most down to floor_v, those of a magnitude below tiny_v apart (there are as many of them in each
-    // octave towards 0), they fit a table of their weights.  A logit's code times 8, minus the first code of its sign's part, is its place.
+    // octave towards 0), they fit a table of their weights.  A logit's place in it is its code minus the first one of its sign's part, in 16 bits modulo 2^16.
     bool tabled = false, cut_in_table = false;       // cut_in_table: logits from cut_v down have no weight there
     int pos_n = 0;
     float tiny_v = 0.0f;
-    uint32_t pos8 = 0, neg8 = 0, end8 = 0;
+    uint16_t pos = 0, neg = 0, end = 0;
     auto tabulate = [&]() SR_INLINE {
         if constexpr (CODES) {
             if (tabled || hot || V < kSampleTabled) return;
@@ -341,10 +355,9 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
                 tiny_v = from > min(first, last) ? __uint_as_float((uint32_t)from << 16) : 0.0f;
             }
             if (pos_n + neg_n > kSampleCodes) return;
-            pos8 = (uint32_t)(pos_n ? from : 0x8000 + from) * 8;
-            neg8 = neg_n ? (uint32_t)(0x8000 + from - pos_n) * 8 : pos8;
-            end8 = (uint32_t)(pos_n + neg_n) * 8;
-            const int end = pos_n + neg_n;
+            pos = (uint16_t)(pos_n ? from : 0x8000 + from);
+            neg = (uint16_t)(neg_n ? 0x8000 + from - pos_n : pos);
+            end = (uint16_t)(pos_n + neg_n);
             for (int i0 = tid; i0 <= end; i0 += 8 * NT) {
                 double d[8];
                 sr_mass m[8];
@@ -365,9 +378,15 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
             __syncthreads();
         }
     };
-    auto place8 = [&](float x) SR_INLINE {
-        const uint32_t at8 = __float_as_uint(x) >> 13;
-        return min(min(at8 - pos8, at8 - neg8), end8);
+    // N logits' places, those of logits behind the table its end, times 2^SHIFT
+    auto places = [&](const auto &v, auto &&at, auto shift) SR_INLINE {
+#pragma unroll
+        for (unsigned i = 0; i < sizeof(v) / sizeof(v[0]); i += 2) {
+            const sr_codes x = __builtin_bit_cast(sr_codes, __builtin_amdgcn_perm(__float_as_uint(v[i + 1]), __float_as_uint(v[i]), 0x07060302u));
+            const sr_codes y = __builtin_elementwise_min(__builtin_elementwise_min((sr_codes)(x - pos), (sr_codes)(x - neg)), sr_codes{end, end}) << (uint16_t)decltype(shift)::value;
+            at[i] = y[0];
+            at[i + 1] = y[1];
+        }
     };
     auto tiny = [&](const auto &v) SR_INLINE {       // some logit of the wavefront's vectors is not in the table
         float small = fabsf(v[0]);
@@ -381,8 +400,10 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
             constexpr int N = sizeof(v) / sizeof(v[0]);
             if (!tabled) return false;
             if (tiny(v)) return false;
+            uint32_t at[N];
+            places(v, at, std::integral_constant<int, 3>{});
 #pragma unroll
-            for (int i = 0; i < N; ++i) m[i] = *reinterpret_cast<const sr_mass *>(reinterpret_cast<const char *>(by_code) + place8(v[i]));
+            for (int i = 0; i < N; ++i) m[i] = *reinterpret_cast<const sr_mass *>(reinterpret_cast<const char *>(by_code) + at[i]);
             return true;
         }
         return false;
@@ -506,13 +527,13 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
             constexpr int PERC = kSampleCodes / NT;
             static_assert(sizeof(lds) >= kSampleCodes * 4 && kSampleCodes % NT == 0, "the counts fit");
             uint32_t *const count = reinterpret_cast<uint32_t *>(&lds);
+            const uint32_t end4 = 4u * end;
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < PERC; ++i) count[i * NT + tid] = 0;
             if (tid == 0) { few_sum[0] = 0; found = ~0u; }
             __syncthreads();
             pass([&](const float (&v)[8], int) SR_INLINE {
-                if (!live(v)) return;
                 const bool some_tiny = tiny(v);
                 if (some_tiny) {
 #pragma unroll 1
@@ -523,17 +544,20 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
                         if (fabsf(x) < tiny_v) atomicAdd(&few_sum[0], mass(x));
                     }
                 }
+                uint32_t at[8];
+                places(v, at, std::integral_constant<int, 2>{});
+                if (some_tiny) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t at8 = place8(v[i]);
-                    if (at8 < end8 && !(some_tiny && fabsf(v[i]) < tiny_v)) atomicAdd(&count[at8 >> 3], 1u);
+                    for (int i = 0; i < 8; ++i) at[i] = fabsf(v[i]) < tiny_v ? end4 : at[i];
                 }
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (at[i] < end4) atomicAdd(reinterpret_cast<uint32_t *>(reinterpret_cast<char *>(count) + at[i]), 1u);
             });
             __syncthreads();
             const sr_mass tiny_sum = few_sum[0];
             // the k-th code from the largest down: positive ones lie the other way round
             auto place = [&](int k) SR_INLINE { return k < pos_n ? pos_n - 1 - k : k; };
-            const int end = (int)(end8 >> 3);
             sr_mass own = 0, total;
 #pragma unroll
             for (int i = 0; i < PERC; ++i) {
@@ -559,7 +583,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
             if (last < 0) return false;
             const uint32_t n_kept = (uint32_t)__builtin_amdgcn_readfirstlane((int)low_s);
             const bool some = uniform(n_kept < high_s);          // not all of the value
-            cut_v = __uint_as_float(((last < pos_n ? pos8 : neg8) / 8 + (uint32_t)last_at) << 16);
+            cut_v = __uint_as_float(((uint32_t)(last < pos_n ? pos : neg) + (uint32_t)last_at) << 16);
             cut_at = some ? -1 : V;
             cut = cut_in_table = true;
             floor_v = scalar(fmaxf(floor_v, cut_v));
@@ -573,7 +597,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
                 masses(v, at, m);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s += m[i];
-                s = sample_wave_sum(s);
+                s = sample_wave_sum46(s);
                 uint32_t ties = 0;
                 if (some) {
 #pragma unroll
@@ -868,7 +892,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
             }
             __builtin_amdgcn_wave_barrier();
         }
-        return sample_wave_sum(s);
+        return sample_wave_sum46(s);                 // (a lane adds eight weights of 2^43 at most)
     }, [&](sr_mass sum) SR_INLINE { return min((sr_mass)((double)(u > 0.0f ? fminf(u, 1.0f) : 0.0f) * (double)sum), sum - 1); }, total);
     if (tid == 0) {
         p.tok[row] = tok;
