@@ -21,12 +21,16 @@
 // chains at a time; below that the row's passes through the last-level cache.
 #pragma once
 #include "fp8.hpp"
+#include <cstddef>
 #include <type_traits>
 
 typedef unsigned long long sr_mass;
 typedef __attribute__((ext_vector_type(2))) uint16_t sr_codes;
 constexpr int kSampleVocab = 1 << 20, kSampleSegment = 512, kSampleSteps = kSampleVocab / kSampleSegment;
-constexpr int kSampleCodes = 5120, kSampleTabled = 16384;                   // entries of the table of bf16 weights
+// The table of bf16 weights: magnitudes from 2^-11 up to 2^9, twenty octaves of 128 codes, of both signs.  Rows of fewer logits than
+// kSampleTabled do without.
+constexpr int kCodeSign = 2560, kCodeFrom = 0x3A00, kSampleCodes = 2 * kCodeSign, kSampleTabled = 16384;
+constexpr float kTinyLogit = 0.00048828125f, kHugeLogit = 512.0f;
 constexpr int kSampleList = 1024, kSampleFew = 64, kSampleBound = 512, kSampleDense = 256;
 #define SR_INLINE __attribute__((always_inline))
 constexpr double kSampleUnit = 8796093022208.0;      // 2^43
@@ -156,11 +160,12 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     constexpr int NW = NT / 64, PER = kSampleSteps / NT;
     static_assert(NW * kSampleDense >= 2 * kSampleSegment, "the weights of a segment fit");
     __shared__ sr_mass red[NW];
-    __shared__ struct {
+    struct Lds {
         sr_mass table[kSampleSteps];                 // sums by step or by segment
         uint32_t list_key[kSampleList];
         int list_at[kSampleList];
-    } lds;
+    };
+    __shared__ Lds lds;
     sr_mass *const table = lds.table;
     uint32_t *const list_key = lds.list_key;
     int *const list_at = lds.list_at;
@@ -172,7 +177,8 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     __shared__ uint32_t found, low_s, high_s, n_list;
     const int64_t row = work_group();
     if (row >= p.rows) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = p.V;
+    int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = p.V;
     const T *L = logits + row * p.ld;
     auto scalar = [](float x) SR_INLINE { return __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(x))); };
     auto uniform = [](bool x) SR_INLINE { return __builtin_amdgcn_readfirstlane((int)x) != 0; };
@@ -191,10 +197,10 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         }
     };
     // fn(values, index of the first); the next vector is on its way meanwhile
-    auto pass = [&](auto &&fn) SR_INLINE {
+    auto first_raw = [&]() SR_INLINE { return raw8(L, wave * kSampleSegment + lane * 8, V); };
+    auto pass_from = [&](Raw8<T> raw, auto &&fn) SR_INLINE {
         constexpr int STEP = NW * kSampleSegment;
         int at = wave * kSampleSegment + lane * 8;
-        Raw8<T> raw = raw8(L, at, V);
         for (int first = wave * kSampleSegment; first < V; first += STEP) {
             const Raw8<T> next = raw8(L, at + STEP, V);
             float v[8];
@@ -204,6 +210,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
             at += STEP;
         }
     };
+    auto pass = [&](auto &&fn) SR_INLINE { pass_from(first_raw(), fn); };
     // exclusive prefix sum over the threads; total: of all
     auto scan = [&](sr_mass v, sr_mass &total) SR_INLINE {
         const sr_mass s = sample_wave_scan(v);
@@ -254,10 +261,68 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         if (lane == 0 && lo <= hi) { atomicMin(&low_s, lo); atomicMax(&high_s, hi); }
     };
 
+    const Raw8<T> raw = first_raw();                 // (on its way while the parameters are read)
+    const float temp = p.temperature ? p.temperature[row] : 1.0f;
+    const float top_p = p.top_p ? p.top_p[row] : 1.0f;
+    const float min_w = p.min_p ? p.min_p[row] : 0.0f;
+    const int top_k = p.top_k ? p.top_k[row] : 0;
+    const bool by_count = uniform(top_k > 0 && top_k < V), by_sum = uniform(top_p < 1.0f);
+
+    // A logit's place in the table of bf16 weights is its code minus the first one of its sign's part, in 16 bits modulo 2^16; logits
+    // that are not in the table have its end for a place, of which those from kHugeLogit up have to be absent and those of a magnitude
+    // below kTinyLogit to be told apart.  Places of N logits times 2^SHIFT:
+    auto places = [&](const auto &v, auto &&at, auto shift) SR_INLINE {
+        constexpr uint16_t pos = kCodeFrom, neg = 0x8000 + kCodeFrom - kCodeSign, end = kSampleCodes;
+#pragma unroll
+        for (unsigned i = 0; i < sizeof(v) / sizeof(v[0]); i += 2) {
+            const sr_codes x = __builtin_bit_cast(sr_codes, __builtin_amdgcn_perm(__float_as_uint(v[i + 1]), __float_as_uint(v[i]), 0x07060302u));
+            const sr_codes y = __builtin_elementwise_min(__builtin_elementwise_min((sr_codes)(x - pos), (sr_codes)(x - neg)), sr_codes{end, end}) << (uint16_t)decltype(shift)::value;
+            at[i] = y[0];
+            at[i + 1] = y[1];
+        }
+    };
+    auto tiny = [&](const auto &v) SR_INLINE {       // one of the wavefront's logits is
+        float small = fabsf(v[0]);
+#pragma unroll
+        for (unsigned i = 1; i < sizeof(v) / sizeof(v[0]); ++i) small = fminf(small, fabsf(v[i]));
+        return __ballot(small < kTinyLogit) != 0;
+    };
+    // Rows of bf16 logits with top-p alone are counted by code while their largest is looked for; the tiny ones are listed.
+    uint32_t *const count = reinterpret_cast<uint32_t *>(&lds);
+    static_assert(offsetof(Lds, list_at) == kSampleCodes * 4 && kSampleCodes % NT == 0, "the counts fit in front of the list");
+    const bool counted = CODES && V >= kSampleTabled && by_sum && !by_count && uniform(temp > 0.0f && top_p > 0.0f && !(min_w > 0.0f));
+    if (counted) {
+#pragma unroll
+        for (int i = 0; i < kSampleCodes / NT; ++i) count[i * NT + tid] = 0;
+        if (tid == 0) n_list = 0;
+        __syncthreads();
+    }
     float own_most = -INFINITY;
-    pass([&](const float (&v)[8], int) SR_INLINE {
+    pass_from(raw, [&](const float (&v)[8], int) SR_INLINE {
 #pragma unroll
         for (int i = 0; i < 8; ++i) own_most = fmaxf(own_most, v[i]);
+        if constexpr (CODES) {
+            if (!counted) return;
+            uint32_t at[8];
+            places(v, at, std::integral_constant<int, 2>{});
+            if (tiny(v)) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) at[i] = fabsf(v[i]) < kTinyLogit ? 4 * kSampleCodes : at[i];
+#pragma unroll 1
+                for (int i = 0; i < 8; ++i) {
+                    float x = v[0];
+#pragma unroll
+                    for (int k = 1; k < 8; ++k) x = i == k ? v[k] : x;
+                    if (fabsf(x) < kTinyLogit) {
+                        const uint32_t k = atomicAdd(&n_list, 1u);
+                        if (k < (uint32_t)kSampleList) list_at[k] = (int)__float_as_uint(x);
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (at[i] < 4 * kSampleCodes) atomicAdd(reinterpret_cast<uint32_t *>(reinterpret_cast<char *>(count) + at[i]), 1u);
+        }
     });
     const uint32_t wave_most = sample_wave_max(sample_key(own_most));
     if (lane == 0) red[wave] = wave_most;
@@ -274,9 +339,6 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         return;
     }
 
-    const float temp = p.temperature ? p.temperature[row] : 1.0f;
-    const float top_p = p.top_p ? p.top_p[row] : 1.0f;
-    const int top_k = p.top_k ? p.top_k[row] : 0;
     if (!(temp > 0.0f) || top_k == 1 || top_p <= 0.0f) {                // one token: the first of the largest
         int first = V;
         if (own_most == most)
@@ -306,7 +368,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     const double most_d = (double)most, per_bit = (double)fminf(temp, 1e30f) * 0.6931471805599453, c = 1.0 / per_bit;
     // (2^-900 and less are alike; also what a NaN counts as)
     const double clamp_d = -900.0 * per_bit;
-    const float min_p = p.min_p && p.min_p[row] > 0.0f ? fminf(p.min_p[row], 1.0f) : 0.0f;
+    const float min_p = min_w > 0.0f ? fminf(min_w, 1.0f) : 0.0f;
     const sr_mass least = min_p > 0.0f ? max((sr_mass)1, (sr_mass)ceil((double)min_p * kSampleUnit)) : 1;
     const bool has_least = uniform(least > 1);
     auto mass = [&](float x) SR_INLINE {
@@ -330,69 +392,30 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         for (int i = 1; i < 8; ++i) top = fmaxf(top, v[i]);
         return __ballot(top >= floor_v) != 0;
     };
-    // bf16 logits have few values: from most down to floor_v, those of a magnitude below tiny_v apart (there are as many of them in each
-    // octave towards 0), they fit a table of their weights.  A logit's place in it is its code minus the first one of its sign's part, in 16 bits modulo 2^16.
+    // bf16 logits have few values, whose weights fit a table (codes above the largest logit's count as that)
     bool tabled = false, cut_in_table = false;       // cut_in_table: logits from cut_v down have no weight there
-    int pos_n = 0;
-    float tiny_v = 0.0f;
-    uint16_t pos = 0, neg = 0, end = 0;
     auto tabulate = [&]() SR_INLINE {
         if constexpr (CODES) {
-            if (tabled || hot || V < kSampleTabled) return;
-            auto code = [](float x) SR_INLINE { return (int)(__float_as_uint(x) >> 16 & 0x7fff); };
-            const int first = code(most), last = code(floor_v);
-            if (max(first, last) >= 0x6000) return;  // (2^65: so that no NaN's code falls into the table)
-            int neg_n = 0, from;                     // entries of each sign; the smallest magnitude
-            if (most > 0.0f && floor_v < 0.0f) {
-                from = max(0x1800, (first + last + 3 - kSampleCodes) / 2);          // (2^-79, for the same reason)
-                pos_n = max(0, first - from + 1);
-                neg_n = max(0, last - from + 1);
-                tiny_v = __uint_as_float((uint32_t)from << 16);
-            } else {
-                const int least_code = max(1, min(first, last));
-                from = max(least_code, max(first, last) - kSampleCodes + 1);
-                (most > 0.0f ? pos_n : neg_n) = max(0, max(first, last) - from + 1);
-                tiny_v = from > min(first, last) ? __uint_as_float((uint32_t)from << 16) : 0.0f;
-            }
-            if (pos_n + neg_n > kSampleCodes) return;
-            pos = (uint16_t)(pos_n ? from : 0x8000 + from);
-            neg = (uint16_t)(neg_n ? 0x8000 + from - pos_n : pos);
-            end = (uint16_t)(pos_n + neg_n);
-            for (int i0 = tid; i0 <= end; i0 += 8 * NT) {
+            if (tabled || hot || V < kSampleTabled || !(most < kHugeLogit && floor_v > -kHugeLogit)) return;
+            for (int i0 = tid; i0 <= kSampleCodes; i0 += 8 * NT) {
                 double d[8];
                 sr_mass m[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const int i = i0 + k * NT;
-                    const uint32_t bits = (uint32_t)(i < pos_n ? from + i : 0x8000 + from + i - pos_n) << 16;
-                    d[k] = fmax((double)__uint_as_float(bits) - most_d, clamp_d);
-                    d[k] = fmin(d[k], 0.0);          // (codes behind the last one)
+                    const uint32_t bits = (uint32_t)(i + (i < kCodeSign ? kCodeFrom : 0x8000 + kCodeFrom - kCodeSign)) << 16;
+                    d[k] = fmin(fmax((double)__uint_as_float(bits) - most_d, clamp_d), 0.0);
                 }
                 sample_mass(d, c, m);
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (i0 + k * NT <= end) by_code[i0 + k * NT] = i0 + k * NT < end && m[k] >= least ? m[k] : 0;
+                for (int k = 0; k < 8; ++k) {
+                    const int i = i0 + k * NT;
+                    if (i <= kSampleCodes) by_code[i] = i < kSampleCodes && m[k] >= least ? m[k] : 0;
+                }
             }
-            tiny_v = scalar(tiny_v);
             tabled = true;
             __syncthreads();
         }
-    };
-    // N logits' places, those of logits behind the table its end, times 2^SHIFT
-    auto places = [&](const auto &v, auto &&at, auto shift) SR_INLINE {
-#pragma unroll
-        for (unsigned i = 0; i < sizeof(v) / sizeof(v[0]); i += 2) {
-            const sr_codes x = __builtin_bit_cast(sr_codes, __builtin_amdgcn_perm(__float_as_uint(v[i + 1]), __float_as_uint(v[i]), 0x07060302u));
-            const sr_codes y = __builtin_elementwise_min(__builtin_elementwise_min((sr_codes)(x - pos), (sr_codes)(x - neg)), sr_codes{end, end}) << (uint16_t)decltype(shift)::value;
-            at[i] = y[0];
-            at[i + 1] = y[1];
-        }
-    };
-    auto tiny = [&](const auto &v) SR_INLINE {       // some logit of the wavefront's vectors is not in the table
-        float small = fabsf(v[0]);
-#pragma unroll
-        for (unsigned i = 1; i < sizeof(v) / sizeof(v[0]); ++i) small = fminf(small, fabsf(v[i]));
-        return __ballot(small < tiny_v) != 0;
     };
     // the weights of N logits from the table; false if one of the wavefront's is not in it
     auto looked_up = [&](auto &v, auto &m) SR_INLINE {
@@ -520,57 +543,30 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         in_list = n <= (uint32_t)kSampleList;
     }
     auto top_p_limit = [&](sr_mass sum) SR_INLINE { return max((sr_mass)ceil((double)top_p * (double)sum), (sr_mass)1); };
-    // top-p of bf16 logits: how many there are of each code, from which follow the last kept value and how many of it are kept; then the
-    // segments' sums and their numbers of that value, in one pass.  false if the limit is reached among the tiny ones.
+    // top-p of counted rows: from the counts follow the last kept value and how many of it are kept; then the segments' sums and their
+    // numbers of that value, in one pass.  false if the limit is reached among the tiny ones.
     auto top_p_by_code = [&]() SR_INLINE {
         if constexpr (CODES) {
             constexpr int PERC = kSampleCodes / NT;
-            static_assert(sizeof(lds) >= kSampleCodes * 4 && kSampleCodes % NT == 0, "the counts fit");
-            uint32_t *const count = reinterpret_cast<uint32_t *>(&lds);
-            const uint32_t end4 = 4u * end;
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < PERC; ++i) count[i * NT + tid] = 0;
             if (tid == 0) { few_sum[0] = 0; found = ~0u; }
             __syncthreads();
-            pass([&](const float (&v)[8], int) SR_INLINE {
-                const bool some_tiny = tiny(v);
-                if (some_tiny) {
-#pragma unroll 1
-                    for (int i = 0; i < 8; ++i) {
-                        float x = v[0];
-#pragma unroll
-                        for (int k = 1; k < 8; ++k) x = i == k ? v[k] : x;
-                        if (fabsf(x) < tiny_v) atomicAdd(&few_sum[0], mass(x));
-                    }
-                }
-                uint32_t at[8];
-                places(v, at, std::integral_constant<int, 2>{});
-                if (some_tiny) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) at[i] = fabsf(v[i]) < tiny_v ? end4 : at[i];
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (at[i] < end4) atomicAdd(reinterpret_cast<uint32_t *>(reinterpret_cast<char *>(count) + at[i]), 1u);
-            });
+            for (uint32_t i = tid; i < n_list; i += NT) atomicAdd(&few_sum[0], mass(__uint_as_float((uint32_t)list_at[i])));
             __syncthreads();
             const sr_mass tiny_sum = few_sum[0];
             // the k-th code from the largest down: positive ones lie the other way round
-            auto place = [&](int k) SR_INLINE { return k < pos_n ? pos_n - 1 - k : k; };
+            auto place = [&](int k) SR_INLINE { return k < kCodeSign ? kCodeSign - 1 - k : k; };
             sr_mass own = 0, total;
 #pragma unroll
             for (int i = 0; i < PERC; ++i) {
                 const int k = tid * PERC + i;
-                if (k < end) own += (sr_mass)count[place(k)] * by_code[place(k)];
+                own += (sr_mass)count[place(k)] * by_code[place(k)];
             }
             sr_mass up = scan(own, total);
             const sr_mass limit = top_p_limit(total + tiny_sum);
 #pragma unroll
             for (int i = 0; i < PERC; ++i) {
                 const int k = tid * PERC + i;
-                if (k >= end) break;
-                const sr_mass one = by_code[place(k)], all_of = (sr_mass)count[place(k)] * one, before = up + (k >= pos_n ? tiny_sum : 0);
+                const sr_mass one = by_code[place(k)], all_of = (sr_mass)count[place(k)] * one, before = up + (k >= kCodeSign ? tiny_sum : 0);
                 if (before < limit && limit - before <= all_of) {
                     found = (uint32_t)k;
                     low_s = (uint32_t)((limit - before + one - 1) / one);
@@ -583,13 +579,13 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
             if (last < 0) return false;
             const uint32_t n_kept = (uint32_t)__builtin_amdgcn_readfirstlane((int)low_s);
             const bool some = uniform(n_kept < high_s);          // not all of the value
-            cut_v = __uint_as_float(((uint32_t)(last < pos_n ? pos : neg) + (uint32_t)last_at) << 16);
+            cut_v = __uint_as_float((uint32_t)(last_at + (last < kCodeSign ? kCodeFrom : 0x8000 + kCodeFrom - kCodeSign)) << 16);
             cut_at = some ? -1 : V;
             cut = cut_in_table = true;
             floor_v = scalar(fmaxf(floor_v, cut_v));
             const sr_mass one = by_code[last_at];
             __syncthreads();
-            for (int k = last + (some ? 0 : 1) + tid; k < end; k += NT) by_code[place(k)] = 0;
+            for (int k = last + (some ? 0 : 1) + tid; k < kSampleCodes; k += NT) by_code[place(k)] = 0;
             clear();
             pass([&](const float (&v)[8], int at) SR_INLINE {
                 if (!live(v)) return;
@@ -646,13 +642,13 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         return false;
     };
     // top-k (their number), then top-p (their mass): the kept tokens end at the first one with which a limit is reached
-    const bool by_count = uniform(top_k > 0 && top_k < V), by_sum = uniform(top_p < 1.0f);
-    if (by_sum && !by_count && !in_list) {
+    if (counted && uniform(n_list <= (uint32_t)kSampleList)) {
         tabulate();
         summed = tabled && top_p_by_code();
     }
     for (int by_mass = summed ? 2 : 0; by_mass < 2; ++by_mass) {
         if (by_mass ? !by_sum : !by_count) continue;
+        asm volatile("" : "+v"(tid), "+v"(lane));    // (addresses formed from them are not held in registers from here to the end)
         auto limit_of = [&](sr_mass sum) SR_INLINE {
             return by_mass ? top_p_limit(sum) : (sr_mass)top_k;
         };

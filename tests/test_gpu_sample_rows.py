@@ -174,6 +174,47 @@ def test_extreme_temperatures(srm, t):
     check(srm, logits, rng.random(8), temperature=[t] * 8, top_p=[0.9, 1.0] * 4)
 
 
+def _odd_rows(rng, V):
+    """Rows on which a table of the weights of bf16 logits, with tiny and huge ones apart, could go wrong."""
+    x = rng.standard_normal((13, V)) * 2.5
+    x[1] *= 4e-4                                              # most magnitudes below 2^-11
+    x[2] /= 5
+    x[2, ::40] = 0.0
+    x[3] = -20.0
+    x[3, rng.permutation(V)[:900]] = 0.0                      # limits among the zeros, few enough to be listed
+    x[4] = 3.0
+    x[5] = rng.choice([2.0, 1.0, -1.0], V)
+    x[6] *= 100                                               # magnitudes above 2^9
+    x[7] = -np.abs(x[7]) - 1
+    x[8, ::2] = -INF
+    x[8, 1::50] = NAN
+    x[9, V // 3] = INF
+    x[10] = rng.uniform(400, 511, V)
+    x[11] = rng.uniform(-5e-4, 5e-4, V)
+    x[11, ::100] = 4.883e-4                                   # on both sides of 2^-11
+    x[12] = np.where(rng.random(V) < 0.5, -510.0, -511.9)
+    return x.astype(np.float32)
+
+
+@pytest.mark.parametrize("V", [16383, 16384, 20011])
+@pytest.mark.parametrize("times", [1, 6])                     # fewer and more rows than compute units
+def test_top_p_of_bf16_logits_of_few_or_odd_values(srm, V, times):
+    rng = np.random.default_rng(V + times)
+    top_p = [0.3, 0.5, 0.9, 0.99, 0.9999, 1.0]
+    x = np.concatenate([np.repeat(_odd_rows(rng, V), len(top_p), axis=0) for _ in range(times)])
+    rows = len(x)
+    check(srm, torch.from_numpy(x).cuda().bfloat16(), rng.random(rows), top_p=top_p * (rows // len(top_p)),
+          temperature=np.tile(np.repeat([1.0, 1.0, 0.5, 1.0, 1.0, 0.7, 100.0, 1.0, 1.0, 1.0, 10.0, 1.0, 1.0], len(top_p)), times))
+
+
+@pytest.mark.parametrize("t", [0.05, 3.0, 11.5, 20.0, 1e4])
+def test_temperatures_of_bf16_rows(srm, t):
+    """From hot rows whose lowest logit with weight lies below -2^9 to cold ones."""
+    rng = np.random.default_rng(31)
+    check(srm, _logits(rng, 8, 30000, 0, torch.bfloat16), rng.random(8), temperature=[t] * 8, top_p=[0.9, 1.0] * 4, top_k=[0] * 6 + [700] * 2,
+          min_p=[0.0] * 4 + [0.01] * 2 + [0.0] * 2)
+
+
 def test_an_infinite_temperature_is_the_largest(srm):
     """Of logits that far apart, the probabilities are those of 1e30."""
     x = torch.tensor([[0.0, -2e30], [3e38, -3e38]], device="cuda")

@@ -49,11 +49,11 @@ def test_the_second_code_object_holds_the_operators(kernels):
 
 
 def test_no_operator_spills(kernels):
-    """sample_rows_kernel of fp32 logits apart: a handful of values that live across its passes lie in scratch memory, outside their loops."""
+    """sample_rows_kernel of bf16 logits apart: three registers that live across its passes lie in scratch memory, outside their loops."""
     spilled = {n: (q[".vgpr_spill_count"], q[".private_segment_fixed_size"]) for n, q in kernels.items()
                if q[".vgpr_spill_count"] or q[".private_segment_fixed_size"]}
-    samplers = {n: v for n, v in spilled.items() if "sample_rows_kernelIf" in n}
-    assert spilled == samplers and all(v[0] <= 8 and v[1] <= 32 for v in samplers.values()), spilled
+    samplers = {n: v for n, v in spilled.items() if "sample_rows_kernelIDF16b" in n}
+    assert spilled == samplers and all(v[0] <= 4 and v[1] <= 16 for v in samplers.values()), spilled
 
 
 def test_operators_fit_the_work_groups_that_their_rules_count_on(kernels):
@@ -64,6 +64,6 @@ def test_operators_fit_the_work_groups_that_their_rules_count_on(kernels):
         if "gemm_fp8_tile_kernel" in n:
             assert registers * waves <= 1024, n                  # a SIMD's 512 registers for a quarter of two work-groups' wavefronts
         if "sample_rows_kernel" in n:
-            assert registers <= 128 and q[".group_segment_fixed_size"] <= 80 * 1024, n
+            assert registers <= 128 and q[".group_segment_fixed_size"] * (2 if waves == 8 else 1) <= 160 * 1024, n
         if "gemm_fp8_persist_kernel" in n:
             assert registers <= 256, n
