@@ -187,7 +187,10 @@ static int launch_fp8_slices(const Fp8Call &c)
 //     9.0 | 11.1 | 9.4, 1024 x 4096 x 4096 33.0 | 36.6 | 30.4
 //   256x256 persistent | 128x128 by eight wavefronts: 8192^3 412 | 582, 4096^3 55.5 | 85, 3001 x 4001 x 1024 18.2 | 19.7, but 2048 x 4096 x 4096
 //     (128 tiles for 256 CUs) 47.5 | 39.7: a tile of 256x256 takes 0.7 of the time of four tiles of 128x128, two of which a CU holds
-//   fp32 outputs, 128x128 by four | eight wavefronts: 8192^3 892 | 1010, 16384 x 1024 x 4096 (+=) 133 | 143, 3001 x 4001 x 1024 (+=) 39.9 | 35.4
+//   fp32 outputs, 128x128 by four | eight wavefronts: 8192^3 892 | 1010, 16384 x 1024 x 4096 (+=) 133 | 143, 3001 x 4001 x 1024 (+=) 39.9 | 35.4;
+//     64x128 while three of them on each CU take a launch in one round, or else 128x64 | the better of those two: 1500 x 4096 x 2048 29.7 | 33.3,
+//     (+=) 34.7 | 38.8, 3000 x 2048 x 8192 106 | 115, 26464 x 156 x 6016 81 | 88 (9000 x 700 x 1024, not one round: 21.9 | 20.1);
+//     two blocks of K, 64x64 | 64x128 | 128x128: 8192 x 2048 x 256 18.8 | 17.8 | 20.3, (+=) 25.2 | 27.6 | 31.1, 16384 x 1024 x 128 (+=) 23.5 | 25.2 | 24.0
 template <int EPI>
 static int linear_fp8(const Fp8Call &c)
 {
@@ -204,6 +207,9 @@ static int linear_fp8(const Fp8Call &c)
     }
     if (tiles(128, 128) >= cus) {
         if constexpr (kFp8Exact<EPI>) {
+            if (c.Kp <= 256) return EPI == EPI_RESID ? launch_fp8_tile<64, 64, 2, 2, 2, EPI>(c) : launch_fp8_tile<64, 128, 2, 2, 2, EPI>(c);
+            if (tiles(64, 128) <= 3 * cus) return launch_fp8_tile<64, 128, 2, 2, 2, EPI>(c);
+            if (tiles(128, 64) <= 3 * cus) return launch_fp8_tile<128, 64, 2, 2, 2, EPI>(c);
             if (tiles(128, 128) >= 2 * cus && (EPI == EPI_F32 || c.Kp >= 2048)) return launch_fp8_tile<128, 128, 2, 2, 2, EPI>(c);
         }
         return launch_fp8_tile<128, 128, 2, 4, 2, EPI>(c);

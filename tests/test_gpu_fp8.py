@@ -201,7 +201,8 @@ def _matrix(srm, rng, rows, K, scale, whole=False):
 SIZES = [(1, 1, 1), (1, 16, 128), (2, 3, 127), (1, 32000, 1024), (15, 100, 129), (16, 16, 512), (17, 64, 513), (33, 257, 640), (37, 4096, 1024),
          (64, 64, 2048), (65, 1000, 1000), (100, 130, 4096), (127, 31, 300), (130, 1024, 128), (256, 256, 256), (257, 260, 384), (300, 512, 1024),
          (513, 1030, 777), (1000, 2000, 128), (1500, 1100, 1152), (2100, 2052, 256), (4099, 516, 640), (77, 8, 16384), (520, 4100, 2100), (9, 5000, 300),
-         (3001, 4001, 1000), (2100, 8200, 256), (2060, 8301, 300), (4100, 4700, 1100), (5000, 3000, 100), (2900, 3000, 2100)]
+         (3001, 4001, 1000), (2100, 8200, 256), (2060, 8301, 300), (4100, 4700, 1100), (5000, 3000, 100), (2900, 3000, 2100),
+         (1450, 4100, 700), (26000, 156, 300)]
 
 
 @pytest.mark.parametrize("M,N,K", SIZES)
