@@ -17,8 +17,18 @@
 //   first ones by index are kept;
 //   sums of the kept weights by segment, one of which holds the token.
 // A list that is too long (nearly equal logits) and a top_k above 512 take the histogram again, of the step's keys or of counts.
-// What bounds it: the instructions of the weights, some 30 per logit and pass that forms them (one, two with top-p), eight independent
-// chains at a time; below that the row's passes through the last-level cache.
+//
+// bf16 logits have few values.  Their weights are formed once per value, not per logit, into a table in LDS, and a row with top-p alone
+// counts its logits by value in its first pass: the counts times the table give the last kept value and how many of it are kept, and the
+// second pass is the last one.
+//
+// What bounds it (us, rows x logits, normal logits): fp32 rows the instructions of the weights, some 30 per logit and pass that forms them
+// (one, two with top-p), eight independent chains at a time; bf16 rows the LDS, 18 clocks of a CU for a wavefront's 64 additions to the counts
+// and as many for its 64 looks into the table; below that the row's passes through the last-level cache.
+//   greedy | no limit | top-p 0.95 | top-k 50 | min-p 0.05: 256 x 32000 fp32 6.3 | 18 | 40 | 17 | 14, bf16 5.7 | 17 | 24 | 16 | 13;
+//   1000 x 128001 fp32 105 | 198 | 426 | 160 | 159, bf16 61 (4.2 TB/s) | 124 | 177 | 97 | 97; one row of 32000 fp32 3.9 | 14 | 35 | 14 | 11.
+//   With weights of bf16 logits formed one by one 1000 x 128001 took 441 with top-p, with a table but a histogram of weights 397, counted in a
+//   pass of its own 205.  A table of the limit's region only (guessed from one segment in eight, fewer LDS additions): 421.
 #pragma once
 #include "fp8.hpp"
 #include <cstddef>
@@ -27,9 +37,10 @@
 typedef unsigned long long sr_mass;
 typedef __attribute__((ext_vector_type(2))) uint16_t sr_codes;
 constexpr int kSampleVocab = 1 << 20, kSampleSegment = 512, kSampleSteps = kSampleVocab / kSampleSegment;
-// The table of bf16 weights: magnitudes from 2^-11 up to 2^9, twenty octaves of 128 codes, of both signs.  Rows of fewer logits than
-// kSampleTabled do without.
-constexpr int kCodeSign = 2560, kCodeFrom = 0x3A00, kSampleCodes = 2 * kCodeSign, kSampleTabled = 16384;
+// The table of bf16 weights: magnitudes from 2^-11 up to 2^9, twenty octaves of 128 codes, of both signs.  Forming it is a good part of
+// a short row's work: with it | without, us, 2000 rows with top-p of 4096 logits 63 | 56, 8192: 73 | 84, 32000: 127 | 220; without limits 16384:
+// 56 | 55, 24576: 69 | 72, 32000: 83 | 90.
+constexpr int kCodeSign = 2560, kCodeFrom = 0x3A00, kSampleCodes = 2 * kCodeSign, kSampleCounted = 6144, kSampleTabled = 20480;
 constexpr float kTinyLogit = 0.00048828125f, kHugeLogit = 512.0f;
 constexpr int kSampleList = 1024, kSampleFew = 64, kSampleBound = 512, kSampleDense = 256;
 #define SR_INLINE __attribute__((always_inline))
@@ -290,7 +301,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     // Rows of bf16 logits with top-p alone are counted by code while their largest is looked for; the tiny ones are listed.
     uint32_t *const count = reinterpret_cast<uint32_t *>(&lds);
     static_assert(offsetof(Lds, list_at) == kSampleCodes * 4 && kSampleCodes % NT == 0, "the counts fit in front of the list");
-    const bool counted = CODES && V >= kSampleTabled && by_sum && !by_count && uniform(temp > 0.0f && top_p > 0.0f && !(min_w > 0.0f));
+    const bool counted = CODES && V >= kSampleCounted && by_sum && !by_count && uniform(temp > 0.0f && top_p > 0.0f && !(min_w > 0.0f));
     if (counted) {
 #pragma unroll
         for (int i = 0; i < kSampleCodes / NT; ++i) count[i * NT + tid] = 0;
@@ -396,7 +407,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
     bool tabled = false, cut_in_table = false;       // cut_in_table: logits from cut_v down have no weight there
     auto tabulate = [&]() SR_INLINE {
         if constexpr (CODES) {
-            if (tabled || hot || V < kSampleTabled || !(most < kHugeLogit && floor_v > -kHugeLogit)) return;
+            if (tabled || hot || !(most < kHugeLogit && floor_v > -kHugeLogit)) return;
             for (int i0 = tid; i0 <= kSampleCodes; i0 += 8 * NT) {
                 double d[8];
                 sr_mass m[8];
@@ -693,7 +704,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
                 if (listed) floor_v = bound;
             }
         }
-        if (by_mass && !listed) tabulate();
+        if (by_mass && !listed && V >= kSampleTabled) tabulate();
         while (!listed) {
             clear();
             pass([&](const float (&v)[8], int at) SR_INLINE {
@@ -840,7 +851,7 @@ sample_rows_kernel(const T *__restrict__ logits, SampleRows p)
         floor_v = scalar(fmaxf(floor_v, cut_v));
     }
 
-    if (!in_list && !cut) tabulate();
+    if (V >= kSampleTabled && !in_list && !cut) tabulate();
     const float u = p.uniform[row];
     sr_mass total;
     const int tok = index_of([&](float x, int) SR_INLINE { return mass(x); }, masses, [&](const float (&v)[8], int at) SR_INLINE {
