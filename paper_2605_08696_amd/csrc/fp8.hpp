@@ -185,7 +185,8 @@ quantize_fp8_kernel(const T *__restrict__ x, int64_t ldx, uint32_t rows, int d, 
 }
 
 // x += add (if there is one), then y = x / sqrt(mean(x^2) + eps) * gain of the row as it is stored -> q, scales.  NW wavefronts hold a
-// row in registers, wavefront w its groups w, w + NW, ..., G of them at most.
+// row in registers, wavefront w its groups w, w + NW, ..., G of them at most.  16384 x 1024 fp32 + bf16 33.5 us (5.5 TB/s, the rate of a copy of
+// as many bytes), one row 2.6 us, a launch and a trip to memory.  Not kept: two rows a wavefront (39 .. 42).
 template <typename T, typename TAdd, int NW, int G>
 __global__ void __launch_bounds__(NW > 4 ? NW * 64 : 256)
 rmsnorm_fp8_kernel(T *__restrict__ x, int64_t ldx, const TAdd *__restrict__ add, int64_t ld_add, const float *__restrict__ gain, float eps,

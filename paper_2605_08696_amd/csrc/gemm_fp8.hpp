@@ -164,6 +164,11 @@ __device__ __forceinline__ unsigned fp8_lds_address(const void *p)
 // A BM x BN tile by WM x WN wavefronts; blocks of K (128 bytes of a row) pass through a ring of NS stages in LDS, NS - 1 of them on their
 // way.  A stage holds BM + BN rows of 128 bytes, 16-byte chunk c of row r at chunk c ^ swz(r), and behind them the word of scales of each
 // row (the word of four blocks, loaded again for each of them).
+// Bound by the trip through L2 and the LDS reads between two barriers, of which other work-groups on the CU fill part: two of 128x128, three of
+// 64x128.  fp32 outputs besides by widening, two values an instruction: 8192^3 892 .. 967 us (1.1 .. 1.2 PFLOP/s; the bf16 product of the same
+// size 1.46), 3001 x 4001 x 1000 with addition 36 us (matrix pipes busy for a quarter of it: 768 tiles are one and a half rounds, and the
+// stored rows are read and written behind the last product).  Not kept: the operands of the next block in registers meanwhile
+// (128x128 spills, 128x64 gains nothing), what is added to requested in front of the first loads (+-2%).
 template <int BM, int BN>
 constexpr int fp8_stage_bytes() { return (BM + BN) * (128 + 4); }
 
@@ -273,7 +278,8 @@ gemm_fp8_tile_kernel(const unsigned char *__restrict__ A, const uint32_t *__rest
 // ------------------------------------------------------------------ few tiles: K cut over the wavefronts
 // A launch with at most a tile for each CU takes as long as one tile's trip through K.  Here eight wavefronts cut K between them, each
 // with its own blocks for the whole (16 RT) x (16 CT) tile through a ring of NS stages of its own, without a barrier; the partial
-// tiles meet in LDS and are added in the wavefronts' order.
+// tiles meet in LDS and are added in the wavefronts' order.  Bound by latency (37 x 4096 x 1024: 3.7 us, of which an empty launch is 2), for
+// one row by reading W: 1 x 32000 x 1024 5.2 us where the caches hold it, 8.4 (3.9 TB/s) where not.
 template <int RT, int CT>
 constexpr int fp8_slice_stage() { return 16 * (RT + CT) * 128 + 512; }           // two loads of 64 words of scales
 template <int RT, int CT, int NS>
@@ -371,8 +377,12 @@ gemm_fp8_slices_kernel(const unsigned char *__restrict__ A, const uint32_t *__re
 //     half 0 of T: products of its first 64 k | operands of its second half | loads of A of T+2 (unit 2T+4: W of T-1 is done)
 //     half 1 of T, its first two products; barrier: T+1 has landed, T has been read by all
 //     the others of the second 64 k | operands of T+1's first half | loads of W of T+2 (unit 2T: A of T is done)
-// An operand of A is read for the next half behind the two products that use it in this one, into the same registers.  The ring is all of the LDS, so the scales are in registers: the words of four blocks for this lane's rows, the lowest byte in use, and
-// those of the next four, requested when the last ones begin to be used.
+// An operand of A is read for the next half behind the two products that use it in this one, into the same registers.  The ring is all of
+// the LDS, so the scales are in registers: the words of four blocks for this lane's rows, the lowest byte in use, and those of the next
+// four, requested when the last ones begin to be used.
+// 8192^3: 408 .. 424 us (2.6 .. 2.7 PFLOP/s, the matrix pipes busy for 72% of the clocks at a sustained 1.7 GHz, where a bare loop of the
+// instruction reaches 3.9 PFLOP/s), 418 with a wait for the stores of a tile in front of the next one's loads; 16384 x 1024 x 4096, one tile
+// a CU, 61 us (2.3 PFLOP/s): the first loads and the last stores have nothing to hide behind.
 constexpr int kFp8PersistLds = 160 * 1024;
 template <int EPI>
 __global__ void __launch_bounds__(512)
