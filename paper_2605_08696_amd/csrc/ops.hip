@@ -240,12 +240,16 @@ extern "C" int srm_linear_fp8(int32_t epilogue, const void *d_a, const void *d_a
 }
 
 // ------------------------------------------------------------------ sampling by request
-// Work-groups of 1024 threads while each row has a CU of its own, behind that of 512, of which a CU holds two.
+// Work-groups of 1024 threads while each row has a CU of its own, behind that of 512, of which a CU holds two; rows of up to
+// 1024 logits by a wavefront each.
 template <typename T>
-static void launch_sample(const void *d_logits, int64_t rows, const SampleRows &p, bool wide, hipStream_t st)
+static void launch_sample(const void *d_logits, const SampleRows &p, hipStream_t st)
 {
-    if (wide) hipLaunchKernelGGL((sample_rows_kernel<T, 1024>), grid_of(rows), dim3(1024), 0, st, static_cast<const T *>(d_logits), p);
-    else hipLaunchKernelGGL((sample_rows_kernel<T, 512>), grid_of(rows), dim3(512), 0, st, static_cast<const T *>(d_logits), p);
+    const T *logits = static_cast<const T *>(d_logits);
+    if (p.V <= kSampleSegment) hipLaunchKernelGGL((sample_short_rows_kernel<T, 1>), grid_of(cdiv(p.rows, 4)), dim3(256), 0, st, logits, p);
+    else if (p.V <= 2 * kSampleSegment) hipLaunchKernelGGL((sample_short_rows_kernel<T, 2>), grid_of(cdiv(p.rows, 4)), dim3(256), 0, st, logits, p);
+    else if (p.rows <= device_cus()) hipLaunchKernelGGL((sample_rows_kernel<T, 1024>), grid_of(p.rows), dim3(1024), 0, st, logits, p);
+    else hipLaunchKernelGGL((sample_rows_kernel<T, 512>), grid_of(p.rows), dim3(512), 0, st, logits, p);
 }
 
 extern "C" int srm_sample_rows(int32_t dtype, const void *d_logits, int64_t ld, int64_t rows, int32_t vocab, const float *d_temperature,
@@ -262,9 +266,8 @@ extern "C" int srm_sample_rows(int32_t dtype, const void *d_logits, int64_t ld, 
     if (!whole) return fail(SRM_EINVAL, "%s: %s", who, kNotWhole);
     const SampleRows p{rows, ld, vocab, d_temperature, d_top_p, d_min_p, d_uniform, d_top_k, d_tok_out, d_logprob};
     hipStream_t st = as_stream(hip_stream);
-    const bool wide = rows <= device_cus();
-    if (dtype == SRM_FP32) launch_sample<float>(d_logits, rows, p, wide, st);
-    else if (dtype == SRM_BF16) launch_sample<bf16>(d_logits, rows, p, wide, st);
+    if (dtype == SRM_FP32) launch_sample<float>(d_logits, p, st);
+    else if (dtype == SRM_BF16) launch_sample<bf16>(d_logits, p, st);
     else return fail(SRM_EINVAL, "%s: unknown dtype %d", who, dtype);
     HIP_TRY(hipGetLastError());
     return SRM_OK;

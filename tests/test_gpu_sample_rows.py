@@ -65,7 +65,7 @@ def _logits(rng, rows, V, pad=0, dtype=torch.float32, offset=0, scale=3.0):
     return t[:, :V]
 
 
-VOCABS = [(1, 0, 0), (2, 1, 0), (63, 0, 1), (64, 3, 0), (513, 0, 0), (1000, 5, 3), (4096, 0, 0), (8192, 0, 0), (8193, 0, 1), (32000, 0, 0),
+VOCABS = [(1, 0, 0), (2, 1, 0), (7, 0, 1), (8, 3, 0), (9, 0, 0), (63, 0, 1), (64, 3, 0), (511, 0, 0), (512, 1, 1), (513, 0, 0), (1000, 5, 3), (1023, 0, 0), (1024, 2, 0), (1025, 0, 1), (4096, 0, 0), (8192, 0, 0), (8193, 0, 1), (32000, 0, 0),
           (32001, 8, 0), (50021, 1, 2), (131072, 0, 0), (150001, 0, 1)]
 
 
@@ -215,6 +215,30 @@ def test_temperatures_of_bf16_rows(srm, t):
           min_p=[0.0] * 4 + [0.01] * 2 + [0.0] * 2)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [5, 300, 512, 513, 1000])
+def test_short_rows_of_few_or_odd_values(srm, V, dtype):
+    """Equal values at the limits, values of all magnitudes (a search by halves that takes long), masks, infinities, NaN."""
+    rng = np.random.default_rng(V)
+    x = rng.standard_normal((10, V)) * 2.5
+    x[1] = 3.0
+    x[2] = rng.choice([2.0, 1.0, -1.0], V)
+    x[3] = 10.0 ** rng.uniform(-30, 1, V)
+    x[4] = -x[3]
+    x[5, ::2] = -INF
+    x[5, 1::7] = NAN
+    x[6, V // 3:V // 3 + 3] = INF
+    x[7] = np.finfo(np.float32).min
+    x[7, V // 2] = -3e38
+    x[8] = -1e30
+    x[8, V // 4:V // 2 + 1] = 4.0
+    x[9] = np.where(rng.random(V) < 0.5, 0.0, -0.0)
+    x = torch.from_numpy(np.repeat(x.astype(np.float32), 9, axis=0)).cuda().to(dtype)
+    n = x.shape[0]
+    check(srm, x, rng.random(n), top_p=[0.3, 0.7, 0.999, 1.0, 1.0, 1.0, 0.5, 0.8, 1.0] * 10, top_k=[0, 0, 0, 3, 200, 1, 4, 250, 0] * 10,
+          min_p=[0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.01, 0.4] * 10)
+
+
 def test_an_infinite_temperature_is_the_largest(srm):
     """Of logits that far apart, the probabilities are those of 1e30."""
     x = torch.tensor([[0.0, -2e30], [3e38, -3e38]], device="cuda")
@@ -239,6 +263,17 @@ def test_more_rows_than_a_dimension_of_a_grid_has_threads_for(srm):
     near = ((run - goal[:, None]).abs() < 1e-9).any(1)        # (8 million draws: a few may lie that near)
     assert near.sum() < 10 and tok[-1] == -7
     assert ((tok[:-1] == want) | near).all()
+
+
+def test_more_work_groups_than_a_row_of_the_grid(srm):
+    rows, V = (1 << 21) + 3, 1025
+    logits = torch.randn(rows, V, device="cuda", dtype=torch.bfloat16)
+    tok = torch.full((rows + 1,), -7, dtype=torch.int32, device="cuda")
+    u, cold = torch.rand(rows, device="cuda"), torch.zeros(rows, device="cuda")
+    srm.sample_rows(logits, u, tok[:-1], temperature=cold)
+    top = logits.amax(1, keepdim=True)
+    assert tok[-1] == -7 and int(tok[:-1].amin()) >= 0
+    assert torch.equal(logits.gather(1, tok[:-1, None].long()), top)
 
 
 def test_the_ends_of_the_draw(srm):
