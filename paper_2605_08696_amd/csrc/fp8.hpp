@@ -129,9 +129,9 @@ __device__ __forceinline__ void store8(bf16 *p, int n, float (&v)[8])
     }
 }
 
-// This lane's eight values of the group's block lane / 16 -> their e4m3 codes; the group's four scales in every lane.  Infinities and
-// NaN do not count for the scale and become NaN.  Absent elements are zeros.
-__device__ __forceinline__ uint2 fp8_of_8(const float (&v)[8], uint32_t &scales)
+// This lane's eight values of the block of its sixteen lanes -> their e4m3 codes and the block's scale.  Infinities and NaN do not count
+// for the scale and become NaN.  Absent elements are zeros.
+__device__ __forceinline__ uint2 fp8_of_block(const float (&v)[8], uint32_t &scale)
 {
     constexpr uint32_t kInf = 0x7f800000u;
     uint32_t top = 0;
@@ -152,9 +152,23 @@ __device__ __forceinline__ uint2 fp8_of_8(const float (&v)[8], uint32_t &scales)
     int lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false), hi = __builtin_amdgcn_cvt_pk_fp8_f32(q[4], q[5], 0, false);
     lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], lo, true);
     hi = __builtin_amdgcn_cvt_pk_fp8_f32(q[6], q[7], hi, true);
-    scales = (uint32_t)__builtin_amdgcn_readlane(s, 0) | (uint32_t)__builtin_amdgcn_readlane(s, 16) << 8 |
-             (uint32_t)__builtin_amdgcn_readlane(s, 32) << 16 | (uint32_t)__builtin_amdgcn_readlane(s, 48) << 24;
+    scale = (uint32_t)s;
     return make_uint2((uint32_t)lo, (uint32_t)hi);
+}
+// The same of a group's four blocks; their scales in every lane.
+__device__ __forceinline__ uint2 fp8_of_8(const float (&v)[8], uint32_t &scales)
+{
+    uint32_t s;
+    const uint2 codes = fp8_of_block(v, s);
+    scales = (uint32_t)__builtin_amdgcn_readlane((int)s, 0) | (uint32_t)__builtin_amdgcn_readlane((int)s, 16) << 8 |
+             (uint32_t)__builtin_amdgcn_readlane((int)s, 32) << 16 | (uint32_t)__builtin_amdgcn_readlane((int)s, 48) << 24;
+    return codes;
+}
+// The word of a row of one or two blocks, of 16 or 32 lanes, from its blocks' scales.
+template <int LANES>
+__device__ __forceinline__ uint32_t fp8_narrow_word(uint32_t s)
+{
+    return LANES == 16 ? s | 0x7f7f7f00u : s | (uint32_t)__shfl_down((int)s, 16) << 8 | 0x7f7f0000u;
 }
 
 // x [rows][d], row stride ldx -> q [rows][dp], dp = d rounded up to 128, and scales [groups][rows].  A wavefront takes a group of R rows,
@@ -255,5 +269,76 @@ rmsnorm_fp8_kernel(T *__restrict__ x, int64_t ldx, const TAdd *__restrict__ add,
         const uint2 codes = fp8_of_8(v[i], s);
         if (col < dp) *reinterpret_cast<uint2 *>(q + row * dp + col) = codes;
         if (lane == 0) scales[(int64_t)g * rows + row] = s;
+    }
+}
+
+// Rows of up to 256 elements take a part of a wavefront: LANES lanes, 16 for one block, 32 for two.  (us, a wavefront a row | this: 45726 x 64
+// fp32 norm 20.8 | 6.9, 48376 x 64 bf16 quantize 15.3 | 5.2; 131072 x 128 fp32 quantize 13.6, 6.2 TB/s.)
+template <typename T, int LANES, int R>
+__global__ void __launch_bounds__(256)
+quantize_fp8_narrow_kernel(const T *__restrict__ x, int64_t ldx, uint32_t rows, int d, unsigned char *__restrict__ q, uint32_t *__restrict__ scales)
+{
+    constexpr int DP = LANES * 8, AT_ONCE = 64 / LANES;
+    const uint32_t unit = work_group() * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, row0 = unit * (R * AT_ONCE) + lane / LANES;
+    const int col = (int)(lane % LANES) * 8;
+    Raw8<T> raw[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) raw[r] = raw8(x + (int64_t)min(row0 + r * AT_ONCE, rows - 1) * ldx, col, d);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        float v[8];
+        widen8(raw[r], col, d, v);
+        uint32_t s;
+        const uint2 codes = fp8_of_block(v, s);
+        const uint32_t row = row0 + r * AT_ONCE, word = fp8_narrow_word<LANES>(s);
+        if (row >= rows) continue;
+        *reinterpret_cast<uint2 *>(q + (int64_t)row * DP + col) = codes;
+        if (col == 0) scales[row] = word;
+    }
+}
+template <typename T, typename TAdd, int LANES, int R>
+__global__ void __launch_bounds__(256)
+rmsnorm_fp8_narrow_kernel(T *__restrict__ x, int64_t ldx, const TAdd *__restrict__ add, int64_t ld_add, const float *__restrict__ gain, float eps,
+                          uint32_t rows, int d, unsigned char *__restrict__ q, uint32_t *__restrict__ scales)
+{
+    constexpr int DP = LANES * 8, AT_ONCE = 64 / LANES;
+    const uint32_t unit = work_group() * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, row0 = unit * (R * AT_ONCE) + lane / LANES;
+    const int col = (int)(lane % LANES) * 8;
+    Raw8<T> rx[R];
+    Raw8<TAdd> ra[R];
+    const Raw8<float> rg = raw8(gain, col, d);
+#pragma unroll
+    for (int r = 0; r < R; ++r) rx[r] = raw8(x + (int64_t)min(row0 + r * AT_ONCE, rows - 1) * ldx, col, d);
+    if (add) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) ra[r] = raw8<true>(add + (int64_t)min(row0 + r * AT_ONCE, rows - 1) * ld_add, col, d);
+    }
+    float g[8];
+    widen8(rg, col, d, g);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const uint32_t row = row0 + r * AT_ONCE;
+        float v[8], sum = 0.0f;
+        widen8(rx[r], col, d, v);
+        if (add) {
+            float t[8];
+            widen8(ra[r], col, d, t);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] += t[k];
+            store8(x + (int64_t)min(row, rows - 1) * ldx + col, row < rows ? d - col : 0, v);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum = fmaf(v[k], v[k], sum);
+        sum = row16_sum(sum);
+        if constexpr (LANES == 32) sum += __shfl_xor(sum, 16);
+        const float scale = 1.0f / sqrtf(sum / (float)d + eps);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = col + k < d ? v[k] * scale * g[k] : 0.0f;              // (scale may be a NaN)
+        uint32_t s;
+        const uint2 codes = fp8_of_block(v, s);
+        const uint32_t word = fp8_narrow_word<LANES>(s);
+        if (row >= rows) continue;
+        *reinterpret_cast<uint2 *>(q + (int64_t)row * DP + col) = codes;
+        if (col == 0) scales[row] = word;
     }
 }

@@ -33,6 +33,7 @@ static int check_fp8(const char *who, const void *d_q, const void *d_scales)
 static unsigned size_of(int32_t dtype) { return dtype == SRM_BF16 ? 2 : 4; }
 static const char *const kNotWhole = "an operand does not lie at a whole element";
 constexpr int64_t kMaxRows = 1ll << 30;
+constexpr int32_t kNarrow = 256;                      // rows of up to so many elements share wavefronts
 constexpr int32_t kMaxWidth = 1 << 22;                // (256 rows of a tile are addressed by 32 bits)
 
 template <typename T, int R>
@@ -48,6 +49,15 @@ static int launch_quantize(const void *d_x, int64_t ldx, int64_t rows, int32_t K
 template <typename T>
 static int quantize(const void *d_x, int64_t ldx, int64_t rows, int32_t K, void *d_q, void *d_scales, hipStream_t st)
 {
+    if (K <= kNarrow) {
+        constexpr int R = 2;
+        const bool two = K > kFp8Block;
+        const auto kernel = two ? quantize_fp8_narrow_kernel<T, 32, R> : quantize_fp8_narrow_kernel<T, 16, R>;
+        hipLaunchKernelGGL(kernel, grid_of(cdiv(rows, (two ? 8 : 16) * R)), dim3(256), 0, st, static_cast<const T *>(d_x), ldx, (uint32_t)rows, K,
+                           static_cast<unsigned char *>(d_q), static_cast<uint32_t *>(d_scales));
+        HIP_TRY(hipGetLastError());
+        return SRM_OK;
+    }
     const int64_t units = rows * cdiv(K, kFp8Group);
     if (units >= 1ll << 31) return fail(SRM_EINVAL, "srm_quantize_fp8: sizes out of range");
     if constexpr (sizeof(T) == 2) {
@@ -88,6 +98,16 @@ static int rmsnorm(void *d_x, int64_t ldx, const void *d_add, int64_t ld_add, co
                    void *d_q, void *d_scales, hipStream_t st)
 {
     const int groups = (int)cdiv(d, kFp8Group);
+    if (d <= kNarrow) {
+        constexpr int R = 2;
+        const bool two = d > kFp8Block;
+        const auto kernel = two ? rmsnorm_fp8_narrow_kernel<T, TAdd, 32, R> : rmsnorm_fp8_narrow_kernel<T, TAdd, 16, R>;
+        hipLaunchKernelGGL(kernel, grid_of(cdiv(rows, (two ? 8 : 16) * R)), dim3(256), 0, st, static_cast<T *>(d_x), ldx,
+                           static_cast<const TAdd *>(d_add), ld_add, d_gain, eps, (uint32_t)rows, d, static_cast<unsigned char *>(d_q),
+                           static_cast<uint32_t *>(d_scales));
+        HIP_TRY(hipGetLastError());
+        return SRM_OK;
+    }
 #define RMS_CASE(NW, G) return launch_rmsnorm<T, TAdd, NW, G>(d_x, ldx, d_add, ld_add, d_gain, eps, rows, d, d_q, d_scales, st)
     if (groups <= 1) RMS_CASE(1, 1);
     if (groups <= 2) RMS_CASE(1, 2);
@@ -184,9 +204,11 @@ static int launch_fp8_slices(const Fp8Call &c)
 //   up to 16 rows of many columns are bound by reading W: 16x32 | 16x16 | 32x32: 16 x 32000 x 4096 28.3 | 30.0 | 29.5, 1 x 32000 x 1024
 //     8.4 | 11.4 | 9.2 (W at 3.9 to 5.9 TB/s)
 //   64x64 with a ring of two | four | 128x128: 300 x 4096 x 1024 6.7 | 6.9 | 8.6, 2048 x 1024 x 4096 18.1 | 17.5 | 23.8, 700 x 4096 x 1024
-//     9.0 | 11.1 | 9.4, 1024 x 4096 x 4096 33.0 | 36.6 | 30.4
+//     9.0 | 11.1 | 9.4, 1024 x 4096 x 4096 33.0 | 36.6 | 30.4; 64x128 once there are three for each two CUs: 3755 x 872 x 1152 9.7 | 11.0 with 64x64,
+//     2620 x 1446 x 1024 with fp32 output 14.8 | 15.1 (882 x 1584 x 768, one for each 1.4: 12.4 | 9.5)
 //   256x256 persistent | 128x128 by eight wavefronts: 8192^3 412 | 582, 4096^3 55.5 | 85, 3001 x 4001 x 1024 18.2 | 19.7, but 2048 x 4096 x 4096
-//     (128 tiles for 256 CUs) 47.5 | 39.7: a tile of 256x256 takes 0.7 of the time of four tiles of 128x128, two of which a CU holds
+//     (128 tiles for 256 CUs) 47.5 | 39.7: a tile of 256x256 takes 0.7 of the time of four tiles of 128x128, two of which a CU holds;
+//     with two blocks of K 0.5: 10837 x 1721 x 256 19.5 | 15.7, 8192 x 2048 x 256 13.2 | 13.1
 //   fp32 outputs, 128x128 by four | eight wavefronts: 8192^3 892 | 1010, 16384 x 1024 x 4096 (+=) 133 | 143, 3001 x 4001 x 1024 (+=) 39.9 | 35.4;
 //     64x128 while three of them on each CU take a launch in one round, or else 128x64 | the better of those two: 1500 x 4096 x 2048 29.7 | 33.3,
 //     (+=) 34.7 | 38.8, 3000 x 2048 x 8192 106 | 115, 26464 x 156 x 6016 81 | 88 (9000 x 700 x 1024, not one round: 21.9 | 20.1);
@@ -203,7 +225,7 @@ static int linear_fp8(const Fp8Call &c)
     if (tiles(64, 64) <= cus) return launch_fp8_slices<4, 4, 1, EPI>(c);
     const int64_t rounds = cdiv(tiles(128, 128), 2 * cus);
     if constexpr (!kFp8Exact<EPI>) {
-        if (c.Kp >= 256 && 10 * cdiv(tiles(256, 256), cus) <= 7 * rounds) return launch_fp8_persist<EPI>(c, cus);
+        if (c.Kp >= 256 && 10 * cdiv(tiles(256, 256), cus) <= (c.Kp > 256 ? 7 : 5) * rounds) return launch_fp8_persist<EPI>(c, cus);
     }
     if (tiles(128, 128) >= cus) {
         if constexpr (kFp8Exact<EPI>) {
@@ -214,6 +236,7 @@ static int linear_fp8(const Fp8Call &c)
         }
         return launch_fp8_tile<128, 128, 2, 4, 2, EPI>(c);
     }
+    if (2 * tiles(64, 128) >= 3 * cus) return launch_fp8_tile<64, 128, 2, 2, 2, EPI>(c);
     return tiles(64, 64) <= 2 * cus ? launch_fp8_tile<64, 64, 2, 2, 4, EPI>(c) : launch_fp8_tile<64, 64, 2, 2, 2, EPI>(c);
 }
 
@@ -241,13 +264,13 @@ extern "C" int srm_linear_fp8(int32_t epilogue, const void *d_a, const void *d_a
 
 // ------------------------------------------------------------------ sampling by request
 // Work-groups of 1024 threads while each row has a CU of its own, behind that of 512, of which a CU holds two; rows of up to
-// 1024 logits by a wavefront each.
+// 512 logits by a wavefront each, and of up to 1024 where there are more than those work-groups take at once.
 template <typename T>
 static void launch_sample(const void *d_logits, const SampleRows &p, hipStream_t st)
 {
     const T *logits = static_cast<const T *>(d_logits);
     if (p.V <= kSampleSegment) hipLaunchKernelGGL((sample_short_rows_kernel<T, 1>), grid_of(cdiv(p.rows, 4)), dim3(256), 0, st, logits, p);
-    else if (p.V <= 2 * kSampleSegment) hipLaunchKernelGGL((sample_short_rows_kernel<T, 2>), grid_of(cdiv(p.rows, 4)), dim3(256), 0, st, logits, p);
+    else if (p.V <= 2 * kSampleSegment && p.rows > 2 * device_cus()) hipLaunchKernelGGL((sample_short_rows_kernel<T, 2>), grid_of(cdiv(p.rows, 4)), dim3(256), 0, st, logits, p);
     else if (p.rows <= device_cus()) hipLaunchKernelGGL((sample_rows_kernel<T, 1024>), grid_of(p.rows), dim3(1024), 0, st, logits, p);
     else hipLaunchKernelGGL((sample_rows_kernel<T, 512>), grid_of(p.rows), dim3(512), 0, st, logits, p);
 }

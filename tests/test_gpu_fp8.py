@@ -54,7 +54,8 @@ def _words(s):
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("rows,d,pad,offset", [
     (1, 1, 0, 0), (3, 2, 0, 1), (1, 127, 0, 0), (2, 128, 0, 0), (5, 129, 3, 0), (4, 511, 1, 1), (7, 512, 0, 0), (3, 513, 0, 3), (64, 1000, 8, 0),
-    (1, 4096, 0, 0), (37, 4096, 0, 0), (33, 4097, 2, 5), (260, 640, 0, 0), (2, 70000, 0, 0), (4099, 1030, 0, 1)])
+    (1, 4096, 0, 0), (37, 4096, 0, 0), (33, 4097, 2, 5), (260, 640, 0, 0), (2, 70000, 0, 0), (4099, 1030, 0, 1), (130, 7, 0, 0), (1000, 64, 5, 1), (77, 100, 0, 0), (70, 129, 1, 1), (41, 255, 0, 0),
+    (19, 256, 0, 0), (35, 257, 0, 0)])
 def test_quantize_has_the_bits_of_the_format(srm, dtype, rows, d, pad, offset):
     rng = np.random.default_rng(rows * 1000 + d)
     x = _wide(rng, rows, d, pad, TYPES[dtype], offset)
@@ -129,7 +130,7 @@ def check_norm(x, gain, eps, q, s, d):
 @pytest.mark.parametrize("rows,d,pad,offset", [
     (1, 1, 0, 0), (1, 1024, 0, 0), (2, 3, 1, 1), (5, 128, 0, 0), (3, 200, 3, 0), (9, 512, 0, 0), (4, 513, 0, 1), (37, 1024, 0, 0), (6, 1025, 7, 2),
     (3, 2048, 0, 0), (2, 2300, 0, 0), (5, 4096, 8, 0), (2, 5000, 1, 0), (3, 8192, 0, 0), (1, 16384, 0, 0), (2, 16385, 0, 0), (1, 32768, 0, 0),
-    (1027, 256, 0, 0)])
+    (1027, 256, 0, 0), (130, 7, 0, 0), (1000, 64, 5, 1), (77, 100, 0, 0), (70, 129, 1, 1), (41, 255, 0, 0), (19, 257, 3, 0)])
 def test_rmsnorm(srm, dtype, add_dtype, rows, d, pad, offset):
     rng = np.random.default_rng(rows * 77 + d)
     x = _wide(rng, rows, d, pad, TYPES[dtype], offset, 0.7)
@@ -202,7 +203,7 @@ SIZES = [(1, 1, 1), (1, 16, 128), (2, 3, 127), (1, 32000, 1024), (15, 100, 129),
          (64, 64, 2048), (65, 1000, 1000), (100, 130, 4096), (127, 31, 300), (130, 1024, 128), (256, 256, 256), (257, 260, 384), (300, 512, 1024),
          (513, 1030, 777), (1000, 2000, 128), (1500, 1100, 1152), (2100, 2052, 256), (4099, 516, 640), (77, 8, 16384), (520, 4100, 2100), (9, 5000, 300),
          (3001, 4001, 1000), (2100, 8200, 256), (2060, 8301, 300), (4100, 4700, 1100), (5000, 3000, 100), (2900, 3000, 2100),
-         (1450, 4100, 700), (26000, 156, 300)]
+         (1450, 4100, 700), (26000, 156, 300), (3755, 872, 1152), (10837, 1721, 256)]
 
 
 @pytest.mark.parametrize("M,N,K", SIZES)
@@ -312,11 +313,11 @@ def test_linear_of_more_than_two_gigabytes(srm):
         assert ((got.double() - ref).abs() <= (K + 3) * 2.0 ** -23 * size).all()
 
 
-def test_more_rows_than_a_dimension_of_a_grid_has_threads_for(srm):
-    """2^26 + 5 rows of 8 (a wavefront each) in 2^24 work-groups: the same codes as in a small call."""
-    rows, d = (1 << 26) + 5, 8
+@pytest.mark.parametrize("rows,d", [((1 << 26) + 5, 8), ((1 << 23) + 5, 257)])
+def test_more_rows_than_a_dimension_of_a_grid_has_threads_for(srm, rows, d):
+    """More work-groups than a row of the grid: the same codes as in a small call."""
     x = torch.zeros(rows, d, device="cuda")
-    some = torch.tensor([0, 1, 12345, (1 << 23) + 1, (1 << 25) - 1, 1 << 25, (1 << 26) - 1, 1 << 26, rows - 1], device="cuda")
+    some = torch.tensor([0, 1, 12345, rows // 8 + 1, rows // 2 - 3, rows // 2, rows - 6, rows - 5, rows - 1], device="cuda")
     few = torch.randn(len(some), d, device="cuda")
     x[some] = few
     (q, s), (qf, sf) = srm.fp8_empty(rows, d), srm.fp8_empty(len(some), d)

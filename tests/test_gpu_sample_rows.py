@@ -216,8 +216,8 @@ def test_temperatures_of_bf16_rows(srm, t):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("V", [5, 300, 512, 513, 1000])
-def test_short_rows_of_few_or_odd_values(srm, V, dtype):
+@pytest.mark.parametrize("V,times", [(5, 1), (300, 1), (512, 1), (513, 1), (513, 6), (1000, 6), (1024, 7)])
+def test_short_rows_of_few_or_odd_values(srm, V, times, dtype):
     """Equal values at the limits, values of all magnitudes (a search by halves that takes long), masks, infinities, NaN."""
     rng = np.random.default_rng(V)
     x = rng.standard_normal((10, V)) * 2.5
@@ -233,10 +233,11 @@ def test_short_rows_of_few_or_odd_values(srm, V, dtype):
     x[8] = -1e30
     x[8, V // 4:V // 2 + 1] = 4.0
     x[9] = np.where(rng.random(V) < 0.5, 0.0, -0.0)
-    x = torch.from_numpy(np.repeat(x.astype(np.float32), 9, axis=0)).cuda().to(dtype)
+    x = np.repeat(x.astype(np.float32), 9, axis=0)
+    x = torch.from_numpy(np.concatenate([x] * times)).cuda().to(dtype)
     n = x.shape[0]
-    check(srm, x, rng.random(n), top_p=[0.3, 0.7, 0.999, 1.0, 1.0, 1.0, 0.5, 0.8, 1.0] * 10, top_k=[0, 0, 0, 3, 200, 1, 4, 250, 0] * 10,
-          min_p=[0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.01, 0.4] * 10)
+    check(srm, x, rng.random(n), top_p=[0.3, 0.7, 0.999, 1.0, 1.0, 1.0, 0.5, 0.8, 1.0] * (10 * times), top_k=[0, 0, 0, 3, 200, 1, 4, 250, 0] * (10 * times),
+          min_p=[0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.01, 0.4] * (10 * times))
 
 
 def test_an_infinite_temperature_is_the_largest(srm):
