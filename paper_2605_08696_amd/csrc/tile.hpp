@@ -44,8 +44,10 @@ __device__ __forceinline__ void static_for(F &&f)
 // GELU value <= 6.5e-7 in fp32 evaluation; the 1 / sqrt(2) is folded into the coefficients), so one exp2
 // and six FMAs, no reciprocal.  With q = 2^-P: x * (1 - q) for x >= 0 and x * q for x < 0 are both
 // max(x, 0) - |x| * q, one max and one FMA instead of a subtraction, a compare, a select and a
-// product.  The result is rounded to bf16 (relative 2^-9) right after, so the approximation error is
-// invisible there.
+// product.  The result is rounded to bf16 (relative 2^-8) right after, so the approximation error is
+// invisible there.  |x| is the clamped one in the product too: beyond the clamp the result is max(x, 0) - 3.3e-9, for
+// infinities as for finite values (the magnitude itself times q would grow without bound, and be NaN for +infinity).
+// min and max leave a NaN out, so the maximum is the instruction that keeps it.
 __device__ __forceinline__ float gelu_bf16out(float x)
 {
     // Eleven instructions, written out: from the C form the compiler made 14 to 18 per element (a
@@ -54,7 +56,7 @@ __device__ __forceinline__ float gelu_bf16out(float x)
     //   w = min(|x|, 6.0811183)                       P(w) by Horner, coefficients high to low:
     //   -1.917465077776602e-05, 0.0006586045579087176, -0.00775440879176911, 0.05296539231773387,
     //   0.4590602540550674, 1.1511220519383694, 0.9999996936263803
-    //   q = 2^-P ;  result = max(x, 0) - |x| * q
+    //   q = 2^-P ;  result = max(x, 0) - w * q
     float w, p, q, r;
     const float c5 = 0.0006586045579087176f;
     asm("v_and_b32 %0, 0x7fffffff, %4\n\t"
@@ -66,8 +68,8 @@ __device__ __forceinline__ float gelu_bf16out(float x)
         "v_fmaak_f32 %1, %0, %1, 0x3f9357f8\n\t"
         "v_fmaak_f32 %1, %0, %1, 0x3f7ffffb\n\t"
         "v_exp_f32_e64 %2, -%1\n\t"
-        "v_max_f32 %3, 0, %4\n\t"
-        "v_fma_f32 %3, -|%4|, %2, %3"
+        "v_maximum3_f32 %3, %4, 0, 0\n\t"
+        "v_fma_f32 %3, -%0, %2, %3"
         : "=&v"(w), "=&v"(p), "=&v"(q), "=&v"(r)
         : "v"(x), "v"(c5));
     return r;
