@@ -400,10 +400,14 @@ gemm_fp8_persist_kernel(const unsigned char *__restrict__ A, const uint32_t *__r
     const int nbm = (int)((M + BM - 1) / BM), nbn = (N + BN - 1) / BN, nblk = nbm * nbn;
     const int KT = Kp / 128, KG = (KT + 3) / 4;      // KT >= 2 (the launcher checks)
 
-    // one wavefront's load: 8 rows x 128 bytes, lane (r = l >> 3, slot = l & 7) fetches chunk slot ^ swz(r) of its row
-    const int ld_r = tid >> 3, ld_voff = ld_r * Kp + (((tid & 7) ^ swz_of_row(ld_r)) << 4);
+    // one wavefront's load: 8 rows x 128 bytes, lane (r = l >> 3, slot = l & 7) fetches chunk slot ^ swz(r) of its row.  The row is in the
+    // lanes' offset, which the descriptor's size bounds by itself; the common one stays within a row, and is 0 for a tile that does not exist.
+    const int ld_r = tid >> 3;
+    int ld_voff[LD_IT];
+#pragma unroll
+    for (int i = 0; i < LD_IT; ++i) ld_voff[i] = (i * 64 + ld_r) * Kp + (((tid & 7) ^ swz_of_row(ld_r)) << 4);
     auto dma_one = [&](int i, const u32x4_t &rs, int kt, unsigned unit) {
-        fp8_dma16(ring + unit + (i * 64 + wave * 8) * 128, rs, ld_voff, i * 64 * Kp + kt * 128);
+        fp8_dma16(ring + unit + (i * 64 + wave * 8) * 128, rs, ld_voff[i], kt * 128);
     };
     struct Tile {
         int64_t m0;
@@ -516,7 +520,7 @@ gemm_fp8_persist_kernel(const unsigned char *__restrict__ A, const uint32_t *__r
             }
             const bool ahead = kt + 2 >= KT;
             const u32x4_t ra = ahead ? nxt.ra : cur.ra, rw = ahead ? nxt.rw : cur.rw;
-            const int kq = ahead ? kt + 2 - KT : kt + 2;
+            const int kq = ahead ? (vn < nblk ? kt + 2 - KT : 0) : kt + 2;
             half(h0, [] {}, at(0), at(1), ra, kq, at(4));
             half(h1, [&] {
                 if (kt) FP8_WAIT_VM(LD_IT);          // block T+1 has landed
