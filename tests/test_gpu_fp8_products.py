@@ -1,9 +1,10 @@
-"""Products of 8-bit rows: operands and outputs that end where their allocations end."""
+"""Products of 8-bit rows: operands and outputs that end where their allocations end, and each of the kernels with its shortest loops."""
 import numpy as np
 import pytest
 import torch
 
 import fp8_ref
+import gpu_util
 
 pytestmark = pytest.mark.gpu
 STORE, GELU, RESIDUAL, LOGITS = 0, 1, 2, 4
@@ -70,3 +71,30 @@ def check_product(srm, M, N, K, epilogue, around=lambda call: call()):
 def test_operands_at_the_end_of_an_allocation(srm, M, N, K, epilogue):
     """Rows of a last tile that do not exist lie behind the allocations: none of them is read or written."""
     check_product(srm, M, N, K, epilogue)
+
+
+# The kernel that each size is there for, on 256 compute units: every kernel with either kind of output, and of the persistent one
+# the fewest blocks of K (two, with one and with several tiles a work-group), three, four (a whole word of scales), five and eight of them.
+KERNELS = [
+    (33, 257, 640, STORE, "slices_kernel<1, 1, 2"), (9, 5000, 300, STORE, "slices_kernel<1, 2, 1"), (37, 4096, 300, GELU, "slices_kernel<2, 2, 1"),
+    (700, 1000, 300, STORE, "slices_kernel<4, 4, 1"), (1100, 1028, 300, STORE, "tile_kernel<64, 64, 2, 2, 4"), (2100, 1030, 300, STORE, "tile_kernel<64, 64, 2, 2, 2"),
+    (3755, 872, 300, STORE, "tile_kernel<64, 128, 2, 2, 2"), (3001, 2060, 128, STORE, "tile_kernel<128, 128, 2, 4, 2"),
+    (10837, 1721, 256, GELU, "tile_kernel<128, 128, 2, 4, 2"),
+    (2900, 3000, 256, STORE, "persist_kernel<"), (8100, 8190, 256, GELU, "persist_kernel<"), (8190, 8100, 200, STORE, "persist_kernel<"),
+    (5000, 5000, 300, STORE, "persist_kernel<"), (8100, 5000, 500, STORE, "persist_kernel<"), (4200, 4700, 640, GELU, "persist_kernel<"),
+    (6000, 4001, 1024, STORE, "persist_kernel<"),
+    (33, 257, 640, RESIDUAL, "slices_kernel<1, 1, 2"), (9, 5000, 300, LOGITS, "slices_kernel<1, 2, 1"), (37, 4096, 300, LOGITS, "slices_kernel<2, 2, 1"),
+    (700, 1000, 300, RESIDUAL, "slices_kernel<4, 4, 1"), (1100, 1028, 300, LOGITS, "tile_kernel<64, 64, 2, 2, 4"),
+    (2100, 1030, 300, RESIDUAL, "tile_kernel<64, 64, 2, 2, 2"), (3755, 872, 300, LOGITS, "tile_kernel<64, 128, 2, 2, 2"),
+    (2900, 3000, 256, RESIDUAL, "tile_kernel<64, 64, 2, 2, 2"), (2900, 3000, 256, LOGITS, "tile_kernel<64, 128, 2, 2, 2"),
+    (26000, 156, 300, LOGITS, "tile_kernel<128, 64, 2, 2, 2"), (3001, 2500, 300, RESIDUAL, "tile_kernel<128, 128, 2, 4, 2"),
+    (3001, 4001, 2000, RESIDUAL, "tile_kernel<128, 128, 2, 2, 2"), (5000, 5000, 300, LOGITS, "tile_kernel<128, 128, 2, 2, 2")]
+
+
+@pytest.mark.parametrize("M,N,K,epilogue,kernel", KERNELS)
+def test_each_kernel(srm, M, N, K, epilogue, kernel):
+    """A change of the rule that sends a size elsewhere leaves a kernel, or the form of it that the size is there for, without a test."""
+    if torch.cuda.get_device_properties(0).multi_processor_count != 256:
+        pytest.skip("the table is that of 256 compute units")
+    events = check_product(srm, M, N, K, epilogue, around=lambda call: gpu_util.kernel_events("gemm_fp8", call))
+    assert [kernel in e.name for e in events] == [True], [e.name for e in events]
