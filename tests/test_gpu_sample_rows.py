@@ -1,8 +1,8 @@
 """Sampling by request through the public binding, against the rule in 64 bits (numpy).
 
 Tokens have to be equal.  A draw that lies within 1e-11 of a border between two tokens, or a top-p target within 1e-11 of a running sum,
-could go either way (weights are held to 2^-43 of the largest): the inputs are seeded, and no row of these tests comes that near, which
-each test asserts.  A log probability is a difference of two numbers of 64 bits, rounded to fp32: 2^-24 relative, and 1e-9 for the sums."""
+could go either way (weights are held to 2^-43 of the largest): the inputs are seeded, and no row comes that near, which is asserted unless
+a test says strict=False (rows of equal or few values; test_gpu_sample_rows_ties.py has the rule in whole numbers for those).  A log probability is a difference of two numbers of 64 bits, rounded to fp32: 2^-24 relative, and 1e-9 for the sums."""
 import math
 
 import numpy as np
