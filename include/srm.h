@@ -596,8 +596,8 @@ size_t srm_linear_argmax_noalloc_max_bytes(void);
  * Rows in 8 bits ("fp8 matrices"), their products and sampling by request: operators that need no model, for the projections and
  * the end of a decode step.
  *
- * An fp8 matrix of `rows` x K holds e4m3 values (OCP: 448 largest, no infinities) with one E8M0 scale (a byte s: 2^(s - 127)) for
- * every block of 128 consecutive elements of a row:
+ * An fp8 matrix of `rows` x K holds e4m3 values (OCP: 448 largest, no infinities) with one E8M0 scale (a byte s: 2^(s - 127), 255: NaN)
+ * for every block of 128 consecutive elements of a row:
  *   q       [rows][Kp], Kp = srm_fp8_row_bytes(K) = K rounded up to 128; zeros behind K; at a multiple of 16 bytes
  *   scales  [ceil(K / 512)][rows][4], srm_fp8_scale_bytes(rows, K) bytes: scales[b / 4][r][b % 4] belongs to
  *           q[r][128 b .. 128 b + 127]; 127 behind the last block; at a multiple of 4 bytes
@@ -618,13 +618,16 @@ size_t srm_linear_argmax_noalloc_max_bytes(void);
  * Errors: SRM_EINVAL (null pointer, rows or d <= 0, rows >= 2^30, d > 32768, a row stride < d, eps < 0 or NaN, unknown dtype,
  * an operand not at a multiple of its element, misaligned q or scales).
  *
- * srm_linear_fp8: out = epilogue(A W^T + bias) of fp8 matrices A [M][K] and W [N][K], accumulated in fp32.  With a bf16 output the
- * matrix cores' 8-bit products are taken, which add eight neighbouring products within some 14 bits of the largest (1e-5 of a
- * result's size, where its rounding is 2e-3); with an fp32 output the operands are widened to bf16, with scales from 2^-117 to 2^119
- * exactly (a block of smaller or larger ones may flush to 0 or overflow), and nothing is lost but the roundings of fp32 sums, at
- * half the rate.  d_bias [N] fp32 or NULL.  Epilogues as in srm_linear: 0 = store bf16, 1 = exact GELU then store bf16, 2 = add into
- * fp32 d_out (residual), 4 = store fp32 (3, the fused argmax, does not exist here: srm_sample_rows with temperature 0 chooses from stored logits).  d_out is
- * [M][N], dense.  Any M, N and K.
+ * srm_linear_fp8: out = epilogue(A W^T + bias) of fp8 matrices A [M][K] and W [N][K].  What the sums are depends on the output's type:
+ *   bf16: the matrix cores' 8-bit products.  The products of elements 8 j .. 8 j + 7 of a row are added without what lies below 2^-13
+ *     of the largest of the eight, and such sums to each other in fp32.  A result is off by at most 7 * 2^-13 of the sum of its products'
+ *     magnitudes, and its rounding, 2^-8 of its value (random rows: 1e-5 of the results' norm, and 2e-3).  Where large products cancel,
+ *     the first can be the larger part; it stays far below what rounding those elements to e4m3 (2^-4 each) has cost.
+ *   fp32: the operands are widened to bf16, with scales from 2^-117 to 2^119 exactly (a block of smaller or larger ones may flush to 0
+ *     or overflow), and nothing is lost but the roundings of fp32 sums, at half the rate.
+ * d_bias [N] fp32 or NULL, added in fp32.  Epilogues as in srm_linear: 0 = store bf16, 1 = GELU (x Phi(x) to 6.5e-7, 0 at -infinity, over
+ * all of fp32's range) then store bf16, 2 = add into fp32 d_out (residual), 4 = store fp32 (3, the fused argmax, does not exist
+ * here: srm_sample_rows with temperature 0 chooses from stored logits).  d_out is [M][N], dense.  Any M, N and K.
  * Errors: SRM_EINVAL (null operand, scales or output, sizes <= 0, M or N >= 2^30, 2^30 tiles, K > 2^22, misaligned operands,
  * output or bias, unknown epilogue).
  *

@@ -4,8 +4,10 @@
 // Two ways to the sum, by the type of the output:
 //   bf16 (EPI_STORE, EPI_GELU): v_mfma_scale_f32_16x16x128_f8f6f4, whose K is a block; a lane hands it the scales of its row of A and of
 //     its row of W with the operands, and the fp32 accumulation runs on over all of K.  The instruction adds the eight products of a
-//     lane's 64-bit words in a window of some 14 bits below the largest (2^16 + 2^3 is held, 2^16 + 2^2 is not, whichever fp8
-//     instruction; random rows: 1.3e-5 of the result's norm), which a bf16 output's rounding of 2^-9 hides.
+//     lane's 64-bit words (eight consecutive k) without what lies below 2^-13 of the largest (2^16 + 2^3 is held, 2^16 + 2^2 is not,
+//     whichever fp8 instruction), and those sums to each other and to what is accumulated in fp32 (2^16 + 2^-7 is held).  Taken for
+//     its rate: on random rows it costs 1.3e-5 of the results' norm, beside 1.7e-3 of a bf16 output's rounding (2^-8 at most), so
+//     that the error against 64 bits stays the same and one output in ninety is the neighbouring bf16 value of that from fp32 sums.
 //   fp32 (EPI_RESID, EPI_F32): the operands are widened to bf16 with their scales (v_cvt_scalef32_pk_bf16_fp8: exact for scales from
 //     2^-117 to 2^119) and multiplied by v_mfma_f32_16x16x32_bf16, which holds products and sums in fp32 (random rows: 8e-8), at half
 //     the rate.
@@ -167,7 +169,7 @@ __device__ __forceinline__ unsigned fp8_lds_address(const void *p)
 // Bound by the trip through L2 and the LDS reads between two barriers, of which other work-groups on the CU fill part: two of 128x128, three of
 // 64x128.  fp32 outputs besides by widening, two values an instruction: 8192^3 892 .. 967 us (1.1 .. 1.2 PFLOP/s; the bf16 product of the same
 // size 1.46), 3001 x 4001 x 1000 with addition 36 us (matrix pipes busy for a quarter of it: 768 tiles are one and a half rounds, and the
-// stored rows are read and written behind the last product).  Not kept: the operands of the next block in registers meanwhile
+// stored rows are read and written behind the last product; 39 .. 44 with operands and output from memory).  Not kept: the operands of the next block in registers meanwhile
 // (128x128 spills, 128x64 gains nothing), what is added to requested in front of the first loads (+-2%).
 template <int BM, int BN>
 constexpr int fp8_stage_bytes() { return (BM + BN) * (128 + 4); }
@@ -380,9 +382,9 @@ gemm_fp8_slices_kernel(const unsigned char *__restrict__ A, const uint32_t *__re
 // An operand of A is read for the next half behind the two products that use it in this one, into the same registers.  The ring is all of
 // the LDS, so the scales are in registers: the words of four blocks for this lane's rows, the lowest byte in use, and those of the next
 // four, requested when the last ones begin to be used.
-// 8192^3: 408 .. 424 us (2.6 .. 2.7 PFLOP/s, the matrix pipes busy for 72% of the clocks at a sustained 1.7 GHz, where a bare loop of the
+// 8192^3: 408 .. 432 us (2.5 .. 2.7 PFLOP/s, the matrix pipes busy for 72% of the clocks at a sustained 1.7 GHz, where a bare loop of the
 // instruction reaches 3.9 PFLOP/s), 418 with a wait for the stores of a tile in front of the next one's loads; 16384 x 1024 x 4096, one tile
-// a CU, 61 us (2.3 PFLOP/s): the first loads and the last stores have nothing to hide behind.
+// a CU, 59 .. 65 us (2.1 .. 2.3 PFLOP/s): the first loads and the last stores have nothing to hide behind.
 constexpr int kFp8PersistLds = 160 * 1024;
 template <int EPI>
 __global__ void __launch_bounds__(512)

@@ -26,7 +26,8 @@
 // (one, two with top-p), eight independent chains at a time; bf16 rows the LDS, 18 clocks of a CU for a wavefront's 64 additions to the counts
 // and as many for its 64 looks into the table; below that the row's passes through the last-level cache.
 //   greedy | no limit | top-p 0.95 | top-k 50 | min-p 0.05: 256 x 32000 fp32 6.3 | 18 | 40 | 17 | 14, bf16 5.7 | 17 | 24 | 16 | 13;
-//   1000 x 128001 fp32 105 | 198 | 426 | 160 | 159, bf16 61 (4.2 TB/s) | 124 | 177 | 97 | 97; one row of 32000 fp32 3.9 | 14 | 35 | 14 | 11.
+//   1000 x 128001 fp32 105 | 190 | 427 | 162 | 160, bf16, the logits in the last-level cache 61 (4.2 TB/s) | 124 | 177 | 97 | 97, from memory
+//   83 | 145 | 190 | 115 | 117; one row of 32000 fp32 3.9 | 14 | 32 | 14 | 10.
 //   With weights of bf16 logits formed one by one 1000 x 128001 took 441 with top-p, with a table but a histogram of weights 397, counted in a
 //   pass of its own 205.  A table of the limit's region only (guessed from one segment in eight, fewer LDS additions): 421.
 #pragma once
