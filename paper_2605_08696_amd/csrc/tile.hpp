@@ -47,10 +47,10 @@ __device__ __forceinline__ void static_for(F &&f)
 // product.  The result is rounded to bf16 (relative 2^-8) right after, so the approximation error is
 // invisible there.  |x| is the clamped one in the product too: beyond the clamp the result is max(x, 0) - 3.3e-9, for
 // infinities as for finite values (the magnitude itself times q would grow without bound, and be NaN for +infinity).
-// min and max leave a NaN out, so the maximum is the instruction that keeps it.
+// The minimum is the instruction that keeps a NaN, which then is all that follows from it.
 __device__ __forceinline__ float gelu_bf16out(float x)
 {
-    // Eleven instructions, written out: from the C form the compiler made 14 to 18 per element (a
+    // Ten instructions, written out: from the C form the compiler made 14 to 18 per element (a
     // NaN-quieting max in front of each min / max, whose inputs come straight from LDS, and a move per
     // constant in every other Horner chain), and this epilogue is bound by its instruction count.
     //   w = min(|x|, 6.0811183)                       P(w) by Horner, coefficients high to low:
@@ -58,9 +58,8 @@ __device__ __forceinline__ float gelu_bf16out(float x)
     //   0.4590602540550674, 1.1511220519383694, 0.9999996936263803
     //   q = 2^-P ;  result = max(x, 0) - w * q
     float w, p, q, r;
-    const float c5 = 0.0006586045579087176f;
-    asm("v_and_b32 %0, 0x7fffffff, %4\n\t"
-        "v_min_f32 %0, 0x40c29885, %0\n\t"
+    const float c5 = 0.0006586045579087176f, clamp = 6.0811183f;
+    asm("v_minimum3_f32 %0, |%4|, %6, %6\n\t"
         "v_fmamk_f32 %1, %0, 0xb7a0d940, %5\n\t"
         "v_fmaak_f32 %1, %0, %1, 0xbbfe18b2\n\t"
         "v_fmaak_f32 %1, %0, %1, 0x3d58f23d\n\t"
@@ -68,9 +67,9 @@ __device__ __forceinline__ float gelu_bf16out(float x)
         "v_fmaak_f32 %1, %0, %1, 0x3f9357f8\n\t"
         "v_fmaak_f32 %1, %0, %1, 0x3f7ffffb\n\t"
         "v_exp_f32_e64 %2, -%1\n\t"
-        "v_maximum3_f32 %3, %4, 0, 0\n\t"
+        "v_max_f32 %3, 0, %4\n\t"
         "v_fma_f32 %3, -%0, %2, %3"
         : "=&v"(w), "=&v"(p), "=&v"(q), "=&v"(r)
-        : "v"(x), "v"(c5));
+        : "v"(x), "v"(c5), "s"(clamp));
     return r;
 }
