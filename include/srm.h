@@ -659,6 +659,82 @@ int srm_sample_rows(int32_t dtype, const void *d_logits, int64_t ld, int64_t row
                     int32_t *d_tok_out, float *d_logprob, void *hip_stream);
 
 /*
+ * A selective recurrence over packed prompts and single tokens, with the short causal convolution in front of it, and the scores of given
+ * tokens: operators that need no model.  Where the mixer of Eq. 2 / Eq. 3 keeps one value per channel with a decay of each head, this one
+ * keeps a matrix for each head, whose decay and input depend on the token.
+ *
+ * Packed prompts: sequence n is rows offsets[n] .. offsets[n + 1] - 1 of every operand, which may be none.  The offsets (N + 1 values, int32,
+ * not falling, the first at least 0) are passed twice, as in srm_prefill_ragged: h_offsets in host memory, which the call validates and plans
+ * by, and d_offsets, the same values in device memory (clamped to those of the host, so that a mismatch cannot cause an access outside the
+ * operands; results are then unspecified).  Rows in front of the first sequence and behind the last are left as they are.
+ * d_pos [N] (device, int32; NULL: all 0) is the position of each sequence's first row in its conversation, for a prompt that comes in
+ * several calls.  At position 0 nothing is read from the slot (it need not be cleared).  A negative position marks a sequence as idle: its
+ * rows of the output become zeros, its slot stays.  d_slot [N] (device, int32; NULL: sequence n has slot n) is where what a sequence leaves
+ * lies in a state of `slots` slots; outside [0, slots), or without a state, a sequence starts from zeros and leaves nothing.  Two sequences of
+ * a call that share a slot leave it unspecified.  Buffers of a call must not overlap.  All calls may be made under stream capture.
+ *
+ * srm_causal_conv: out[t, c] = act(bias[c] + sum_k w[c, k] x[t - (width - 1) + k, c]), each channel by itself; act: 0 = none,
+ * 1 = SiLU, v / (1 + e^-v).  d_x and d_out [rows][channels] of type dtype (SRM_FP32 | SRM_BF16), row strides ldx, ld_out; d_weight
+ * [channels][width] and d_bias [channels] (may be NULL) fp32; width 1 to 8; sums in fp32.  Rows in front of position 0 count as zeros,
+ * rows of an earlier call come from the slot: d_state [slots][width][channels] of type dtype holds the last `width` rows of x, position p
+ * in row p % width, and is updated (may be NULL).
+ * Errors: SRM_EINVAL (null pointer, sizes <= 0, channels > 2^24, width > 8, rows >= 2^30, a row stride < channels, offsets that fall or are
+ * negative, unknown dtype or activation, an operand not at a multiple of its element), SRM_EHIP.
+ *
+ * srm_selective_scan: for head h of group g = h / (heads / groups), along each sequence,
+ *   dt = softplus(dt_raw + dt_bias[h])       (softplus = 0: dt = dt_raw + dt_bias[h])
+ *   S <- exp(dt a[h]) S + dt x[h] B[g]^T     y = S C[g] + skip[h] x[h]     out = y silu(z)
+ * d_xbc [rows][heads * head_dim + 2 * groups * state_dim] holds x [heads][head_dim] | B [groups][state_dim] | C [groups][state_dim], row stride
+ * ld_xbc, and d_z [rows][heads * head_dim] (may be NULL: out = y) and d_out as x, row strides ld_z, ld_out, all of type dtype; d_dt
+ * [rows][heads] of type dt_dtype; d_a, d_dt_bias, d_skip [heads] fp32 (the last two may be NULL).  a <= 0 is meant: with a > 0 the formula
+ * holds as long as nothing overflows.  d_state [slots][heads][head_dim][state_dim] fp32 (may be NULL) is read (from position 1 on) and
+ * updated.  state_dim up to 256.  The state, decays and all sums are fp32.  With bf16 operands, states and the weights of earlier tokens are
+ * rounded to bf16 (2^-9 of their values) where they are multiplied on the matrix cores for y; what is kept is not.
+ * d_workspace: a call with few sequences and heads is cut into segments of time, whose states lie there;
+ * srm_selective_scan_workspace_bytes(the same arguments) is what the best cut takes (0: none), and with less, or NULL, there are fewer
+ * segments or none.  Its content means nothing between calls; calls that may overlap in time need one each.  Results may differ in the
+ * order of sums with the cut, which depends on the offsets, the sizes and workspace_bytes alone.
+ * Errors: SRM_EINVAL (as above; heads not a multiple of groups, heads > 65536, head_dim > 4096, state_dim > 256), SRM_EHIP.
+ *
+ * srm_selective_step: one token for each of `rows` requests: the convolution (d_weight NULL: none) of d_xbc's rows with the slots' rings
+ * and the update of the slots' states, in one launch; row r's output equals that of srm_causal_conv and srm_selective_scan for a sequence of
+ * this one row, up to roundings (x, B and C are not rounded to dtype between the two).  d_xbc holds the rows in front of the convolution,
+ * d_conv_state [slots][width][channels] of type dtype (needed if width > 1), d_pos [rows] and d_state must be given; a row of negative position
+ * is idle, a slot outside [0, slots) counts as zeros and leaves nothing.
+ * Errors: SRM_EINVAL (as above), SRM_EHIP.
+ *
+ * srm_token_logprobs: what each row of d_logits [rows][vocab] (dtype, row stride ld) says about given tokens.  With l the logits over
+ * temperature[r] (fp32 [rows], NULL: 1; a temperature <= 0 or NaN counts as 1, others are held
+ * between 1e-30 and 1e30) and p = softmax(l):
+ *   d_logprob[r] = log p[token[r]] (d_token int32 [rows]; 0 where the token is outside [0, vocab), as behind the end of a padded row)
+ *   d_entropy[r] = -sum p log p    (may be NULL)
+ *   d_top_token, d_top_logprob [rows][top]: the `top` most likely tokens, equal logits by their index, and their log p; top up to 32; tokens
+ *   of logit -infinity are none of them: -1 and -infinity where there are fewer.
+ * A logit that is NaN counts as -infinity; logits of +infinity share the probability equally; a row that holds nothing else than -infinity
+ * has logprob -infinity, entropy 0 and no top tokens.  Sums in fp32, in an order that depends on vocab and dtype alone.
+ * Errors: SRM_EINVAL (null pointer, nothing to compute, sizes <= 0, rows >= 2^30, vocab > 2^30, top > 32, ld < vocab, unknown dtype, an
+ * operand not at a multiple of its element), SRM_EHIP.
+ */
+int srm_causal_conv(int32_t dtype, const void *d_x, int64_t ldx, const float *d_weight, const float *d_bias, int32_t activation,
+                    int32_t channels, int32_t width, const int32_t *h_offsets, const int32_t *d_offsets, int32_t N, const int32_t *d_pos,
+                    const int32_t *d_slot, int64_t slots, void *d_state, void *d_out, int64_t ld_out, void *hip_stream);
+size_t srm_selective_scan_workspace_bytes(int32_t dtype, const int32_t *h_offsets, int32_t N, int32_t heads, int32_t head_dim,
+                                          int32_t state_dim);
+int srm_selective_scan(int32_t dtype, const void *d_xbc, int64_t ld_xbc, int32_t dt_dtype, const void *d_dt, int64_t ld_dt, const float *d_a,
+                       const float *d_dt_bias, const float *d_skip, int32_t softplus, const void *d_z, int64_t ld_z, int32_t heads,
+                       int32_t head_dim, int32_t groups, int32_t state_dim, const int32_t *h_offsets, const int32_t *d_offsets, int32_t N,
+                       const int32_t *d_pos, const int32_t *d_slot, int64_t slots, float *d_state, void *d_out, int64_t ld_out,
+                       void *d_workspace, size_t workspace_bytes, void *hip_stream);
+int srm_selective_step(int32_t dtype, const void *d_xbc, int64_t ld_xbc, const float *d_weight, const float *d_bias, int32_t activation,
+                       int32_t width, void *d_conv_state, int32_t dt_dtype, const void *d_dt, int64_t ld_dt, const float *d_a,
+                       const float *d_dt_bias, const float *d_skip, int32_t softplus, const void *d_z, int64_t ld_z, int32_t heads,
+                       int32_t head_dim, int32_t groups, int32_t state_dim, int64_t rows, const int32_t *d_pos, const int32_t *d_slot,
+                       int64_t slots, float *d_state, void *d_out, int64_t ld_out, void *hip_stream);
+int srm_token_logprobs(int32_t dtype, const void *d_logits, int64_t ld, int64_t rows, int32_t vocab, const float *d_temperature,
+                       const int32_t *d_token, float *d_logprob, float *d_entropy, int32_t top, int32_t *d_top_token, float *d_top_logprob,
+                       void *hip_stream);
+
+/*
  * Work-groups of the one-kernel path that srm_generate / srm_generate_topp take
  * for a batch of B samples, or 0 if such a call runs the ordinary step kernels.
  * The one-kernel path ("MAX model details": per-call overhead dominates small

@@ -139,6 +139,18 @@ def lib():
         L.srm_linear_fp8.argtypes = [i32, vp, vp, vp, vp, vp, i64, i32, i32, vp, vp]
         L.srm_sample_rows.restype = C.c_int
         L.srm_sample_rows.argtypes = [i32, vp, i64, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.srm_causal_conv.restype = C.c_int
+        L.srm_causal_conv.argtypes = [i32, vp, i64, vp, vp, i32, i32, i32, vp, vp, i32, vp, vp, i64, vp, vp, i64, vp]
+        L.srm_selective_scan_workspace_bytes.restype = sz
+        L.srm_selective_scan_workspace_bytes.argtypes = [i32, vp, i32, i32, i32, i32]
+        L.srm_selective_scan.restype = C.c_int
+        L.srm_selective_scan.argtypes = [i32, vp, i64, i32, vp, i64, vp, vp, vp, i32, vp, i64, i32, i32, i32, i32, vp, vp, i32, vp, vp, i64, vp,
+                                         vp, i64, vp, sz, vp]
+        L.srm_selective_step.restype = C.c_int
+        L.srm_selective_step.argtypes = [i32, vp, i64, vp, vp, i32, i32, vp, i32, vp, i64, vp, vp, vp, i32, vp, i64, i32, i32, i32, i32, i64, vp,
+                                         vp, i64, vp, vp, i64, vp]
+        L.srm_token_logprobs.restype = C.c_int
+        L.srm_token_logprobs.argtypes = [i32, vp, i64, i64, i32, vp, vp, vp, vp, i32, vp, vp, vp]
         L.srm_last_error.restype = C.c_char_p
         L.srm_last_error.argtypes = []
         _lib = L
@@ -671,3 +683,166 @@ def sample_rows(logits, uniform, tok_out, temperature=None, top_k=None, top_p=No
                                     None if top_p is None else top_p.data_ptr(), None if min_p is None else min_p.data_ptr(),
                                     uniform.data_ptr(), tok_out.data_ptr(), None if logprob is None else logprob.data_ptr()),
             logits, (uniform, tok_out, temperature, top_k, top_p, min_p, logprob), stream)
+
+
+# ---- a selective recurrence over packed prompts and single tokens, scores of given tokens ---------------------------
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _vector(t, n: int, dtype, name: str):
+    if t is not None and (t.dtype is not dtype or t.numel() != n or not t.is_contiguous()):
+        raise ValueError(f"{name}: must be {n} contiguous {str(dtype)[6:]} values")
+
+
+def _offsets(offsets, d_offsets, rows: int):
+    """The host's offsets as an array that the library may read, and the number of sequences."""
+    if isinstance(offsets, _torch().Tensor):
+        if offsets.is_cuda:
+            raise ValueError("offsets: must be host memory (d_offsets: the same values on the device)")
+        offsets = offsets.numpy()
+    h = np.ascontiguousarray(offsets, dtype=np.int32)
+    n = h.size - 1
+    if h.ndim != 1 or n < 1:
+        raise ValueError("offsets: need at least two boundaries")
+    if h[n] > rows:
+        raise ValueError(f"offsets: {int(h[n])} rows, the operands have {rows}")
+    _vector(d_offsets, n + 1, _torch().int32, "d_offsets")
+    return h, n
+
+
+def _same_rows(t, rows: int, cols: int, name: str, dtype=None):
+    n, c, ld = _rows_of(t, name)
+    if n != rows or c != cols:
+        raise ValueError(f"{name}: shape {(n, c)}, expected {(rows, cols)}")
+    if dtype is not None and t.dtype is not dtype:
+        raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
+    return ld
+
+
+def _slots_of(state, shape, dtype, name: str) -> int:
+    if state is None:
+        return 0
+    if state.dtype is not dtype or tuple(state.shape[1:]) != shape or not state.is_contiguous():
+        raise ValueError(f"{name}: must be contiguous {str(dtype)[6:]} of shape (slots, {', '.join(map(str, shape))})")
+    return state.shape[0]
+
+
+def causal_conv(x, weight, bias, offsets, d_offsets, out, pos=None, slot=None, state=None, activation=True, stream=None):
+    """srm_causal_conv: rows of x (float32 or bfloat16, any row stride) of the packed sequences `offsets` (host int32) = `d_offsets` (device)
+    -> out; weight [channels][width] and bias [channels] or None float32; pos, slot int32 [N] or None; state [slots][width][channels] of
+    x's type or None, updated; activation: SiLU."""
+    torch = _torch()
+    rows, channels, ldx = _rows_of(x, "x")
+    h, n = _offsets(offsets, d_offsets, rows)
+    if weight.dim() != 2:
+        raise ValueError("weight: must be a matrix")
+    width = weight.shape[1]
+    _vector(weight, channels * width, torch.float32, "weight")
+    _vector(bias, channels, torch.float32, "bias")
+    _vector(pos, n, torch.int32, "pos")
+    _vector(slot, n, torch.int32, "slot")
+    slots = _slots_of(state, (width, channels), x.dtype, "state")
+    ld_out = _same_rows(out, rows, channels, "out", x.dtype)
+    _launch(lib().srm_causal_conv, (_row_dtype(x, "x"), x.data_ptr(), ldx, weight.data_ptr(), _ptr(bias), 1 if activation else 0, channels, width,
+                                    h.ctypes.data, d_offsets.data_ptr(), n, _ptr(pos), _ptr(slot), slots, _ptr(state), out.data_ptr(), ld_out),
+            x, (weight, bias, d_offsets, pos, slot, state, out), stream)
+
+
+def _heads(xbc, dt, a, out, groups, dt_bias, skip, z):
+    """(rows, ld_xbc, ld_dt, ld_z, ld_out, heads, head_dim, state_dim) of the recurrence's operands after their checks."""
+    torch = _torch()
+    rows, channels, ld = _rows_of(xbc, "xbc")
+    heads = a.numel()
+    inner = _rows_of(out, "out")[1]
+    if groups <= 0 or heads <= 0 or heads % groups or inner % heads:
+        raise ValueError(f"{heads} heads in {groups} groups, rows of {inner}")
+    left = channels - inner
+    if left <= 0 or left % (2 * groups):
+        raise ValueError(f"xbc: {channels} columns are not {inner} + 2 x {groups} x state_dim")
+    for t, name in ((a, "a"), (dt_bias, "dt_bias"), (skip, "skip")):
+        _vector(t, heads, torch.float32, name)
+    ld_out = _same_rows(out, rows, inner, "out", xbc.dtype)
+    ld_z = 0 if z is None else _same_rows(z, rows, inner, "z", xbc.dtype)
+    return rows, ld, _same_rows(dt, rows, heads, "dt"), ld_z, ld_out, heads, inner // heads, left // (2 * groups)
+
+
+def selective_scan_workspace_bytes(dtype: int, offsets, heads: int, head_dim: int, state_dim: int) -> int:
+    """srm_selective_scan_workspace_bytes (host only); dtype SRM_FP32 | SRM_BF16, offsets host int32."""
+    h = np.ascontiguousarray(offsets, dtype=np.int32)
+    return lib().srm_selective_scan_workspace_bytes(dtype, h.ctypes.data, h.size - 1, heads, head_dim, state_dim)
+
+
+def selective_scan(xbc, dt, a, offsets, d_offsets, out, groups=1, dt_bias=None, skip=None, z=None, softplus=True, pos=None, slot=None, state=None,
+                   workspace=None, stream=None):
+    """srm_selective_scan: rows x | B | C (float32 or bfloat16, any row stride) of the packed sequences `offsets` (host int32) = `d_offsets`
+    (device), dt [rows][heads] float32 or bfloat16 -> out [rows][heads * head_dim]; a, dt_bias, skip [heads] float32; z as out; pos, slot int32
+    [N]; state [slots][heads][head_dim][state_dim] float32, updated.  workspace: uint8 of selective_scan_workspace_bytes, allocated here if
+    not given."""
+    torch = _torch()
+    rows, ld, ld_dt, ld_z, ld_out, heads, head_dim, state_dim = _heads(xbc, dt, a, out, groups, dt_bias, skip, z)
+    h, n = _offsets(offsets, d_offsets, rows)
+    _vector(pos, n, torch.int32, "pos")
+    _vector(slot, n, torch.int32, "slot")
+    slots = _slots_of(state, (heads, head_dim, state_dim), torch.float32, "state")
+    code = _row_dtype(xbc, "xbc")
+    if workspace is None:
+        need = lib().srm_selective_scan_workspace_bytes(code, h.ctypes.data, n, heads, head_dim, state_dim)
+        if need and xbc.is_cuda:
+            workspace = torch.empty(need, dtype=torch.uint8, device=xbc.device)
+            if stream is not None:
+                workspace.record_stream(stream)
+    elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace: must be contiguous uint8")
+    _launch(lib().srm_selective_scan,
+            (code, xbc.data_ptr(), ld, _row_dtype(dt, "dt"), dt.data_ptr(), ld_dt, a.data_ptr(), _ptr(dt_bias), _ptr(skip), 1 if softplus else 0,
+             _ptr(z), ld_z, heads, head_dim, groups, state_dim, h.ctypes.data, d_offsets.data_ptr(), n, _ptr(pos), _ptr(slot), slots, _ptr(state),
+             out.data_ptr(), ld_out, _ptr(workspace), 0 if workspace is None else workspace.numel()),
+            xbc, (dt, a, dt_bias, skip, z, d_offsets, pos, slot, state, out, workspace), stream)
+
+
+def selective_step(xbc, dt, a, pos, state, out, groups=1, weight=None, bias=None, conv_state=None, activation=True, dt_bias=None, skip=None, z=None,
+                   softplus=True, slot=None, stream=None):
+    """srm_selective_step: one token for each row of xbc, in place in the rows' slots of `state` [slots][heads][head_dim][state_dim] float32
+    and `conv_state` [slots][width][channels] of xbc's type; pos int32 [rows], slot int32 [rows] or None; the other operands as in
+    causal_conv and selective_scan.  Without weight there is no convolution."""
+    torch = _torch()
+    rows, ld, ld_dt, ld_z, ld_out, heads, head_dim, state_dim = _heads(xbc, dt, a, out, groups, dt_bias, skip, z)
+    _vector(pos, rows, torch.int32, "pos")
+    _vector(slot, rows, torch.int32, "slot")
+    slots = _slots_of(state, (heads, head_dim, state_dim), torch.float32, "state")
+    width = 0
+    if weight is not None:
+        channels = xbc.shape[1]
+        if weight.dim() != 2:
+            raise ValueError("weight: must be a matrix")
+        width = weight.shape[1]
+        _vector(weight, channels * width, torch.float32, "weight")
+        _vector(bias, channels, torch.float32, "bias")
+        if conv_state is not None and _slots_of(conv_state, (width, channels), xbc.dtype, "conv_state") != slots:
+            raise ValueError(f"conv_state: {conv_state.shape[0]} slots, state has {slots}")
+    _launch(lib().srm_selective_step,
+            (_row_dtype(xbc, "xbc"), xbc.data_ptr(), ld, _ptr(weight), _ptr(bias), 1 if activation else 0, width, _ptr(conv_state),
+             _row_dtype(dt, "dt"), dt.data_ptr(), ld_dt, a.data_ptr(), _ptr(dt_bias), _ptr(skip), 1 if softplus else 0, _ptr(z), ld_z, heads,
+             head_dim, groups, state_dim, rows, _ptr(pos), _ptr(slot), slots, _ptr(state), out.data_ptr(), ld_out),
+            xbc, (dt, a, dt_bias, skip, z, pos, slot, state, weight, bias, conv_state, out), stream)
+
+
+def token_logprobs(logits, token, logprob, temperature=None, entropy=None, top_token=None, top_logprob=None, stream=None):
+    """srm_token_logprobs: logits [rows][vocab] (float32 or bfloat16, any row stride), token [rows] int32 -> logprob [rows] float32 (both may
+    be None), entropy [rows] float32, top_token [rows][k] int32 with top_logprob [rows][k] float32; temperature float32 [rows] or None."""
+    torch = _torch()
+    rows, vocab, ld = _rows_of(logits, "logits")
+    _vector(token, rows, torch.int32, "token")
+    for t, name in ((logprob, "logprob"), (temperature, "temperature"), (entropy, "entropy")):
+        _vector(t, rows, torch.float32, name)
+    top = 0
+    if top_token is not None or top_logprob is not None:
+        if top_token is None or top_logprob is None or top_token.dim() != 2:
+            raise ValueError("top_token, top_logprob: both matrices, or neither")
+        top = top_token.shape[1]
+        _vector(top_token, rows * top, torch.int32, "top_token")
+        _vector(top_logprob, rows * top, torch.float32, "top_logprob")
+    _launch(lib().srm_token_logprobs, (_row_dtype(logits, "logits"), logits.data_ptr(), ld, rows, vocab, _ptr(temperature), _ptr(token),
+                                       _ptr(logprob), _ptr(entropy), top, _ptr(top_token), _ptr(top_logprob)),
+            logits, (token, logprob, temperature, entropy, top_token, top_logprob), stream)

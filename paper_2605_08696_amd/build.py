@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libsrm.so")
 # (srm.hip first: its code object is the first in the library)
-SOURCES = [os.path.join(HERE, "csrc", name) for name in ("srm.hip", "ops.hip")]
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("srm.hip", "ops.hip", "recur.hip")]
 HEADERS = sorted(glob.glob(os.path.join(HERE, "csrc", "*.hpp"))) + [os.path.join(ROOT, "include", "srm.h")]
 
 

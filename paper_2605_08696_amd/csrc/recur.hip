@@ -1,0 +1,326 @@
+// The selective recurrence over packed prompts and single tokens with its short convolution, and the scores of given tokens: operators of
+// libsrm that need no model.  (A translation unit of its own, so that the code objects of the others stay as they are.)
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "srm.h"
+#include "conv.hpp"
+#include "selective.hpp"
+#include "score.hpp"
+#include "status.hpp"
+
+static hipStream_t as_stream(void *s) { return static_cast<hipStream_t>(s); }
+// blocks < 2^31
+static dim3 grid_of(int64_t blocks) { return dim3((unsigned)std::min<int64_t>(blocks, kGridRow), (unsigned)cdiv(blocks, kGridRow)); }
+static bool misaligned(const void *p, unsigned to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
+static bool known(int32_t dtype) { return dtype == SRM_BF16 || dtype == SRM_FP32; }
+static unsigned size_of(int32_t dtype) { return dtype == SRM_BF16 ? 2 : 4; }
+static const char *const kNotWhole = "an operand does not lie at a whole element";
+constexpr int64_t kMaxRows = 1ll << 30, kMaxBlocks = 1ll << 31;
+
+// ------------------------------------------------------------------ packed sequences
+static int check_offsets(const char *who, const int32_t *h, int32_t n, int32_t &longest)
+{
+    if (n <= 0 || n >= kMaxRows) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    if (h[0] < 0) return fail(SRM_EINVAL, "%s: offsets must not be negative", who);
+    longest = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        if (h[i + 1] < h[i]) return fail(SRM_EINVAL, "%s: offsets must not fall (sequence %d)", who, i);
+        longest = std::max(longest, h[i + 1] - h[i]);
+    }
+    if (h[n] >= kMaxRows) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    return SRM_OK;
+}
+static int check_packed(const char *who, const int32_t *h_offsets, const int32_t *d_offsets, int32_t n, const int32_t *d_pos, const int32_t *d_slot,
+                        int64_t slots, const void *d_state, Packed &packed, int32_t &longest)
+{
+    if (!h_offsets || !d_offsets) return fail(SRM_EINVAL, "%s: null argument", who);
+    SRM_TRY(check_offsets(who, h_offsets, n, longest));
+    if (slots < 0 || (d_state && slots == 0)) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    if (misaligned(d_offsets, 4) || misaligned(d_pos, 4) || misaligned(d_slot, 4)) return fail(SRM_EINVAL, "%s: %s", who, kNotWhole);
+    packed = Packed{d_offsets, d_pos, d_slot, n, h_offsets[0], h_offsets[n], d_state ? slots : 0};
+    return SRM_OK;
+}
+
+// ------------------------------------------------------------------ the short convolution
+template <typename T, int W>
+static void launch_conv(const void *d_x, void *d_out, ConvCall c, int64_t tokens, hipStream_t st)
+{
+    constexpr int R = 8;
+    c.runs = cdiv(tokens, R);
+    const int64_t waves = c.units > 64 ? c.runs * cdiv(c.units, 64) : cdiv(c.runs, 64 / c.per_run);
+    hipLaunchKernelGGL((causal_conv_kernel<T, W, R>), grid_of(cdiv(waves, 4)), dim3(256), 0, st, static_cast<const T *>(d_x), static_cast<T *>(d_out), c);
+}
+template <typename T>
+static void conv(int width, const void *d_x, void *d_out, const ConvCall &c, int64_t tokens, hipStream_t st)
+{
+    switch (width) {
+    case 1: return launch_conv<T, 1>(d_x, d_out, c, tokens, st);
+    case 2: return launch_conv<T, 2>(d_x, d_out, c, tokens, st);
+    case 3: return launch_conv<T, 3>(d_x, d_out, c, tokens, st);
+    case 4: return launch_conv<T, 4>(d_x, d_out, c, tokens, st);
+    case 5: return launch_conv<T, 5>(d_x, d_out, c, tokens, st);
+    case 6: return launch_conv<T, 6>(d_x, d_out, c, tokens, st);
+    case 7: return launch_conv<T, 7>(d_x, d_out, c, tokens, st);
+    default: return launch_conv<T, 8>(d_x, d_out, c, tokens, st);
+    }
+}
+
+extern "C" int srm_causal_conv(int32_t dtype, const void *d_x, int64_t ldx, const float *d_weight, const float *d_bias, int32_t activation,
+                               int32_t channels, int32_t width, const int32_t *h_offsets, const int32_t *d_offsets, int32_t N, const int32_t *d_pos,
+                               const int32_t *d_slot, int64_t slots, void *d_state, void *d_out, int64_t ld_out, void *hip_stream)
+{
+    const char *who = "srm_causal_conv";
+    if (!d_x || !d_weight || !d_out) return fail(SRM_EINVAL, "%s: null argument", who);
+    if (!known(dtype)) return fail(SRM_EINVAL, "%s: unknown dtype %d", who, dtype);
+    if (channels <= 0 || channels > (1 << 24) || width <= 0 || width > kConvTaps) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    if (activation != 0 && activation != 1) return fail(SRM_EINVAL, "%s: unknown activation %d", who, activation);
+    if (ldx < channels || ld_out < channels) return fail(SRM_EINVAL, "%s: a row stride is less than %d", who, channels);
+    ConvCall c{};
+    int32_t longest;
+    SRM_TRY(check_packed(who, h_offsets, d_offsets, N, d_pos, d_slot, slots, d_state, c.seqs, longest));
+    const unsigned size = size_of(dtype);
+    if (misaligned(d_x, size) || misaligned(d_out, size) || misaligned(d_state, size) || misaligned(d_weight, 4) || misaligned(d_bias, 4))
+        return fail(SRM_EINVAL, "%s: %s", who, kNotWhole);
+    const int64_t tokens = c.seqs.hi - c.seqs.lo;
+    if (cdiv(tokens, 8) * cdiv(channels, 512) >= kMaxBlocks) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    if (tokens == 0) return SRM_OK;
+    c.ldx = ldx;
+    c.ld_out = ld_out;
+    c.weight = d_weight;
+    c.bias = d_bias;
+    c.channels = channels;
+    c.silu = activation;
+    c.units = (int)cdiv(channels, 8);
+    for (c.per_run = 1; c.per_run < std::min(c.units, 64); c.per_run *= 2) {}
+    c.ring = d_state;
+    if (dtype == SRM_BF16) conv<bf16>(width, d_x, d_out, c, tokens, as_stream(hip_stream));
+    else conv<float>(width, d_x, d_out, c, tokens, as_stream(hip_stream));
+    HIP_TRY(hipGetLastError());
+    return SRM_OK;
+}
+
+// ------------------------------------------------------------------ the selective recurrence
+struct HeadSizes {
+    int32_t H, P, G, N;
+};
+static bool fits(const HeadSizes &s)
+{
+    return s.H > 0 && s.H <= 65536 && s.P > 0 && s.P <= 4096 && s.N > 0 && s.N <= 256 && s.G > 0 && s.H % s.G == 0 &&
+           (int64_t)s.H * s.P + 2ll * s.G * s.N < (1 << 30);
+}
+static int check_heads(const char *who, int32_t dtype, int32_t dt_dtype, const HeadSizes &s, const void *xbc, int64_t ld, const void *dt, int64_t ld_dt,
+                       const float *a, const float *dt_bias, const float *skip, const void *z, int64_t ld_z, const void *out, int64_t ld_out,
+                       const float *state)
+{
+    if (!xbc || !dt || !a || !out) return fail(SRM_EINVAL, "%s: null argument", who);
+    if (!known(dtype) || !known(dt_dtype)) return fail(SRM_EINVAL, "%s: unknown dtype %d, %d", who, dtype, dt_dtype);
+    if (!fits(s)) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    const int64_t inner = (int64_t)s.H * s.P;
+    if (ld < inner + 2ll * s.G * s.N || ld_dt < s.H || (z && ld_z < inner) || ld_out < inner) return fail(SRM_EINVAL, "%s: a row stride is less than its row", who);
+    const unsigned size = size_of(dtype);
+    if (misaligned(xbc, size) || misaligned(z, size) || misaligned(out, size) || misaligned(dt, size_of(dt_dtype)) || misaligned(a, 4) ||
+        misaligned(dt_bias, 4) || misaligned(skip, 4) || misaligned(state, 4))
+        return fail(SRM_EINVAL, "%s: %s", who, kNotWhole);
+    return SRM_OK;
+}
+
+// How a scan is cut over time.  `lanes`: rows of P that a work-group holds, `chip`: work-groups that the chip runs at its full rate.
+struct ScanPlan {
+    int parts, seg, segments;                        // segments 0: every sequence as a whole
+};
+static int scan_rows(int32_t N) { return N <= 8 ? 256 : N <= 16 ? 128 : N <= 32 ? 64 : N <= 64 ? 32 : 16; }
+static ScanPlan scan_plan(const HeadSizes &s, int64_t tokens, int32_t longest)
+{
+    ScanPlan p{(int)cdiv(s.P, scan_rows(s.N)), 0, 0};
+    const int64_t chip = 2048, units = (int64_t)s.H * p.parts, least = 64;
+    const int64_t seg = std::max(least, (cdiv(tokens * units, chip) + 15) / 16 * 16);
+    if (longest > 2 * seg + 2 * least) {
+        p.seg = (int)seg;
+        p.segments = (int)cdiv(tokens, seg);
+    }
+    return p;
+}
+static size_t segment_bytes(const HeadSizes &s) { return ((size_t)2 * s.P * s.N + 1) * s.H * 4; }
+
+extern "C" size_t srm_selective_scan_workspace_bytes(int32_t dtype, const int32_t *h_offsets, int32_t N, int32_t heads, int32_t head_dim,
+                                                     int32_t state_dim)
+{
+    const HeadSizes s{heads, head_dim, 1, state_dim};
+    int32_t longest;
+    if (!h_offsets || !known(dtype) || !fits(s) || check_offsets("srm_selective_scan_workspace_bytes", h_offsets, N, longest) != SRM_OK) return 0;
+    return scan_plan(s, h_offsets[N] - h_offsets[0], longest).segments * segment_bytes(s);
+}
+
+template <typename T, int NL, int NR>
+static int launch_scan(const void *d_xbc, void *d_out, const ScanCall &c, const ScanPlan &p, hipStream_t st)
+{
+    const int64_t units = (int64_t)c.H * c.parts;
+    const T *x = static_cast<const T *>(d_xbc);
+    T *out = static_cast<T *>(d_out);
+    if (p.segments == 0) {
+        hipLaunchKernelGGL((selective_scan_kernel<T, NL, NR, SCAN_WHOLE>), grid_of(c.seqs.n * units), dim3(64), 0, st, x, out, c);
+    } else {
+        hipLaunchKernelGGL((selective_scan_kernel<T, NL, NR, SCAN_CARRY>), grid_of(p.segments * units), dim3(64), 0, st, x, out, c);
+        HIP_TRY(hipGetLastError());
+        hipLaunchKernelGGL((selective_scan_kernel<T, NL, NR, SCAN_SEGMENTS>), grid_of(p.segments * units), dim3(64), 0, st, x, out, c);
+    }
+    HIP_TRY(hipGetLastError());
+    return SRM_OK;
+}
+template <typename T>
+static int scan(const void *d_xbc, void *d_out, const ScanCall &c, const ScanPlan &p, hipStream_t st)
+{
+    if (c.N <= 8) return launch_scan<T, 1, 8>(d_xbc, d_out, c, p, st);
+    if (c.N <= 16) return launch_scan<T, 2, 8>(d_xbc, d_out, c, p, st);
+    if (c.N <= 32) return launch_scan<T, 4, 8>(d_xbc, d_out, c, p, st);
+    if (c.N <= 64) return launch_scan<T, 8, 8>(d_xbc, d_out, c, p, st);
+    if (c.N <= 128) return launch_scan<T, 16, 8>(d_xbc, d_out, c, p, st);
+    return launch_scan<T, 16, 16>(d_xbc, d_out, c, p, st);
+}
+
+extern "C" int srm_selective_scan(int32_t dtype, const void *d_xbc, int64_t ld_xbc, int32_t dt_dtype, const void *d_dt, int64_t ld_dt, const float *d_a,
+                                  const float *d_dt_bias, const float *d_skip, int32_t softplus, const void *d_z, int64_t ld_z, int32_t heads,
+                                  int32_t head_dim, int32_t groups, int32_t state_dim, const int32_t *h_offsets, const int32_t *d_offsets, int32_t N,
+                                  const int32_t *d_pos, const int32_t *d_slot, int64_t slots, float *d_state, void *d_out, int64_t ld_out,
+                                  void *d_workspace, size_t workspace_bytes, void *hip_stream)
+{
+    const char *who = "srm_selective_scan";
+    const HeadSizes s{heads, head_dim, groups, state_dim};
+    SRM_TRY(check_heads(who, dtype, dt_dtype, s, d_xbc, ld_xbc, d_dt, ld_dt, d_a, d_dt_bias, d_skip, d_z, ld_z, d_out, ld_out, d_state));
+    ScanCall c{};
+    int32_t longest;
+    SRM_TRY(check_packed(who, h_offsets, d_offsets, N, d_pos, d_slot, slots, d_state, c.seqs, longest));
+    if (misaligned(d_workspace, 4)) return fail(SRM_EINVAL, "%s: %s", who, kNotWhole);
+    const int64_t tokens = c.seqs.hi - c.seqs.lo;
+    ScanPlan p = scan_plan(s, tokens, longest);
+    const int64_t room = d_workspace ? (int64_t)(workspace_bytes / segment_bytes(s)) : 0;
+    if (p.segments > room) {                         // fewer and longer segments, or none
+        p.segments = 0;
+        if (room > 1) {
+            p.seg = (int)((cdiv(tokens, room) + 63) / 64 * 64);
+            p.segments = (int)cdiv(tokens, p.seg);
+        }
+    }
+    if (std::max<int64_t>(p.segments, N) * heads * p.parts >= kMaxBlocks) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    if (tokens == 0) return SRM_OK;
+    c.dt = StepSizes{d_dt, ld_dt, d_dt_bias, dt_dtype == SRM_BF16, softplus != 0};
+    c.ld = ld_xbc;
+    c.ld_z = ld_z;
+    c.ld_out = ld_out;
+    c.z = d_z;
+    c.a = d_a;
+    c.skip = d_skip;
+    c.H = heads;
+    c.P = head_dim;
+    c.G = groups;
+    c.N = state_dim;
+    c.state = d_state;
+    c.seg = p.segments ? p.seg : 1;
+    c.parts = p.parts;
+    if (p.segments) {
+        const size_t all = (size_t)p.segments * heads * head_dim * state_dim;
+        c.carry = static_cast<float *>(d_workspace);
+        c.held = c.carry + all;
+        c.decay = c.held + all;
+    }
+    return dtype == SRM_BF16 ? scan<bf16>(d_xbc, d_out, c, p, as_stream(hip_stream)) : scan<float>(d_xbc, d_out, c, p, as_stream(hip_stream));
+}
+
+// ------------------------------------------------------------------ single tokens
+template <typename T, int NL, int U>
+static void launch_step(const void *d_xbc, void *d_out, StepCall c, hipStream_t st)
+{
+    c.parts = (int)cdiv(c.P, 4 * (64 / NL) * U);
+    hipLaunchKernelGGL((selective_step_kernel<T, NL, U>), grid_of(c.rows * c.H * c.parts), dim3(256), 0, st, static_cast<const T *>(d_xbc),
+                       static_cast<T *>(d_out), c);
+}
+template <typename T>
+static void step(const void *d_xbc, void *d_out, const StepCall &c, hipStream_t st)
+{
+    if (c.N <= 16) return launch_step<T, 4, 2>(d_xbc, d_out, c, st);
+    if (c.N <= 32) return launch_step<T, 8, 4>(d_xbc, d_out, c, st);
+    if (c.N <= 64) return launch_step<T, 16, 4>(d_xbc, d_out, c, st);
+    if (c.N <= 128) return launch_step<T, 32, 8>(d_xbc, d_out, c, st);
+    return launch_step<T, 64, 8>(d_xbc, d_out, c, st);
+}
+
+extern "C" int srm_selective_step(int32_t dtype, const void *d_xbc, int64_t ld_xbc, const float *d_weight, const float *d_bias, int32_t activation,
+                                  int32_t width, void *d_conv_state, int32_t dt_dtype, const void *d_dt, int64_t ld_dt, const float *d_a,
+                                  const float *d_dt_bias, const float *d_skip, int32_t softplus, const void *d_z, int64_t ld_z, int32_t heads,
+                                  int32_t head_dim, int32_t groups, int32_t state_dim, int64_t rows, const int32_t *d_pos, const int32_t *d_slot,
+                                  int64_t slots, float *d_state, void *d_out, int64_t ld_out, void *hip_stream)
+{
+    const char *who = "srm_selective_step";
+    const HeadSizes s{heads, head_dim, groups, state_dim};
+    SRM_TRY(check_heads(who, dtype, dt_dtype, s, d_xbc, ld_xbc, d_dt, ld_dt, d_a, d_dt_bias, d_skip, d_z, ld_z, d_out, ld_out, d_state));
+    if (!d_state || !d_pos) return fail(SRM_EINVAL, "%s: null argument", who);
+    if (rows <= 0 || rows >= kMaxRows || slots <= 0) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    if (d_weight) {
+        if (width <= 0 || width > kConvTaps) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+        if (width > 1 && !d_conv_state) return fail(SRM_EINVAL, "%s: null argument", who);
+        if (activation != 0 && activation != 1) return fail(SRM_EINVAL, "%s: unknown activation %d", who, activation);
+    }
+    if (misaligned(d_weight, 4) || misaligned(d_bias, 4) || misaligned(d_conv_state, size_of(dtype)) || misaligned(d_pos, 4) || misaligned(d_slot, 4))
+        return fail(SRM_EINVAL, "%s: %s", who, kNotWhole);
+    if (rows * heads * cdiv(head_dim, 16) >= kMaxBlocks) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    StepCall c{};
+    c.dt = StepSizes{d_dt, ld_dt, d_dt_bias, dt_dtype == SRM_BF16, softplus != 0};
+    c.rows = rows;
+    c.slots = slots;
+    c.ld = ld_xbc;
+    c.ld_z = ld_z;
+    c.ld_out = ld_out;
+    c.pos = d_pos;
+    c.slot = d_slot;
+    c.weight = d_weight;
+    c.bias = d_bias;
+    c.width = d_weight ? width : 1;
+    c.silu = activation;
+    c.ring = d_weight ? d_conv_state : nullptr;
+    c.z = d_z;
+    c.a = d_a;
+    c.skip = d_skip;
+    c.H = heads;
+    c.P = head_dim;
+    c.G = groups;
+    c.N = state_dim;
+    c.state = d_state;
+    if (dtype == SRM_BF16) step<bf16>(d_xbc, d_out, c, as_stream(hip_stream));
+    else step<float>(d_xbc, d_out, c, as_stream(hip_stream));
+    HIP_TRY(hipGetLastError());
+    return SRM_OK;
+}
+
+// ------------------------------------------------------------------ scores of given tokens
+template <typename T>
+static void launch_score(const void *d_logits, const ScoreCall &c, hipStream_t st)
+{
+    const T *logits = static_cast<const T *>(d_logits);
+    if (c.V <= 8192) hipLaunchKernelGGL((token_logprobs_kernel<T, 256>), grid_of(c.rows), dim3(256), 0, st, logits, c);
+    else hipLaunchKernelGGL((token_logprobs_kernel<T, 1024>), grid_of(c.rows), dim3(1024), 0, st, logits, c);
+}
+
+extern "C" int srm_token_logprobs(int32_t dtype, const void *d_logits, int64_t ld, int64_t rows, int32_t vocab, const float *d_temperature,
+                                  const int32_t *d_token, float *d_logprob, float *d_entropy, int32_t top, int32_t *d_top_token,
+                                  float *d_top_logprob, void *hip_stream)
+{
+    const char *who = "srm_token_logprobs";
+    if (!d_logits || (d_token && !d_logprob) || (d_logprob && !d_token)) return fail(SRM_EINVAL, "%s: null argument", who);
+    if (!known(dtype)) return fail(SRM_EINVAL, "%s: unknown dtype %d", who, dtype);
+    if (rows <= 0 || rows >= kMaxRows || vocab <= 0 || vocab > kScoreVocab || top < 0 || top > kScoreTop)
+        return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    if (top > 0 && (!d_top_token || !d_top_logprob)) return fail(SRM_EINVAL, "%s: null argument", who);
+    if (!d_token && !d_entropy && top == 0) return fail(SRM_EINVAL, "%s: nothing to compute", who);
+    if (ld < vocab) return fail(SRM_EINVAL, "%s: row stride %lld is less than %d", who, (long long)ld, vocab);
+    const void *const words[] = {d_temperature, d_token, d_logprob, d_entropy, d_top_token, d_top_logprob};
+    bool whole = !misaligned(d_logits, size_of(dtype));
+    for (const void *w : words) whole = whole && !misaligned(w, 4);
+    if (!whole) return fail(SRM_EINVAL, "%s: %s", who, kNotWhole);
+    const ScoreCall c{rows, ld, vocab, top, d_token, d_temperature, d_logprob, d_entropy, d_top_logprob, d_top_token};
+    if (dtype == SRM_BF16) launch_score<bf16>(d_logits, c, as_stream(hip_stream));
+    else launch_score<float>(d_logits, c, as_stream(hip_stream));
+    HIP_TRY(hipGetLastError());
+    return SRM_OK;
+}

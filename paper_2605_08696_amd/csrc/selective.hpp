@@ -1,0 +1,337 @@
+// The selective recurrence: for each head a matrix of state S [P][N] whose decay and input depend on the token,
+//   dt = softplus(dt_raw + dt_bias[h])     S <- exp(dt A[h]) S + dt x[h] B[g]^T     y = S C[g] + D[h] x[h]     out = y silu(z)
+// with x [H][P] | B [G][N] | C [G][N] in a row and g = h / (H / G).  Here: what its kernels share, the kernel for operands in fp32 (and a
+// simple form for bf16), and the kernel of single tokens.
+//
+// Work over time.  A work-group takes one head (a part of its P rows) of one sequence from its first token to its last, the state in
+// registers.  Where there are too few of those, the packed tokens are cut into segments of equal length, whatever sequences they hold:
+// a first pass leaves, for each segment that a sequence runs on from, the state at its end that the segment itself brings (`carry`) and
+// the factor by which it decays what came before (`decay`); the second pass starts each segment from the decayed sum of the carries in
+// front of it and writes the outputs.
+#pragma once
+#include "conv.hpp"
+
+struct StepSizes {                                   // dt_raw [tokens][H] and what dt is made of
+    const void *raw;
+    int64_t ld;
+    const float *bias;
+    int is_bf16, softplus;
+};
+struct ScanCall {
+    Packed seqs;
+    StepSizes dt;
+    int64_t ld, ld_z, ld_out;                        // of x | B | C, z, out
+    const void *z;
+    const float *a, *skip;
+    int H, P, G, N;
+    float *state;                                    // [slots][H][P][N]
+    int seg, parts;                                  // tokens of a segment; parts of a head's P rows
+    float *carry, *held, *decay;                     // [segments][H][P][N] twice, [segments][H]
+};
+enum { SCAN_WHOLE = 0, SCAN_CARRY = 1, SCAN_SEGMENTS = 2 };
+
+__device__ __forceinline__ float dt_of(const StepSizes &c, int64_t t, int h)
+{
+    const int64_t at = t * c.ld + h;
+    float v = c.is_bf16 ? (float)static_cast<const bf16 *>(c.raw)[at] : static_cast<const float *>(c.raw)[at];
+    if (c.bias) v += c.bias[h];
+    // (log(1 + e^v) without loss on either side; a NaN stays one)
+    if (c.softplus) v = (v > 0.0f ? v : v == v ? 0.0f : v) + log1pf(__expf(-fabsf(v)));
+    return v;
+}
+// The decay's exponent in steps of a factor of two.  Below 2^-200 a decay leaves nothing of a state of fp32; the limit keeps sums of
+// exponents small enough that their differences are exact where the decays are not 0.  (A comparison, so that a NaN stays one.)
+__device__ __forceinline__ float decay_exponent(float dt, float a)
+{
+    const float e = dt * a * 1.44269504088896340736f;
+    return e < -200.0f ? -200.0f : e;
+}
+
+// Sum over groups of NL neighbouring lanes, in every lane of a group.
+template <int NL>
+__device__ __forceinline__ float lanes_sum(float v)
+{
+    auto step = [](float x, int moved) { return x + __builtin_bit_cast(float, moved); };
+    if constexpr (NL > 1) v = step(v, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0xB1, 0xF, 0xF, true));
+    if constexpr (NL > 2) v = step(v, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x4E, 0xF, 0xF, true));
+    if constexpr (NL > 4) v = step(v, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x141, 0xF, 0xF, true));
+    if constexpr (NL > 8) v = step(v, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x140, 0xF, 0xF, true));
+    return v;
+}
+
+// One wavefront takes PR rows of P a lane, NL lanes with NR elements of N each: 64 / NL * PR rows, NL NR >= N.  Sixteen tokens at a time
+// are brought to LDS; then for every token each lane updates its PR x NR elements (multiply, multiply-add) and adds their products with C.
+// What bounds it: three vector instructions for each element of state and token.
+template <typename T, int NL, int NR, int MODE>
+__global__ void __launch_bounds__(64)
+selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c)
+{
+    constexpr int PR = 4, PW = 64 / NL * PR, NP = NL * NR, TT = 16;
+    __shared__ __align__(16) float sb[TT][NP + 4], sc[TT][NP + 4], sx[TT][PW + 4];
+    __shared__ float2 sd[TT];
+    const int lane = threadIdx.x, ln = lane % NL, lp = lane / NL;
+    const int64_t id = work_group();
+    const int per = c.H * c.parts;
+    const int64_t work = id / per;
+    const int h = (int)(id % per) / c.parts, p0 = (int)(id % per) % c.parts * PW, g = h / (c.H / c.G);
+    const int P = c.P, N = c.N, np = min(PW, P - p0);
+    const int segments = (c.seqs.hi - c.seqs.lo + c.seg - 1) / c.seg;
+    if (MODE == SCAN_WHOLE ? work >= c.seqs.n : work >= segments) return;
+    const float a = c.a[h], skip = c.skip ? c.skip[h] : 0.0f;
+    const int64_t head_at = ((int64_t)h * P + p0) * N, slot_size = (int64_t)c.H * P * N;
+
+    float S[PR][NR];
+    auto clear = [&]() {
+#pragma unroll
+        for (int i = 0; i < PR; ++i)
+#pragma unroll
+            for (int j = 0; j < NR; ++j) S[i][j] = 0.0f;
+    };
+    auto each = [&](auto &&fn) {                     // fn(element, offset from the head's first) of those that exist
+#pragma unroll
+        for (int i = 0; i < PR; ++i)
+#pragma unroll
+            for (int j = 0; j < NR; ++j)
+                if (lp * PR + i < np && ln * NR + j < N) fn(S[i][j], (int64_t)(lp * PR + i) * N + ln * NR + j);
+    };
+    // Tokens [t0, t1) of one sequence; adds their decay exponents to `sum`.
+    auto run = [&](int t0, int t1, float &sum) {
+        for (int t = t0; t < t1; t += TT) {
+            const int nt = min(TT, t1 - t);
+            __syncthreads();
+            for (int e = lane; e < nt * NP; e += 64) {
+                const int r = e / NP, n = e % NP;
+                const T *row = xbc + (int64_t)(t + r) * c.ld + (int64_t)c.H * P + (int64_t)g * N;
+                sb[r][n] = n < N ? (float)row[n] : 0.0f;
+                if (MODE != SCAN_CARRY) sc[r][n] = n < N ? (float)row[(int64_t)c.G * N + n] : 0.0f;
+            }
+            for (int e = lane; e < nt * PW; e += 64) {
+                const int r = e / PW, p = e % PW;
+                sx[r][p] = p < np ? (float)xbc[(int64_t)(t + r) * c.ld + (int64_t)h * P + p0 + p] : 0.0f;
+            }
+            if (lane < nt) {
+                const float dt = dt_of(c.dt, t + lane, h), ex = decay_exponent(dt, a);
+                sd[lane] = make_float2(__builtin_amdgcn_exp2f(ex), dt);
+                if (MODE == SCAN_CARRY) sb[lane][NP] = ex;
+            }
+            __syncthreads();
+            for (int r = 0; r < nt; ++r) {
+                const float2 d = sd[r];
+                if (MODE == SCAN_CARRY) sum += sb[r][NP];
+                float y[PR];
+#pragma unroll
+                for (int i = 0; i < PR; ++i) {
+                    const float x = sx[r][lp * PR + i] * d.y;
+                    y[i] = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < NR; ++j) {
+                        S[i][j] = fmaf(x, sb[r][ln * NR + j], d.x * S[i][j]);
+                        if (MODE != SCAN_CARRY) y[i] = fmaf(S[i][j], sc[r][ln * NR + j], y[i]);
+                    }
+                }
+                if (MODE != SCAN_CARRY) {
+#pragma unroll
+                    for (int i = 0; i < PR; ++i) y[i] = lanes_sum<NL>(y[i]);
+                    if (ln == 0) {
+#pragma unroll
+                        for (int i = 0; i < PR; ++i) {
+                            const int p = lp * PR + i;
+                            sx[r][p] = fmaf(skip, sx[r][p], y[i]);
+                        }
+                    }
+                }
+            }
+            if (MODE != SCAN_CARRY) {
+                __syncthreads();
+                for (int e = lane; e < nt * PW; e += 64) {
+                    const int r = e / PW, p = e % PW;
+                    if (p >= np) continue;
+                    float y = sx[r][p];
+                    const int64_t col = (int64_t)h * P + p0 + p;
+                    if (c.z) y *= silu((float)static_cast<const T *>(c.z)[(int64_t)(t + r) * c.ld_z + col]);
+                    store1(out + (int64_t)(t + r) * c.ld_out + col, y);
+                }
+            }
+        }
+    };
+    auto zeros = [&](int t0, int t1) {
+        for (int t = t0; t < t1; ++t)
+            for (int p = lane; p < np; p += 64) store1(out + (int64_t)t * c.ld_out + (int64_t)h * P + p0 + p, 0.0f);
+    };
+    auto load = [&](const float *from) { each([&](float &v, int64_t at) { v = from[at]; }); };
+    auto store = [&](float *to) { each([&](float &v, int64_t at) { to[at] = v; }); };
+    auto slot_of = [&](const Sequence &s) { return c.state + s.slot * slot_size + head_at; };
+
+    float sum = 0.0f;
+    if constexpr (MODE == SCAN_WHOLE) {
+        const Sequence s = packed_sequence(c.seqs, (int)work);
+        if (s.begin == s.end) return;
+        if (s.pos < 0) return zeros(s.begin, s.end);
+        clear();
+        if (s.slot >= 0 && s.pos > 0) load(slot_of(s));
+        run(s.begin, s.end, sum);
+        if (s.slot >= 0) store(slot_of(s));
+    } else if constexpr (MODE == SCAN_CARRY) {
+        const int t0 = c.seqs.lo + (int)work * c.seg, t1 = t0 + c.seg;
+        if (t1 >= c.seqs.hi) return;
+        const Sequence s = packed_sequence(c.seqs, packed_find(c.seqs, t1 - 1, lane));
+        if (s.end <= t1 || s.pos < 0) return;
+        const int64_t at = work * slot_size + head_at;
+        clear();
+        if (s.begin >= t0 && s.slot >= 0 && s.pos > 0) {
+            load(slot_of(s));
+            store(c.held + at);                      // (the slot may be written before the second pass comes to read it)
+        }
+        run(max(s.begin, t0), t1, sum);
+        store(c.carry + at);
+        if (lane == 0 && p0 == 0) c.decay[work * c.H + h] = __builtin_amdgcn_exp2f(sum);
+    } else {
+        const int t0 = c.seqs.lo + (int)work * c.seg, t1 = min(t0 + c.seg, c.seqs.hi);
+        int n = packed_find(c.seqs, t0, lane);
+        for (int t = t0; t < t1;) {
+            Sequence s = packed_sequence(c.seqs, n);
+            while (t >= s.end && n + 1 < c.seqs.n) s = packed_sequence(c.seqs, ++n);
+            if (t >= s.end) break;                   // (offsets that are not the host's)
+            const int e = min(s.end, t1);
+            if (s.pos < 0) {
+                zeros(t, e);
+            } else {
+                clear();
+                if (t == s.begin) {
+                    if (s.slot >= 0 && s.pos > 0) load(s.end > t1 ? c.held + work * slot_size + head_at : slot_of(s));
+                } else {
+                    float scale = 1.0f;
+                    const int64_t first = (s.begin - c.seqs.lo) / c.seg;
+                    for (int64_t j = work - 1; j >= first; --j) {   // (a scale of 0 too: what is not finite stays so)
+                        const float *from = c.carry + j * slot_size + head_at;
+                        each([&](float &v, int64_t at) { v = fmaf(scale, from[at], v); });
+                        if (j > first) scale *= c.decay[j * c.H + h];
+                    }
+                }
+                run(t, e, sum);
+                if (e == s.end && s.slot >= 0) store(slot_of(s));
+            }
+            t = e;
+        }
+    }
+}
+
+// ------------------------------------------------------------------ single tokens
+// A work-group takes PW rows of P of one head of one request.  The state's loads start as soon as the slot is known, the convolution of
+// the head's x and its group's B and C runs while they travel.  B and C are formed by every work-group of a group; the ring's row of the
+// new token, which none of the taps reads, is written by the work-groups of the group's first head.
+// What bounds it: the state is read and written once.
+struct StepCall {
+    StepSizes dt;
+    int64_t rows, slots, ld, ld_z, ld_out;
+    const int32_t *pos, *slot;
+    const float *weight, *bias;                      // weight NULL: x | B | C as they are
+    int width, silu;
+    void *ring;
+    const void *z;
+    const float *a, *skip;
+    int H, P, G, N, parts;
+    float *state;
+};
+typedef f32x4_t __attribute__((aligned(4))) f32x4_any;
+
+// NL lanes with four elements of N each hold a row of P, a work-group U rows of them in each lane.
+template <typename T, int NL, int U>
+__global__ void __launch_bounds__(256)
+selective_step_kernel(const T *__restrict__ xbc, T *__restrict__ out, StepCall c)
+{
+    constexpr int PL = 64 / NL, PW = 4 * PL * U;
+    __shared__ __align__(16) float sb[4 * NL], sc[4 * NL], sx[PW];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane % NL;
+    const int64_t id = work_group();
+    const int per = c.H * c.parts;
+    const int64_t r = id / per;
+    if (r >= c.rows) return;
+    const int h = (int)(id % per) / c.parts, p0 = (int)(id % per) % c.parts * PW, g = h / (c.H / c.G);
+    const int P = c.P, N = c.N, np = min(PW, P - p0), C = c.H * P + 2 * c.G * N;
+    const int pos = c.pos[r];
+    const int64_t at = c.slot ? c.slot[r] : r;
+    const bool kept = at >= 0 && at < c.slots;
+    T *o = out + r * c.ld_out + (int64_t)h * P + p0;
+    if (pos < 0) {
+        for (int p = tid; p < np; p += 256) store1(o + p, 0.0f);
+        return;
+    }
+    float *S = kept ? c.state + ((at * c.H + h) * P + p0) * (int64_t)N : nullptr;
+    auto row_of = [&](int u) { return (u * 4 + wave) * PL + lane / NL; };
+    f32x4_t v[U];
+    const bool whole = ln * 4 + 4 <= N;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        v[u] = f32x4_t{0, 0, 0, 0};
+        if (kept && pos > 0 && row_of(u) < np && ln * 4 < N) {
+            const float *from = S + (int64_t)row_of(u) * N + ln * 4;
+            if (whole) v[u] = __builtin_nontemporal_load(reinterpret_cast<const f32x4_any *>(from));
+            else
+                for (int i = 0; i < 3; ++i)
+                    if (ln * 4 + i < N) v[u][i] = from[i];
+        }
+    }
+    const float dt = dt_of(c.dt, r, h);
+    const float decay = __builtin_amdgcn_exp2f(decay_exponent(dt, c.a[h])), skip = c.skip ? c.skip[h] : 0.0f;
+    const bool first = h % (c.H / c.G) == 0 && p0 == 0;
+    const T *x = xbc + r * c.ld;
+    T *ring = c.ring && kept ? static_cast<T *>(c.ring) + at * c.width * (int64_t)C : nullptr;
+    for (int e = tid; e < PW + 8 * NL; e += 256) {
+        int ch;
+        float *to;
+        bool mine = true;
+        if (e < PW) {
+            ch = e < np ? h * P + p0 + e : -1;
+            to = sx + e;
+        } else {
+            const int which = (e - PW) / (4 * NL), n = (e - PW) % (4 * NL);
+            ch = n < N ? c.H * P + which * c.G * N + g * N + n : -1;
+            to = (which ? sc : sb) + n;
+            mine = first;
+        }
+        float q = 0.0f;
+        if (ch >= 0) {
+            q = (float)x[ch];
+            if (c.weight) {
+                const float *w = c.weight + (int64_t)ch * c.width;
+                float acc = fmaf(w[c.width - 1], q, c.bias ? c.bias[ch] : 0.0f);
+                for (int k = 0; k < c.width - 1; ++k) {
+                    const int p = pos - (c.width - 1) + k;
+                    if (p >= 0 && ring) acc = fmaf(w[k], (float)ring[(int64_t)(p % c.width) * C + ch], acc);
+                }
+                if (ring && mine) ring[(int64_t)(pos % c.width) * C + ch] = x[ch];
+                q = c.silu ? silu(acc) : acc;
+            }
+        }
+        *to = q;
+    }
+    __syncthreads();
+    const f32x4_t b = *reinterpret_cast<const f32x4_t *>(sb + ln * 4), cc = *reinterpret_cast<const f32x4_t *>(sc + ln * 4);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int p = row_of(u);
+        const float xd = sx[p] * dt;
+        float y = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[u][i] = fmaf(xd, b[i], decay * v[u][i]);
+            y = fmaf(v[u][i], cc[i], y);
+        }
+        if (kept && p < np && ln * 4 < N) {
+            float *to = S + (int64_t)p * N + ln * 4;
+            if (whole) __builtin_nontemporal_store(v[u], reinterpret_cast<f32x4_any *>(to));
+            else
+                for (int i = 0; i < 3; ++i)
+                    if (ln * 4 + i < N) to[i] = v[u][i];
+        }
+        y = lanes_sum<(NL < 16 ? NL : 16)>(y);
+        if constexpr (NL > 16) y += __shfl_xor(y, 16);
+        if constexpr (NL > 32) y += __shfl_xor(y, 32);
+        if (ln == 0 && p < np) {
+            y = fmaf(skip, sx[p], y);
+            if (c.z) y *= silu((float)static_cast<const T *>(c.z)[r * c.ld_z + (int64_t)h * P + p0 + p]);
+            store1(o + p, y);
+        }
+    }
+}
