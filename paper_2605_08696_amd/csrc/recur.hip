@@ -7,6 +7,7 @@
 #include "srm.h"
 #include "conv.hpp"
 #include "selective.hpp"
+#include "selective_mfma.hpp"
 #include "score.hpp"
 #include "status.hpp"
 
@@ -126,16 +127,20 @@ static int check_heads(const char *who, int32_t dtype, int32_t dt_dtype, const H
     return SRM_OK;
 }
 
-// How a scan is cut over time.  `lanes`: rows of P that a work-group holds, `chip`: work-groups that the chip runs at its full rate.
+// How a scan is cut over time.  A work-group holds `rows` rows of P; `chip` of them run at the chip's full rate together.
 struct ScanPlan {
     int parts, seg, segments;                        // segments 0: every sequence as a whole
 };
-static int scan_rows(int32_t N) { return N <= 8 ? 256 : N <= 16 ? 128 : N <= 32 ? 64 : N <= 64 ? 32 : 16; }
-static ScanPlan scan_plan(const HeadSizes &s, int64_t tokens, int32_t longest)
+static int scan_rows(int32_t dtype, int32_t N)
 {
-    ScanPlan p{(int)cdiv(s.P, scan_rows(s.N)), 0, 0};
-    const int64_t chip = 2048, units = (int64_t)s.H * p.parts, least = 64;
-    const int64_t seg = std::max(least, (cdiv(tokens * units, chip) + 15) / 16 * 16);
+    if (dtype == SRM_BF16) return kScanBlock;
+    return N <= 8 ? 256 : N <= 16 ? 128 : N <= 32 ? 64 : N <= 64 ? 32 : 16;
+}
+static ScanPlan scan_plan(int32_t dtype, const HeadSizes &s, int64_t tokens, int32_t longest)
+{
+    ScanPlan p{(int)cdiv(s.P, scan_rows(dtype, s.N)), 0, 0};
+    const int64_t chip = dtype == SRM_BF16 ? 512 : 2048, units = (int64_t)s.H * p.parts, least = 64;
+    const int64_t seg = std::max(least, cdiv(cdiv(tokens * units, chip), 64) * 64);
     if (longest > 2 * seg + 2 * least) {
         p.seg = (int)seg;
         p.segments = (int)cdiv(tokens, seg);
@@ -150,34 +155,48 @@ extern "C" size_t srm_selective_scan_workspace_bytes(int32_t dtype, const int32_
     const HeadSizes s{heads, head_dim, 1, state_dim};
     int32_t longest;
     if (!h_offsets || !known(dtype) || !fits(s) || check_offsets("srm_selective_scan_workspace_bytes", h_offsets, N, longest) != SRM_OK) return 0;
-    return scan_plan(s, h_offsets[N] - h_offsets[0], longest).segments * segment_bytes(s);
+    return scan_plan(dtype, s, h_offsets[N] - h_offsets[0], longest).segments * segment_bytes(s);
 }
 
-template <typename T, int NL, int NR>
-static int launch_scan(const void *d_xbc, void *d_out, const ScanCall &c, const ScanPlan &p, hipStream_t st)
+template <typename T, auto WHOLE, auto CARRY, auto SEGMENTS>
+static int launch_scan(const void *d_xbc, void *d_out, const ScanCall &c, const ScanPlan &p, int threads, hipStream_t st)
 {
     const int64_t units = (int64_t)c.H * c.parts;
     const T *x = static_cast<const T *>(d_xbc);
     T *out = static_cast<T *>(d_out);
     if (p.segments == 0) {
-        hipLaunchKernelGGL((selective_scan_kernel<T, NL, NR, SCAN_WHOLE>), grid_of(c.seqs.n * units), dim3(64), 0, st, x, out, c);
+        hipLaunchKernelGGL(WHOLE, grid_of(c.seqs.n * units), dim3(threads), 0, st, x, out, c);
     } else {
-        hipLaunchKernelGGL((selective_scan_kernel<T, NL, NR, SCAN_CARRY>), grid_of(p.segments * units), dim3(64), 0, st, x, out, c);
+        hipLaunchKernelGGL(CARRY, grid_of(p.segments * units), dim3(threads), 0, st, x, out, c);
         HIP_TRY(hipGetLastError());
-        hipLaunchKernelGGL((selective_scan_kernel<T, NL, NR, SCAN_SEGMENTS>), grid_of(p.segments * units), dim3(64), 0, st, x, out, c);
+        hipLaunchKernelGGL(SEGMENTS, grid_of(p.segments * units), dim3(threads), 0, st, x, out, c);
     }
     HIP_TRY(hipGetLastError());
     return SRM_OK;
 }
-template <typename T>
-static int scan(const void *d_xbc, void *d_out, const ScanCall &c, const ScanPlan &p, hipStream_t st)
+static int scan_f32(const void *d_xbc, void *d_out, const ScanCall &c, const ScanPlan &p, hipStream_t st)
 {
-    if (c.N <= 8) return launch_scan<T, 1, 8>(d_xbc, d_out, c, p, st);
-    if (c.N <= 16) return launch_scan<T, 2, 8>(d_xbc, d_out, c, p, st);
-    if (c.N <= 32) return launch_scan<T, 4, 8>(d_xbc, d_out, c, p, st);
-    if (c.N <= 64) return launch_scan<T, 8, 8>(d_xbc, d_out, c, p, st);
-    if (c.N <= 128) return launch_scan<T, 16, 8>(d_xbc, d_out, c, p, st);
-    return launch_scan<T, 16, 16>(d_xbc, d_out, c, p, st);
+#define SCAN_CASE(NL, NR)                                                                                                                     \
+    return launch_scan<float, selective_scan_kernel<float, NL, NR, SCAN_WHOLE>, selective_scan_kernel<float, NL, NR, SCAN_CARRY>,           \
+                       selective_scan_kernel<float, NL, NR, SCAN_SEGMENTS>>(d_xbc, d_out, c, p, 64, st)
+    if (c.N <= 8) SCAN_CASE(1, 8);
+    if (c.N <= 16) SCAN_CASE(2, 8);
+    if (c.N <= 32) SCAN_CASE(4, 8);
+    if (c.N <= 64) SCAN_CASE(8, 8);
+    if (c.N <= 128) SCAN_CASE(16, 8);
+    SCAN_CASE(16, 16);
+#undef SCAN_CASE
+}
+static int scan_bf16(const void *d_xbc, void *d_out, const ScanCall &c, const ScanPlan &p, hipStream_t st)
+{
+#define SCAN_CASE(NP)                                                                                                                         \
+    return launch_scan<bf16, selective_scan_mfma_kernel<NP, SCAN_WHOLE>, selective_scan_mfma_kernel<NP, SCAN_CARRY>,                        \
+                       selective_scan_mfma_kernel<NP, SCAN_SEGMENTS>>(d_xbc, d_out, c, p, 256, st)
+    if (c.N <= 32) SCAN_CASE(32);
+    if (c.N <= 64) SCAN_CASE(64);
+    if (c.N <= 128) SCAN_CASE(128);
+    SCAN_CASE(256);
+#undef SCAN_CASE
 }
 
 extern "C" int srm_selective_scan(int32_t dtype, const void *d_xbc, int64_t ld_xbc, int32_t dt_dtype, const void *d_dt, int64_t ld_dt, const float *d_a,
@@ -194,7 +213,7 @@ extern "C" int srm_selective_scan(int32_t dtype, const void *d_xbc, int64_t ld_x
     SRM_TRY(check_packed(who, h_offsets, d_offsets, N, d_pos, d_slot, slots, d_state, c.seqs, longest));
     if (misaligned(d_workspace, 4)) return fail(SRM_EINVAL, "%s: %s", who, kNotWhole);
     const int64_t tokens = c.seqs.hi - c.seqs.lo;
-    ScanPlan p = scan_plan(s, tokens, longest);
+    ScanPlan p = scan_plan(dtype, s, tokens, longest);
     const int64_t room = d_workspace ? (int64_t)(workspace_bytes / segment_bytes(s)) : 0;
     if (p.segments > room) {                         // fewer and longer segments, or none
         p.segments = 0;
@@ -225,7 +244,7 @@ extern "C" int srm_selective_scan(int32_t dtype, const void *d_xbc, int64_t ld_x
         c.held = c.carry + all;
         c.decay = c.held + all;
     }
-    return dtype == SRM_BF16 ? scan<bf16>(d_xbc, d_out, c, p, as_stream(hip_stream)) : scan<float>(d_xbc, d_out, c, p, as_stream(hip_stream));
+    return dtype == SRM_BF16 ? scan_bf16(d_xbc, d_out, c, p, as_stream(hip_stream)) : scan_f32(d_xbc, d_out, c, p, as_stream(hip_stream));
 }
 
 // ------------------------------------------------------------------ single tokens

@@ -59,6 +59,68 @@ __device__ __forceinline__ float lanes_sum(float v)
     return v;
 }
 
+// What a work-group does over time, whatever its kernel: `work` is a sequence or a segment; clear, load(from), store(to) and
+// add(from, scale) act on the state that it holds of a head's part (whose first element lies at head_at in a slot), run(t0, t1, sum) takes
+// it over tokens of one sequence and adds their decay exponents to sum, zeros(t0, t1) writes an idle sequence's output.
+template <int MODE, typename Clear, typename Load, typename Store, typename Add, typename Run, typename Zeros>
+__device__ __forceinline__ void scan_drive(const ScanCall &c, int64_t work, int h, int p0, int64_t head_at, int lane, Clear &&clear, Load &&load,
+                                           Store &&store, Add &&add, Run &&run, Zeros &&zeros)
+{
+    const int64_t slot_size = (int64_t)c.H * c.P * c.N;
+    auto slot_of = [&](const Sequence &s) { return c.state + s.slot * slot_size + head_at; };
+    float sum = 0.0f;
+    if constexpr (MODE == SCAN_WHOLE) {
+        const Sequence s = packed_sequence(c.seqs, (int)work);
+        if (s.begin == s.end) return;
+        if (s.pos < 0) return zeros(s.begin, s.end);
+        clear();
+        if (s.slot >= 0 && s.pos > 0) load(slot_of(s));
+        run(s.begin, s.end, sum);
+        if (s.slot >= 0) store(slot_of(s));
+    } else if constexpr (MODE == SCAN_CARRY) {
+        const int t0 = c.seqs.lo + (int)work * c.seg, t1 = t0 + c.seg;
+        if (t1 >= c.seqs.hi) return;
+        const Sequence s = packed_sequence(c.seqs, packed_find(c.seqs, t1 - 1, lane));
+        if (s.end <= t1 || s.pos < 0) return;
+        const int64_t at = work * slot_size + head_at;
+        clear();
+        if (s.begin >= t0 && s.slot >= 0 && s.pos > 0) {
+            load(slot_of(s));
+            store(c.held + at);                      // (the slot may be written before the second pass comes to read it)
+        }
+        run(max(s.begin, t0), t1, sum);
+        store(c.carry + at);
+        if (threadIdx.x == 0 && p0 == 0) c.decay[work * c.H + h] = __builtin_amdgcn_exp2f(sum);
+    } else {
+        const int t0 = c.seqs.lo + (int)work * c.seg, t1 = min(t0 + c.seg, c.seqs.hi);
+        int n = packed_find(c.seqs, t0, lane);
+        for (int t = t0; t < t1;) {
+            Sequence s = packed_sequence(c.seqs, n);
+            while (t >= s.end && n + 1 < c.seqs.n) s = packed_sequence(c.seqs, ++n);
+            if (t >= s.end) break;                   // (offsets that are not the host's)
+            const int e = min(s.end, t1);
+            if (s.pos < 0) {
+                zeros(t, e);
+            } else {
+                clear();
+                if (t == s.begin) {
+                    if (s.slot >= 0 && s.pos > 0) load(s.end > t1 ? c.held + work * slot_size + head_at : slot_of(s));
+                } else {
+                    float scale = 1.0f;
+                    const int64_t first = (s.begin - c.seqs.lo) / c.seg;
+                    for (int64_t j = work - 1; j >= first; --j) {   // (a scale of 0 too: what is not finite stays so)
+                        add(c.carry + j * slot_size + head_at, scale);
+                        if (j > first) scale *= c.decay[j * c.H + h];
+                    }
+                }
+                run(t, e, sum);
+                if (e == s.end && s.slot >= 0) store(slot_of(s));
+            }
+            t = e;
+        }
+    }
+}
+
 // One wavefront takes PR rows of P a lane, NL lanes with NR elements of N each: 64 / NL * PR rows, NL NR >= N.  Sixteen tokens at a time
 // are brought to LDS; then for every token each lane updates its PR x NR elements (multiply, multiply-add) and adds their products with C.
 // What bounds it: three vector instructions for each element of state and token.
@@ -78,7 +140,7 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
     const int segments = (c.seqs.hi - c.seqs.lo + c.seg - 1) / c.seg;
     if (MODE == SCAN_WHOLE ? work >= c.seqs.n : work >= segments) return;
     const float a = c.a[h], skip = c.skip ? c.skip[h] : 0.0f;
-    const int64_t head_at = ((int64_t)h * P + p0) * N, slot_size = (int64_t)c.H * P * N;
+    const int64_t head_at = ((int64_t)h * P + p0) * N;
 
     float S[PR][NR];
     auto clear = [&]() {
@@ -160,60 +222,8 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
     };
     auto load = [&](const float *from) { each([&](float &v, int64_t at) { v = from[at]; }); };
     auto store = [&](float *to) { each([&](float &v, int64_t at) { to[at] = v; }); };
-    auto slot_of = [&](const Sequence &s) { return c.state + s.slot * slot_size + head_at; };
-
-    float sum = 0.0f;
-    if constexpr (MODE == SCAN_WHOLE) {
-        const Sequence s = packed_sequence(c.seqs, (int)work);
-        if (s.begin == s.end) return;
-        if (s.pos < 0) return zeros(s.begin, s.end);
-        clear();
-        if (s.slot >= 0 && s.pos > 0) load(slot_of(s));
-        run(s.begin, s.end, sum);
-        if (s.slot >= 0) store(slot_of(s));
-    } else if constexpr (MODE == SCAN_CARRY) {
-        const int t0 = c.seqs.lo + (int)work * c.seg, t1 = t0 + c.seg;
-        if (t1 >= c.seqs.hi) return;
-        const Sequence s = packed_sequence(c.seqs, packed_find(c.seqs, t1 - 1, lane));
-        if (s.end <= t1 || s.pos < 0) return;
-        const int64_t at = work * slot_size + head_at;
-        clear();
-        if (s.begin >= t0 && s.slot >= 0 && s.pos > 0) {
-            load(slot_of(s));
-            store(c.held + at);                      // (the slot may be written before the second pass comes to read it)
-        }
-        run(max(s.begin, t0), t1, sum);
-        store(c.carry + at);
-        if (lane == 0 && p0 == 0) c.decay[work * c.H + h] = __builtin_amdgcn_exp2f(sum);
-    } else {
-        const int t0 = c.seqs.lo + (int)work * c.seg, t1 = min(t0 + c.seg, c.seqs.hi);
-        int n = packed_find(c.seqs, t0, lane);
-        for (int t = t0; t < t1;) {
-            Sequence s = packed_sequence(c.seqs, n);
-            while (t >= s.end && n + 1 < c.seqs.n) s = packed_sequence(c.seqs, ++n);
-            if (t >= s.end) break;                   // (offsets that are not the host's)
-            const int e = min(s.end, t1);
-            if (s.pos < 0) {
-                zeros(t, e);
-            } else {
-                clear();
-                if (t == s.begin) {
-                    if (s.slot >= 0 && s.pos > 0) load(s.end > t1 ? c.held + work * slot_size + head_at : slot_of(s));
-                } else {
-                    float scale = 1.0f;
-                    const int64_t first = (s.begin - c.seqs.lo) / c.seg;
-                    for (int64_t j = work - 1; j >= first; --j) {   // (a scale of 0 too: what is not finite stays so)
-                        const float *from = c.carry + j * slot_size + head_at;
-                        each([&](float &v, int64_t at) { v = fmaf(scale, from[at], v); });
-                        if (j > first) scale *= c.decay[j * c.H + h];
-                    }
-                }
-                run(t, e, sum);
-                if (e == s.end && s.slot >= 0) store(slot_of(s));
-            }
-            t = e;
-        }
-    }
+    auto add = [&](const float *from, float scale) { each([&](float &v, int64_t at) { v = fmaf(scale, from[at], v); }); };
+    scan_drive<MODE>(c, work, h, p0, head_at, lane, clear, load, store, add, run, zeros);
 }
 
 // ------------------------------------------------------------------ single tokens
