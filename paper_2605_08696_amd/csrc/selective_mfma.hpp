@@ -22,6 +22,7 @@
 typedef __attribute__((ext_vector_type(4))) short i16x4_t;
 typedef __attribute__((ext_vector_type(8))) short i16x8_t;
 
+#define SCAN_INLINE __attribute__((always_inline))
 constexpr int kScanBlock = 64;                       // tokens of a block, rows of P of a work-group
 
 // LDS rows of CH chunks of sixteen bytes: chunk c of row r lies at c ^ f(r).  Sixteen rows' chunks c then lie on all banks, and so do the
@@ -69,7 +70,7 @@ struct ScanBlockSizes {                              // of a block's tokens: run
 };
 
 template <int NP, int MODE>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 2)
 selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out, ScanCall c)
 {
     constexpr int CH = NP / 8, NJ = NP / 32, Q = kScanBlock, BC = Q * CH / 256;      // chunks of a thread of B or C
@@ -91,20 +92,20 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
 
     f32x4_t S[2 * NJ];                               // S^T: tile 2 j + e, row 4 g4 + i is n = 32 j + 8 g4 + 4 e + i; column p = 16 wave + l16
     const int my_p = wave * 16 + l16;
-    auto clear = [&]() {
+    auto clear = [&]() SCAN_INLINE {
 #pragma unroll
         for (int j = 0; j < 2 * NJ; ++j) S[j] = f32x4_t{0, 0, 0, 0};
     };
-    auto each = [&](auto &&fn) {                     // fn(four elements, offset from the head's first, how many of them exist)
+    auto each = [&](auto &&fn) SCAN_INLINE {                     // fn(four elements, offset from the head's first, how many of them exist)
         if (my_p < np) {
-#pragma unroll
-            for (int j = 0; j < 2 * NJ; ++j) {
+            static_for<0, 2 * NJ>([&](auto j_) SCAN_INLINE {
+                constexpr int j = decltype(j_)::value;
                 const int n = 32 * (j >> 1) + 8 * g4 + 4 * (j & 1);
                 if (n < N) fn(S[j], (int64_t)my_p * N + n, min(4, N - n));
-            }
+            });
         }
     };
-    auto four = [&](const float *from, int many) {
+    auto four = [&](const float *from, int many) SCAN_INLINE {
         if (many == 4) return (f32x4_t)*reinterpret_cast<const f32x4_any *>(from);
         f32x4_t v = {0, 0, 0, 0};
 #pragma unroll
@@ -112,16 +113,16 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
             if (i < many) v[i] = from[i];
         return v;
     };
-    auto load = [&](const float *from) { each([&](f32x4_t &v, int64_t at, int many) { v = four(from + at, many); }); };
-    auto add = [&](const float *from, float scale) {
-        each([&](f32x4_t &v, int64_t at, int many) {
+    auto load = [&](const float *from) SCAN_INLINE { each([&](f32x4_t &v, int64_t at, int many) SCAN_INLINE { v = four(from + at, many); }); };
+    auto add = [&](const float *from, float scale) SCAN_INLINE {
+        each([&](f32x4_t &v, int64_t at, int many) SCAN_INLINE {
             const f32x4_t w = four(from + at, many);
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = fmaf(scale, w[i], v[i]);
         });
     };
-    auto store = [&](float *to) {
-        each([&](f32x4_t &v, int64_t at, int many) {
+    auto store = [&](float *to) SCAN_INLINE {
+        each([&](f32x4_t &v, int64_t at, int many) SCAN_INLINE {
             if (many == 4) *reinterpret_cast<f32x4_any *>(to + at) = v;
             else
 #pragma unroll
@@ -129,55 +130,62 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
                     if (i < many) to[at + i] = v[i];
         });
     };
-    auto zeros = [&](int t0, int t1) {
+    auto zeros = [&](int t0, int t1) SCAN_INLINE {
         for (int t = t0 + wave; t < t1; t += 4)
             if (lane < np) out[(int64_t)t * c.ld_out + x_at + lane] = (bf16)0.0f;
     };
 
-    // Sixteen bytes of a row from column `col` of `cols` on; chunks behind them come from its first column and are cleared when they are
-    // put to LDS.  (Rows behind the block's last are the last one again.)
-    auto fetch = [&](int64_t t, int64_t at, int col, int cols) -> bf16x8_t {
-        typedef bf16x8_t __attribute__((aligned(2))) unaligned;
-        const bf16 *row = xbc + t * c.ld + at;
-        if (whole) return *reinterpret_cast<const unaligned *>(row + (col < cols ? col : 0));
-        bf16x8_t v;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = col + i < cols ? row[col + i] : (bf16)0.0f;
-        return v;
-    };
+    // The next block's rows travel in registers: sixteen bytes at a time (rows behind the sequence's last are the last one again, chunks
+    // behind a row's part its first, and both are cleared on their way to LDS).  Where eight elements do not divide N or P, the rows come
+    // one element at a time, when they are put to LDS.
+    typedef bf16x8_t __attribute__((aligned(2))) bf16x8_any;
     bf16x8_t rb[BC], rc[Y ? BC : 1], rx[2];
-    float raw_dt = 0.0f;
-    auto fetch_block = [&](int t, int t1) {
-#pragma unroll
-        for (int i = 0; i < BC; ++i) {
+    auto fetch_block = [&](int t, int t1) SCAN_INLINE {
+        if (!whole) return;
+        static_for<0, BC>([&](auto i_) SCAN_INLINE {
+            constexpr int i = decltype(i_)::value;
             const int e = tid + 256 * i, r = e / CH, col = e % CH * 8;
-            const int64_t row = min(t + r, t1 - 1);
-            rb[i] = fetch(row, b_at, col, N);
-            if constexpr (Y) rc[i] = fetch(row, c_at, col, N);
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
+            const bf16 *row = xbc + (int64_t)min(t + r, t1 - 1) * c.ld + (col < N ? col : 0);
+            rb[i] = *reinterpret_cast<const bf16x8_any *>(row + b_at);
+            if constexpr (Y) rc[i] = *reinterpret_cast<const bf16x8_any *>(row + c_at);
+        });
+        static_for<0, 2>([&](auto i_) SCAN_INLINE {
+            constexpr int i = decltype(i_)::value;
             const int e = tid + 256 * i, r = e >> 3, col = (e & 7) * 8;
-            rx[i] = fetch(min(t + r, t1 - 1), x_at, col, np);
-        }
+            rx[i] = *reinterpret_cast<const bf16x8_any *>(xbc + (int64_t)min(t + r, t1 - 1) * c.ld + x_at + (col < np ? col : 0));
+        });
     };
-    auto put_block = [&](int t, int t1) {
+    auto put_block = [&](int t, int t1) SCAN_INLINE {
+        if (!whole) {
+            for (int e = tid; e < Q * NP; e += 256) {
+                const int r = e / NP, n = e % NP;
+                const bool there = t + r < t1 && n < N;
+                const bf16 *row = xbc + (int64_t)(t + r) * c.ld + n;
+                sb[scan_chunk<CH>(r, n >> 3) + (n & 7)] = there ? row[b_at] : (bf16)0.0f;
+                if constexpr (Y) sc[scan_chunk<CH>(r, n >> 3) + (n & 7)] = there ? row[c_at] : (bf16)0.0f;
+            }
+            for (int e = tid; e < Q * 64; e += 256) {
+                const int r = e >> 6, p = e & 63;
+                sx[scan_chunk<8>(r, p >> 3) + (p & 7)] = t + r < t1 && p < np ? xbc[(int64_t)(t + r) * c.ld + x_at + p] : (bf16)0.0f;
+            }
+            return;
+        }
         const bf16x8_t zero = {};
-#pragma unroll
-        for (int i = 0; i < BC; ++i) {
+        static_for<0, BC>([&](auto i_) SCAN_INLINE {
+            constexpr int i = decltype(i_)::value;
             const int e = tid + 256 * i, r = e / CH, ch = e % CH;
             const bool there = t + r < t1 && ch * 8 < N;
             *reinterpret_cast<bf16x8_t *>(sb + scan_chunk<CH>(r, ch)) = there ? rb[i] : zero;
             if constexpr (Y) *reinterpret_cast<bf16x8_t *>(sc + scan_chunk<CH>(r, ch)) = there ? rc[i] : zero;
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        });
+        static_for<0, 2>([&](auto i_) SCAN_INLINE {
+            constexpr int i = decltype(i_)::value;
             const int e = tid + 256 * i, r = e >> 3, ch = e & 7;
             *reinterpret_cast<bf16x8_t *>(sx + scan_chunk<8>(r, ch)) = t + r < t1 && ch * 8 < np ? rx[i] : zero;
-        }
+        });
     };
     // A block's sizes, by one wavefront, a token in each lane.
-    auto put_sizes = [&](ScanBlockSizes &to, int t, int t1) {
+    auto put_sizes = [&](ScanBlockSizes &to, int t, int t1) SCAN_INLINE {
         const bool there = t + lane < t1;
         float dt = dt_of(c.dt, min(t + lane, t1 - 1), h);
         dt = there ? dt : 0.0f;
@@ -196,7 +204,7 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
     };
 
     // Tokens [t0, t1) of one sequence.
-    auto run = [&](int t0, int t1, float &sum) {
+    auto run = [&](int t0, int t1, float &sum) SCAN_INLINE {
         fetch_block(t0, t1);
         __syncthreads();                             // (nobody reads what an earlier call has left)
         if (wave == 0) put_sizes(sizes[0], t0, t1);
