@@ -30,14 +30,16 @@ struct ScanCall {
 };
 enum { SCAN_WHOLE = 0, SCAN_CARRY = 1, SCAN_SEGMENTS = 2 };
 
-__device__ __forceinline__ float dt_of(const StepSizes &c, int64_t t, int h)
+__device__ __forceinline__ float dt_raw(const StepSizes &c, int64_t t, int h)
 {
     const int64_t at = t * c.ld + h;
-    float v = c.is_bf16 ? (float)static_cast<const bf16 *>(c.raw)[at] : static_cast<const float *>(c.raw)[at];
-    if (c.bias) v += c.bias[h];
+    return c.is_bf16 ? (float)static_cast<const bf16 *>(c.raw)[at] : static_cast<const float *>(c.raw)[at];
+}
+__device__ __forceinline__ float dt_of(const StepSizes &c, float raw, float bias)
+{
+    const float v = raw + bias;
     // (log(1 + e^v) without loss on either side; a NaN stays one)
-    if (c.softplus) v = (v > 0.0f ? v : v == v ? 0.0f : v) + log1pf(__expf(-fabsf(v)));
-    return v;
+    return c.softplus ? (v > 0.0f ? v : v == v ? 0.0f : v) + log1pf(__expf(-fabsf(v))) : v;
 }
 // The decay's exponent in steps of a factor of two.  Below 2^-200 a decay leaves nothing of a state of fp32; the limit keeps sums of
 // exponents small enough that their differences are exact where the decays are not 0.  (A comparison, so that a NaN stays one.)
@@ -139,7 +141,7 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
     const int P = c.P, N = c.N, np = min(PW, P - p0);
     const int segments = (c.seqs.hi - c.seqs.lo + c.seg - 1) / c.seg;
     if (MODE == SCAN_WHOLE ? work >= c.seqs.n : work >= segments) return;
-    const float a = c.a[h], skip = c.skip ? c.skip[h] : 0.0f;
+    const float a = c.a[h], skip = c.skip ? c.skip[h] : 0.0f, bias = c.dt.bias ? c.dt.bias[h] : 0.0f;
     const int64_t head_at = ((int64_t)h * P + p0) * N;
 
     float S[PR][NR];
@@ -172,7 +174,7 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
                 sx[r][p] = p < np ? (float)xbc[(int64_t)(t + r) * c.ld + (int64_t)h * P + p0 + p] : 0.0f;
             }
             if (lane < nt) {
-                const float dt = dt_of(c.dt, t + lane, h), ex = decay_exponent(dt, a);
+                const float dt = dt_of(c.dt, dt_raw(c.dt, t + lane, h), bias), ex = decay_exponent(dt, a);
                 sd[lane] = make_float2(__builtin_amdgcn_exp2f(ex), dt);
                 if (MODE == SCAN_CARRY) sb[lane][NP] = ex;
             }
@@ -282,7 +284,7 @@ selective_step_kernel(const T *__restrict__ xbc, T *__restrict__ out, StepCall c
                     if (ln * 4 + i < N) v[u][i] = from[i];
         }
     }
-    const float dt = dt_of(c.dt, r, h);
+    const float dt = dt_of(c.dt, dt_raw(c.dt, r, h), c.dt.bias ? c.dt.bias[h] : 0.0f);
     const float decay = __builtin_amdgcn_exp2f(decay_exponent(dt, c.a[h])), skip = c.skip ? c.skip[h] : 0.0f;
     const bool first = h % (c.H / c.G) == 0 && p0 == 0;
     const T *x = xbc + r * c.ld;

@@ -85,7 +85,7 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
     const int P = c.P, N = c.N, np = min(64, P - p0);
     const int segments = (c.seqs.hi - c.seqs.lo + c.seg - 1) / c.seg;
     if (MODE == SCAN_WHOLE ? work >= c.seqs.n : work >= segments) return;
-    const float a = c.a[h], skip = c.skip ? c.skip[h] : 0.0f;
+    const float a = c.a[h], skip = c.skip ? c.skip[h] : 0.0f, bias = c.dt.bias ? c.dt.bias[h] : 0.0f;
     const int64_t head_at = ((int64_t)h * P + p0) * N;
     const bool whole = N % 8 == 0 && P % 8 == 0;     // chunks of eight are all there or not at all
     const int64_t x_at = (int64_t)h * P + p0, b_at = (int64_t)c.H * P + (int64_t)g * N, c_at = b_at + (int64_t)c.G * N;
@@ -139,6 +139,7 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
     // behind a row's part its first, and both are cleared on their way to LDS).  Where eight elements do not divide N or P, the rows come
     // one element at a time, when they are put to LDS.
     typedef bf16x8_t __attribute__((aligned(2))) bf16x8_any;
+    typedef bf16x4_t __attribute__((aligned(2))) bf16x4_any;
     bf16x8_t rb[BC], rc[Y ? BC : 1], rx[2];
     auto fetch_block = [&](int t, int t1) SCAN_INLINE {
         if (!whole) return;
@@ -185,9 +186,8 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
         });
     };
     // A block's sizes, by one wavefront, a token in each lane.
-    auto put_sizes = [&](ScanBlockSizes &to, int t, int t1) SCAN_INLINE {
-        const bool there = t + lane < t1;
-        float dt = dt_of(c.dt, min(t + lane, t1 - 1), h);
+    auto put_sizes = [&](ScanBlockSizes &to, float raw, bool there) SCAN_INLINE {
+        float dt = dt_of(c.dt, raw, bias);
         dt = there ? dt : 0.0f;
         const double upto = wave_scan(there ? (double)decay_exponent(dt, a) : 0.0);
         const unsigned long long u = __builtin_bit_cast(unsigned long long, upto);
@@ -207,7 +207,7 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
     auto run = [&](int t0, int t1, float &sum) SCAN_INLINE {
         fetch_block(t0, t1);
         __syncthreads();                             // (nobody reads what an earlier call has left)
-        if (wave == 0) put_sizes(sizes[0], t0, t1);
+        if (wave == 0) put_sizes(sizes[0], dt_raw(c.dt, min(t0 + lane, t1 - 1), h), t0 + lane < t1);
         put_block(t0, t1);
         if constexpr (Y) {                           // the tiles above the diagonal that a step of k = 32 takes along
             for (int e = tid; e < 2 * 16 * 2; e += 256) {
@@ -219,7 +219,18 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
         int now = 0;
         for (int t = t0; t < t1; t += Q, now ^= 1) {
             const ScanBlockSizes &z = sizes[now];
-            const bool more = t + Q < t1;
+            const bool more = t + Q < t1, sizer = more && wave == (now ? 1 : 3);
+            bf16x4_t gate[Y ? 4 : 1];                // z, as the lane's four tiles of y^T lie
+            if constexpr (Y)
+                if (c.z && whole)
+                    static_for<0, 4>([&](auto i_) SCAN_INLINE {
+                        constexpr int i = decltype(i_)::value;
+                        const int p = wave * 16 + 4 * g4;
+                        gate[i] = *reinterpret_cast<const bf16x4_any *>(static_cast<const bf16 *>(c.z) + (int64_t)min(t + 16 * i + l16, t1 - 1) * c.ld_z + x_at +
+                                                                        (p < np ? p : 0));
+                    });
+            float raw = 0.0f;
+            if (sizer) raw = dt_raw(c.dt, min(t + Q + lane, t1 - 1), h);
             if (more) fetch_block(t + Q, t1);
             sum += z.total;
             f32x4_t acc[4];
@@ -346,7 +357,7 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
                     for (int q = 0; q < 3; ++q) S[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bt, xw[q], S[j], 0, 0, 0);
                 }
             }
-            if (more && wave == (now ? 1 : 3)) put_sizes(sizes[now ^ 1], t + Q, t1);
+            if (sizer) put_sizes(sizes[now ^ 1], raw, t + Q + lane < t1);
             if constexpr (Y) {
                 const int p = wave * 16 + 4 * g4;
 #pragma unroll
@@ -354,28 +365,23 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
                     const int r = tt * 16 + l16;
                     const bf16x4_t x = *reinterpret_cast<const bf16x4_t *>(sx + scan_chunk<8>(r, p >> 3) + (p & 4));
                     if (t + r < t1 && p < np) {
-                        const bf16 *zg = c.z ? static_cast<const bf16 *>(c.z) + (int64_t)(t + r) * c.ld_z + x_at + p : nullptr;
                         bf16 *o = out + (int64_t)(t + r) * c.ld_out + x_at + p;
-                        typedef bf16x4_t __attribute__((aligned(2))) unaligned;
-                        bf16x4_t gate = {}, q;
-                        const bool all = p + 4 <= np;
-                        if (zg) {
-                            if (all) gate = *reinterpret_cast<const unaligned *>(zg);
-                            else
+                        if (c.z && !whole) {
+                            const bf16 *zg = static_cast<const bf16 *>(c.z) + (int64_t)(t + r) * c.ld_z + x_at + p;
 #pragma unroll
-                                for (int i = 0; i < 3; ++i)
-                                    if (p + i < np) gate[i] = zg[i];
+                            for (int i = 0; i < 4; ++i) gate[tt][i] = p + i < np ? zg[i] : (bf16)0.0f;
                         }
+                        bf16x4_t q;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             float y = fmaf(skip, (float)x[i], acc[tt][i]);
-                            if (zg) y *= silu((float)gate[i]);
+                            if (c.z) y *= silu((float)gate[tt][i]);
                             q[i] = (bf16)y;
                         }
-                        if (all) *reinterpret_cast<unaligned *>(o) = q;
+                        if (whole) *reinterpret_cast<bf16x4_any *>(o) = q;
                         else
 #pragma unroll
-                            for (int i = 0; i < 3; ++i)
+                            for (int i = 0; i < 4; ++i)
                                 if (p + i < np) o[i] = q[i];
                     }
                 }
