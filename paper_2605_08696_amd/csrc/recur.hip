@@ -187,11 +187,12 @@ static int scan_f32(const void *d_xbc, void *d_out, const ScanCall &c, const Sca
     SCAN_CASE(16, 16);
 #undef SCAN_CASE
 }
+template <bool W>
 static int scan_bf16(const void *d_xbc, void *d_out, const ScanCall &c, const ScanPlan &p, hipStream_t st)
 {
 #define SCAN_CASE(NP)                                                                                                                         \
-    return launch_scan<bf16, selective_scan_mfma_kernel<NP, SCAN_WHOLE>, selective_scan_mfma_kernel<NP, SCAN_CARRY>,                        \
-                       selective_scan_mfma_kernel<NP, SCAN_SEGMENTS>>(d_xbc, d_out, c, p, 256, st)
+    return launch_scan<bf16, selective_scan_mfma_kernel<NP, SCAN_WHOLE, W>, selective_scan_mfma_kernel<NP, SCAN_CARRY, W>,                  \
+                       selective_scan_mfma_kernel<NP, SCAN_SEGMENTS, W>>(d_xbc, d_out, c, p, 256, st)
     if (c.N <= 32) SCAN_CASE(32);
     if (c.N <= 64) SCAN_CASE(64);
     if (c.N <= 128) SCAN_CASE(128);
@@ -235,6 +236,9 @@ extern "C" int srm_selective_scan(int32_t dtype, const void *d_xbc, int64_t ld_x
     c.P = head_dim;
     c.G = groups;
     c.N = state_dim;
+    // (offsets inside a block of rows are 32 bits)
+    auto words = [](const void *q, int64_t ld) { return !q || (!misaligned(q, 4) && ld % 2 == 0 && ld < (1 << 23)); };
+    const bool whole = state_dim % 8 == 0 && head_dim % 8 == 0 && words(d_xbc, ld_xbc) && words(d_z, ld_z) && words(d_out, ld_out);
     c.state = d_state;
     c.seg = p.segments ? p.seg : 1;
     c.parts = p.parts;
@@ -244,7 +248,8 @@ extern "C" int srm_selective_scan(int32_t dtype, const void *d_xbc, int64_t ld_x
         c.held = c.carry + all;
         c.decay = c.held + all;
     }
-    return dtype == SRM_BF16 ? scan_bf16(d_xbc, d_out, c, p, as_stream(hip_stream)) : scan_f32(d_xbc, d_out, c, p, as_stream(hip_stream));
+    if (dtype == SRM_BF16 && whole) return scan_bf16<true>(d_xbc, d_out, c, p, as_stream(hip_stream));
+    return dtype == SRM_BF16 ? scan_bf16<false>(d_xbc, d_out, c, p, as_stream(hip_stream)) : scan_f32(d_xbc, d_out, c, p, as_stream(hip_stream));
 }
 
 // ------------------------------------------------------------------ single tokens

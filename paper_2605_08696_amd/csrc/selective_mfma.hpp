@@ -69,7 +69,8 @@ struct ScanBlockSizes {                              // of a block's tokens: run
     float total, factor;                             // the block's exponent and 2^it
 };
 
-template <int NP, int MODE>
+// WHOLE: rows in whole chunks of eight elements, all at multiples of four bytes, row strides of less than 2^23.
+template <int NP, int MODE, bool WHOLE>
 __global__ void __launch_bounds__(256, 2)
 selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out, ScanCall c)
 {
@@ -87,7 +88,6 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
     if (MODE == SCAN_WHOLE ? work >= c.seqs.n : work >= segments) return;
     const float a = c.a[h], skip = c.skip ? c.skip[h] : 0.0f, bias = c.dt.bias ? c.dt.bias[h] : 0.0f;
     const int64_t head_at = ((int64_t)h * P + p0) * N;
-    const bool whole = N % 8 == 0 && P % 8 == 0;     // chunks of eight are all there or not at all
     const int64_t x_at = (int64_t)h * P + p0, b_at = (int64_t)c.H * P + (int64_t)g * N, c_at = b_at + (int64_t)c.G * N;
 
     f32x4_t S[2 * NJ];                               // S^T: tile 2 j + e, row 4 g4 + i is n = 32 j + 8 g4 + 4 e + i; column p = 16 wave + l16
@@ -135,29 +135,36 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
             if (lane < np) out[(int64_t)t * c.ld_out + x_at + lane] = (bf16)0.0f;
     };
 
-    // The next block's rows travel in registers: sixteen bytes at a time (rows behind the sequence's last are the last one again, chunks
-    // behind a row's part its first, and both are cleared on their way to LDS).  Where eight elements do not divide N or P, the rows come
-    // one element at a time, when they are put to LDS.
-    typedef bf16x8_t __attribute__((aligned(2))) bf16x8_any;
-    typedef bf16x4_t __attribute__((aligned(2))) bf16x4_any;
+    // The next block's rows travel in registers, sixteen bytes at a time, by loads that bring zeros from behind the sequence's last row and
+    // for chunks behind a row's part.  Where the operands do not lie in whole chunks and words, the rows come one element at a time, when
+    // they are put to LDS.
     bf16x8_t rb[BC], rc[Y ? BC : 1], rx[2];
+    constexpr uint32_t kNone = 0x80000000u;          // behind every row
+    const uint32_t row_bytes = (uint32_t)c.ld * 2;
+    const int b_ch = (tid % CH), x_ch = tid & 7;
+    const uint32_t b_off = b_ch * 8 < N ? (uint32_t)(tid / CH) * row_bytes + (uint32_t)b_at * 2 + b_ch * 16 : kNone;
+    const uint32_t x_off = x_ch * 8 < np ? (uint32_t)(tid >> 3) * row_bytes + (uint32_t)x_at * 2 + x_ch * 16 : kNone;
+    const uint32_t y_col = wave * 16 + 4 * g4 < np ? (wave * 16 + 4 * g4) * 2 : kNone;
+    auto rows_of = [&](const void *base, int64_t ld, int64_t at, int rows, int row) SCAN_INLINE {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16 *>(static_cast<const bf16 *>(base) + at), 0,
+                                                 (uint32_t)(rows - 1) * (uint32_t)ld * 2 + (uint32_t)row * 2, 0x27000);
+    };
     auto fetch_block = [&](int t, int t1) SCAN_INLINE {
-        if (!whole) return;
+        if constexpr (!WHOLE) return;
+        const auto rs = rows_of(xbc, c.ld, (int64_t)t * c.ld, min(Q, t1 - t), c.H * P + 2 * c.G * N);
         static_for<0, BC>([&](auto i_) SCAN_INLINE {
             constexpr int i = decltype(i_)::value;
-            const int e = tid + 256 * i, r = e / CH, col = e % CH * 8;
-            const bf16 *row = xbc + (int64_t)min(t + r, t1 - 1) * c.ld + (col < N ? col : 0);
-            rb[i] = *reinterpret_cast<const bf16x8_any *>(row + b_at);
-            if constexpr (Y) rc[i] = *reinterpret_cast<const bf16x8_any *>(row + c_at);
+            const uint32_t off = b_off + i * (256 / CH) * row_bytes;
+            rb[i] = __builtin_bit_cast(bf16x8_t, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, 0, 0));
+            if constexpr (Y) rc[i] = __builtin_bit_cast(bf16x8_t, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, c.G * N * 2, 0));
         });
         static_for<0, 2>([&](auto i_) SCAN_INLINE {
             constexpr int i = decltype(i_)::value;
-            const int e = tid + 256 * i, r = e >> 3, col = (e & 7) * 8;
-            rx[i] = *reinterpret_cast<const bf16x8_any *>(xbc + (int64_t)min(t + r, t1 - 1) * c.ld + x_at + (col < np ? col : 0));
+            rx[i] = __builtin_bit_cast(bf16x8_t, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(x_off + i * 32 * row_bytes), 0, 0));
         });
     };
     auto put_block = [&](int t, int t1) SCAN_INLINE {
-        if (!whole) {
+        if constexpr (!WHOLE) {
             for (int e = tid; e < Q * NP; e += 256) {
                 const int r = e / NP, n = e % NP;
                 const bool there = t + r < t1 && n < N;
@@ -171,18 +178,15 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
             }
             return;
         }
-        const bf16x8_t zero = {};
         static_for<0, BC>([&](auto i_) SCAN_INLINE {
             constexpr int i = decltype(i_)::value;
-            const int e = tid + 256 * i, r = e / CH, ch = e % CH;
-            const bool there = t + r < t1 && ch * 8 < N;
-            *reinterpret_cast<bf16x8_t *>(sb + scan_chunk<CH>(r, ch)) = there ? rb[i] : zero;
-            if constexpr (Y) *reinterpret_cast<bf16x8_t *>(sc + scan_chunk<CH>(r, ch)) = there ? rc[i] : zero;
+            const int at = scan_chunk<CH>(tid / CH + i * (256 / CH), b_ch);
+            *reinterpret_cast<bf16x8_t *>(sb + at) = rb[i];
+            if constexpr (Y) *reinterpret_cast<bf16x8_t *>(sc + at) = rc[i];
         });
         static_for<0, 2>([&](auto i_) SCAN_INLINE {
             constexpr int i = decltype(i_)::value;
-            const int e = tid + 256 * i, r = e >> 3, ch = e & 7;
-            *reinterpret_cast<bf16x8_t *>(sx + scan_chunk<8>(r, ch)) = t + r < t1 && ch * 8 < np ? rx[i] : zero;
+            *reinterpret_cast<bf16x8_t *>(sx + scan_chunk<8>((tid >> 3) + 32 * i, x_ch)) = rx[i];
         });
     };
     // A block's sizes, by one wavefront, a token in each lane.
@@ -222,23 +226,26 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
             const bool more = t + Q < t1, sizer = more && wave == (now ? 1 : 3);
             bf16x4_t gate[Y ? 4 : 1];                // z, as the lane's four tiles of y^T lie
             if constexpr (Y)
-                if (c.z && whole)
+                if (WHOLE && c.z) {
+                    const auto rs = rows_of(c.z, c.ld_z, (int64_t)t * c.ld_z + x_at, min(Q, t1 - t), np);
                     static_for<0, 4>([&](auto i_) SCAN_INLINE {
                         constexpr int i = decltype(i_)::value;
-                        const int p = wave * 16 + 4 * g4;
-                        gate[i] = *reinterpret_cast<const bf16x4_any *>(static_cast<const bf16 *>(c.z) + (int64_t)min(t + 16 * i + l16, t1 - 1) * c.ld_z + x_at +
-                                                                        (p < np ? p : 0));
+                        gate[i] = __builtin_bit_cast(bf16x4_t, __builtin_amdgcn_raw_buffer_load_b64(rs, (int)(y_col + (16 * i + l16) * (uint32_t)c.ld_z * 2), 0, 0));
                     });
+                }
             float raw = 0.0f;
             if (sizer) raw = dt_raw(c.dt, min(t + Q + lane, t1 - 1), h);
             if (more) fetch_block(t + Q, t1);
             sum += z.total;
             f32x4_t acc[4];
             if constexpr (Y) {
-                // M, its tiles (token tile tt, earlier tokens ss) in turn
+                // M, its tiles (token tile tt, earlier tokens ss) in turn.  (The compiler must not know that their addresses are the same in
+                // every block: it would keep some forty of them in registers.)
+                int first = wave;
+                asm volatile("" : "+s"(first));
 #pragma unroll
                 for (int k = 0; k < 3; ++k) {
-                    const int tile = wave + 4 * k;
+                    const int tile = first + 4 * k;
                     if (tile >= 10) break;
                     const int tt = tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3, ss = tile - tt * (tt + 1) / 2;
                     f32x4_t m = {0, 0, 0, 0};
@@ -309,11 +316,13 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
                     for (int k = 0; k <= tt >> 1; ++k)
                         acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xg[k], scan_row8<8>(sm, tt * 16 + l16, 4 * k + g4), acc[tt], 0, 0, 0);
                 if (any) {
+                    int column = l16;
+                    asm volatile("" : "+v"(column)); // (nor of these)
                     for (int s = 0; s < Q; ++s) {
                         const bf16x4_t v = *reinterpret_cast<const bf16x4_t *>(sx + scan_chunk<8>(s, 2 * wave + (g4 >> 1)) + (g4 & 1) * 4);
 #pragma unroll
                         for (int tt = 0; tt < 4; ++tt) {
-                            const int row = tt * 16 + l16;
+                            const int row = tt * 16 + column;
                             if (row < s) continue;
                             const float m = (float)sm[scan_chunk<8>(row, s >> 3) + (s & 7)];
 #pragma unroll
@@ -360,31 +369,33 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
             if (sizer) put_sizes(sizes[now ^ 1], raw, t + Q + lane < t1);
             if constexpr (Y) {
                 const int p = wave * 16 + 4 * g4;
-#pragma unroll
-                for (int tt = 0; tt < 4; ++tt) {
+                const auto rs = rows_of(out, c.ld_out, (int64_t)t * c.ld_out + x_at, min(Q, t1 - t), np);
+                static_for<0, 4>([&](auto tt_) SCAN_INLINE {
+                    constexpr int tt = decltype(tt_)::value;
                     const int r = tt * 16 + l16;
                     const bf16x4_t x = *reinterpret_cast<const bf16x4_t *>(sx + scan_chunk<8>(r, p >> 3) + (p & 4));
-                    if (t + r < t1 && p < np) {
-                        bf16 *o = out + (int64_t)(t + r) * c.ld_out + x_at + p;
-                        if (c.z && !whole) {
-                            const bf16 *zg = static_cast<const bf16 *>(c.z) + (int64_t)(t + r) * c.ld_z + x_at + p;
+                    float y[4];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) gate[tt][i] = p + i < np ? zg[i] : (bf16)0.0f;
-                        }
+                    for (int i = 0; i < 4; ++i) y[i] = fmaf(skip, (float)x[i], acc[tt][i]);
+                    if constexpr (WHOLE) {
                         bf16x4_t q;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            float y = fmaf(skip, (float)x[i], acc[tt][i]);
-                            if (c.z) y *= silu((float)gate[tt][i]);
-                            q[i] = (bf16)y;
+                            if (c.z) y[i] *= silu((float)gate[tt][i]);
+                            q[i] = (bf16)y[i];
                         }
-                        if (whole) *reinterpret_cast<bf16x4_any *>(o) = q;
-                        else
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                if (p + i < np) o[i] = q[i];
+                        typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+                        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2_t, q), rs, (int)(y_col + r * (uint32_t)c.ld_out * 2), 0, 0);
+                    } else if (t + r < t1) {
+                        for (int i = 0; i < 4; ++i)
+                            if (p + i < np) {
+                                const float v = i == 0 ? y[0] : i == 1 ? y[1] : i == 2 ? y[2] : y[3];
+                                const int64_t col = x_at + p + i;
+                                const float u = c.z ? v * silu((float)static_cast<const bf16 *>(c.z)[(int64_t)(t + r) * c.ld_z + col]) : v;
+                                out[(int64_t)(t + r) * c.ld_out + col] = (bf16)u;
+                            }
                     }
-                }
+                });
             }
             __syncthreads();
             if (more) {
