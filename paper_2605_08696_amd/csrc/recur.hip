@@ -133,13 +133,13 @@ struct ScanPlan {
 };
 static int scan_rows(int32_t dtype, int32_t N)
 {
-    if (dtype == SRM_BF16) return kScanBlock;
+    if (dtype == SRM_BF16) return kScanRows;
     return N <= 8 ? 256 : N <= 16 ? 128 : N <= 32 ? 64 : N <= 64 ? 32 : 16;
 }
 static ScanPlan scan_plan(int32_t dtype, const HeadSizes &s, int64_t tokens, int32_t longest)
 {
     ScanPlan p{(int)cdiv(s.P, scan_rows(dtype, s.N)), 0, 0};
-    const int64_t chip = dtype == SRM_BF16 ? 512 : 2048, units = (int64_t)s.H * p.parts, least = 64;
+    const int64_t chip = dtype == SRM_BF16 ? 768 : 2048, units = (int64_t)s.H * p.parts, least = 64;
     const int64_t seg = std::max(least, cdiv(cdiv(tokens * units, chip), 64) * 64);
     if (longest > 2 * seg + 2 * least) {
         p.seg = (int)seg;
@@ -237,8 +237,8 @@ extern "C" int srm_selective_scan(int32_t dtype, const void *d_xbc, int64_t ld_x
     c.G = groups;
     c.N = state_dim;
     // (offsets inside a block of rows are 32 bits)
-    auto words = [](const void *q, int64_t ld) { return !q || (!misaligned(q, 4) && ld % 2 == 0 && ld < (1 << 23)); };
-    const bool whole = state_dim % 8 == 0 && head_dim % 8 == 0 && words(d_xbc, ld_xbc) && words(d_z, ld_z) && words(d_out, ld_out);
+    auto chunks = [](const void *q, int64_t ld) { return !q || (!misaligned(q, 16) && ld % 8 == 0 && ld < (1 << 23)); };
+    const bool whole = state_dim % 8 == 0 && head_dim % 8 == 0 && chunks(d_xbc, ld_xbc) && chunks(d_z, ld_z) && chunks(d_out, ld_out);
     c.state = d_state;
     c.seg = p.segments ? p.seg : 1;
     c.parts = p.parts;

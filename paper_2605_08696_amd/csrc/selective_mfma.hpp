@@ -1,9 +1,9 @@
-// The selective recurrence of bf16 operands on the matrix cores, sixty-four tokens of one head at a time.
+// The selective recurrence of bf16 operands on the matrix cores, thirty-two tokens of one head at a time.
 //
 // With e_t the decay exponents' running sum from the block's first token to token t, S the state in front of it:
 //   y_t = 2^e_t S C_t + sum_{s <= t} M_ts x_s      M_ts = (C_t . B_s) 2^(e_t - e_s) dt_s
-//   S' = 2^e_63 S + sum_s (2^(e_63 - e_s) dt_s x_s) B_s^T
-// that is four products with 64 tokens as one side.  The running sum is formed in 64 bits, so that the exponents of S', which are small where
+//   S' = 2^e_31 S + sum_s (2^(e_31 - e_s) dt_s x_s) B_s^T
+// that is four products with 32 tokens as one side.  The running sum is formed in 64 bits, so that the exponents of S', which are small where
 // the weights are not, and of M lose nothing to what came before them.
 //
 // Roundings.  The state stays in fp32 in the accumulators of its own product.  What is rounded to bf16 is, for y alone, M and the copy of S
@@ -23,7 +23,7 @@ typedef __attribute__((ext_vector_type(4))) short i16x4_t;
 typedef __attribute__((ext_vector_type(8))) short i16x8_t;
 
 #define SCAN_INLINE __attribute__((always_inline))
-constexpr int kScanBlock = 64;                       // tokens of a block, rows of P of a work-group
+constexpr int kScanBlock = 32, kScanRows = 64;       // tokens of a block, rows of P of a work-group
 
 // LDS rows of CH chunks of sixteen bytes: chunk c of row r lies at c ^ f(r).  Sixteen rows' chunks c then lie on all banks, and so do the
 // sixteen chunks or halves of chunks that a transposing read takes from four rows.
@@ -69,14 +69,43 @@ struct ScanBlockSizes {                              // of a block's tokens: run
     float total, factor;                             // the block's exponent and 2^it
 };
 
-// WHOLE: rows in whole chunks of eight elements, all at multiples of four bytes, row strides of less than 2^23.
+// Loads from memory to LDS are issued from asm statements: for one that it knows the compiler would wait in front of the next LDS read that
+// it cannot prove disjoint.  16 bytes of every lane to 1024 bytes at LDS address `dst`, in the lanes' order; zeros from behind the operand.
+__device__ __forceinline__ u32x4_t scan_rows_at(const void *base, uint32_t bytes)
+{
+    u32x4_t rs;
+    const unsigned long long a = reinterpret_cast<unsigned long long>(base);
+    rs[0] = __builtin_amdgcn_readfirstlane((unsigned)a);
+    rs[1] = __builtin_amdgcn_readfirstlane((unsigned)(a >> 32));                 // stride 0: raw buffer
+    rs[2] = __builtin_amdgcn_readfirstlane(bytes);
+    rs[3] = 0x00020000u;
+    return rs;
+}
+__device__ __forceinline__ void scan_dma16(unsigned dst, const u32x4_t &rs, uint32_t voff, int soff)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(dst), "v"(voff), "s"(rs), "s"(soff) : "memory");
+}
+__device__ __forceinline__ unsigned scan_lds_address(const void *p)
+{
+    typedef __attribute__((address_space(3))) const unsigned char lds_byte;
+    return __builtin_amdgcn_readfirstlane((unsigned)reinterpret_cast<unsigned long long>((lds_byte *)p));
+}
+// all but this wavefront's youngest N requests to memory have come back, its LDS writes are done, and so are the other wavefronts'
+template <int N>
+__device__ __forceinline__ void scan_barrier() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "i"(N) : "memory"); }
+__device__ __forceinline__ void scan_barrier_lds() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
+
+// WHOLE: rows in whole chunks of eight elements, all at multiples of sixteen bytes, row strides of less than 2^23.
+//
+// A block's rows come to one of two LDS buffers while the block in front of it is worked on in the other, straight from memory (WHOLE; else
+// one element at a time).  Two barriers a block: its rows are there; M is there.
 template <int NP, int MODE, bool WHOLE>
-__global__ void __launch_bounds__(256, 2)
+__global__ void __launch_bounds__(256, NP <= 128 ? 3 : 2)
 selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out, ScanCall c)
 {
-    constexpr int CH = NP / 8, NJ = NP / 32, Q = kScanBlock, BC = Q * CH / 256;      // chunks of a thread of B or C
+    constexpr int CH = NP / 8, NJ = NP / 32, Q = kScanBlock, SLOTS = Q * CH / 64;    // loads of 64 chunks that B or C of a block takes
     constexpr bool Y = MODE != SCAN_CARRY;
-    __shared__ __align__(16) bf16 sb[Q * NP], sc[Y ? Q * NP : 8], sx[Q * 64], sm[Y ? Q * Q : 8];
+    __shared__ __align__(16) bf16 sb[2][Q * NP], sc[Y ? 2 : 1][Y ? Q * NP : 8], sx[2][Q * 64], sm[Y ? Q * Q : 8];
     __shared__ __align__(16) ScanBlockSizes sizes[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
     const int64_t id = work_group();
@@ -90,23 +119,19 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
     const int64_t head_at = ((int64_t)h * P + p0) * N;
     const int64_t x_at = (int64_t)h * P + p0, b_at = (int64_t)c.H * P + (int64_t)g * N, c_at = b_at + (int64_t)c.G * N;
 
-    f32x4_t S[2 * NJ];                               // S^T: tile 2 j + e, row 4 g4 + i is n = 32 j + 8 g4 + 4 e + i; column p = 16 wave + l16
+    f32x4_t S[2 * NJ];                               // S^T: tile j, row 4 g4 + i is n = 16 j + 4 g4 + i; column p = 16 wave + l16
     const int my_p = wave * 16 + l16;
-    auto clear = [&]() SCAN_INLINE {
-#pragma unroll
-        for (int j = 0; j < 2 * NJ; ++j) S[j] = f32x4_t{0, 0, 0, 0};
-    };
-    auto each = [&](auto &&fn) SCAN_INLINE {                     // fn(four elements, offset from the head's first, how many of them exist)
-        if (my_p < np) {
+    auto clear = [&]() SCAN_INLINE { static_for<0, 2 * NJ>([&](auto j_) SCAN_INLINE { S[decltype(j_)::value] = f32x4_t{0, 0, 0, 0}; }); };
+    auto each = [&](auto &&fn) SCAN_INLINE {         // fn(four elements, offset from the head's first, how many of them exist)
+        if (my_p < np)
             static_for<0, 2 * NJ>([&](auto j_) SCAN_INLINE {
                 constexpr int j = decltype(j_)::value;
-                const int n = 32 * (j >> 1) + 8 * g4 + 4 * (j & 1);
+                const int n = 16 * j + 4 * g4;
                 if (n < N) fn(S[j], (int64_t)my_p * N + n, min(4, N - n));
             });
-        }
     };
     auto four = [&](const float *from, int many) SCAN_INLINE {
-        if (many == 4) return (f32x4_t)*reinterpret_cast<const f32x4_any *>(from);
+        if (WHOLE || many == 4) return (f32x4_t)*reinterpret_cast<const f32x4_any *>(from);
         f32x4_t v = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < 3; ++i)
@@ -123,7 +148,7 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
     };
     auto store = [&](float *to) SCAN_INLINE {
         each([&](f32x4_t &v, int64_t at, int many) SCAN_INLINE {
-            if (many == 4) *reinterpret_cast<f32x4_any *>(to + at) = v;
+            if (WHOLE || many == 4) *reinterpret_cast<f32x4_any *>(to + at) = v;
             else
 #pragma unroll
                 for (int i = 0; i < 3; ++i)
@@ -135,61 +160,71 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
             if (lane < np) out[(int64_t)t * c.ld_out + x_at + lane] = (bf16)0.0f;
     };
 
-    // The next block's rows travel in registers, sixteen bytes at a time, by loads that bring zeros from behind the sequence's last row and
-    // for chunks behind a row's part.  Where the operands do not lie in whole chunks and words, the rows come one element at a time, when
-    // they are put to LDS.
-    bf16x8_t rb[BC], rc[Y ? BC : 1], rx[2];
-    constexpr uint32_t kNone = 0x80000000u;          // behind every row
+    // This lane's chunk of each load: LDS slot s holds chunk (s % CH) ^ f(r) of row r = s / CH.
+    constexpr uint32_t kNone = 0x80000000u;          // behind every operand
     const uint32_t row_bytes = (uint32_t)c.ld * 2;
-    const int b_ch = (tid % CH), x_ch = tid & 7;
-    const uint32_t b_off = b_ch * 8 < N ? (uint32_t)(tid / CH) * row_bytes + (uint32_t)b_at * 2 + b_ch * 16 : kNone;
-    const uint32_t x_off = x_ch * 8 < np ? (uint32_t)(tid >> 3) * row_bytes + (uint32_t)x_at * 2 + x_ch * 16 : kNone;
-    const uint32_t y_col = wave * 16 + 4 * g4 < np ? (wave * 16 + 4 * g4) * 2 : kNone;
-    auto rows_of = [&](const void *base, int64_t ld, int64_t at, int rows, int row) SCAN_INLINE {
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16 *>(static_cast<const bf16 *>(base) + at), 0,
-                                                 (uint32_t)(rows - 1) * (uint32_t)ld * 2 + (uint32_t)row * 2, 0x27000);
-    };
-    auto fetch_block = [&](int t, int t1) SCAN_INLINE {
-        if constexpr (!WHOLE) return;
-        const auto rs = rows_of(xbc, c.ld, (int64_t)t * c.ld, min(Q, t1 - t), c.H * P + 2 * c.G * N);
-        static_for<0, BC>([&](auto i_) SCAN_INLINE {
+    constexpr int LOADS = SLOTS >= 4 ? SLOTS / 4 : 1;                   // of a wavefront (with two slots: wavefronts 0, 1 B, 2, 3 C)
+    uint32_t b_off[LOADS], x_off, y_col = kNone;
+    unsigned lds_b = 0, lds_c = 0, lds_x = 0;
+    if constexpr (WHOLE) {
+        static_for<0, LOADS>([&](auto i_) SCAN_INLINE {
             constexpr int i = decltype(i_)::value;
-            const uint32_t off = b_off + i * (256 / CH) * row_bytes;
-            rb[i] = __builtin_bit_cast(bf16x8_t, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, 0, 0));
-            if constexpr (Y) rc[i] = __builtin_bit_cast(bf16x8_t, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, c.G * N * 2, 0));
+            const int s = ((SLOTS >= 4 ? wave + 4 * i : wave & 1) * 64) + lane, r = s / CH, ch = scan_chunk<CH>(r, s % CH) / 8 % CH;
+            b_off[i] = ch * 8 < N ? (uint32_t)r * row_bytes + (uint32_t)b_at * 2 + ch * 16 : kNone;
         });
-        static_for<0, 2>([&](auto i_) SCAN_INLINE {
-            constexpr int i = decltype(i_)::value;
-            rx[i] = __builtin_bit_cast(bf16x8_t, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(x_off + i * 32 * row_bytes), 0, 0));
-        });
-    };
-    auto put_block = [&](int t, int t1) SCAN_INLINE {
-        if constexpr (!WHOLE) {
+        const int r = tid >> 3, ch = scan_chunk<8>(r, tid & 7) / 8 % 8;
+        x_off = ch * 8 < np ? (uint32_t)r * row_bytes + (uint32_t)x_at * 2 + ch * 16 : kNone;
+        lds_b = scan_lds_address(sb), lds_c = scan_lds_address(sc), lds_x = scan_lds_address(sx);
+        if (wave * 16 + 4 * g4 < np) y_col = (wave * 16 + 4 * g4) * 2;
+    }
+    // Rows [t, t + Q) up to t1 on their way to buffer `to`.
+    auto bring = [&](int t, int t1, auto to_) SCAN_INLINE {
+        constexpr int to = decltype(to_)::value;
+        if constexpr (WHOLE) {
+            const u32x4_t rs = scan_rows_at(xbc + (int64_t)t * c.ld, (uint32_t)(min(Q, t1 - t) - 1) * row_bytes + (uint32_t)(c.H * P + 2 * c.G * N) * 2);
+            const int to_c = c.G * N * 2;
+            if constexpr (SLOTS >= 4) {
+                static_for<0, LOADS>([&](auto i_) SCAN_INLINE {
+                    constexpr int i = decltype(i_)::value;
+                    scan_dma16(lds_b + to * Q * NP * 2 + (wave + 4 * i) * 1024, rs, b_off[i], 0);
+                    if constexpr (Y) scan_dma16(lds_c + to * Q * NP * 2 + (wave + 4 * i) * 1024, rs, b_off[i], to_c);
+                });
+            } else {
+                if (wave < 2) scan_dma16(lds_b + to * Q * NP * 2 + (wave & 1) * 1024, rs, b_off[0], 0);
+                else if (Y) scan_dma16(lds_c + to * Q * NP * 2 + (wave & 1) * 1024, rs, b_off[0], to_c);
+            }
+            scan_dma16(lds_x + to * Q * 64 * 2 + wave * 1024, rs, x_off, 0);
+        } else {
             for (int e = tid; e < Q * NP; e += 256) {
                 const int r = e / NP, n = e % NP;
                 const bool there = t + r < t1 && n < N;
                 const bf16 *row = xbc + (int64_t)(t + r) * c.ld + n;
-                sb[scan_chunk<CH>(r, n >> 3) + (n & 7)] = there ? row[b_at] : (bf16)0.0f;
-                if constexpr (Y) sc[scan_chunk<CH>(r, n >> 3) + (n & 7)] = there ? row[c_at] : (bf16)0.0f;
+                sb[to][scan_chunk<CH>(r, n >> 3) + (n & 7)] = there ? row[b_at] : (bf16)0.0f;
+                if constexpr (Y) sc[to][scan_chunk<CH>(r, n >> 3) + (n & 7)] = there ? row[c_at] : (bf16)0.0f;
             }
             for (int e = tid; e < Q * 64; e += 256) {
                 const int r = e >> 6, p = e & 63;
-                sx[scan_chunk<8>(r, p >> 3) + (p & 7)] = t + r < t1 && p < np ? xbc[(int64_t)(t + r) * c.ld + x_at + p] : (bf16)0.0f;
+                sx[to][scan_chunk<8>(r, p >> 3) + (p & 7)] = t + r < t1 && p < np ? xbc[(int64_t)(t + r) * c.ld + x_at + p] : (bf16)0.0f;
             }
-            return;
         }
-        static_for<0, BC>([&](auto i_) SCAN_INLINE {
-            constexpr int i = decltype(i_)::value;
-            const int at = scan_chunk<CH>(tid / CH + i * (256 / CH), b_ch);
-            *reinterpret_cast<bf16x8_t *>(sb + at) = rb[i];
-            if constexpr (Y) *reinterpret_cast<bf16x8_t *>(sc + at) = rc[i];
-        });
-        static_for<0, 2>([&](auto i_) SCAN_INLINE {
-            constexpr int i = decltype(i_)::value;
-            *reinterpret_cast<bf16x8_t *>(sx + scan_chunk<8>((tid >> 3) + 32 * i, x_ch)) = rx[i];
-        });
     };
-    // A block's sizes, by one wavefront, a token in each lane.
+    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+    auto rows_of = [&](const void *base, int64_t ld, int t, int t1) SCAN_INLINE {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16 *>(static_cast<const bf16 *>(base) + (int64_t)t * ld + x_at), 0,
+                                                 (uint32_t)(min(Q, t1 - t) - 1) * (uint32_t)ld * 2 + (uint32_t)np * 2, 0x00020000);
+    };
+    // z of a block, as the lane's two tiles of y^T lie
+    u32x2_t gate[2] = {};
+    auto bring_gate = [&](int t, int t1) SCAN_INLINE {
+        if (WHOLE && Y && c.z) {
+            const auto rs = rows_of(c.z, c.ld_z, t, t1);
+            static_for<0, 2>([&](auto i_) SCAN_INLINE {
+                constexpr int i = decltype(i_)::value;
+                gate[i] = __builtin_amdgcn_raw_buffer_load_b64(rs, (int)(y_col + (16 * i + l16) * (uint32_t)c.ld_z * 2), 0, 0);
+            });
+        }
+    };
+    // A block's sizes, by one wavefront, a token in each of its lanes' first half.
     auto put_sizes = [&](ScanBlockSizes &to, float raw, bool there) SCAN_INLINE {
         float dt = dt_of(c.dt, raw, bias);
         dt = there ? dt : 0.0f;
@@ -197,212 +232,218 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
         const unsigned long long u = __builtin_bit_cast(unsigned long long, upto);
         const double total = __builtin_bit_cast(double, (unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), 63) << 32 |
                                                             (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, 63));
-        to.e[lane] = (float)upto;
-        to.dt[lane] = dt;
-        to.w[lane] = __builtin_amdgcn_exp2f((float)(total - upto)) * dt;
-        to.f[lane] = __builtin_amdgcn_exp2f((float)upto);
+        if (lane < Q) {
+            to.e[lane] = (float)upto;
+            to.dt[lane] = dt;
+            to.w[lane] = __builtin_amdgcn_exp2f((float)(total - upto)) * dt;
+            to.f[lane] = __builtin_amdgcn_exp2f((float)upto);
+        }
         if (lane == 0) {
             to.total = (float)total;
             to.factor = __builtin_amdgcn_exp2f((float)total);
         }
     };
+    auto there = [&](int t, int t1) SCAN_INLINE { return lane < Q && t + lane < t1; };
+    auto raw_of = [&](int t, int t1) SCAN_INLINE { return dt_raw(c.dt, min(t + (lane & (Q - 1)), t1 - 1), h); };
 
-    // Tokens [t0, t1) of one sequence.
-    auto run = [&](int t0, int t1, float &sum) SCAN_INLINE {
-        fetch_block(t0, t1);
-        __syncthreads();                             // (nobody reads what an earlier call has left)
-        if (wave == 0) put_sizes(sizes[0], dt_raw(c.dt, min(t0 + lane, t1 - 1), h), t0 + lane < t1);
-        put_block(t0, t1);
-        if constexpr (Y) {                           // the tiles above the diagonal that a step of k = 32 takes along
-            for (int e = tid; e < 2 * 16 * 2; e += 256) {
-                const int r = (e >> 5) * 32 + (e >> 1 & 15), ch = (e >> 5) * 4 + 2 + (e & 1);
-                *reinterpret_cast<bf16x8_t *>(sm + scan_chunk<8>(r, ch)) = bf16x8_t{};
+    float raw = 0.0f, sum_of = 0.0f;                 // the sizes' wavefront: dt_raw of the next block
+    // Block [t, t + Q) up to t1, which lies in buffer `now`.
+    auto block = [&](int t, int t1, auto now_) SCAN_INLINE {
+        constexpr int now = decltype(now_)::value;
+        // (behind the youngest loads there are the two stores of the block before)
+        if constexpr (WHOLE) scan_barrier<Y ? 2 : 0>();
+        else scan_barrier_lds();
+        // The gate and dt have come with the block's rows; the compiler, which does not count those, must not wait for them later.
+        bf16x4_t z[2];
+        if constexpr (WHOLE && Y) {
+            asm volatile("" : "+v"(gate[0]), "+v"(gate[1]));
+            z[0] = __builtin_bit_cast(bf16x4_t, gate[0]);
+            z[1] = __builtin_bit_cast(bf16x4_t, gate[1]);
+        }
+        const bool more = t + Q < t1;
+        float next = 0.0f;
+        if (wave == 3) {
+            asm volatile("" : "+v"(raw));
+            next = raw;
+        }
+        if (more) {
+            bring(t + Q, t1, std::integral_constant<int, 1 - now>{});
+            bring_gate(t + Q, t1);
+            if (wave == 3 && t + 2 * Q < t1) raw = raw_of(t + 2 * Q, t1);
+        }
+        const ScanBlockSizes &sz = sizes[now];
+        const bf16 *const xs = sx[now], *const bs = sb[now], *const cs = sc[Y ? now : 0];
+        sum_of += sz.total;
+        const int q4 = l16 >> 2, c4 = l16 & 3;
+        f32x4_t acc[2];
+        if constexpr (Y) {
+            // M: three of the wavefronts take a tile each (tokens tt, earlier tokens ss); the fourth the next block's sizes
+            if (wave < 3) {
+                const int tt = wave > 0, ss = wave == 2;
+                f32x4_t m = {0, 0, 0, 0};
+                static_for<0, NJ>([&](auto j_) SCAN_INLINE {
+                    constexpr int j = decltype(j_)::value;
+                    m = __builtin_amdgcn_mfma_f32_16x16x32_bf16(scan_row8<CH>(bs, ss * 16 + l16, 4 * j + g4), scan_row8<CH>(cs, tt * 16 + l16, 4 * j + g4), m, 0, 0, 0);
+                });
+                const int row = tt * 16 + l16, s0 = ss * 16 + 4 * g4;
+                const float e = sz.e[row];
+                const f32x4_t es = *reinterpret_cast<const f32x4_t *>(sz.e + s0), ds = *reinterpret_cast<const f32x4_t *>(sz.dt + s0);
+                bf16x4_t q;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float v = m[i] * (__builtin_amdgcn_exp2f(e - es[i]) * ds[i]);
+                    q[i] = (bf16)(s0 + i <= row ? v : 0.0f);
+                }
+                *reinterpret_cast<bf16x4_t *>(sm + scan_chunk<4>(row, s0 >> 3) + (s0 & 4)) = q;
+            } else if (more) {
+                put_sizes(sizes[1 - now], next, there(t + Q, t1));
+            }
+            // what the state in front of the block brings
+            acc[0] = acc[1] = f32x4_t{0, 0, 0, 0};
+            static_for<0, NJ>([&](auto j_) SCAN_INLINE {
+                constexpr int j = decltype(j_)::value;
+                bf16x8_t s;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[i] = (bf16)S[2 * j + (i >> 2)][i & 3];
+#pragma unroll
+                for (int tt = 0; tt < 2; ++tt) {
+                    auto part = [&](int e) SCAN_INLINE {
+                        return *reinterpret_cast<const i16x4_t *>(cs + scan_chunk<CH>(tt * 16 + l16, 4 * j + 2 * e + (g4 >> 1)) + (g4 & 1) * 4);
+                    };
+                    acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(s, scan_pair(part(0), part(1)), acc[tt], 0, 0, 0);
+                }
+            });
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+                const float f = sz.f[tt * 16 + l16];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[tt][i] *= f;
+            }
+        } else {
+            if (wave == 3 && more) put_sizes(sizes[1 - now], next, there(t + Q, t1));
+        }
+        // x^T: row p, eight tokens from 8 g4 on
+        bf16x8_t xf;
+        {
+            const int r = 8 * g4 + q4, ch = 2 * wave + (c4 >> 1), half = (c4 & 1) * 4;
+            xf = scan_pair(scan_transposed(xs + scan_chunk<8>(r, ch) + half), scan_transposed(xs + scan_chunk<8>(r + 4, ch) + half));
+        }
+        if constexpr (Y) {
+            scan_barrier_lds();
+            // An x that is not finite would make NaN of the tokens in front of it too (0 times it): such are left out here and added
+            // where they belong, one by one.
+            uint32_t odd = 0;
+            const u32x4_t u = __builtin_bit_cast(u32x4_t, xf);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) odd |= (u[i] & 0x7f807f80u) + 0x00800080u;
+            const bool any = __ballot((odd & 0x80008000u) != 0) != 0;
+            bf16x8_t xg = xf;
+            if (any) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float v = (float)xg[i];
+                    if (!(fabsf(v) < INFINITY)) xg[i] = (bf16)0.0f;
+                }
+            }
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xg, scan_row8<4>(sm, tt * 16 + l16, g4), acc[tt], 0, 0, 0);
+            if (any) {
+                int column = l16;
+                asm volatile("" : "+v"(column));     // (addresses of this path are not kept in registers for all blocks)
+                for (int s = 0; s < Q; ++s) {
+                    const bf16x4_t v = *reinterpret_cast<const bf16x4_t *>(xs + scan_chunk<8>(s, 2 * wave + (g4 >> 1)) + (g4 & 1) * 4);
+#pragma unroll
+                    for (int tt = 0; tt < 2; ++tt) {
+                        const int row = tt * 16 + column;
+                        if (row < s) continue;
+                        const float m = (float)sm[scan_chunk<4>(row, s >> 3) + (s & 7)];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (!(fabsf((float)v[i]) < INFINITY)) acc[tt][i] = fmaf(m, (float)v[i], acc[tt][i]);
+                    }
+                }
             }
         }
-        __syncthreads();
-        int now = 0;
-        for (int t = t0; t < t1; t += Q, now ^= 1) {
-            const ScanBlockSizes &z = sizes[now];
-            const bool more = t + Q < t1, sizer = more && wave == (now ? 1 : 3);
-            bf16x4_t gate[Y ? 4 : 1];                // z, as the lane's four tiles of y^T lie
-            if constexpr (Y)
-                if (WHOLE && c.z) {
-                    const auto rs = rows_of(c.z, c.ld_z, (int64_t)t * c.ld_z + x_at, min(Q, t1 - t), np);
-                    static_for<0, 4>([&](auto i_) SCAN_INLINE {
-                        constexpr int i = decltype(i_)::value;
-                        gate[i] = __builtin_bit_cast(bf16x4_t, __builtin_amdgcn_raw_buffer_load_b64(rs, (int)(y_col + (16 * i + l16) * (uint32_t)c.ld_z * 2), 0, 0));
-                    });
-                }
-            float raw = 0.0f;
-            if (sizer) raw = dt_raw(c.dt, min(t + Q + lane, t1 - 1), h);
-            if (more) fetch_block(t + Q, t1);
-            sum += z.total;
-            f32x4_t acc[4];
-            if constexpr (Y) {
-                // M, its tiles (token tile tt, earlier tokens ss) in turn.  (The compiler must not know that their addresses are the same in
-                // every block: it would keep some forty of them in registers.)
-                int first = wave;
-                asm volatile("" : "+s"(first));
+        // S'
+        const float factor = sz.factor;
+        const f32x4_t w0 = *reinterpret_cast<const f32x4_t *>(sz.w + 8 * g4), w1 = *reinterpret_cast<const f32x4_t *>(sz.w + 8 * g4 + 4);
+        uint32_t part[3][8];                         // the upper halves of three numbers that add up to x times its weight
 #pragma unroll
-                for (int k = 0; k < 3; ++k) {
-                    const int tile = first + 4 * k;
-                    if (tile >= 10) break;
-                    const int tt = tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3, ss = tile - tt * (tt + 1) / 2;
-                    f32x4_t m = {0, 0, 0, 0};
+        for (int i = 0; i < 8; ++i) {
+            const float v = (float)xf[i] * (i < 4 ? w0[i & 3] : w1[i & 3]);
+            part[0][i] = __float_as_uint(v);
+            const float r = v - __uint_as_float(part[0][i] & 0xffff0000u);
+            part[1][i] = __float_as_uint(r);
+            part[2][i] = __float_as_uint(r - __uint_as_float(part[1][i] & 0xffff0000u));
+        }
+        bf16x8_t xw[3];
 #pragma unroll
-                    for (int j = 0; j < NJ; ++j)
-                        m = __builtin_amdgcn_mfma_f32_16x16x32_bf16(scan_row8<CH>(sb, ss * 16 + l16, 4 * j + g4), scan_row8<CH>(sc, tt * 16 + l16, 4 * j + g4), m, 0, 0, 0);
-                    const int row = tt * 16 + l16, s0 = ss * 16 + 4 * g4;
-                    const float e = z.e[row];
-                    const f32x4_t es = *reinterpret_cast<const f32x4_t *>(z.e + s0), ds = *reinterpret_cast<const f32x4_t *>(z.dt + s0);
+        for (int q = 0; q < 3; ++q) {
+            u32x4_t v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_perm(part[q][2 * i + 1], part[q][2 * i], 0x07060302u);
+            xw[q] = __builtin_bit_cast(bf16x8_t, v);
+        }
+        static_for<0, 2 * NJ>([&](auto j_) SCAN_INLINE {
+            constexpr int j = decltype(j_)::value;
+            const int r = 8 * g4 + q4, ch = 2 * j + (c4 >> 1), half = (c4 & 1) * 4;
+            const bf16x8_t bt = scan_pair(scan_transposed(bs + scan_chunk<CH>(r, ch) + half), scan_transposed(bs + scan_chunk<CH>(r + 4, ch) + half));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) S[j][i] *= factor;
+#pragma unroll
+            for (int q = 0; q < 3; ++q) S[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bt, xw[q], S[j], 0, 0, 0);
+        });
+        if constexpr (Y) {
+            const int p = wave * 16 + 4 * g4;
+            const auto rs = rows_of(out, c.ld_out, t, t1);
+            static_for<0, 2>([&](auto tt_) SCAN_INLINE {
+                constexpr int tt = decltype(tt_)::value;
+                const int r = tt * 16 + l16;
+                const bf16x4_t x = *reinterpret_cast<const bf16x4_t *>(xs + scan_chunk<8>(r, p >> 3) + (p & 4));
+                float y[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] = fmaf(skip, (float)x[i], acc[tt][i]);
+                if constexpr (WHOLE) {
                     bf16x4_t q;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float v = m[i] * (__builtin_amdgcn_exp2f(e - es[i]) * ds[i]);
-                        q[i] = (bf16)(s0 + i <= row ? v : 0.0f);
+                        if (c.z) y[i] *= silu((float)z[tt][i]);
+                        q[i] = (bf16)y[i];
                     }
-                    *reinterpret_cast<bf16x4_t *>(sm + scan_chunk<8>(row, s0 >> 3) + (s0 & 4)) = q;
-                }
-                // what the state in front of the block brings
-                bf16x8_t sf[NJ];
-#pragma unroll
-                for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) sf[j][i] = (bf16)S[2 * j + (i >> 2)][i & 3];
-#pragma unroll
-                for (int tt = 0; tt < 4; ++tt) {
-                    acc[tt] = f32x4_t{0, 0, 0, 0};
-#pragma unroll
-                    for (int j = 0; j < NJ; ++j)
-                        acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sf[j], scan_row8<CH>(sc, tt * 16 + l16, 4 * j + g4), acc[tt], 0, 0, 0);
-                    const float f = z.f[tt * 16 + l16];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[tt][i] *= f;
-                }
-            }
-            // x^T: row p, eight tokens from 32 k + 8 g4 on
-            bf16x8_t xf[2];
-            const int q4 = l16 >> 2, c4 = l16 & 3;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int r = 32 * k + 8 * g4 + q4, ch = 2 * wave + (c4 >> 1), half = (c4 & 1) * 4;
-                xf[k] = scan_pair(scan_transposed(sx + scan_chunk<8>(r, ch) + half), scan_transposed(sx + scan_chunk<8>(r + 4, ch) + half));
-            }
-            if constexpr (Y) {
-                __syncthreads();
-                // An x that is not finite would make NaN of the tokens in front of it too (0 times it): such are left out here and added
-                // where they belong, one by one.
-                uint32_t odd = 0;
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const u32x4_t u = __builtin_bit_cast(u32x4_t, xf[k]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) odd |= (u[i] & 0x7f807f80u) + 0x00800080u;
-                }
-                const bool any = __ballot((odd & 0x80008000u) != 0) != 0;
-                bf16x8_t xg[2] = {xf[0], xf[1]};
-                if (any) {
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float v = (float)xg[k][i];
-                            if (!(fabsf(v) < INFINITY)) xg[k][i] = (bf16)0.0f;
+                    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2_t, q), rs, (int)(y_col + r * (uint32_t)c.ld_out * 2), 0, 0);
+                } else if (t + r < t1) {
+                    for (int i = 0; i < 4; ++i)
+                        if (p + i < np) {
+                            const float v = i == 0 ? y[0] : i == 1 ? y[1] : i == 2 ? y[2] : y[3];
+                            const int64_t col = x_at + p + i;
+                            const float u = c.z ? v * silu((float)static_cast<const bf16 *>(c.z)[(int64_t)(t + r) * c.ld_z + col]) : v;
+                            out[(int64_t)(t + r) * c.ld_out + col] = (bf16)u;
                         }
                 }
-#pragma unroll
-                for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-                    for (int k = 0; k <= tt >> 1; ++k)
-                        acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xg[k], scan_row8<8>(sm, tt * 16 + l16, 4 * k + g4), acc[tt], 0, 0, 0);
-                if (any) {
-                    int column = l16;
-                    asm volatile("" : "+v"(column)); // (nor of these)
-                    for (int s = 0; s < Q; ++s) {
-                        const bf16x4_t v = *reinterpret_cast<const bf16x4_t *>(sx + scan_chunk<8>(s, 2 * wave + (g4 >> 1)) + (g4 & 1) * 4);
-#pragma unroll
-                        for (int tt = 0; tt < 4; ++tt) {
-                            const int row = tt * 16 + column;
-                            if (row < s) continue;
-                            const float m = (float)sm[scan_chunk<8>(row, s >> 3) + (s & 7)];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                if (!(fabsf((float)v[i]) < INFINITY)) acc[tt][i] = fmaf(m, (float)v[i], acc[tt][i]);
-                        }
-                    }
-                }
-            }
-            // S'
-            const float factor = z.factor;
-#pragma unroll
-            for (int j = 0; j < 2 * NJ; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) S[j][i] *= factor;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const f32x4_t w0 = *reinterpret_cast<const f32x4_t *>(z.w + 32 * k + 8 * g4), w1 = *reinterpret_cast<const f32x4_t *>(z.w + 32 * k + 8 * g4 + 4);
-                uint32_t part[3][8];                 // the upper halves of three numbers that add up to x times its weight
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float v = (float)xf[k][i] * (i < 4 ? w0[i & 3] : w1[i & 3]);
-                    part[0][i] = __float_as_uint(v);
-                    const float r = v - __uint_as_float(part[0][i] & 0xffff0000u);
-                    part[1][i] = __float_as_uint(r);
-                    part[2][i] = __float_as_uint(r - __uint_as_float(part[1][i] & 0xffff0000u));
-                }
-                bf16x8_t xw[3];
-#pragma unroll
-                for (int q = 0; q < 3; ++q) {
-                    u32x4_t u;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) u[i] = __builtin_amdgcn_perm(part[q][2 * i + 1], part[q][2 * i], 0x07060302u);
-                    xw[q] = __builtin_bit_cast(bf16x8_t, u);
-                }
-#pragma unroll
-                for (int j = 0; j < 2 * NJ; ++j) {
-                    const int r = 32 * k + 8 * g4 + q4, ch = 4 * (j >> 1) + c4, half = (j & 1) * 4;
-                    const bf16x8_t bt = scan_pair(scan_transposed(sb + scan_chunk<CH>(r, ch) + half), scan_transposed(sb + scan_chunk<CH>(r + 4, ch) + half));
-#pragma unroll
-                    for (int q = 0; q < 3; ++q) S[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bt, xw[q], S[j], 0, 0, 0);
-                }
-            }
-            if (sizer) put_sizes(sizes[now ^ 1], raw, t + Q + lane < t1);
-            if constexpr (Y) {
-                const int p = wave * 16 + 4 * g4;
-                const auto rs = rows_of(out, c.ld_out, (int64_t)t * c.ld_out + x_at, min(Q, t1 - t), np);
-                static_for<0, 4>([&](auto tt_) SCAN_INLINE {
-                    constexpr int tt = decltype(tt_)::value;
-                    const int r = tt * 16 + l16;
-                    const bf16x4_t x = *reinterpret_cast<const bf16x4_t *>(sx + scan_chunk<8>(r, p >> 3) + (p & 4));
-                    float y[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) y[i] = fmaf(skip, (float)x[i], acc[tt][i]);
-                    if constexpr (WHOLE) {
-                        bf16x4_t q;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            if (c.z) y[i] *= silu((float)gate[tt][i]);
-                            q[i] = (bf16)y[i];
-                        }
-                        typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
-                        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2_t, q), rs, (int)(y_col + r * (uint32_t)c.ld_out * 2), 0, 0);
-                    } else if (t + r < t1) {
-                        for (int i = 0; i < 4; ++i)
-                            if (p + i < np) {
-                                const float v = i == 0 ? y[0] : i == 1 ? y[1] : i == 2 ? y[2] : y[3];
-                                const int64_t col = x_at + p + i;
-                                const float u = c.z ? v * silu((float)static_cast<const bf16 *>(c.z)[(int64_t)(t + r) * c.ld_z + col]) : v;
-                                out[(int64_t)(t + r) * c.ld_out + col] = (bf16)u;
-                            }
-                    }
-                });
-            }
-            __syncthreads();
-            if (more) {
-                put_block(t + Q, t1);
-                __syncthreads();
-            }
+            });
         }
+    };
+
+    // Tokens [t0, t1) of one sequence.
+    auto run = [&](int t0, int t1, float &sum) SCAN_INLINE {
+        __syncthreads();                             // (nobody reads what an earlier call has left)
+        bring(t0, t1, std::integral_constant<int, 0>{});
+        bring_gate(t0, t1);
+        if (wave == 3) {
+            put_sizes(sizes[0], raw_of(t0, t1), there(t0, t1));
+            if (t0 + Q < t1) raw = raw_of(t0 + Q, t1);
+        }
+        if constexpr (Y)                             // the tile above the diagonal
+            if (tid < 32) *reinterpret_cast<bf16x8_t *>(sm + scan_chunk<4>(tid & 15, 2 + (tid >> 4))) = bf16x8_t{};
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        sum_of = 0.0f;
+        for (int t = t0;;) {
+            block(t, t1, std::integral_constant<int, 0>{});
+            if ((t += Q) >= t1) break;
+            block(t, t1, std::integral_constant<int, 1>{});
+            if ((t += Q) >= t1) break;
+        }
+        sum += sum_of;
     };
     scan_drive<MODE>(c, work, h, p0, head_at, lane, clear, load, store, add, run, zeros);
 }
