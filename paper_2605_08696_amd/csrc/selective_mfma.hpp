@@ -24,6 +24,7 @@ typedef __attribute__((ext_vector_type(8))) short i16x8_t;
 
 #define SCAN_INLINE __attribute__((always_inline))
 constexpr int kScanBlock = 32, kScanRows = 64;       // tokens of a block, rows of P of a work-group
+constexpr int kScanAhead = 8;                        // blocks whose sizes are formed together, two by each wavefront
 
 // LDS rows of CH chunks of sixteen bytes: chunk c of row r lies at c ^ f(r).  Sixteen rows' chunks c then lie on all banks, and so do the
 // sixteen chunks or halves of chunks that a transposing read takes from four rows.
@@ -45,8 +46,8 @@ __device__ __forceinline__ bf16x8_t scan_pair(i16x4_t a, i16x4_t b)
     return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// Running sum over the wavefront's lanes, this one's included.
-__device__ __forceinline__ double wave_scan(double v)
+// Running sum over each half of the wavefront's lanes, this one's included.
+__device__ __forceinline__ double half_scan(double v)
 {
     auto moved = [](double x, auto ctrl, auto rows) {
         const unsigned long long u = __builtin_bit_cast(unsigned long long, x);
@@ -60,7 +61,6 @@ __device__ __forceinline__ double wave_scan(double v)
     v += moved(v, integral_constant<int, 0x114>{}, integral_constant<int, 0xF>{});
     v += moved(v, integral_constant<int, 0x118>{}, integral_constant<int, 0xF>{});
     v += moved(v, integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});     // row_bcast:15 into rows 1 and 3
-    v += moved(v, integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});     // row_bcast:31 into rows 2 and 3
     return v;
 }
 
@@ -106,7 +106,7 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
     constexpr int CH = NP / 8, NJ = NP / 32, Q = kScanBlock, SLOTS = Q * CH / 64;    // loads of 64 chunks that B or C of a block takes
     constexpr bool Y = MODE != SCAN_CARRY;
     __shared__ __align__(16) bf16 sb[2][Q * NP], sc[Y ? 2 : 1][Y ? Q * NP : 8], sx[2][Q * 64], sm[Y ? Q * Q : 8];
-    __shared__ __align__(16) ScanBlockSizes sizes[2];
+    __shared__ __align__(16) ScanBlockSizes sizes[kScanAhead];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
     const int64_t id = work_group();
     const int per = c.H * c.parts;
@@ -224,31 +224,34 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
             });
         }
     };
-    // A block's sizes, by one wavefront, a token in each of its lanes' first half.
-    auto put_sizes = [&](ScanBlockSizes &to, float raw, bool there) SCAN_INLINE {
+    // The sizes of the kScanAhead blocks from t on: a token in each lane.
+    auto raw_of = [&](int t, int t1) SCAN_INLINE { return dt_raw(c.dt, min(t + tid, t1 - 1), h); };
+    auto put_sizes = [&](float raw, int t, int t1) SCAN_INLINE {
+        const bool there = t + tid < t1;
         float dt = dt_of(c.dt, raw, bias);
         dt = there ? dt : 0.0f;
-        const double upto = wave_scan(there ? (double)decay_exponent(dt, a) : 0.0);
+        const double upto = half_scan(there ? (double)decay_exponent(dt, a) : 0.0);
         const unsigned long long u = __builtin_bit_cast(unsigned long long, upto);
-        const double total = __builtin_bit_cast(double, (unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), 63) << 32 |
-                                                            (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, 63));
-        if (lane < Q) {
-            to.e[lane] = (float)upto;
-            to.dt[lane] = dt;
-            to.w[lane] = __builtin_amdgcn_exp2f((float)(total - upto)) * dt;
-            to.f[lane] = __builtin_amdgcn_exp2f((float)upto);
-        }
-        if (lane == 0) {
+        auto last_of = [&](int lane_) SCAN_INLINE {
+            return __builtin_bit_cast(double, (unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), lane_) << 32 |
+                                                  (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, lane_));
+        };
+        const double first = last_of(31), second = last_of(63), total = lane < 32 ? first : second;
+        ScanBlockSizes &to = sizes[tid >> 5];
+        const int at = lane & 31;
+        to.e[at] = (float)upto;
+        to.dt[at] = dt;
+        to.w[at] = __builtin_amdgcn_exp2f((float)(total - upto)) * dt;
+        to.f[at] = __builtin_amdgcn_exp2f((float)upto);
+        if (at == 0) {
             to.total = (float)total;
             to.factor = __builtin_amdgcn_exp2f((float)total);
         }
     };
-    auto there = [&](int t, int t1) SCAN_INLINE { return lane < Q && t + lane < t1; };
-    auto raw_of = [&](int t, int t1) SCAN_INLINE { return dt_raw(c.dt, min(t + (lane & (Q - 1)), t1 - 1), h); };
 
-    float raw = 0.0f, sum_of = 0.0f;                 // the sizes' wavefront: dt_raw of the next block
-    // Block [t, t + Q) up to t1, which lies in buffer `now`.
-    auto block = [&](int t, int t1, auto now_) SCAN_INLINE {
+    float raw = 0.0f, sum_of = 0.0f;                 // dt_raw of the next blocks whose sizes are formed
+    // Block [t, t + Q) up to t1, number n of its sequence, which lies in buffer `now`.
+    auto block = [&](int t, int t1, int n, auto now_) SCAN_INLINE {
         constexpr int now = decltype(now_)::value;
         // (behind the youngest loads there are the two stores of the block before)
         if constexpr (WHOLE) scan_barrier<Y ? 2 : 0>();
@@ -261,23 +264,23 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
             z[1] = __builtin_bit_cast(bf16x4_t, gate[1]);
         }
         const bool more = t + Q < t1;
-        float next = 0.0f;
-        if (wave == 3) {
-            asm volatile("" : "+v"(raw));
-            next = raw;
-        }
+        asm volatile("" : "+v"(raw));
         if (more) {
             bring(t + Q, t1, std::integral_constant<int, 1 - now>{});
             bring_gate(t + Q, t1);
-            if (wave == 3 && t + 2 * Q < t1) raw = raw_of(t + 2 * Q, t1);
         }
-        const ScanBlockSizes &sz = sizes[now];
+        if (n % kScanAhead == 0) {
+            put_sizes(raw, t, t1);
+            if (t + kScanAhead * Q < t1) raw = raw_of(t + kScanAhead * Q, t1);
+            scan_barrier_lds();
+        }
+        const ScanBlockSizes &sz = sizes[n % kScanAhead];
         const bf16 *const xs = sx[now], *const bs = sb[now], *const cs = sc[Y ? now : 0];
         sum_of += sz.total;
         const int q4 = l16 >> 2, c4 = l16 & 3;
         f32x4_t acc[2];
         if constexpr (Y) {
-            // M: three of the wavefronts take a tile each (tokens tt, earlier tokens ss); the fourth the next block's sizes
+            // M: three of the wavefronts take a tile each (tokens tt, earlier tokens ss)
             if (wave < 3) {
                 const int tt = wave > 0, ss = wave == 2;
                 f32x4_t m = {0, 0, 0, 0};
@@ -295,8 +298,6 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
                     q[i] = (bf16)(s0 + i <= row ? v : 0.0f);
                 }
                 *reinterpret_cast<bf16x4_t *>(sm + scan_chunk<4>(row, s0 >> 3) + (s0 & 4)) = q;
-            } else if (more) {
-                put_sizes(sizes[1 - now], next, there(t + Q, t1));
             }
             // what the state in front of the block brings
             acc[0] = acc[1] = f32x4_t{0, 0, 0, 0};
@@ -319,8 +320,6 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[tt][i] *= f;
             }
-        } else {
-            if (wave == 3 && more) put_sizes(sizes[1 - now], next, there(t + Q, t1));
         }
         // x^T: row p, eight tokens from 8 g4 on
         bf16x8_t xf;
@@ -429,18 +428,15 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
         __syncthreads();                             // (nobody reads what an earlier call has left)
         bring(t0, t1, std::integral_constant<int, 0>{});
         bring_gate(t0, t1);
-        if (wave == 3) {
-            put_sizes(sizes[0], raw_of(t0, t1), there(t0, t1));
-            if (t0 + Q < t1) raw = raw_of(t0 + Q, t1);
-        }
+        raw = raw_of(t0, t1);
         if constexpr (Y)                             // the tile above the diagonal
             if (tid < 32) *reinterpret_cast<bf16x8_t *>(sm + scan_chunk<4>(tid & 15, 2 + (tid >> 4))) = bf16x8_t{};
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         sum_of = 0.0f;
-        for (int t = t0;;) {
-            block(t, t1, std::integral_constant<int, 0>{});
+        for (int t = t0, n = 0;; n += 2) {
+            block(t, t1, n, std::integral_constant<int, 0>{});
             if ((t += Q) >= t1) break;
-            block(t, t1, std::integral_constant<int, 1>{});
+            block(t, t1, n + 1, std::integral_constant<int, 1>{});
             if ((t += Q) >= t1) break;
         }
         sum += sum_of;
