@@ -119,14 +119,14 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
     const int64_t head_at = ((int64_t)h * P + p0) * N;
     const int64_t x_at = (int64_t)h * P + p0, b_at = (int64_t)c.H * P + (int64_t)g * N, c_at = b_at + (int64_t)c.G * N;
 
-    f32x4_t S[2 * NJ];                               // S^T: tile j, row 4 g4 + i is n = 16 j + 4 g4 + i; column p = 16 wave + l16
+    f32x4_t S[2 * NJ];                               // S^T: tile 2 j + e, row 4 g4 + i is n = 32 j + 8 g4 + 4 e + i; column p = 16 wave + l16
     const int my_p = wave * 16 + l16;
     auto clear = [&]() SCAN_INLINE { static_for<0, 2 * NJ>([&](auto j_) SCAN_INLINE { S[decltype(j_)::value] = f32x4_t{0, 0, 0, 0}; }); };
     auto each = [&](auto &&fn) SCAN_INLINE {         // fn(four elements, offset from the head's first, how many of them exist)
         if (my_p < np)
             static_for<0, 2 * NJ>([&](auto j_) SCAN_INLINE {
                 constexpr int j = decltype(j_)::value;
-                const int n = 16 * j + 4 * g4;
+                const int n = 32 * (j >> 1) + 8 * g4 + 4 * (j & 1);
                 if (n < N) fn(S[j], (int64_t)my_p * N + n, min(4, N - n));
             });
     };
@@ -291,12 +291,14 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
                 const int row = tt * 16 + l16, s0 = ss * 16 + 4 * g4;
                 const float e = sz.e[row];
                 const f32x4_t es = *reinterpret_cast<const f32x4_t *>(sz.e + s0), ds = *reinterpret_cast<const f32x4_t *>(sz.dt + s0);
-                bf16x4_t q;
+                float v[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float v = m[i] * (__builtin_amdgcn_exp2f(e - es[i]) * ds[i]);
-                    q[i] = (bf16)(s0 + i <= row ? v : 0.0f);
+                    v[i] = m[i] * (__builtin_amdgcn_exp2f(e - es[i]) * ds[i]);
+                    v[i] = s0 + i <= row ? v[i] : 0.0f;
                 }
+                const bf16x2_t lo = __builtin_convertvector(f32x2_t{v[0], v[1]}, bf16x2_t), hi = __builtin_convertvector(f32x2_t{v[2], v[3]}, bf16x2_t);
+                const bf16x4_t q = __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
                 *reinterpret_cast<bf16x4_t *>(sm + scan_chunk<4>(row, s0 >> 3) + (s0 & 4)) = q;
             }
             // what the state in front of the block brings
@@ -307,12 +309,8 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s[i] = (bf16)S[2 * j + (i >> 2)][i & 3];
 #pragma unroll
-                for (int tt = 0; tt < 2; ++tt) {
-                    auto part = [&](int e) SCAN_INLINE {
-                        return *reinterpret_cast<const i16x4_t *>(cs + scan_chunk<CH>(tt * 16 + l16, 4 * j + 2 * e + (g4 >> 1)) + (g4 & 1) * 4);
-                    };
-                    acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(s, scan_pair(part(0), part(1)), acc[tt], 0, 0, 0);
-                }
+                for (int tt = 0; tt < 2; ++tt)
+                    acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(s, scan_row8<CH>(cs, tt * 16 + l16, 4 * j + g4), acc[tt], 0, 0, 0);
             });
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt) {
@@ -327,6 +325,35 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
             const int r = 8 * g4 + q4, ch = 2 * wave + (c4 >> 1), half = (c4 & 1) * 4;
             xf = scan_pair(scan_transposed(xs + scan_chunk<8>(r, ch) + half), scan_transposed(xs + scan_chunk<8>(r + 4, ch) + half));
         }
+        // S'
+        const float factor = sz.factor;
+        const f32x4_t w0 = *reinterpret_cast<const f32x4_t *>(sz.w + 8 * g4), w1 = *reinterpret_cast<const f32x4_t *>(sz.w + 8 * g4 + 4);
+        uint32_t part[3][8];                         // the upper halves of three numbers that add up to x times its weight
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float v = (float)xf[i] * (i < 4 ? w0[i & 3] : w1[i & 3]);
+            part[0][i] = __float_as_uint(v);
+            const float r = v - __uint_as_float(part[0][i] & 0xffff0000u);
+            part[1][i] = __float_as_uint(r);
+            part[2][i] = __float_as_uint(r - __uint_as_float(part[1][i] & 0xffff0000u));
+        }
+        bf16x8_t xw[3];
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            u32x4_t v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_perm(part[q][2 * i + 1], part[q][2 * i], 0x07060302u);
+            xw[q] = __builtin_bit_cast(bf16x8_t, v);
+        }
+        static_for<0, 2 * NJ>([&](auto j_) SCAN_INLINE {
+            constexpr int j = decltype(j_)::value;
+            const int r = 8 * g4 + q4, ch = 4 * (j >> 1) + c4, half = (j & 1) * 4;
+            const bf16x8_t bt = scan_pair(scan_transposed(bs + scan_chunk<CH>(r, ch) + half), scan_transposed(bs + scan_chunk<CH>(r + 4, ch) + half));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) S[j][i] *= factor;
+#pragma unroll
+            for (int q = 0; q < 3; ++q) S[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bt, xw[q], S[j], 0, 0, 0);
+        });
         if constexpr (Y) {
             scan_barrier_lds();
             // An x that is not finite would make NaN of the tokens in front of it too (0 times it): such are left out here and added
@@ -363,63 +390,41 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
                 }
             }
         }
-        // S'
-        const float factor = sz.factor;
-        const f32x4_t w0 = *reinterpret_cast<const f32x4_t *>(sz.w + 8 * g4), w1 = *reinterpret_cast<const f32x4_t *>(sz.w + 8 * g4 + 4);
-        uint32_t part[3][8];                         // the upper halves of three numbers that add up to x times its weight
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float v = (float)xf[i] * (i < 4 ? w0[i & 3] : w1[i & 3]);
-            part[0][i] = __float_as_uint(v);
-            const float r = v - __uint_as_float(part[0][i] & 0xffff0000u);
-            part[1][i] = __float_as_uint(r);
-            part[2][i] = __float_as_uint(r - __uint_as_float(part[1][i] & 0xffff0000u));
-        }
-        bf16x8_t xw[3];
-#pragma unroll
-        for (int q = 0; q < 3; ++q) {
-            u32x4_t v;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_perm(part[q][2 * i + 1], part[q][2 * i], 0x07060302u);
-            xw[q] = __builtin_bit_cast(bf16x8_t, v);
-        }
-        static_for<0, 2 * NJ>([&](auto j_) SCAN_INLINE {
-            constexpr int j = decltype(j_)::value;
-            const int r = 8 * g4 + q4, ch = 2 * j + (c4 >> 1), half = (c4 & 1) * 4;
-            const bf16x8_t bt = scan_pair(scan_transposed(bs + scan_chunk<CH>(r, ch) + half), scan_transposed(bs + scan_chunk<CH>(r + 4, ch) + half));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) S[j][i] *= factor;
-#pragma unroll
-            for (int q = 0; q < 3; ++q) S[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bt, xw[q], S[j], 0, 0, 0);
-        });
         if constexpr (Y) {
             const int p = wave * 16 + 4 * g4;
             const auto rs = rows_of(out, c.ld_out, t, t1);
-            static_for<0, 2>([&](auto tt_) SCAN_INLINE {
-                constexpr int tt = decltype(tt_)::value;
-                const int r = tt * 16 + l16;
-                const bf16x4_t x = *reinterpret_cast<const bf16x4_t *>(xs + scan_chunk<8>(r, p >> 3) + (p & 4));
-                float y[4];
+            float y[2][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = fmaf(skip, (float)x[i], acc[tt][i]);
-                if constexpr (WHOLE) {
-                    bf16x4_t q;
+            for (int tt = 0; tt < 2; ++tt) {
+                const bf16x4_t x = *reinterpret_cast<const bf16x4_t *>(xs + scan_chunk<8>(tt * 16 + l16, p >> 3) + (p & 4));
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (c.z) y[i] *= silu((float)z[tt][i]);
-                        q[i] = (bf16)y[i];
-                    }
-                    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2_t, q), rs, (int)(y_col + r * (uint32_t)c.ld_out * 2), 0, 0);
-                } else if (t + r < t1) {
+                for (int i = 0; i < 4; ++i) y[tt][i] = fmaf(skip, (float)x[i], acc[tt][i]);
+            }
+            if constexpr (WHOLE) {
+                if (c.z)
+#pragma unroll
+                    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y[tt][i] *= silu((float)z[tt][i]);
+#pragma unroll
+                for (int tt = 0; tt < 2; ++tt) {
+                    const bf16x2_t lo = __builtin_convertvector(f32x2_t{y[tt][0], y[tt][1]}, bf16x2_t), hi = __builtin_convertvector(f32x2_t{y[tt][2], y[tt][3]}, bf16x2_t);
+                    __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)}, rs,
+                                                          (int)(y_col + (tt * 16 + l16) * (uint32_t)c.ld_out * 2), 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int tt = 0; tt < 2; ++tt) {
+                    const int64_t row = t + tt * 16 + l16;
+#pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (p + i < np) {
-                            const float v = i == 0 ? y[0] : i == 1 ? y[1] : i == 2 ? y[2] : y[3];
-                            const int64_t col = x_at + p + i;
-                            const float u = c.z ? v * silu((float)static_cast<const bf16 *>(c.z)[(int64_t)(t + r) * c.ld_z + col]) : v;
-                            out[(int64_t)(t + r) * c.ld_out + col] = (bf16)u;
+                        if (row < t1 && p + i < np) {
+                            float v = y[tt][i];
+                            if (c.z) v *= silu((float)static_cast<const bf16 *>(c.z)[row * c.ld_z + x_at + p + i]);
+                            out[row * c.ld_out + x_at + p + i] = (bf16)v;
                         }
                 }
-            });
+            }
         }
     };
 
