@@ -164,12 +164,13 @@ static int launch_scan(const void *d_xbc, void *d_out, const ScanCall &c, const 
     const int64_t units = (int64_t)c.H * c.parts;
     const T *x = static_cast<const T *>(d_xbc);
     T *out = static_cast<T *>(d_out);
+    const dim3 grid = grid_of(cdiv((p.segments ? p.segments : c.seqs.n) * units, 8 * kScanRun) * 8 * kScanRun);
     if (p.segments == 0) {
-        hipLaunchKernelGGL(WHOLE, grid_of(c.seqs.n * units), dim3(threads), 0, st, x, out, c);
+        hipLaunchKernelGGL(WHOLE, grid, dim3(threads), 0, st, x, out, c);
     } else {
-        hipLaunchKernelGGL(CARRY, grid_of(p.segments * units), dim3(threads), 0, st, x, out, c);
+        hipLaunchKernelGGL(CARRY, grid, dim3(threads), 0, st, x, out, c);
         HIP_TRY(hipGetLastError());
-        hipLaunchKernelGGL(SEGMENTS, grid_of(p.segments * units), dim3(threads), 0, st, x, out, c);
+        hipLaunchKernelGGL(SEGMENTS, grid, dim3(threads), 0, st, x, out, c);
     }
     HIP_TRY(hipGetLastError());
     return SRM_OK;
@@ -223,7 +224,7 @@ extern "C" int srm_selective_scan(int32_t dtype, const void *d_xbc, int64_t ld_x
             p.segments = (int)cdiv(tokens, p.seg);
         }
     }
-    if (std::max<int64_t>(p.segments, N) * heads * p.parts >= kMaxBlocks) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    if (std::max<int64_t>(p.segments, N) * heads * p.parts >= kMaxBlocks - 64) return fail(SRM_EINVAL, "%s: sizes out of range", who);
     if (tokens == 0) return SRM_OK;
     c.dt = StepSizes{d_dt, ld_dt, d_dt_bias, dt_dtype == SRM_BF16, softplus != 0};
     c.ld = ld_xbc;

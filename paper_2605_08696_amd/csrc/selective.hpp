@@ -28,6 +28,14 @@ struct ScanCall {
     int seg, parts;                                  // tokens of a segment; parts of a head's P rows
     float *carry, *held, *decay;                     // [segments][H][P][N] twice, [segments][H]
 };
+// Work-groups are dealt to the eight XCDs in turn, each with an L2 of its own.  Runs of kScanRun heads, which share B and C or whose rows
+// lie side by side, go to one of them.  (The last runs may lie behind the last head: their `work` is behind the last sequence or segment.)
+constexpr int kScanRun = 8;
+__device__ __forceinline__ int64_t scan_unit()
+{
+    const uint32_t id = work_group(), j = id >> 3;
+    return (int64_t)(j / kScanRun * 8 + (id & 7)) * kScanRun + j % kScanRun;
+}
 enum { SCAN_WHOLE = 0, SCAN_CARRY = 1, SCAN_SEGMENTS = 2 };
 
 __device__ __forceinline__ float dt_raw(const StepSizes &c, int64_t t, int h)
@@ -134,7 +142,7 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
     __shared__ __align__(16) float sb[TT][NP + 4], sc[TT][NP + 4], sx[TT][PW + 4];
     __shared__ float2 sd[TT];
     const int lane = threadIdx.x, ln = lane % NL, lp = lane / NL;
-    const int64_t id = work_group();
+    const int64_t id = scan_unit();
     const int per = c.H * c.parts;
     const int64_t work = id / per;
     const int h = (int)(id % per) / c.parts, p0 = (int)(id % per) % c.parts * PW, g = h / (c.H / c.G);

@@ -108,7 +108,7 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
     __shared__ __align__(16) bf16 sb[2][Q * NP], sc[Y ? 2 : 1][Y ? Q * NP : 8], sx[2][Q * 64], sm[Y ? Q * Q : 8];
     __shared__ __align__(16) ScanBlockSizes sizes[kScanAhead];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
-    const int64_t id = work_group();
+    const int64_t id = scan_unit();
     const int per = c.H * c.parts;
     const int64_t work = id / per;
     const int h = (int)(id % per) / c.parts, p0 = (int)(id % per) % c.parts * 64, g = h / (c.H / c.G);
