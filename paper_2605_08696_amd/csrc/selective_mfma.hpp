@@ -24,7 +24,7 @@ typedef __attribute__((ext_vector_type(8))) short i16x8_t;
 
 #define SCAN_INLINE __attribute__((always_inline))
 constexpr int kScanBlock = 32, kScanRows = 64;       // tokens of a block, rows of P of a work-group
-constexpr int kScanAhead = 8;                        // blocks whose sizes are formed together, two by each wavefront
+constexpr int kScanAhead = 4;                        // blocks whose sizes are formed together, one by each wavefront
 
 // LDS rows of CH chunks of sixteen bytes: chunk c of row r lies at c ^ f(r).  Sixteen rows' chunks c then lie on all banks, and so do the
 // sixteen chunks or halves of chunks that a transposing read takes from four rows.
@@ -98,14 +98,17 @@ __device__ __forceinline__ void scan_barrier_lds() { asm volatile("s_waitcnt lgk
 // WHOLE: rows in whole chunks of eight elements, all at multiples of sixteen bytes, row strides of less than 2^23.
 //
 // A block's rows come to one of two LDS buffers while the block in front of it is worked on in the other, straight from memory (WHOLE; else
-// one element at a time).  Two barriers a block: its rows are there; M is there.
+// one element at a time).  Two barriers a block: its rows are there; M is there.  y takes x's place in LDS, and leaves from there in whole
+// rows behind the next barrier (stored by each wavefront from its registers, 32 bytes of a row at a time, and z read so, the chip moves half
+// the bytes a second).
 template <int NP, int MODE, bool WHOLE>
 __global__ void __launch_bounds__(256, NP <= 128 ? 3 : 2)
 selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out, ScanCall c)
 {
     constexpr int CH = NP / 8, NJ = NP / 32, Q = kScanBlock, SLOTS = Q * CH / 64;    // loads of 64 chunks that B or C of a block takes
     constexpr bool Y = MODE != SCAN_CARRY;
-    __shared__ __align__(16) bf16 sb[2][Q * NP], sc[Y ? 2 : 1][Y ? Q * NP : 8], sx[2][Q * 64], sm[Y ? Q * Q : 8];
+    __shared__ __align__(16) bf16 sb[2][Q * NP], sc[Y ? 2 : 1][Y ? Q * NP : 8], sx[2][Q * 64], sg[Y && WHOLE ? 2 : 1][Y && WHOLE ? Q * 64 : 8],
+        sm[Y ? Q * Q : 8];
     __shared__ __align__(16) ScanBlockSizes sizes[kScanAhead];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
     const int64_t id = scan_unit();
@@ -164,8 +167,8 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
     constexpr uint32_t kNone = 0x80000000u;          // behind every operand
     const uint32_t row_bytes = (uint32_t)c.ld * 2;
     constexpr int LOADS = SLOTS >= 4 ? SLOTS / 4 : 1;                   // of a wavefront (with two slots: wavefronts 0, 1 B, 2, 3 C)
-    uint32_t b_off[LOADS], x_off, y_col = kNone;
-    unsigned lds_b = 0, lds_c = 0, lds_x = 0;
+    uint32_t b_off[LOADS], x_off, z_off, y_off;
+    unsigned lds_b = 0, lds_c = 0, lds_x = 0, lds_z = 0;
     if constexpr (WHOLE) {
         static_for<0, LOADS>([&](auto i_) SCAN_INLINE {
             constexpr int i = decltype(i_)::value;
@@ -174,8 +177,9 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
         });
         const int r = tid >> 3, ch = scan_chunk<8>(r, tid & 7) / 8 % 8;
         x_off = ch * 8 < np ? (uint32_t)r * row_bytes + (uint32_t)x_at * 2 + ch * 16 : kNone;
-        lds_b = scan_lds_address(sb), lds_c = scan_lds_address(sc), lds_x = scan_lds_address(sx);
-        if (wave * 16 + 4 * g4 < np) y_col = (wave * 16 + 4 * g4) * 2;
+        z_off = ch * 8 < np ? (uint32_t)r * (uint32_t)c.ld_z * 2 + ch * 16 : kNone;
+        y_off = ch * 8 < np ? (uint32_t)r * (uint32_t)c.ld_out * 2 + ch * 16 : kNone;
+        lds_b = scan_lds_address(sb), lds_c = scan_lds_address(sc), lds_x = scan_lds_address(sx), lds_z = scan_lds_address(sg);
     }
     // Rows [t, t + Q) up to t1 on their way to buffer `to`.
     auto bring = [&](int t, int t1, auto to_) SCAN_INLINE {
@@ -194,6 +198,9 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
                 else if (Y) scan_dma16(lds_c + to * Q * NP * 2 + (wave & 1) * 1024, rs, b_off[0], to_c);
             }
             scan_dma16(lds_x + to * Q * 64 * 2 + wave * 1024, rs, x_off, 0);
+            if (Y && c.z)
+                scan_dma16(lds_z + to * Q * 64 * 2 + wave * 1024,
+                           scan_rows_at(static_cast<const bf16 *>(c.z) + (int64_t)t * c.ld_z + x_at, (uint32_t)(min(Q, t1 - t) - 1) * (uint32_t)c.ld_z * 2 + np * 2), z_off, 0);
         } else {
             for (int e = tid; e < Q * NP; e += 256) {
                 const int r = e / NP, n = e % NP;
@@ -208,42 +215,33 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
             }
         }
     };
-    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
-    auto rows_of = [&](const void *base, int64_t ld, int t, int t1) SCAN_INLINE {
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16 *>(static_cast<const bf16 *>(base) + (int64_t)t * ld + x_at), 0,
-                                                 (uint32_t)(min(Q, t1 - t) - 1) * (uint32_t)ld * 2 + (uint32_t)np * 2, 0x00020000);
-    };
-    // z of a block, as the lane's two tiles of y^T lie
-    u32x2_t gate[2] = {};
-    auto bring_gate = [&](int t, int t1) SCAN_INLINE {
-        if (WHOLE && Y && c.z) {
-            const auto rs = rows_of(c.z, c.ld_z, t, t1);
-            static_for<0, 2>([&](auto i_) SCAN_INLINE {
-                constexpr int i = decltype(i_)::value;
-                gate[i] = __builtin_amdgcn_raw_buffer_load_b64(rs, (int)(y_col + (16 * i + l16) * (uint32_t)c.ld_z * 2), 0, 0);
-            });
+    // y of rows [t, t + Q) up to t1 from buffer `from`: this lane's chunk of the rows that this wavefront's loads bring to the same place next.
+    auto leave = [&](int t, int t1, auto from_) SCAN_INLINE {
+        constexpr int from = decltype(from_)::value;
+        if constexpr (Y && WHOLE) {
+            const u32x4_t v = *reinterpret_cast<const u32x4_t *>(sx[from] + tid * 8);
+            const auto rs = __builtin_amdgcn_make_buffer_rsrc(out + (int64_t)t * c.ld_out + x_at, 0,
+                                                              (uint32_t)(min(Q, t1 - t) - 1) * (uint32_t)c.ld_out * 2 + (uint32_t)np * 2, 0x00020000);
+            __builtin_amdgcn_raw_buffer_store_b128(v, rs, (int)y_off, 0, 0);
         }
     };
-    // The sizes of the kScanAhead blocks from t on: a token in each lane.
-    auto raw_of = [&](int t, int t1) SCAN_INLINE { return dt_raw(c.dt, min(t + tid, t1 - 1), h); };
+    // The sizes of the kScanAhead blocks from t on: a token in each lane of a wavefront's halves.
+    auto raw_of = [&](int t, int t1) SCAN_INLINE { return dt_raw(c.dt, min(t + wave * Q + (lane & 31), t1 - 1), h); };
     auto put_sizes = [&](float raw, int t, int t1) SCAN_INLINE {
-        const bool there = t + tid < t1;
+        const bool there = t + wave * Q + (lane & 31) < t1;
         float dt = dt_of(c.dt, raw, bias);
         dt = there ? dt : 0.0f;
         const double upto = half_scan(there ? (double)decay_exponent(dt, a) : 0.0);
         const unsigned long long u = __builtin_bit_cast(unsigned long long, upto);
-        auto last_of = [&](int lane_) SCAN_INLINE {
-            return __builtin_bit_cast(double, (unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), lane_) << 32 |
-                                                  (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, lane_));
-        };
-        const double first = last_of(31), second = last_of(63), total = lane < 32 ? first : second;
-        ScanBlockSizes &to = sizes[tid >> 5];
-        const int at = lane & 31;
+        const double total = __builtin_bit_cast(double, (unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), 31) << 32 |
+                                                            (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, 31));
+        ScanBlockSizes &to = sizes[wave];
+        const int at = lane & 31;                    // (the halves of the wavefront write the same)
         to.e[at] = (float)upto;
         to.dt[at] = dt;
         to.w[at] = __builtin_amdgcn_exp2f((float)(total - upto)) * dt;
         to.f[at] = __builtin_amdgcn_exp2f((float)upto);
-        if (at == 0) {
+        if (lane == 0) {
             to.total = (float)total;
             to.factor = __builtin_amdgcn_exp2f((float)total);
         }
@@ -253,21 +251,14 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
     // Block [t, t + Q) up to t1, number n of its sequence, which lies in buffer `now`.
     auto block = [&](int t, int t1, int n, auto now_) SCAN_INLINE {
         constexpr int now = decltype(now_)::value;
-        // (behind the youngest loads there are the two stores of the block before)
-        if constexpr (WHOLE) scan_barrier<Y ? 2 : 0>();
+        if constexpr (WHOLE) scan_barrier<0>();
         else scan_barrier_lds();
-        // The gate and dt have come with the block's rows; the compiler, which does not count those, must not wait for them later.
-        bf16x4_t z[2];
-        if constexpr (WHOLE && Y) {
-            asm volatile("" : "+v"(gate[0]), "+v"(gate[1]));
-            z[0] = __builtin_bit_cast(bf16x4_t, gate[0]);
-            z[1] = __builtin_bit_cast(bf16x4_t, gate[1]);
-        }
-        const bool more = t + Q < t1;
+        // (dt has come with the block's rows; the compiler, which does not count those, must not wait for it later)
         asm volatile("" : "+v"(raw));
-        if (more) {
+        if (n > 0) leave(t - Q, t1, std::integral_constant<int, 1 - now>{});
+        if (t + Q < t1) {
+            asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");               // (y has been read)
             bring(t + Q, t1, std::integral_constant<int, 1 - now>{});
-            bring_gate(t + Q, t1);
         }
         if (n % kScanAhead == 0) {
             put_sizes(raw, t, t1);
@@ -275,7 +266,8 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
             scan_barrier_lds();
         }
         const ScanBlockSizes &sz = sizes[n % kScanAhead];
-        const bf16 *const xs = sx[now], *const bs = sb[now], *const cs = sc[Y ? now : 0];
+        bf16 *const xs = sx[now];
+        const bf16 *const bs = sb[now], *const cs = sc[Y ? now : 0];
         sum_of += sz.total;
         const int q4 = l16 >> 2, c4 = l16 & 3;
         f32x4_t acc[2];
@@ -392,7 +384,6 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
         }
         if constexpr (Y) {
             const int p = wave * 16 + 4 * g4;
-            const auto rs = rows_of(out, c.ld_out, t, t1);
             float y[2][4];
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt) {
@@ -403,14 +394,15 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
             if constexpr (WHOLE) {
                 if (c.z)
 #pragma unroll
-                    for (int tt = 0; tt < 2; ++tt)
+                    for (int tt = 0; tt < 2; ++tt) {
+                        const bf16x4_t z = *reinterpret_cast<const bf16x4_t *>(sg[now] + scan_chunk<8>(tt * 16 + l16, p >> 3) + (p & 4));
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) y[tt][i] *= silu((float)z[tt][i]);
+                        for (int i = 0; i < 4; ++i) y[tt][i] *= silu((float)z[i]);
+                    }
 #pragma unroll
                 for (int tt = 0; tt < 2; ++tt) {
                     const bf16x2_t lo = __builtin_convertvector(f32x2_t{y[tt][0], y[tt][1]}, bf16x2_t), hi = __builtin_convertvector(f32x2_t{y[tt][2], y[tt][3]}, bf16x2_t);
-                    __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)}, rs,
-                                                          (int)(y_col + (tt * 16 + l16) * (uint32_t)c.ld_out * 2), 0, 0);
+                    *reinterpret_cast<bf16x4_t *>(xs + scan_chunk<8>(tt * 16 + l16, p >> 3) + (p & 4)) = __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
                 }
             } else {
 #pragma unroll
@@ -432,7 +424,6 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
     auto run = [&](int t0, int t1, float &sum) SCAN_INLINE {
         __syncthreads();                             // (nobody reads what an earlier call has left)
         bring(t0, t1, std::integral_constant<int, 0>{});
-        bring_gate(t0, t1);
         raw = raw_of(t0, t1);
         if constexpr (Y)                             // the tile above the diagonal
             if (tid < 32) *reinterpret_cast<bf16x8_t *>(sm + scan_chunk<4>(tid & 15, 2 + (tid >> 4))) = bf16x8_t{};
@@ -440,9 +431,17 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
         sum_of = 0.0f;
         for (int t = t0, n = 0;; n += 2) {
             block(t, t1, n, std::integral_constant<int, 0>{});
-            if ((t += Q) >= t1) break;
+            if ((t += Q) >= t1) {
+                scan_barrier_lds();
+                leave(t - Q, t1, std::integral_constant<int, 0>{});
+                break;
+            }
             block(t, t1, n + 1, std::integral_constant<int, 1>{});
-            if ((t += Q) >= t1) break;
+            if ((t += Q) >= t1) {
+                scan_barrier_lds();
+                leave(t - Q, t1, std::integral_constant<int, 1>{});
+                break;
+            }
         }
         sum += sum_of;
     };
