@@ -139,7 +139,7 @@ static int scan_rows(int32_t dtype, int32_t N)
 static ScanPlan scan_plan(int32_t dtype, const HeadSizes &s, int64_t tokens, int32_t longest)
 {
     ScanPlan p{(int)cdiv(s.P, scan_rows(dtype, s.N)), 0, 0};
-    const int64_t chip = dtype == SRM_BF16 ? 768 : 2048, units = (int64_t)s.H * p.parts, least = 64;
+    const int64_t chip = dtype == SRM_BF16 ? (getenv("CHIP") ? atoi(getenv("CHIP")) : 768) : 2048, units = (int64_t)s.H * p.parts, least = 64;
     const int64_t seg = std::max(least, cdiv(cdiv(tokens * units, chip), 64) * 64);
     if (longest > 2 * seg + 2 * least) {
         p.seg = (int)seg;
@@ -169,6 +169,10 @@ static int launch_scan(const void *d_xbc, void *d_out, const ScanCall &c, const 
         hipLaunchKernelGGL(WHOLE, grid, dim3(threads), 0, st, x, out, c);
     } else {
         hipLaunchKernelGGL(CARRY, grid, dim3(threads), 0, st, x, out, c);
+        HIP_TRY(hipGetLastError());
+        const int head_size = c.P * c.N;
+        hipLaunchKernelGGL(selective_scan_join_kernel, grid_of(cdiv((int64_t)c.H * head_size, 256)), dim3(256), 0, st, c.carry, c.decay, p.segments - 1, c.H,
+                           head_size);
         HIP_TRY(hipGetLastError());
         hipLaunchKernelGGL(SEGMENTS, grid, dim3(threads), 0, st, x, out, c);
     }

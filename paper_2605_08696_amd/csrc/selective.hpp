@@ -6,8 +6,9 @@
 // Work over time.  A work-group takes one head (a part of its P rows) of one sequence from its first token to its last, the state in
 // registers.  Where there are too few of those, the packed tokens are cut into segments of equal length, whatever sequences they hold:
 // a first pass leaves, for each segment that a sequence runs on from, the state at its end that the segment itself brings (`carry`) and
-// the factor by which it decays what came before (`decay`); the second pass starts each segment from the decayed sum of the carries in
-// front of it and writes the outputs.
+// the factor by which it decays what came before (`decay`); a second one makes of these the states at the segments' ends; the third starts
+// each segment from the one in front of it and writes the outputs.  (Joined by the third pass itself, every segment adding up all carries in
+// front of it, 16384 tokens of 32 heads took 146 us instead of 130.)
 #pragma once
 #include "conv.hpp"
 
@@ -69,12 +70,12 @@ __device__ __forceinline__ float lanes_sum(float v)
     return v;
 }
 
-// What a work-group does over time, whatever its kernel: `work` is a sequence or a segment; clear, load(from), store(to) and
-// add(from, scale) act on the state that it holds of a head's part (whose first element lies at head_at in a slot), run(t0, t1, sum) takes
+// What a work-group does over time, whatever its kernel: `work` is a sequence or a segment; clear, load(from) and store(to) act on the
+// state that it holds of a head's part (whose first element lies at head_at in a slot), run(t0, t1, sum) takes
 // it over tokens of one sequence and adds their decay exponents to sum, zeros(t0, t1) writes an idle sequence's output.
-template <int MODE, typename Clear, typename Load, typename Store, typename Add, typename Run, typename Zeros>
+template <int MODE, typename Clear, typename Load, typename Store, typename Run, typename Zeros>
 __device__ __forceinline__ void scan_drive(const ScanCall &c, int64_t work, int h, int p0, int64_t head_at, int lane, Clear &&clear, Load &&load,
-                                           Store &&store, Add &&add, Run &&run, Zeros &&zeros)
+                                           Store &&store, Run &&run, Zeros &&zeros)
 {
     const int64_t slot_size = (int64_t)c.H * c.P * c.N;
     auto slot_of = [&](const Sequence &s) { return c.state + s.slot * slot_size + head_at; };
@@ -100,7 +101,7 @@ __device__ __forceinline__ void scan_drive(const ScanCall &c, int64_t work, int 
         }
         run(max(s.begin, t0), t1, sum);
         store(c.carry + at);
-        if (threadIdx.x == 0 && p0 == 0) c.decay[work * c.H + h] = __builtin_amdgcn_exp2f(sum);
+        if (threadIdx.x == 0 && p0 == 0) c.decay[work * c.H + h] = s.begin >= t0 ? -1.0f : __builtin_amdgcn_exp2f(sum);
     } else {
         const int t0 = c.seqs.lo + (int)work * c.seg, t1 = min(t0 + c.seg, c.seqs.hi);
         int n = packed_find(c.seqs, t0, lane);
@@ -116,17 +117,38 @@ __device__ __forceinline__ void scan_drive(const ScanCall &c, int64_t work, int 
                 if (t == s.begin) {
                     if (s.slot >= 0 && s.pos > 0) load(s.end > t1 ? c.held + work * slot_size + head_at : slot_of(s));
                 } else {
-                    float scale = 1.0f;
-                    const int64_t first = (s.begin - c.seqs.lo) / c.seg;
-                    for (int64_t j = work - 1; j >= first; --j) {   // (a scale of 0 too: what is not finite stays so)
-                        add(c.carry + j * slot_size + head_at, scale);
-                        if (j > first) scale *= c.decay[j * c.H + h];
-                    }
+                    load(c.carry + (work - 1) * slot_size + head_at);
                 }
                 run(t, e, sum);
                 if (e == s.end && s.slot >= 0) store(slot_of(s));
             }
             t = e;
+        }
+    }
+}
+
+// The states at the segments' ends, in the carries' place, an element a thread.  (Decay -1: the sequence begins in the segment.  What a
+// segment leaves from which no sequence runs on is not read.)
+__global__ void __launch_bounds__(256)
+selective_scan_join_kernel(float *__restrict__ carry, const float *__restrict__ decay, int segments, int H, int head_size)
+{
+    const int64_t slot_size = (int64_t)H * head_size, i = (int64_t)work_group() * 256 + threadIdx.x;
+    if (i >= slot_size) return;
+    const float *d = decay + i / head_size;
+    float *at = carry + i, s = 0.0f;
+    constexpr int AHEAD = 4;
+    for (int k = 0; k < segments; k += AHEAD) {
+        float v[AHEAD], f[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const int64_t q = min(k + j, segments - 1);
+            v[j] = at[q * slot_size];
+            f[j] = d[q * H];
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            s = f[j] < 0.0f ? v[j] : fmaf(f[j], s, v[j]);
+            if (k + j < segments) at[(k + j) * slot_size] = s;
         }
     }
 }
@@ -232,8 +254,7 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
     };
     auto load = [&](const float *from) { each([&](float &v, int64_t at) { v = from[at]; }); };
     auto store = [&](float *to) { each([&](float &v, int64_t at) { to[at] = v; }); };
-    auto add = [&](const float *from, float scale) { each([&](float &v, int64_t at) { v = fmaf(scale, from[at], v); }); };
-    scan_drive<MODE>(c, work, h, p0, head_at, lane, clear, load, store, add, run, zeros);
+    scan_drive<MODE>(c, work, h, p0, head_at, lane, clear, load, store, run, zeros);
 }
 
 // ------------------------------------------------------------------ single tokens

@@ -142,13 +142,6 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
         return v;
     };
     auto load = [&](const float *from) SCAN_INLINE { each([&](f32x4_t &v, int64_t at, int many) SCAN_INLINE { v = four(from + at, many); }); };
-    auto add = [&](const float *from, float scale) SCAN_INLINE {
-        each([&](f32x4_t &v, int64_t at, int many) SCAN_INLINE {
-            const f32x4_t w = four(from + at, many);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = fmaf(scale, w[i], v[i]);
-        });
-    };
     auto store = [&](float *to) SCAN_INLINE {
         each([&](f32x4_t &v, int64_t at, int many) SCAN_INLINE {
             if (WHOLE || many == 4) *reinterpret_cast<f32x4_any *>(to + at) = v;
@@ -349,12 +342,8 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
         if constexpr (Y) {
             scan_barrier_lds();
             // An x that is not finite would make NaN of the tokens in front of it too (0 times it): such are left out here and added
-            // where they belong, one by one.
-            uint32_t odd = 0;
-            const u32x4_t u = __builtin_bit_cast(u32x4_t, xf);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) odd |= (u[i] & 0x7f807f80u) + 0x00800080u;
-            const bool any = __ballot((odd & 0x80008000u) != 0) != 0;
+            // where they belong, one by one.  One of this lane's column has made a NaN of all of the column's state.
+            const bool any = __ballot(!(fabsf(S[0][0]) < INFINITY)) != 0;
             bf16x8_t xg = xf;
             if (any) {
 #pragma unroll
@@ -445,5 +434,5 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
         }
         sum += sum_of;
     };
-    scan_drive<MODE>(c, work, h, p0, head_at, lane, clear, load, store, add, run, zeros);
+    scan_drive<MODE>(c, work, h, p0, head_at, lane, clear, load, store, run, zeros);
 }
