@@ -3,8 +3,12 @@
 // A slot keeps the last W rows of x, position p in row p % W: a single token then overwrites the one row that none of its taps reads, which
 // lets the kernel of single tokens read and write the ring without an order among its work-groups.
 //
-// A thread takes eight channels of R consecutive tokens: R + W - 1 loads without a branch between them, then the products from registers.
-// What bounds it is memory: x is read once (the W - 1 rows in front of a run come from the caches) and out written once.
+// A thread takes eight channels of a run of tokens, eight tokens at a time: their rows' loads are in flight together, without a branch
+// between them, while the eight in front of them are worked on, and the filter's W - 1 rows in front of a row stay in registers.  A sequence
+// that begins inside a run is a piece of its own; its first W - 1 tokens, whose taps reach into the slot's ring, all belong to the run that
+// holds the first of them, in which the same thread writes the ring behind them.
+// What bounds it: memory (x is read once, out written once) and, for bf16, the instructions of the activation (five for a value, two of them
+// at a quarter of the rate).
 #pragma once
 #include "fp8.hpp"
 #include "packed.hpp"
@@ -15,63 +19,54 @@ struct ConvCall {
     Packed seqs;
     int64_t ldx, ld_out;
     const float *weight, *bias;
-    int channels, units, per_run, silu;              // units of eight channels; lanes that share a run of tokens (a power of two)
+    int channels, units, per_run, silu, run;         // units of eight channels; lanes that share a run (a power of two), tokens of a run
     int64_t runs;
     void *ring;
 };
 
 __device__ __forceinline__ float silu(float v) { return v * __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
 
-template <typename T>
-__device__ __forceinline__ void store_part(T *p, int n, const float (&v)[8])
-{
-    float w[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = v[i];
-    store8(p, n, w);
-}
-
-template <typename T, int W, int R>
+template <typename T, int W>
 __global__ void __launch_bounds__(256)
 causal_conv_kernel(const T *__restrict__ x, T *__restrict__ out, ConvCall c)
 {
+    constexpr int R = 8, HIST = W > 1 ? W - 1 : 1;
     const int lane = threadIdx.x & 63;
-    const int64_t wave = (int64_t)work_group() * 4 + (threadIdx.x >> 6);
+    const int64_t wave = (int64_t)work_group() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // a wavefront: 64 units of one run, or, of few channels, several runs
     const int groups = c.units > 64 ? (c.units + 63) >> 6 : 1, shift = __builtin_ctz(c.per_run);
-    const int64_t run = wave / groups * (64 >> shift) + (c.units > 64 ? 0 : lane >> shift);
+    const int64_t run0 = wave / groups * (64 >> shift), run = run0 + (lane >> shift);
     const int unit = (int)(wave % groups) * 64 + (lane & (c.per_run - 1)), col = unit * 8, C = c.channels;
+    if (run0 >= c.runs) return;
     const bool there = run < c.runs && unit < c.units;
-    if (!__ballot(there)) return;
-    const int t0 = there ? c.seqs.lo + (int)(run * R) : c.seqs.lo, n_cols = min(8, C - col);
+    const int t0 = c.seqs.lo + (int)min(run, c.runs - 1) * c.run, t1 = min(t0 + c.run, c.seqs.hi), n_cols = min(8, C - col);
 
     float w[W][8], b[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int ch = min(max(col, 0) + i, C - 1);
+        const int ch = min(col + i, C - 1);
         b[i] = c.bias ? c.bias[ch] : 0.0f;
 #pragma unroll
         for (int k = 0; k < W; ++k) w[k][i] = c.weight[(int64_t)ch * W + k];
     }
-    // this lane's sequence: by all lanes together where they share a run or few sequences do, else by halves
+    // this lane's sequence: between those of the wavefront's first and last run
     int n = 0;
     if (c.seqs.n > 1) {
-        if (c.units > 64 || c.per_run == 64) {
-            n = packed_find(c.seqs, __builtin_amdgcn_readfirstlane(t0), lane);
-        } else {
-            int lo = 0, hi = c.seqs.n;               // the last n in [lo, hi) that begins at or before t0
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (c.seqs.offsets[mid] <= t0) lo = mid;
-                else hi = mid;
+        const int first = __builtin_amdgcn_readfirstlane(t0), last = __builtin_amdgcn_readlane(t0, 63);
+        n = packed_find(c.seqs, first, lane);
+        if (last != first) {
+            int up = packed_find(c.seqs, last, lane) + 1;
+            while (up - n > 1) {
+                const int mid = (n + up) >> 1;
+                if (c.seqs.offsets[mid] <= t0) n = mid;
+                else up = mid;
             }
-            n = lo;
         }
     }
     if (!there) return;
-    auto load = [&](const T *row, float (&v)[8]) {
-        raw8_values(raw8(row, col, C), v);
-        const int late = C >= 8 ? col + 8 - C : 0;   // the row's last eight: moved to their places
+    const int late = C >= 8 ? max(col + 8 - C, 0) : 0;                  // the row's last eight are moved to their places
+    auto values = [&](const Raw8<T> &raw, float (&v)[8]) {
+        raw8_values(raw, v);
         if (late > 0) {
 #pragma unroll
             for (int s = 4; s >= 1; s >>= 1)
@@ -80,87 +75,92 @@ causal_conv_kernel(const T *__restrict__ x, T *__restrict__ out, ConvCall c)
                     if (late & s) v[i] = i + s < 8 ? v[i + s] : 0.0f;
         }
     };
-    auto row_of = [&](int t) { return x + (int64_t)t * c.ldx; };
-    auto put = [&](int t, float (&acc)[8]) {
-        if (c.silu) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) acc[i] = silu(acc[i]);
-        }
-        store_part(out + (int64_t)t * c.ld_out + col, n_cols, acc);
+    auto put = [&](int t, float (&v)[8]) {
+        T *to = out + (int64_t)t * c.ld_out + col;
+        store8(to, n_cols, v);
     };
+    auto row_of = [&](int t) { return x + (int64_t)t * c.ldx; };
 
-    Sequence s = packed_sequence(c.seqs, n);
-    const int t1 = min(t0 + R, c.seqs.hi);
-    if (t0 - max(W - 1, 1) >= s.begin && t0 + R <= s.end && s.pos >= 0) {
-        // the run and the rows in front of it lie in one sequence
-        Raw8<T> raw[R + W - 1];
-#pragma unroll
-        for (int j = 0; j < R + W - 1; ++j) raw[j] = raw8(row_of(t0 - (W - 1) + j), col, C);
-        float v[W][8];
-        auto values = [&](int j, float (&to)[8]) {
-            raw8_values(raw[j], to);
-            const int late = C >= 8 ? col + 8 - C : 0;
-            if (late > 0) {
-#pragma unroll
-                for (int sh = 4; sh >= 1; sh >>= 1)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (late & sh) to[i] = i + sh < 8 ? to[i + sh] : 0.0f;
-            }
-        };
-#pragma unroll
-        for (int j = 0; j < W - 1; ++j) values(j, v[j]);
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-            values(W - 1 + j, v[(W - 1 + j) % W]);
-            float acc[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                acc[i] = b[i];
-#pragma unroll
-                for (int k = 0; k < W; ++k) acc[i] = fmaf(w[k][i], v[(j + k) % W][i], acc[i]);
-            }
-            put(t0 + j, acc);
-        }
-        return;
-    }
-    // A sequence begins or ends here.  The W - 1 first tokens of a sequence, whose taps reach into the slot's ring, belong to the run that
-    // holds the first of them, in which the same thread writes the ring behind them.
-    T *const ring_all = static_cast<T *>(c.ring);
     for (int t = t0; t < t1;) {
+        Sequence s = packed_sequence(c.seqs, n);
         while (t >= s.end && n + 1 < c.seqs.n) s = packed_sequence(c.seqs, ++n);
         if (t >= s.end) break;                       // (offsets that are not the host's)
-        const bool starts = t == s.begin;
-        if (!starts && t - s.begin < W - 1 && s.begin < t0) { ++t; continue; }
-        T *ring = s.slot >= 0 && ring_all ? ring_all + s.slot * W * C : nullptr;
-        const int until = starts && W > 2 ? min(s.end, s.begin + W - 1) : t + 1;
-        for (int u = t; u < until; ++u) {
-            float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-            if (s.pos >= 0) {
+        int u = t, until = min(s.end, t1);
+        if (s.begin < t0 && t - s.begin < W - 1) u = min(until, s.begin + W - 1);      // an earlier run's
+        const bool starts = u == s.begin;
+        if (starts) until = max(until, min(s.end, s.begin + W - 1));
+        t = max(until, t + 1);
+        if (u >= until) continue;
+        if (s.pos < 0) {
+            for (; u < until; ++u) {
+                float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                put(u, zero);
+            }
+            continue;
+        }
+        T *ring = s.slot >= 0 && c.ring ? static_cast<T *>(c.ring) + s.slot * W * C : nullptr;
+        Raw8<T> next[R], hist[HIST];
+        bool none[HIST];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) acc[i] = b[i];
+        for (int j = 0; j < W - 1; ++j) {
+            const int at = u - (W - 1) + j;
+            const int64_t p = (int64_t)s.pos + at - s.begin;
+            const bool old = at < s.begin;
+            none[j] = old && (p < 0 || !ring);
+            hist[j] = raw8(none[j] || !old ? row_of(max(at, s.begin)) : ring + p % W * C, col, C);
+        }
 #pragma unroll
-                for (int k = 0; k < W; ++k) {
-                    const int at = u - (W - 1) + k;
-                    const int64_t p = (int64_t)s.pos + at - s.begin;
-                    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                    if (at >= s.begin) load(row_of(at), v);
-                    else if (p >= 0 && ring) load(ring + p % W * C, v);
+        for (int j = 0; j < R; ++j) next[j] = raw8(row_of(min(u + j, until - 1)), col, C);
+        float v[W][8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) acc[i] = fmaf(w[k][i], v[i], acc[i]);
-                }
-                put(u, acc);
-            } else {
-                store_part(out + (int64_t)u * c.ld_out + col, n_cols, acc);
+        for (int j = 0; j < W - 1; ++j) {
+            values(hist[j], v[j]);
+            if (none[j]) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[j][i] = 0.0f;
             }
         }
-        if (starts && ring && s.pos >= 0)
-            for (int u = max(s.begin, s.end - W); u < s.end; ++u) {
-                const int64_t p = (int64_t)s.pos + u - s.begin;
-                float v[8];
-                load(row_of(u), v);
-                store_part(ring + p % W * C + col, n_cols, v);
+        if (starts && ring)
+            for (int e = max(s.begin, s.end - W); e < s.end; ++e) {
+                float q[8];
+                values(raw8(row_of(e), col, C), q);
+                store8(ring + ((int64_t)s.pos + e - s.begin) % W * C + col, n_cols, q);
             }
-        t = until;
+        for (; u < until; u += R) {
+            Raw8<T> now[R];
+#pragma unroll
+            for (int j = 0; j < R; ++j) now[j] = next[j];
+            if (u + R < until) {
+#pragma unroll
+                for (int j = 0; j < R; ++j) next[j] = raw8(row_of(min(u + R + j, until - 1)), col, C);
+            }
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                values(now[j], v[(W - 1 + j) % W]);
+                float acc[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    acc[i] = b[i];
+#pragma unroll
+                    for (int k = 0; k < W; ++k) acc[i] = fmaf(w[k][i], v[(j + k) % W][i], acc[i]);
+                }
+                if (c.silu) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[i] = silu(acc[i]);
+                }
+                if (u + j < until) put(u + j, acc);
+            }
+            if constexpr (R % W != 0) {              // the window begins at its first row again
+                float q[HIST][8];
+#pragma unroll
+                for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) q[j][i] = v[(R + j) % W][i];
+#pragma unroll
+                for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[j][i] = q[j][i];
+            }
+        }
     }
 }

@@ -45,13 +45,16 @@ static int check_packed(const char *who, const int32_t *h_offsets, const int32_t
 }
 
 // ------------------------------------------------------------------ the short convolution
+// Runs of 32 tokens, over which a thread's filter (32 W bytes) is read once, as long as they are two rounds of the chip's wavefronts.
 template <typename T, int W>
 static void launch_conv(const void *d_x, void *d_out, ConvCall c, int64_t tokens, hipStream_t st)
 {
-    constexpr int R = 8;
-    c.runs = cdiv(tokens, R);
-    const int64_t waves = c.units > 64 ? c.runs * cdiv(c.units, 64) : cdiv(c.runs, 64 / c.per_run);
-    hipLaunchKernelGGL((causal_conv_kernel<T, W, R>), grid_of(cdiv(waves, 4)), dim3(256), 0, st, static_cast<const T *>(d_x), static_cast<T *>(d_out), c);
+    auto waves = [&]() { return c.units > 64 ? c.runs * cdiv(c.units, 64) : cdiv(c.runs, 64 / c.per_run); };
+    for (c.run = 32;; c.run /= 2) {
+        c.runs = cdiv(tokens, c.run);
+        if (c.run == 8 || waves() >= 8192) break;
+    }
+    hipLaunchKernelGGL((causal_conv_kernel<T, W>), grid_of(cdiv(waves(), 4)), dim3(256), 0, st, static_cast<const T *>(d_x), static_cast<T *>(d_out), c);
 }
 template <typename T>
 static void conv(int width, const void *d_x, void *d_out, const ConvCall &c, int64_t tokens, hipStream_t st)
@@ -139,7 +142,7 @@ static int scan_rows(int32_t dtype, int32_t N)
 static ScanPlan scan_plan(int32_t dtype, const HeadSizes &s, int64_t tokens, int32_t longest)
 {
     ScanPlan p{(int)cdiv(s.P, scan_rows(dtype, s.N)), 0, 0};
-    const int64_t chip = dtype == SRM_BF16 ? (getenv("CHIP") ? atoi(getenv("CHIP")) : 768) : 2048, units = (int64_t)s.H * p.parts, least = 64;
+    const int64_t chip = dtype == SRM_BF16 ? 768 : 2048, units = (int64_t)s.H * p.parts, least = 64;
     const int64_t seg = std::max(least, cdiv(cdiv(tokens * units, chip), 64) * 64);
     if (longest > 2 * seg + 2 * least) {
         p.seg = (int)seg;

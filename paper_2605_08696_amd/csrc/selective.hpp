@@ -154,7 +154,8 @@ selective_scan_join_kernel(float *__restrict__ carry, const float *__restrict__ 
 }
 
 // One wavefront takes PR rows of P a lane, NL lanes with NR elements of N each: 64 / NL * PR rows, NL NR >= N.  Sixteen tokens at a time
-// are brought to LDS; then for every token each lane updates its PR x NR elements (multiply, multiply-add) and adds their products with C.
+// are brought to LDS, the next sixteen on their way in registers; then for every token each lane updates its PR x NR elements (multiply,
+// multiply-add) and adds their products with C.
 // What bounds it: three vector instructions for each element of state and token.
 template <typename T, int NL, int NR, int MODE>
 __global__ void __launch_bounds__(64)
@@ -188,26 +189,49 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
             for (int j = 0; j < NR; ++j)
                 if (lp * PR + i < np && ln * NR + j < N) fn(S[i][j], (int64_t)(lp * PR + i) * N + ln * NR + j);
     };
+    // Sixteen tokens' rows in registers: element 64 i + lane of [TT][NP] or [TT][PW] (rows behind the last are the last one again).
+    constexpr int LB = TT * NP / 64, LX = TT * PW / 64;
+    float rb[LB], rc[MODE != SCAN_CARRY ? LB : 1], rx[LX], raw = 0.0f;
+    const T *const rows = xbc + (int64_t)c.H * P + (int64_t)g * N, *const xs = xbc + (int64_t)h * P + p0;
+    const int64_t to_c = (int64_t)c.G * N;
+    auto fetch = [&](int t, int t1) {
+#pragma unroll
+        for (int i = 0; i < LB; ++i) {
+            const int e = 64 * i + lane, n = e % NP;
+            const T *row = rows + (int64_t)min(t + e / NP, t1 - 1) * c.ld + (n < N ? n : 0);
+            rb[i] = (float)row[0];
+            if constexpr (MODE != SCAN_CARRY) rc[i] = (float)row[to_c];
+        }
+#pragma unroll
+        for (int i = 0; i < LX; ++i) {
+            const int e = 64 * i + lane, p = e % PW;
+            rx[i] = (float)xs[(int64_t)min(t + e / PW, t1 - 1) * c.ld + (p < np ? p : 0)];
+        }
+        raw = dt_raw(c.dt, min(t + lane % TT, t1 - 1), h);
+    };
     // Tokens [t0, t1) of one sequence; adds their decay exponents to `sum`.
     auto run = [&](int t0, int t1, float &sum) {
+        fetch(t0, t1);
         for (int t = t0; t < t1; t += TT) {
             const int nt = min(TT, t1 - t);
             __syncthreads();
-            for (int e = lane; e < nt * NP; e += 64) {
-                const int r = e / NP, n = e % NP;
-                const T *row = xbc + (int64_t)(t + r) * c.ld + (int64_t)c.H * P + (int64_t)g * N;
-                sb[r][n] = n < N ? (float)row[n] : 0.0f;
-                if (MODE != SCAN_CARRY) sc[r][n] = n < N ? (float)row[(int64_t)c.G * N + n] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < LB; ++i) {
+                const int e = 64 * i + lane, n = e % NP;
+                sb[e / NP][n] = n < N ? rb[i] : 0.0f;
+                if constexpr (MODE != SCAN_CARRY) sc[e / NP][n] = n < N ? rc[i] : 0.0f;
             }
-            for (int e = lane; e < nt * PW; e += 64) {
-                const int r = e / PW, p = e % PW;
-                sx[r][p] = p < np ? (float)xbc[(int64_t)(t + r) * c.ld + (int64_t)h * P + p0 + p] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < LX; ++i) {
+                const int e = 64 * i + lane;
+                sx[e / PW][e % PW] = e % PW < np ? rx[i] : 0.0f;
             }
-            if (lane < nt) {
-                const float dt = dt_of(c.dt, dt_raw(c.dt, t + lane, h), bias), ex = decay_exponent(dt, a);
+            if (lane < TT) {
+                const float dt = dt_of(c.dt, raw, bias), ex = decay_exponent(dt, a);
                 sd[lane] = make_float2(__builtin_amdgcn_exp2f(ex), dt);
                 if (MODE == SCAN_CARRY) sb[lane][NP] = ex;
             }
+            if (t + TT < t1) fetch(t + TT, t1);
             __syncthreads();
             for (int r = 0; r < nt; ++r) {
                 const float2 d = sd[r];
