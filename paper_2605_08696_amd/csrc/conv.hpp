@@ -3,8 +3,8 @@
 // A slot keeps the last W rows of x, position p in row p % W: a single token then overwrites the one row that none of its taps reads, which
 // lets the kernel of single tokens read and write the ring without an order among its work-groups.
 //
-// A thread takes eight channels of a run of tokens, eight tokens at a time: their rows' loads are in flight together, without a branch
-// between them, while the eight in front of them are worked on, and the filter's W - 1 rows in front of a row stay in registers.  A sequence
+// A thread takes eight channels of a run of tokens, R tokens at a time: their rows' loads are in flight together, without a branch
+// between them, while the R in front of them are worked on, and the filter's W - 1 rows in front of a row stay in registers.  A sequence
 // that begins inside a run is a piece of its own; its first W - 1 tokens, whose taps reach into the slot's ring, all belong to the run that
 // holds the first of them, in which the same thread writes the ring behind them.
 // What bounds it: memory (x is read once, out written once) and, for bf16, the instructions of the activation (five for a value, two of them
@@ -26,11 +26,11 @@ struct ConvCall {
 
 __device__ __forceinline__ float silu(float v) { return v * __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
 
-template <typename T, int W>
+template <typename T, int W, int R>
 __global__ void __launch_bounds__(256)
 causal_conv_kernel(const T *__restrict__ x, T *__restrict__ out, ConvCall c)
 {
-    constexpr int R = 8, HIST = W > 1 ? W - 1 : 1;
+    constexpr int HIST = W > 1 ? W - 1 : 1;
     const int lane = threadIdx.x & 63;
     const int64_t wave = (int64_t)work_group() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // a wavefront: 64 units of one run, or, of few channels, several runs

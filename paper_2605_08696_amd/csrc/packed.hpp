@@ -15,8 +15,13 @@ struct Sequence {
 __device__ __forceinline__ Sequence packed_sequence(const Packed &c, int n)
 {
     Sequence s;
-    s.begin = min(max(c.offsets[n], c.lo), c.hi);
-    s.end = min(max(c.offsets[n + 1], s.begin), c.hi);
+    if (c.n == 1) {                                  // (one trip to memory less)
+        s.begin = c.lo;
+        s.end = c.hi;
+    } else {
+        s.begin = min(max(c.offsets[n], c.lo), c.hi);
+        s.end = min(max(c.offsets[n + 1], s.begin), c.hi);
+    }
     s.pos = c.pos ? c.pos[n] : 0;
     const int64_t slot = c.slot ? c.slot[n] : n;
     s.slot = slot >= 0 && slot < c.slots ? slot : -1;

@@ -18,6 +18,7 @@ static bool misaligned(const void *p, unsigned to) { return reinterpret_cast<uin
 static bool known(int32_t dtype) { return dtype == SRM_BF16 || dtype == SRM_FP32; }
 static unsigned size_of(int32_t dtype) { return dtype == SRM_BF16 ? 2 : 4; }
 static const char *const kNotWhole = "an operand does not lie at a whole element";
+constexpr int kChipCus = 256;
 constexpr int64_t kMaxRows = 1ll << 30, kMaxBlocks = 1ll << 31;
 
 // ------------------------------------------------------------------ packed sequences
@@ -45,16 +46,27 @@ static int check_packed(const char *who, const int32_t *h_offsets, const int32_t
 }
 
 // ------------------------------------------------------------------ the short convolution
-// Runs of 32 tokens, over which a thread's filter (32 W bytes) is read once, as long as they are two rounds of the chip's wavefronts.
+// Runs of 32 tokens, over which a thread's filter (32 W bytes) is read once, as long as they are two rounds of the chip's wavefronts; four
+// tokens at a time where the shortest runs are less than one.  (Four | eight, us: 37 x 2304 7.7 | 8.9, 300 x 2304 10.4 | 12.6, 32768 x 4352 135 |
+// 135, fp32 16384 x 4352 141 | 128, 4000 x 2304 of eight taps 39 | 32.)
 template <typename T, int W>
 static void launch_conv(const void *d_x, void *d_out, ConvCall c, int64_t tokens, hipStream_t st)
 {
-    auto waves = [&]() { return c.units > 64 ? c.runs * cdiv(c.units, 64) : cdiv(c.runs, 64 / c.per_run); };
-    for (c.run = 32;; c.run /= 2) {
-        c.runs = cdiv(tokens, c.run);
-        if (c.run == 8 || waves() >= 8192) break;
+    auto waves = [&](int run) {
+        c.runs = cdiv(tokens, c.run = run);
+        return c.units > 64 ? c.runs * cdiv(c.units, 64) : cdiv(c.runs, 64 / c.per_run);
+    };
+    const bool few = waves(8) < 4096;
+    int64_t n;
+    if (few) {
+        n = waves(4);
+    } else {
+        int run = 32;
+        while (run > 8 && waves(run) < 8192) run /= 2;
+        n = waves(run);
     }
-    hipLaunchKernelGGL((causal_conv_kernel<T, W>), grid_of(cdiv(waves(), 4)), dim3(256), 0, st, static_cast<const T *>(d_x), static_cast<T *>(d_out), c);
+    hipLaunchKernelGGL((few ? causal_conv_kernel<T, W, 4> : causal_conv_kernel<T, W, 8>), grid_of(cdiv(n, 4)), dim3(256), 0, st, static_cast<const T *>(d_x),
+                       static_cast<T *>(d_out), c);
 }
 template <typename T>
 static void conv(int width, const void *d_x, void *d_out, const ConvCall &c, int64_t tokens, hipStream_t st)
@@ -88,7 +100,7 @@ extern "C" int srm_causal_conv(int32_t dtype, const void *d_x, int64_t ldx, cons
     if (misaligned(d_x, size) || misaligned(d_out, size) || misaligned(d_state, size) || misaligned(d_weight, 4) || misaligned(d_bias, 4))
         return fail(SRM_EINVAL, "%s: %s", who, kNotWhole);
     const int64_t tokens = c.seqs.hi - c.seqs.lo;
-    if (cdiv(tokens, 8) * cdiv(channels, 512) >= kMaxBlocks) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    if (cdiv(tokens, 4) * cdiv(channels, 512) >= kMaxBlocks) return fail(SRM_EINVAL, "%s: sizes out of range", who);
     if (tokens == 0) return SRM_OK;
     c.ldx = ldx;
     c.ld_out = ld_out;
@@ -261,21 +273,24 @@ extern "C" int srm_selective_scan(int32_t dtype, const void *d_xbc, int64_t ld_x
 }
 
 // ------------------------------------------------------------------ single tokens
-template <typename T, int NL, int U>
+// Four wavefronts of a work-group share a head of a request where its state takes them, else each has one of its own.
+template <typename T, int NL, int U, int WAVES>
 static void launch_step(const void *d_xbc, void *d_out, StepCall c, hipStream_t st)
 {
-    c.parts = (int)cdiv(c.P, 4 * (64 / NL) * U);
-    hipLaunchKernelGGL((selective_step_kernel<T, NL, U>), grid_of(c.rows * c.H * c.parts), dim3(256), 0, st, static_cast<const T *>(d_xbc),
-                       static_cast<T *>(d_out), c);
+    c.parts = (int)cdiv(c.P, WAVES * (64 / NL) * U);
+    hipLaunchKernelGGL((selective_step_kernel<T, NL, U, WAVES>), grid_of(cdiv(c.rows * c.H * c.parts, 4 / WAVES)), dim3(256), 0, st,
+                       static_cast<const T *>(d_xbc), static_cast<T *>(d_out), c);
 }
 template <typename T>
 static void step(const void *d_xbc, void *d_out, const StepCall &c, hipStream_t st)
 {
-    if (c.N <= 16) return launch_step<T, 4, 2>(d_xbc, d_out, c, st);
-    if (c.N <= 32) return launch_step<T, 8, 4>(d_xbc, d_out, c, st);
-    if (c.N <= 64) return launch_step<T, 16, 4>(d_xbc, d_out, c, st);
-    if (c.N <= 128) return launch_step<T, 32, 8>(d_xbc, d_out, c, st);
-    return launch_step<T, 64, 8>(d_xbc, d_out, c, st);
+    // (few work-groups: smaller ones)
+    const bool few = c.rows * c.H * cdiv(c.P, 64) < 2 * kChipCus;
+    if (c.N <= 16) return c.P > 32 ? launch_step<T, 4, 2, 4>(d_xbc, d_out, c, st) : c.P > 16 ? launch_step<T, 4, 2, 1>(d_xbc, d_out, c, st) : launch_step<T, 4, 1, 1>(d_xbc, d_out, c, st);
+    if (c.N <= 32) return c.P > 32 ? launch_step<T, 8, 2, 4>(d_xbc, d_out, c, st) : launch_step<T, 8, 4, 1>(d_xbc, d_out, c, st);
+    if (c.N <= 64) return c.P > 16 ? (few ? launch_step<T, 16, 1, 4>(d_xbc, d_out, c, st) : launch_step<T, 16, 4, 4>(d_xbc, d_out, c, st)) : launch_step<T, 16, 4, 1>(d_xbc, d_out, c, st);
+    if (c.N <= 128) return few ? launch_step<T, 32, 2, 4>(d_xbc, d_out, c, st) : launch_step<T, 32, 8, 4>(d_xbc, d_out, c, st);
+    return few ? launch_step<T, 64, 4, 4>(d_xbc, d_out, c, st) : launch_step<T, 64, 8, 4>(d_xbc, d_out, c, st);
 }
 
 extern "C" int srm_selective_step(int32_t dtype, const void *d_xbc, int64_t ld_xbc, const float *d_weight, const float *d_bias, int32_t activation,
@@ -296,7 +311,7 @@ extern "C" int srm_selective_step(int32_t dtype, const void *d_xbc, int64_t ld_x
     }
     if (misaligned(d_weight, 4) || misaligned(d_bias, 4) || misaligned(d_conv_state, size_of(dtype)) || misaligned(d_pos, 4) || misaligned(d_slot, 4))
         return fail(SRM_EINVAL, "%s: %s", who, kNotWhole);
-    if (rows * heads * cdiv(head_dim, 16) >= kMaxBlocks) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    if (rows * heads * cdiv(head_dim, 8) >= kMaxBlocks) return fail(SRM_EINVAL, "%s: sizes out of range", who);
     StepCall c{};
     c.dt = StepSizes{d_dt, ld_dt, d_dt_bias, dt_dtype == SRM_BF16, softplus != 0};
     c.rows = rows;
@@ -326,12 +341,19 @@ extern "C" int srm_selective_step(int32_t dtype, const void *d_xbc, int64_t ld_x
 }
 
 // ------------------------------------------------------------------ scores of given tokens
+// Work-groups of 1024 threads while every row has a CU, behind that of 512, two of which a CU holds; few logits by fewer threads.
+// (1024 | 512 threads, us: 1 x 32000 fp32 8.8 | 11.0, 37 x 128001 bf16 22 | 29, 300 x 32000 fp32 20.5 | 19.1, 2001 x 128001 bf16 161 | 140;
+// 4096 x 512 fp32 by 256 threads 25, by a wavefront a row 11.7.)
 template <typename T>
 static void launch_score(const void *d_logits, const ScoreCall &c, hipStream_t st)
 {
     const T *logits = static_cast<const T *>(d_logits);
-    if (c.V <= 8192) hipLaunchKernelGGL((token_logprobs_kernel<T, 256>), grid_of(c.rows), dim3(256), 0, st, logits, c);
-    else hipLaunchKernelGGL((token_logprobs_kernel<T, 1024>), grid_of(c.rows), dim3(1024), 0, st, logits, c);
+    const int threads = c.V <= 2048 ? 64 : c.V <= 8192 ? 256 : c.rows > kChipCus ? 512 : 1024;
+    const auto kernel = threads == 64    ? token_logprobs_kernel<T, 64>
+                        : threads == 256 ? token_logprobs_kernel<T, 256>
+                        : threads == 512 ? token_logprobs_kernel<T, 512>
+                                         : token_logprobs_kernel<T, 1024>;
+    hipLaunchKernelGGL(kernel, grid_of(c.rows), dim3(threads), 0, st, logits, c);
 }
 
 extern "C" int srm_token_logprobs(int32_t dtype, const void *d_logits, int64_t ld, int64_t rows, int32_t vocab, const float *d_temperature,

@@ -4,12 +4,18 @@
 // With m the largest logit, d = (m - l) / T >= 0 and w = e^-d:
 //   Z = sum w      log p(v) = -d_v - log Z      entropy = log Z + (sum w d) / Z
 // (both parts of the entropy are positive: nothing cancels).  A thread keeps its largest logit and the two sums relative to it, 32 logits at
-// a time, and rescales them when a larger one comes; the threads' sums are joined in a fixed order.
+// a time, and rescales them when a larger one comes; the threads' sums are joined in a fixed order.  d counts in factors of two and is
+// held at 1000, beyond which w is 0 in fp32: a logit of -infinity, and a NaN, then add nothing without being looked for.
 //
 // The k most likely tokens: the k-th largest of 64 disjoint groups' largest logits is at or below the k-th largest of the row, so the
-// logits from it on (some 1.3 k of them where the groups are alike) hold all that are wanted; the second reading lists them, and they are
-// put in order by counting, equal ones by their index.  A list that overflows (equal logits in bulk) is not used: the tokens are then looked
-// for one after the other, a reading each.
+// logits from it on (some 1.3 k of them where the groups are alike) hold all that are wanted.  A row's first 32 logits a thread, which stay
+// in registers, give such a bound; from there on every logit above it is listed as it comes, and a few hundred of 128000 are.  A list that
+// overflows is made again, in a second reading, with the bound that the whole row gives.  The listed ones are put in order by counting,
+// equal ones by their index.  A list that overflows again (equal logits in bulk) is not used: the tokens are then looked for one after the
+// other, a reading each.
+//
+// What bounds it: the row is read once; for bf16 rows about as much the ten instruction slots that a logit takes, four of them its
+// exponential's.  One row: one CU's share of both.
 #pragma once
 #include "fp8.hpp"
 
@@ -43,99 +49,203 @@ __device__ __forceinline__ ScoreSums score_rescaled(const ScoreSums &a, float m,
     const float d = (m - a.m) * inv, f = score_weight(d);
     return {m, f * a.z, f > 0.0f ? f * fmaf(d, a.z, a.e) : 0.0f};
 }
-__device__ __forceinline__ ScoreSums score_join(const ScoreSums &a, const ScoreSums &b, float inv)
+__device__ __forceinline__ uint32_t score_wave_max(uint32_t v)
 {
-    const float m = fmaxf(a.m, b.m);
-    const ScoreSums x = score_rescaled(a, m, inv), y = score_rescaled(b, m, inv);
-    return {m, x.z + y.z, x.e + y.e};
+    const int r = (int)row16_max_u32(v);
+    return max(max((uint32_t)__builtin_amdgcn_readlane(r, 0), (uint32_t)__builtin_amdgcn_readlane(r, 16)),
+               max((uint32_t)__builtin_amdgcn_readlane(r, 32), (uint32_t)__builtin_amdgcn_readlane(r, 48)));
 }
 
 template <typename T, int NT>
 __global__ void __launch_bounds__(NT)
 token_logprobs_kernel(const T *__restrict__ logits, ScoreCall c)
 {
-    constexpr int NW = NT / 64, STEP = NT * 8;
-    __shared__ ScoreSums sums[NW];
-    __shared__ uint32_t group[64], list_key[kScoreList], bound_s, found_key[NW];
-    __shared__ int list_at[kScoreList], n_list, found_at[NW];
+    constexpr int NW = NT / 64, STEP = NT * 8, PER = 4, G = NT / 64;    // PER vectors of eight logits at a time; G lanes of a group
+    __shared__ float wave_m[NW], wave_z[NW], wave_e[NW];
+    __shared__ __align__(16) unsigned long long listed[kScoreList + 2];  // key of the logit, behind it its index upside down
+    __shared__ uint32_t group[64], bound_s, found_key[NW];
+    __shared__ int n_list, found_at[NW];
     const int64_t row = work_group();
     if (row >= c.rows) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = c.V;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = c.V, k = c.k;
     const T *L = logits + row * c.ld;
     const int token = c.token ? c.token[row] : -1;
     const bool given = token >= 0 && token < V;
     float t = c.temperature ? c.temperature[row] : 1.0f;
     t = t > 0.0f ? fminf(fmaxf(t, 1e-30f), 1e30f) : 1.0f;
-    const float inv = 1.0f / t;
+    const float inv = 1.0f / t, inv2 = inv * 1.44269504088896340736f;
     float l_given = given ? (float)L[token] : 0.0f;
     if (l_given != l_given) l_given = -INFINITY;
 
-    // eight logits from `at` on; a NaN, or what lies behind the row, counts as -infinity
-    auto values = [&](const Raw8<T> &raw, int at, float (&v)[8]) {
-        widen8(raw, at, V, v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = fmaxf(v[i], -INFINITY);
+    // eight logits from `at` on (NaN among them), -infinity behind the row
+    auto values = [&](const Raw8<T> &raw, int at, float (&v)[8]) __attribute__((always_inline)) {
+        raw8_values(raw, v);
         if (__ballot(at + 8 > V)) {
+            if (V >= 8) {
+                const int late = at + 8 - V;
+#pragma unroll
+                for (int s = 4; s >= 1; s >>= 1)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (late > 0 && (late & s)) v[i] = i + s < 8 ? v[i + s] : 0.0f;
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = at + i < V ? v[i] : -INFINITY;
         }
     };
+    // The largest of eight, -infinity of none but NaN.  (Written out, as three at a time; the compiler would quiet each value first.  A NaN
+    // that signals, which the instruction makes a result of, is looked for.)
+    auto largest = [](const float (&v)[8]) __attribute__((always_inline)) {
+        float m;
+        asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(v[0]), "v"(v[1]), "v"(v[2]));
+        asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(m), "v"(v[3]), "v"(v[4]));
+        asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(m), "v"(v[5]), "v"(v[6]));
+        asm("v_max_f32 %0, %1, %2" : "=v"(m) : "v"(m), "v"(v[7]));
+        if (m != m) {
+            m = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = fmaxf(m, v[i]);
+        }
+        return m;
+    };
     ScoreSums s = {-INFINITY, 0.0f, 0.0f};
-    bool hot = false;                                // an infinite logit leaves all others without weight
-    for (int at = tid * 8; at - lane * 8 < V; at += STEP * 4) {
-        Raw8<T> raw[4];
+    // 32 logits join the thread's sums
+    float tops[PER];                                 // the vectors' largest
+    auto take = [&](const float (&v)[PER][8]) __attribute__((always_inline)) {
+        float m = s.m;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) raw[j] = raw8(L, at + j * STEP, V);
-        float v[4][8], m = s.m;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            values(raw[j], at + j * STEP, v[j]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) m = fmaxf(m, v[j][i]);
+        for (int j = 0; j < PER; ++j) {
+            tops[j] = largest(v[j]);
+            m = tops[j] > m ? tops[j] : m;
         }
         s = score_rescaled(s, m, inv);
-        if (m == INFINITY || m == -INFINITY) {
-            if (m == INFINITY) {
-                if (!hot) s.z = s.e = 0.0f;
-                hot = true;
+        if (m == -INFINITY) return;
+        if (m == INFINITY) {                         // leaves all others without weight
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < PER; ++j)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) s.z += v[j][i] == INFINITY ? 1.0f : 0.0f;
-            }
-            continue;
+                for (int i = 0; i < 8; ++i) s.z += v[j][i] == INFINITY ? 1.0f : 0.0f;
+            return;
         }
+        float z[2] = {0.0f, 0.0f}, e[2] = {0.0f, 0.0f};
+        const float at_m = m * inv2;
+        if (fabsf(at_m) < 1e6f) {
+            // One multiply-add to the logit's distance from the rounded product; what the rounding took is the same for all of them.
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < PER; ++j)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float d = (m - v[j][i]) * inv, w = score_weight(d);
-                s.z += w;
-                s.e = w > 0.0f ? fmaf(w, d, s.e) : s.e;
-            }
-    }
-    // the largest of each group of NT / 64 threads, then the sums of all
-    {
-        const uint32_t mine = score_key(s.m);
-        uint32_t top = mine;
-        constexpr int G = NT / 64;                   // lanes of a group: 4, 8 or 16
+                for (int i = 0; i < 8; ++i) {
+                    const float d = fminf(fmaf(v[j][i], -inv2, at_m), 1000.0f), w = __builtin_amdgcn_exp2f(-d);
+                    z[i & 1] += w;
+                    e[i & 1] = fmaf(w, d, e[i & 1]);
+                }
+        } else {
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float d = fminf((m - v[j][i]) * inv2, 1000.0f), w = __builtin_amdgcn_exp2f(-d);
+                    z[i & 1] += w;
+                    e[i & 1] = fmaf(w, d, e[i & 1]);
+                }
+        }
+        const float off = fabsf(at_m) < 1e6f ? fmaf(m, inv2, -at_m) : 0.0f, f = __builtin_amdgcn_exp2f(-off), zs = z[0] + z[1];
+        s.z = fmaf(f, zs, s.z);
+        s.e = fmaf(f * 0.69314718055994530942f, fmaf(off, zs, e[0] + e[1]), s.e);
+    };
+    // the k-th largest of the groups' largest, equal ones by number; -infinity is no alternative
+    float least = INFINITY;
+    auto bound = [&]() __attribute__((always_inline)) {
+        uint32_t top = score_key(s.m);
         if constexpr (G > 1) top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, true));
         if constexpr (G > 2) top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xF, 0xF, true));
         if constexpr (G > 4) top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x141, 0xF, 0xF, true));
         if constexpr (G > 8) top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x140, 0xF, 0xF, true));
         if (lane % G == 0) group[tid / G] = top;
-    }
+        if (tid == 0) n_list = 0;
+        __syncthreads();
+        if (wave == 0) {
+            const uint32_t mine = group[lane];
+            int before = 0;
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const ScoreSums o = {__shfl_xor(s.m, off), __shfl_xor(s.z, off), __shfl_xor(s.e, off)};
-        s = score_join(s, o, inv);
-    }
-    if (lane == 0) sums[wave] = s;
-    if (tid == 0) n_list = 0;
-    __syncthreads();
-    s = sums[0];
+            for (int j = 0; j < 64; ++j) {
+                const uint32_t o = (uint32_t)__builtin_amdgcn_readlane((int)mine, j);
+                before += o > mine || (o == mine && j < lane);
+            }
+            if (before == k - 1) bound_s = max(mine, score_key(-INFINITY) + 1);
+        }
+        __syncthreads();
+        least = score_value(bound_s);
+    };
+    auto list = [&](const float (&v)[8], float top, int at) __attribute__((always_inline)) {
+        if (top >= least) {
 #pragma unroll
-    for (int w = 1; w < NW; ++w) s = score_join(s, sums[w], inv);
+            for (int i = 0; i < 8; ++i)
+                if (v[i] >= least) {
+                    const int to = atomicAdd(&n_list, 1);
+                    if (to < kScoreList) listed[to] = (unsigned long long)score_key(v[i]) << 32 | (uint32_t)~(at + i);
+                }
+        }
+    };
+    auto fetch = [&](Raw8<T> (&raw)[PER], int at) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) raw[j] = raw8(L, at + j * STEP, V);
+    };
+    auto widen = [&](const Raw8<T> (&raw)[PER], int at, float (&v)[PER][8]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) values(raw[j], at + j * STEP, v[j]);
+    };
+    const int mine = tid * 8, ours = mine - lane * 8;                   // a thread's, its wavefront's first logit
+    {
+        Raw8<T> raw[PER], next[PER];
+        float v[PER][8];
+        fetch(raw, mine);
+        if (ours + PER * STEP < V) fetch(next, mine + PER * STEP);
+        widen(raw, mine, v);
+        take(v);
+        if (k > 0) {
+            bound();
+#pragma unroll
+            for (int j = 0; j < PER; ++j) list(v[j], tops[j], mine + j * STEP);
+        }
+        for (int at = PER * STEP; ours + at < V; at += PER * STEP) {
+#pragma unroll
+            for (int j = 0; j < PER; ++j) raw[j] = next[j];
+            if (ours + at + PER * STEP < V) fetch(next, mine + at + PER * STEP);
+            widen(raw, mine + at, v);
+            take(v);
+            if (k > 0) {
+#pragma unroll
+                for (int j = 0; j < PER; ++j) list(v[j], tops[j], mine + at + j * STEP);
+            }
+        }
+    }
+    // the row's largest, then the sums relative to it
+    const float own_m = s.m;
+    {
+        const float top = score_value(score_wave_max(score_key(s.m)));
+        if (lane == 0) wave_m[wave] = top;
+        __syncthreads();
+        float m = wave_m[0];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) m = fmaxf(m, wave_m[w]);
+        s = score_rescaled(s, m, inv);
+        s.z = wave_sum(s.z);
+        s.e = wave_sum(s.e);
+        if constexpr (NW > 1) {
+            if (lane == 0) {
+                wave_z[wave] = s.z;
+                wave_e[wave] = s.e;
+            }
+            __syncthreads();
+            s.z = s.e = 0.0f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                s.z += wave_z[w];
+                s.e += wave_e[w];
+            }
+        }
+    }
     const float log_z = logf(s.z);                   // (a row of -infinity: z is 0)
     auto logprob = [&](float l) {
         if (l == -INFINITY || s.z == 0.0f) return -INFINITY;
@@ -145,62 +255,43 @@ token_logprobs_kernel(const T *__restrict__ logits, ScoreCall c)
         if (c.logprob) c.logprob[row] = given ? logprob(l_given) : 0.0f;
         if (c.entropy) c.entropy[row] = s.z > 0.0f ? log_z + s.e / s.z : 0.0f;
     }
-    if (c.k == 0) return;
+    if (k == 0) return;
 
-    if (wave == 0) {                                 // the k-th largest of the groups', equal ones by number
-        const uint32_t mine = group[lane];
-        int before = 0;
-#pragma unroll
-        for (int j = 0; j < 64; ++j) {
-            const uint32_t o = (uint32_t)__builtin_amdgcn_readlane((int)mine, j);
-            before += o > mine || (o == mine && j < lane);
-        }
-        if (before == c.k - 1) bound_s = mine;
-    }
-    __syncthreads();
-    // (-infinity is no alternative)
-    const uint32_t bound = max(bound_s, score_key(-INFINITY) + 1);
-    const float least = score_value(bound);
-    for (int at = tid * 8; at - lane * 8 < V; at += STEP * 4) {
-        Raw8<T> raw[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) raw[j] = raw8(L, at + j * STEP, V);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
+    int n = n_list;
+    if (n > kScoreList) {
+        __syncthreads();                             // (all have read it)
+        const ScoreSums whole = s;
+        s.m = own_m;
+        bound();
+        s = whole;
+        for (int at = 0; ours + at < V; at += STEP) {
             float v[8];
-            values(raw[j], at + j * STEP, v);
-            float m = v[0];
-#pragma unroll
-            for (int i = 1; i < 8; ++i) m = fmaxf(m, v[i]);
-            if (m >= least) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (v[i] >= least) {
-                        const int to = atomicAdd(&n_list, 1);
-                        if (to < kScoreList) {
-                            list_key[to] = score_key(v[i]);
-                            list_at[to] = at + j * STEP + i;
-                        }
-                    }
-            }
+            values(raw8(L, mine + at, V), mine + at, v);
+            list(v, largest(v), mine + at);
         }
+        __syncthreads();
+        n = n_list;
     }
-    __syncthreads();
-    const int n = n_list;
-    float *const top_logprob = c.top_logprob + row * c.k;
-    int32_t *const top_token = c.top_token + row * c.k;
+    float *const top_logprob = c.top_logprob + row * k;
+    int32_t *const top_token = c.top_token + row * k;
     if (n <= kScoreList) {
+        if (tid < 2) listed[n + tid] = 0;            // (behind the last, for the reads in pairs)
+        __syncthreads();
+        typedef __attribute__((ext_vector_type(2))) unsigned long long pair;
         for (int i = tid; i < n; i += NT) {
-            const uint32_t key = list_key[i];
-            const int at = list_at[i];
+            const unsigned long long own = listed[i];
             int before = 0;
-            for (int j = 0; j < n; ++j) before += list_key[j] > key || (list_key[j] == key && list_at[j] < at);
-            if (before < c.k) {
-                top_token[before] = at;
-                top_logprob[before] = logprob(score_value(key));
+#pragma unroll 4
+            for (int j = 0; j < n; j += 2) {
+                const pair o = *reinterpret_cast<const pair *>(listed + j);
+                before += (int)(o[0] > own) + (int)(o[1] > own);
+            }
+            if (before < k) {
+                top_token[before] = (int)~(uint32_t)own;
+                top_logprob[before] = logprob(score_value((uint32_t)(own >> 32)));
             }
         }
-        for (int i = n + tid; i < c.k; i += NT) {
+        for (int i = n + tid; i < k; i += NT) {
             top_token[i] = -1;
             top_logprob[i] = -INFINITY;
         }
@@ -209,24 +300,25 @@ token_logprobs_kernel(const T *__restrict__ logits, ScoreCall c)
     // one after the other: the best logit behind the last one found
     uint32_t last_key = 0xffffffffu;
     int last_at = -1;
-    for (int i = 0; i < c.k; ++i) {
+    for (int i = 0; i < k; ++i) {
         uint32_t key = 0;
         int where = V;
-        for (int at = tid * 8; at - lane * 8 < V; at += STEP) {
+        for (int at = 0; ours + at < V; at += STEP) {
             float v[8];
-            values(raw8(L, at, V), at, v);
+            values(raw8(L, mine + at, V), mine + at, v);
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-                const uint32_t k = score_key(v[q]);
-                const bool behind = k < last_key || (k == last_key && at + q > last_at);
-                if (at + q < V && behind && (k > key || (k == key && at + q < where))) { key = k; where = at + q; }
+                const int index = mine + at + q;
+                const uint32_t u = score_key(fmaxf(v[q], -INFINITY));
+                const bool behind = u < last_key || (u == last_key && index > last_at);
+                if (index < V && behind && (u > key || (u == key && index < where))) { key = u; where = index; }
             }
         }
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) {
-            const uint32_t k = (uint32_t)__shfl_xor((int)key, off);
+            const uint32_t u = (uint32_t)__shfl_xor((int)key, off);
             const int w = __shfl_xor(where, off);
-            if (k > key || (k == key && w < where)) { key = k; where = w; }
+            if (u > key || (u == key && w < where)) { key = u; where = w; }
         }
         __syncthreads();
         if (lane == 0) { found_key[wave] = key; found_at[wave] = where; }

@@ -282,9 +282,9 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
 }
 
 // ------------------------------------------------------------------ single tokens
-// A work-group takes PW rows of P of one head of one request.  The state's loads start as soon as the slot is known, the convolution of
-// the head's x and its group's B and C runs while they travel.  B and C are formed by every work-group of a group; the ring's row of the
-// new token, which none of the taps reads, is written by the work-groups of the group's first head.
+// Four wavefronts of a work-group, or one, take PW rows of P of one head of one request.  The state's loads start as soon as the slot is
+// known, the convolution of the head's x and its group's B and C runs while they travel.  B and C are formed anew for every head of a group;
+// the ring's row of the new token, which none of the taps reads, is written for the group's first head alone.
 // What bounds it: the state is read and written once.
 struct StepCall {
     StepSizes dt;
@@ -300,18 +300,20 @@ struct StepCall {
 };
 typedef f32x4_t __attribute__((aligned(4))) f32x4_any;
 
-// NL lanes with four elements of N each hold a row of P, a work-group U rows of them in each lane.
-template <typename T, int NL, int U>
+// NL lanes with four elements of N each hold a row of P, a wavefront U rows of them in each lane; WAVES of them (4 or 1) share a head.
+template <typename T, int NL, int U, int WAVES>
 __global__ void __launch_bounds__(256)
 selective_step_kernel(const T *__restrict__ xbc, T *__restrict__ out, StepCall c)
 {
-    constexpr int PL = 64 / NL, PW = 4 * PL * U;
-    __shared__ __align__(16) float sb[4 * NL], sc[4 * NL], sx[PW];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane % NL;
-    const int64_t id = work_group();
+    constexpr int PL = 64 / NL, PW = WAVES * PL * U, NT = 64 * WAVES, TAPS = 3;
+    __shared__ __align__(16) float shared_x[4 / WAVES][PW], shared_bc[4 / WAVES][2][4 * NL];
+    const int lane = threadIdx.x & 63, in_group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ln = lane % NL;
+    const int wave = WAVES == 4 ? in_group : 0, mine = WAVES == 4 ? 0 : in_group, tid = wave * 64 + lane;
+    float *const sx = shared_x[mine], *const sb = shared_bc[mine][0], *const sc = shared_bc[mine][1];
+    const int64_t id = (int64_t)work_group() * (4 / WAVES) + mine;
     const int per = c.H * c.parts;
     const int64_t r = id / per;
-    if (r >= c.rows) return;
+    if (r >= c.rows) return;                         // (wavefronts that share nothing meet no barrier)
     const int h = (int)(id % per) / c.parts, p0 = (int)(id % per) % c.parts * PW, g = h / (c.H / c.G);
     const int P = c.P, N = c.N, np = min(PW, P - p0), C = c.H * P + 2 * c.G * N;
     const int pos = c.pos[r];
@@ -319,11 +321,11 @@ selective_step_kernel(const T *__restrict__ xbc, T *__restrict__ out, StepCall c
     const bool kept = at >= 0 && at < c.slots;
     T *o = out + r * c.ld_out + (int64_t)h * P + p0;
     if (pos < 0) {
-        for (int p = tid; p < np; p += 256) store1(o + p, 0.0f);
+        for (int p = tid; p < np; p += NT) store1(o + p, 0.0f);
         return;
     }
     float *S = kept ? c.state + ((at * c.H + h) * P + p0) * (int64_t)N : nullptr;
-    auto row_of = [&](int u) { return (u * 4 + wave) * PL + lane / NL; };
+    auto row_of = [&](int u) { return (u * WAVES + wave) * PL + lane / NL; };
     f32x4_t v[U];
     const bool whole = ln * 4 + 4 <= N;
 #pragma unroll
@@ -342,36 +344,35 @@ selective_step_kernel(const T *__restrict__ xbc, T *__restrict__ out, StepCall c
     const bool first = h % (c.H / c.G) == 0 && p0 == 0;
     const T *x = xbc + r * c.ld;
     T *ring = c.ring && kept ? static_cast<T *>(c.ring) + at * c.width * (int64_t)C : nullptr;
-    for (int e = tid; e < PW + 8 * NL; e += 256) {
-        int ch;
-        float *to;
-        bool mine = true;
-        if (e < PW) {
-            ch = e < np ? h * P + p0 + e : -1;
-            to = sx + e;
-        } else {
-            const int which = (e - PW) / (4 * NL), n = (e - PW) % (4 * NL);
-            ch = n < N ? c.H * P + which * c.G * N + g * N + n : -1;
-            to = (which ? sc : sb) + n;
-            mine = first;
-        }
-        float q = 0.0f;
-        if (ch >= 0) {
-            q = (float)x[ch];
-            if (c.weight) {
-                const float *w = c.weight + (int64_t)ch * c.width;
-                float acc = fmaf(w[c.width - 1], q, c.bias ? c.bias[ch] : 0.0f);
-                for (int k = 0; k < c.width - 1; ++k) {
-                    const int p = pos - (c.width - 1) + k;
-                    if (p >= 0 && ring) acc = fmaf(w[k], (float)ring[(int64_t)(p % c.width) * C + ch], acc);
-                }
-                if (ring && mine) ring[(int64_t)(pos % c.width) * C + ch] = x[ch];
-                q = c.silu ? silu(acc) : acc;
+    // (the filter's first taps: loads without a branch between them, further ones one by one)
+    for (int e = tid; e < PW + 8 * NL; e += NT) {
+        const int which = e < PW ? 0 : (e - PW) / (4 * NL), n = (e - PW) % (4 * NL);
+        const bool there = e < PW ? e < np : n < N;
+        const int ch = !there ? 0 : e < PW ? h * P + p0 + e : c.H * P + which * c.G * N + g * N + n;
+        const T now = x[ch];
+        float q = (float)now;
+        if (c.weight) {
+            const float *w = c.weight + (int64_t)ch * c.width;
+            float acc = c.bias ? c.bias[ch] : 0.0f, u[TAPS], f[TAPS];
+            const float last = w[c.width - 1];
+#pragma unroll
+            for (int k = 0; k < TAPS; ++k) {         // k + 1 tokens ago
+                const bool tap = k + 1 < c.width && pos > k && ring;
+                u[k] = tap ? (float)ring[(int64_t)((pos - 1 - k) % c.width) * C + ch] : 0.0f;
+                f[k] = tap ? w[c.width - 2 - k] : 0.0f;
             }
+            for (int k = TAPS; k + 1 < c.width; ++k)
+                if (pos > k && ring) acc = fmaf(w[c.width - 2 - k], (float)ring[(int64_t)((pos - 1 - k) % c.width) * C + ch], acc);
+#pragma unroll
+            for (int k = TAPS - 1; k >= 0; --k) acc = fmaf(f[k], u[k], acc);
+            acc = fmaf(last, q, acc);
+            if (ring && there && (e < PW || first)) ring[(int64_t)(pos % c.width) * C + ch] = now;
+            q = c.silu ? silu(acc) : acc;
         }
-        *to = q;
+        (e < PW ? sx + e : (which ? sc : sb) + n)[0] = there ? q : 0.0f;
     }
-    __syncthreads();
+    if constexpr (WAVES == 4) __syncthreads();
+    else __builtin_amdgcn_wave_barrier();
     const f32x4_t b = *reinterpret_cast<const f32x4_t *>(sb + ln * 4), cc = *reinterpret_cast<const f32x4_t *>(sc + ln * 4);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
