@@ -691,24 +691,33 @@ def _ptr(t):
 
 
 def _vector(t, n: int, dtype, name: str):
-    if t is not None and (t.dtype is not dtype or t.numel() != n or not t.is_contiguous()):
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name}: must be {n} contiguous {str(dtype)[6:]} values")
 
 
+def _vectors(n: int, dtype, **named):
+    for name, t in named.items():
+        if t is not None and (t.dtype is not dtype or t.numel() != n or not t.is_contiguous()):
+            _vector(t, n, dtype, name)
+
+
 def _offsets(offsets, d_offsets, rows: int):
-    """The host's offsets as an array that the library may read, and the number of sequences."""
-    if isinstance(offsets, _torch().Tensor):
-        if offsets.is_cuda:
+    """(address of the host's offsets, the number of sequences, what keeps the address alive)."""
+    torch = _torch()
+    if type(offsets) is torch.Tensor and not offsets.is_cuda and offsets.dtype is torch.int32 and offsets.is_contiguous():
+        at, n, keep = offsets.data_ptr(), offsets.numel() - 1, offsets
+    else:
+        if isinstance(offsets, torch.Tensor) and offsets.is_cuda:
             raise ValueError("offsets: must be host memory (d_offsets: the same values on the device)")
-        offsets = offsets.numpy()
-    h = np.ascontiguousarray(offsets, dtype=np.int32)
-    n = h.size - 1
-    if h.ndim != 1 or n < 1:
+        keep = np.ascontiguousarray(offsets, dtype=np.int32)
+        at, n = keep.ctypes.data, keep.size - 1
+    if n < 1:
         raise ValueError("offsets: need at least two boundaries")
-    if h[n] > rows:
-        raise ValueError(f"offsets: {int(h[n])} rows, the operands have {rows}")
-    _vector(d_offsets, n + 1, _torch().int32, "d_offsets")
-    return h, n
+    last = C.c_int32.from_address(at + 4 * n).value
+    if last > rows:
+        raise ValueError(f"offsets: {last} rows, the operands have {rows}")
+    _vector(d_offsets, n + 1, torch.int32, "d_offsets")
+    return at, n, keep
 
 
 def _same_rows(t, rows: int, cols: int, name: str, dtype=None):
@@ -723,7 +732,7 @@ def _same_rows(t, rows: int, cols: int, name: str, dtype=None):
 def _slots_of(state, shape, dtype, name: str) -> int:
     if state is None:
         return 0
-    if state.dtype is not dtype or tuple(state.shape[1:]) != shape or not state.is_contiguous():
+    if state.dtype is not dtype or state.shape[1:] != shape or not state.is_contiguous():
         raise ValueError(f"{name}: must be contiguous {str(dtype)[6:]} of shape (slots, {', '.join(map(str, shape))})")
     return state.shape[0]
 
@@ -734,35 +743,34 @@ def causal_conv(x, weight, bias, offsets, d_offsets, out, pos=None, slot=None, s
     x's type or None, updated; activation: SiLU."""
     torch = _torch()
     rows, channels, ldx = _rows_of(x, "x")
-    h, n = _offsets(offsets, d_offsets, rows)
+    h, n, keep = _offsets(offsets, d_offsets, rows)
     if weight.dim() != 2:
         raise ValueError("weight: must be a matrix")
     width = weight.shape[1]
     _vector(weight, channels * width, torch.float32, "weight")
-    _vector(bias, channels, torch.float32, "bias")
-    _vector(pos, n, torch.int32, "pos")
-    _vector(slot, n, torch.int32, "slot")
+    if bias is not None:
+        _vector(bias, channels, torch.float32, "bias")
+    _vectors(n, torch.int32, pos=pos, slot=slot)
     slots = _slots_of(state, (width, channels), x.dtype, "state")
     ld_out = _same_rows(out, rows, channels, "out", x.dtype)
     _launch(lib().srm_causal_conv, (_row_dtype(x, "x"), x.data_ptr(), ldx, weight.data_ptr(), _ptr(bias), 1 if activation else 0, channels, width,
-                                    h.ctypes.data, d_offsets.data_ptr(), n, _ptr(pos), _ptr(slot), slots, _ptr(state), out.data_ptr(), ld_out),
+                                    h, d_offsets.data_ptr(), n, _ptr(pos), _ptr(slot), slots, _ptr(state), out.data_ptr(), ld_out),
             x, (weight, bias, d_offsets, pos, slot, state, out), stream)
 
 
 def _heads(xbc, dt, a, out, groups, dt_bias, skip, z):
     """(rows, ld_xbc, ld_dt, ld_z, ld_out, heads, head_dim, state_dim) of the recurrence's operands after their checks."""
-    torch = _torch()
     rows, channels, ld = _rows_of(xbc, "xbc")
     heads = a.numel()
-    inner = _rows_of(out, "out")[1]
+    n, inner, ld_out = _rows_of(out, "out")
     if groups <= 0 or heads <= 0 or heads % groups or inner % heads:
         raise ValueError(f"{heads} heads in {groups} groups, rows of {inner}")
+    if n != rows or out.dtype is not xbc.dtype:
+        raise ValueError(f"out: {n} rows of {out.dtype}, expected {rows} of {xbc.dtype}")
     left = channels - inner
     if left <= 0 or left % (2 * groups):
         raise ValueError(f"xbc: {channels} columns are not {inner} + 2 x {groups} x state_dim")
-    for t, name in ((a, "a"), (dt_bias, "dt_bias"), (skip, "skip")):
-        _vector(t, heads, torch.float32, name)
-    ld_out = _same_rows(out, rows, inner, "out", xbc.dtype)
+    _vectors(heads, _torch().float32, a=a, dt_bias=dt_bias, skip=skip)
     ld_z = 0 if z is None else _same_rows(z, rows, inner, "z", xbc.dtype)
     return rows, ld, _same_rows(dt, rows, heads, "dt"), ld_z, ld_out, heads, inner // heads, left // (2 * groups)
 
@@ -781,13 +789,12 @@ def selective_scan(xbc, dt, a, offsets, d_offsets, out, groups=1, dt_bias=None, 
     not given."""
     torch = _torch()
     rows, ld, ld_dt, ld_z, ld_out, heads, head_dim, state_dim = _heads(xbc, dt, a, out, groups, dt_bias, skip, z)
-    h, n = _offsets(offsets, d_offsets, rows)
-    _vector(pos, n, torch.int32, "pos")
-    _vector(slot, n, torch.int32, "slot")
+    h, n, keep = _offsets(offsets, d_offsets, rows)
+    _vectors(n, torch.int32, pos=pos, slot=slot)
     slots = _slots_of(state, (heads, head_dim, state_dim), torch.float32, "state")
     code = _row_dtype(xbc, "xbc")
     if workspace is None:
-        need = lib().srm_selective_scan_workspace_bytes(code, h.ctypes.data, n, heads, head_dim, state_dim)
+        need = lib().srm_selective_scan_workspace_bytes(code, h, n, heads, head_dim, state_dim)
         if need and xbc.is_cuda:
             workspace = torch.empty(need, dtype=torch.uint8, device=xbc.device)
             if stream is not None:
@@ -796,7 +803,7 @@ def selective_scan(xbc, dt, a, offsets, d_offsets, out, groups=1, dt_bias=None, 
         raise ValueError("workspace: must be contiguous uint8")
     _launch(lib().srm_selective_scan,
             (code, xbc.data_ptr(), ld, _row_dtype(dt, "dt"), dt.data_ptr(), ld_dt, a.data_ptr(), _ptr(dt_bias), _ptr(skip), 1 if softplus else 0,
-             _ptr(z), ld_z, heads, head_dim, groups, state_dim, h.ctypes.data, d_offsets.data_ptr(), n, _ptr(pos), _ptr(slot), slots, _ptr(state),
+             _ptr(z), ld_z, heads, head_dim, groups, state_dim, h, d_offsets.data_ptr(), n, _ptr(pos), _ptr(slot), slots, _ptr(state),
              out.data_ptr(), ld_out, _ptr(workspace), 0 if workspace is None else workspace.numel()),
             xbc, (dt, a, dt_bias, skip, z, d_offsets, pos, slot, state, out, workspace), stream)
 
@@ -809,7 +816,8 @@ def selective_step(xbc, dt, a, pos, state, out, groups=1, weight=None, bias=None
     torch = _torch()
     rows, ld, ld_dt, ld_z, ld_out, heads, head_dim, state_dim = _heads(xbc, dt, a, out, groups, dt_bias, skip, z)
     _vector(pos, rows, torch.int32, "pos")
-    _vector(slot, rows, torch.int32, "slot")
+    if slot is not None:
+        _vector(slot, rows, torch.int32, "slot")
     slots = _slots_of(state, (heads, head_dim, state_dim), torch.float32, "state")
     width = 0
     if weight is not None:
@@ -818,7 +826,8 @@ def selective_step(xbc, dt, a, pos, state, out, groups=1, weight=None, bias=None
             raise ValueError("weight: must be a matrix")
         width = weight.shape[1]
         _vector(weight, channels * width, torch.float32, "weight")
-        _vector(bias, channels, torch.float32, "bias")
+        if bias is not None:
+            _vector(bias, channels, torch.float32, "bias")
         if conv_state is not None and _slots_of(conv_state, (width, channels), xbc.dtype, "conv_state") != slots:
             raise ValueError(f"conv_state: {conv_state.shape[0]} slots, state has {slots}")
     _launch(lib().srm_selective_step,
@@ -833,9 +842,9 @@ def token_logprobs(logits, token, logprob, temperature=None, entropy=None, top_t
     be None), entropy [rows] float32, top_token [rows][k] int32 with top_logprob [rows][k] float32; temperature float32 [rows] or None."""
     torch = _torch()
     rows, vocab, ld = _rows_of(logits, "logits")
-    _vector(token, rows, torch.int32, "token")
-    for t, name in ((logprob, "logprob"), (temperature, "temperature"), (entropy, "entropy")):
-        _vector(t, rows, torch.float32, name)
+    if token is not None:
+        _vector(token, rows, torch.int32, "token")
+    _vectors(rows, torch.float32, logprob=logprob, temperature=temperature, entropy=entropy)
     top = 0
     if top_token is not None or top_logprob is not None:
         if top_token is None or top_logprob is None or top_token.dim() != 2:
