@@ -146,14 +146,19 @@ static int check_heads(const char *who, int32_t dtype, int32_t dt_dtype, const H
 struct ScanPlan {
     int parts, seg, segments;                        // segments 0: every sequence as a whole
 };
-static int scan_rows(int32_t dtype, int32_t N)
+static int scan_rows(int32_t dtype, const HeadSizes &s)
 {
     if (dtype == SRM_BF16) return kScanRows;
-    return N <= 8 ? 256 : N <= 16 ? 128 : N <= 32 ? 64 : N <= 64 ? 32 : 16;
+    // (as the kernels that scan_f32 takes)
+    if (s.N <= 8) return s.P > 64 ? 256 : 64;
+    if (s.N <= 16) return s.P > 64 ? 128 : s.P > 32 ? 64 : 32;
+    if (s.N <= 32) return s.P > 32 ? 64 : 32;
+    if (s.N <= 64) return s.P > 16 ? 32 : 16;
+    return 16;
 }
 static ScanPlan scan_plan(int32_t dtype, const HeadSizes &s, int64_t tokens, int32_t longest)
 {
-    ScanPlan p{(int)cdiv(s.P, scan_rows(dtype, s.N)), 0, 0};
+    ScanPlan p{(int)cdiv(s.P, scan_rows(dtype, s)), 0, 0};
     const int64_t chip = dtype == SRM_BF16 ? 768 : 2048, units = (int64_t)s.H * p.parts, least = 64;
     const int64_t seg = std::max(least, cdiv(cdiv(tokens * units, chip), 64) * 64);
     if (longest > 2 * seg + 2 * least) {
@@ -199,10 +204,24 @@ static int scan_f32(const void *d_xbc, void *d_out, const ScanCall &c, const Sca
 #define SCAN_CASE(NL, NR)                                                                                                                     \
     return launch_scan<float, selective_scan_kernel<float, NL, NR, SCAN_WHOLE>, selective_scan_kernel<float, NL, NR, SCAN_CARRY>,           \
                        selective_scan_kernel<float, NL, NR, SCAN_SEGMENTS>>(d_xbc, d_out, c, p, 64, st)
-    if (c.N <= 8) SCAN_CASE(1, 8);
-    if (c.N <= 16) SCAN_CASE(2, 8);
-    if (c.N <= 32) SCAN_CASE(4, 8);
-    if (c.N <= 64) SCAN_CASE(8, 8);
+    // (as few lanes along N as leave none along P without rows)
+    if (c.N <= 8) {
+        if (c.P > 64) SCAN_CASE(1, 8);
+        SCAN_CASE(4, 2);
+    }
+    if (c.N <= 16) {
+        if (c.P > 64) SCAN_CASE(2, 8);
+        if (c.P > 32) SCAN_CASE(4, 4);
+        SCAN_CASE(8, 2);
+    }
+    if (c.N <= 32) {
+        if (c.P > 32) SCAN_CASE(4, 8);
+        SCAN_CASE(8, 4);
+    }
+    if (c.N <= 64) {
+        if (c.P > 16) SCAN_CASE(8, 8);
+        SCAN_CASE(16, 4);
+    }
     if (c.N <= 128) SCAN_CASE(16, 8);
     SCAN_CASE(16, 16);
 #undef SCAN_CASE

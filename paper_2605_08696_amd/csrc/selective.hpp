@@ -11,6 +11,9 @@
 // front of it, 16384 tokens of 32 heads took 146 us instead of 130.)
 #pragma once
 #include "conv.hpp"
+#include "tile.hpp"
+
+#define SCAN_INLINE __attribute__((always_inline))
 
 struct StepSizes {                                   // dt_raw [tokens][H] and what dt is made of
     const void *raw;
@@ -155,14 +158,14 @@ selective_scan_join_kernel(float *__restrict__ carry, const float *__restrict__ 
 
 // One wavefront takes PR rows of P a lane, NL lanes with NR elements of N each: 64 / NL * PR rows, NL NR >= N.  Sixteen tokens at a time
 // are brought to LDS, the next sixteen on their way in registers; then for every token each lane updates its PR x NR elements (multiply,
-// multiply-add) and adds their products with C.
+// multiply-add) and adds their products with C.  (Eight at a time of the widest rows, for the registers' sake.)
 // What bounds it: three vector instructions for each element of state and token.
 template <typename T, int NL, int NR, int MODE>
-__global__ void __launch_bounds__(64)
+__global__ void __launch_bounds__(64, NL * NR > 128 ? 1 : 2)
 selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c)
 {
-    constexpr int PR = 4, PW = 64 / NL * PR, NP = NL * NR, TT = 16;
-    __shared__ __align__(16) float sb[TT][NP + 4], sc[TT][NP + 4], sx[TT][PW + 4];
+    constexpr int PR = 4, PW = 64 / NL * PR, NP = NL * NR, TT = NP > 128 || PW > 128 ? 8 : 16;
+    __shared__ __align__(16) float sb[TT][NP + 4], sc[TT][NP + 4], sx[TT][PW + 4], sy[TT][PW + 4];
     __shared__ float2 sd[TT];
     const int lane = threadIdx.x, ln = lane % NL, lp = lane / NL;
     const int64_t id = scan_unit();
@@ -176,13 +179,13 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
     const int64_t head_at = ((int64_t)h * P + p0) * N;
 
     float S[PR][NR];
-    auto clear = [&]() {
+    auto clear = [&]() SCAN_INLINE {
 #pragma unroll
         for (int i = 0; i < PR; ++i)
 #pragma unroll
             for (int j = 0; j < NR; ++j) S[i][j] = 0.0f;
     };
-    auto each = [&](auto &&fn) {                     // fn(element, offset from the head's first) of those that exist
+    auto each = [&](auto &&fn) SCAN_INLINE {                     // fn(element, offset from the head's first) of those that exist
 #pragma unroll
         for (int i = 0; i < PR; ++i)
 #pragma unroll
@@ -194,46 +197,53 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
     float rb[LB], rc[MODE != SCAN_CARRY ? LB : 1], rx[LX], raw = 0.0f;
     const T *const rows = xbc + (int64_t)c.H * P + (int64_t)g * N, *const xs = xbc + (int64_t)h * P + p0;
     const int64_t to_c = (int64_t)c.G * N;
-    auto fetch = [&](int t, int t1) {
-#pragma unroll
-        for (int i = 0; i < LB; ++i) {
+    auto fetch = [&](int t, int t1) SCAN_INLINE {
+        static_for<0, LB>([&](auto i_) SCAN_INLINE {
+            constexpr int i = decltype(i_)::value;
             const int e = 64 * i + lane, n = e % NP;
             const T *row = rows + (int64_t)min(t + e / NP, t1 - 1) * c.ld + (n < N ? n : 0);
             rb[i] = (float)row[0];
             if constexpr (MODE != SCAN_CARRY) rc[i] = (float)row[to_c];
-        }
-#pragma unroll
-        for (int i = 0; i < LX; ++i) {
+        });
+        static_for<0, LX>([&](auto i_) SCAN_INLINE {
+            constexpr int i = decltype(i_)::value;
             const int e = 64 * i + lane, p = e % PW;
             rx[i] = (float)xs[(int64_t)min(t + e / PW, t1 - 1) * c.ld + (p < np ? p : 0)];
-        }
+        });
         raw = dt_raw(c.dt, min(t + lane % TT, t1 - 1), h);
     };
     // Tokens [t0, t1) of one sequence; adds their decay exponents to `sum`.
-    auto run = [&](int t0, int t1, float &sum) {
+    auto run = [&](int t0, int t1, float &sum) SCAN_INLINE {
         fetch(t0, t1);
         for (int t = t0; t < t1; t += TT) {
             const int nt = min(TT, t1 - t);
             __syncthreads();
-#pragma unroll
-            for (int i = 0; i < LB; ++i) {
+            static_for<0, LB>([&](auto i_) SCAN_INLINE {
+                constexpr int i = decltype(i_)::value;
                 const int e = 64 * i + lane, n = e % NP;
                 sb[e / NP][n] = n < N ? rb[i] : 0.0f;
                 if constexpr (MODE != SCAN_CARRY) sc[e / NP][n] = n < N ? rc[i] : 0.0f;
-            }
-#pragma unroll
-            for (int i = 0; i < LX; ++i) {
+            });
+            static_for<0, LX>([&](auto i_) SCAN_INLINE {
+                constexpr int i = decltype(i_)::value;
                 const int e = 64 * i + lane;
                 sx[e / PW][e % PW] = e % PW < np ? rx[i] : 0.0f;
-            }
+            });
             if (lane < TT) {
                 const float dt = dt_of(c.dt, raw, bias), ex = decay_exponent(dt, a);
                 sd[lane] = make_float2(__builtin_amdgcn_exp2f(ex), dt);
                 if (MODE == SCAN_CARRY) sb[lane][NP] = ex;
             }
             if (t + TT < t1) fetch(t + TT, t1);
+            float gate[MODE != SCAN_CARRY ? LX : 1]; // z of these tokens
+            if (MODE != SCAN_CARRY && c.z)
+                static_for<0, LX>([&](auto i_) SCAN_INLINE {
+                    constexpr int i = decltype(i_)::value;
+                    const int e = 64 * i + lane, p = e % PW;
+                    gate[i] = (float)static_cast<const T *>(c.z)[(int64_t)min(t + e / PW, t1 - 1) * c.ld_z + (int64_t)h * P + p0 + (p < np ? p : 0)];
+                });
             __syncthreads();
-            for (int r = 0; r < nt; ++r) {
+            auto token = [&](int r) SCAN_INLINE {
                 const float2 d = sd[r];
                 if (MODE == SCAN_CARRY) sum += sb[r][NP];
                 float y[PR];
@@ -250,34 +260,29 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
                 if (MODE != SCAN_CARRY) {
 #pragma unroll
                     for (int i = 0; i < PR; ++i) y[i] = lanes_sum<NL>(y[i]);
-                    if (ln == 0) {
-#pragma unroll
-                        for (int i = 0; i < PR; ++i) {
-                            const int p = lp * PR + i;
-                            sx[r][p] = fmaf(skip, sx[r][p], y[i]);
-                        }
-                    }
+                    if (ln == 0) *reinterpret_cast<f32x4_t *>(&sy[r][lp * PR]) = f32x4_t{y[0], y[1], y[2], y[3]};
                 }
-            }
+            };
+#pragma unroll 2
+            for (int r = 0; r < nt; ++r) token(r);
             if (MODE != SCAN_CARRY) {
                 __syncthreads();
-                for (int e = lane; e < nt * PW; e += 64) {
-                    const int r = e / PW, p = e % PW;
-                    if (p >= np) continue;
-                    float y = sx[r][p];
-                    const int64_t col = (int64_t)h * P + p0 + p;
-                    if (c.z) y *= silu((float)static_cast<const T *>(c.z)[(int64_t)(t + r) * c.ld_z + col]);
-                    store1(out + (int64_t)(t + r) * c.ld_out + col, y);
-                }
+                static_for<0, LX>([&](auto i_) SCAN_INLINE {
+                    constexpr int i = decltype(i_)::value;
+                    const int e = 64 * i + lane, r = e / PW, p = e % PW;
+                    float y = fmaf(skip, sx[r][p], sy[r][p]);
+                    if (c.z) y *= silu(gate[i]);
+                    if (r < nt && p < np) store1(out + (int64_t)(t + r) * c.ld_out + (int64_t)h * P + p0 + p, y);
+                });
             }
         }
     };
-    auto zeros = [&](int t0, int t1) {
+    auto zeros = [&](int t0, int t1) SCAN_INLINE {
         for (int t = t0; t < t1; ++t)
             for (int p = lane; p < np; p += 64) store1(out + (int64_t)t * c.ld_out + (int64_t)h * P + p0 + p, 0.0f);
     };
-    auto load = [&](const float *from) { each([&](float &v, int64_t at) { v = from[at]; }); };
-    auto store = [&](float *to) { each([&](float &v, int64_t at) { to[at] = v; }); };
+    auto load = [&](const float *from) SCAN_INLINE { each([&](float &v, int64_t at) SCAN_INLINE { v = from[at]; }); };
+    auto store = [&](float *to) SCAN_INLINE { each([&](float &v, int64_t at) SCAN_INLINE { to[at] = v; }); };
     scan_drive<MODE>(c, work, h, p0, head_at, lane, clear, load, store, run, zeros);
 }
 

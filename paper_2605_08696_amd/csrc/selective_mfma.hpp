@@ -17,12 +17,10 @@
 // LDS, since the wavefronts share it: its ten tiles of sixteen by sixteen tokens are dealt to them.
 #pragma once
 #include "selective.hpp"
-#include "tile.hpp"
 
 typedef __attribute__((ext_vector_type(4))) short i16x4_t;
 typedef __attribute__((ext_vector_type(8))) short i16x8_t;
 
-#define SCAN_INLINE __attribute__((always_inline))
 constexpr int kScanBlock = 32, kScanRows = 64;       // tokens of a block, rows of P of a work-group
 constexpr int kScanAhead = 4;                        // blocks whose sizes are formed together, one by each wavefront
 
