@@ -276,8 +276,9 @@ extern "C" int srm_selective_scan(int32_t dtype, const void *d_xbc, int64_t ld_x
     c.G = groups;
     c.N = state_dim;
     // (offsets inside a block of rows are 32 bits)
-    auto chunks = [](const void *q, int64_t ld) { return !q || (!misaligned(q, 16) && ld % 8 == 0 && ld < (1 << 23)); };
-    const bool whole = state_dim % 8 == 0 && head_dim % 8 == 0 && chunks(d_xbc, ld_xbc) && chunks(d_z, ld_z) && chunks(d_out, ld_out);
+    auto lies_whole = [](const void *q, int64_t ld) { return !q || (!misaligned(q, 16) && ld % 8 == 0 && ld < (1 << 23)); };
+    c.chunks = state_dim % 8 == 0 && head_dim % 8 == 0;
+    const bool whole = c.chunks && lies_whole(d_xbc, ld_xbc) && lies_whole(d_z, ld_z) && lies_whole(d_out, ld_out);
     c.state = d_state;
     c.seg = p.segments ? p.seg : 1;
     c.parts = p.parts;

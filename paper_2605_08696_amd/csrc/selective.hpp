@@ -28,6 +28,7 @@ struct ScanCall {
     const void *z;
     const float *a, *skip;
     int H, P, G, N;
+    int chunks;                                      // eight divides N and P
     float *state;                                    // [slots][H][P][N]
     int seg, parts;                                  // tokens of a segment; parts of a head's P rows
     float *carry, *held, *decay;                     // [segments][H][P][N] twice, [segments][H]

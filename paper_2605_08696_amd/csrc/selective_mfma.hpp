@@ -95,17 +95,17 @@ __device__ __forceinline__ void scan_barrier_lds() { asm volatile("s_waitcnt lgk
 
 // WHOLE: rows in whole chunks of eight elements, all at multiples of sixteen bytes, row strides of less than 2^23.
 //
-// A block's rows come to one of two LDS buffers while the block in front of it is worked on in the other, straight from memory (WHOLE; else
-// one element at a time).  Two barriers a block: its rows are there; M is there.  y takes x's place in LDS, and leaves from there in whole
+// A block's rows come to one of two LDS buffers while the block in front of it is worked on in the other, straight from memory (WHOLE), or by
+// way of registers where rows in whole chunks lie at any element, or one element at a time.  Two barriers a block: its rows are there; M is there.  y takes x's place in LDS, and leaves from there in whole
 // rows behind the next barrier (stored by each wavefront from its registers, 32 bytes of a row at a time, and z read so, the chip moves half
 // the bytes a second).
 template <int NP, int MODE, bool WHOLE>
-__global__ void __launch_bounds__(256, NP <= 128 ? 3 : 2)
+__global__ void __launch_bounds__(256, NP > 128 ? (MODE == SCAN_CARRY ? 2 : 1) : WHOLE || NP <= 64 ? 3 : 2)
 selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out, ScanCall c)
 {
     constexpr int CH = NP / 8, NJ = NP / 32, Q = kScanBlock, SLOTS = Q * CH / 64;    // loads of 64 chunks that B or C of a block takes
     constexpr bool Y = MODE != SCAN_CARRY;
-    __shared__ __align__(16) bf16 sb[2][Q * NP], sc[Y ? 2 : 1][Y ? Q * NP : 8], sx[2][Q * 64], sg[Y && WHOLE ? 2 : 1][Y && WHOLE ? Q * 64 : 8],
+    __shared__ __align__(16) bf16 sb[2][Q * NP], sc[Y ? 2 : 1][Y ? Q * NP : 8], sx[2][Q * 64], sg[Y ? 2 : 1][Y ? Q * 64 : 8],
         sm[Y ? Q * Q : 8];
     __shared__ __align__(16) ScanBlockSizes sizes[kScanAhead];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
@@ -172,6 +172,9 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
         y_off = ch * 8 < np ? (uint32_t)r * (uint32_t)c.ld_out * 2 + ch * 16 : kNone;
         lds_b = scan_lds_address(sb), lds_c = scan_lds_address(sc), lds_x = scan_lds_address(sx), lds_z = scan_lds_address(sg);
     }
+    typedef u32x4_t __attribute__((aligned(2))) u32x4_any;
+    constexpr int BC = (Q * CH + 255) / 256;
+    u32x4_t rb[WHOLE ? 1 : BC], rc[WHOLE || !Y ? 1 : BC], rx[2];
     // Rows [t, t + Q) up to t1 on their way to buffer `to`.
     auto bring = [&](int t, int t1, auto to_) SCAN_INLINE {
         constexpr int to = decltype(to_)::value;
@@ -193,6 +196,20 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
                 scan_dma16(lds_z + to * Q * 64 * 2 + wave * 1024,
                            scan_rows_at(static_cast<const bf16 *>(c.z) + (int64_t)t * c.ld_z + x_at, (uint32_t)(min(Q, t1 - t) - 1) * (uint32_t)c.ld_z * 2 + np * 2), z_off, 0);
         } else {
+            if (c.chunks) {
+                static_for<0, BC>([&](auto i_) SCAN_INLINE {
+                    constexpr int i = decltype(i_)::value;
+                    const int e = min(tid + 256 * i, Q * CH - 1), r = e / CH, ch = scan_chunk<CH>(r, e % CH) / 8 % CH;
+                    const bf16 *row = xbc + (int64_t)min(t + r, t1 - 1) * c.ld + min(ch * 8, N - 8);
+                    rb[i] = *reinterpret_cast<const u32x4_any *>(row + b_at);
+                    if constexpr (Y) rc[i] = *reinterpret_cast<const u32x4_any *>(row + c_at);
+                });
+                const int64_t row = min(t + (tid >> 3), t1 - 1);
+                const int col = min(scan_chunk<8>(tid >> 3, tid & 7) / 8 % 8 * 8, np - 8);
+                rx[0] = *reinterpret_cast<const u32x4_any *>(xbc + row * c.ld + x_at + col);
+                if (Y && c.z) rx[1] = *reinterpret_cast<const u32x4_any *>(static_cast<const bf16 *>(c.z) + row * c.ld_z + x_at + col);
+                return;
+            }
             for (int e = tid; e < Q * NP; e += 256) {
                 const int r = e / NP, n = e % NP;
                 const bool there = t + r < t1 && n < N;
@@ -200,20 +217,52 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
                 sb[to][scan_chunk<CH>(r, n >> 3) + (n & 7)] = there ? row[b_at] : (bf16)0.0f;
                 if constexpr (Y) sc[to][scan_chunk<CH>(r, n >> 3) + (n & 7)] = there ? row[c_at] : (bf16)0.0f;
             }
-            for (int e = tid; e < Q * 64; e += 256) {
-                const int r = e >> 6, p = e & 63;
-                sx[to][scan_chunk<8>(r, p >> 3) + (p & 7)] = t + r < t1 && p < np ? xbc[(int64_t)(t + r) * c.ld + x_at + p] : (bf16)0.0f;
+            for (int k = 0; k < 8; ++k) {            // (the rows whose y this wavefront has taken from there)
+                const int r = wave * 8 + k, p = lane;
+                const bool there = t + r < t1 && p < np;
+                sx[to][scan_chunk<8>(r, p >> 3) + (p & 7)] = there ? xbc[(int64_t)(t + r) * c.ld + x_at + p] : (bf16)0.0f;
+                if (Y && c.z) sg[to][scan_chunk<8>(r, p >> 3) + (p & 7)] = there ? static_cast<const bf16 *>(c.z)[(int64_t)(t + r) * c.ld_z + x_at + p] : (bf16)0.0f;
             }
+        }
+    };
+    // ... and from registers, where they came that way.
+    auto put = [&](int t, int t1, auto to_) SCAN_INLINE {
+        constexpr int to = decltype(to_)::value;
+        if constexpr (!WHOLE) {
+            if (!c.chunks) return;
+            const u32x4_t zero = {0, 0, 0, 0};
+            static_for<0, BC>([&](auto i_) SCAN_INLINE {
+                constexpr int i = decltype(i_)::value;
+                const int e = tid + 256 * i, r = e / CH, ch = scan_chunk<CH>(r, e % CH) / 8 % CH;
+                if (e >= Q * CH) return;
+                const bool there = t + r < t1 && ch * 8 < N;
+                *reinterpret_cast<u32x4_t *>(sb[to] + e * 8) = there ? rb[i] : zero;
+                if constexpr (Y) *reinterpret_cast<u32x4_t *>(sc[to] + e * 8) = there ? rc[i] : zero;
+            });
+            const bool there = t + (tid >> 3) < t1 && scan_chunk<8>(tid >> 3, tid & 7) / 8 % 8 * 8 < np;
+            *reinterpret_cast<u32x4_t *>(sx[to] + tid * 8) = there ? rx[0] : zero;
+            if (Y && c.z) *reinterpret_cast<u32x4_t *>(sg[to] + tid * 8) = there ? rx[1] : zero;
         }
     };
     // y of rows [t, t + Q) up to t1 from buffer `from`: this lane's chunk of the rows that this wavefront's loads bring to the same place next.
     auto leave = [&](int t, int t1, auto from_) SCAN_INLINE {
         constexpr int from = decltype(from_)::value;
-        if constexpr (Y && WHOLE) {
-            const u32x4_t v = *reinterpret_cast<const u32x4_t *>(sx[from] + tid * 8);
-            const auto rs = __builtin_amdgcn_make_buffer_rsrc(out + (int64_t)t * c.ld_out + x_at, 0,
-                                                              (uint32_t)(min(Q, t1 - t) - 1) * (uint32_t)c.ld_out * 2 + (uint32_t)np * 2, 0x00020000);
-            __builtin_amdgcn_raw_buffer_store_b128(v, rs, (int)y_off, 0, 0);
+        if constexpr (Y) {
+            if constexpr (WHOLE) {
+                const u32x4_t v = *reinterpret_cast<const u32x4_t *>(sx[from] + tid * 8);
+                const auto rs = __builtin_amdgcn_make_buffer_rsrc(out + (int64_t)t * c.ld_out + x_at, 0,
+                                                                  (uint32_t)(min(Q, t1 - t) - 1) * (uint32_t)c.ld_out * 2 + (uint32_t)np * 2, 0x00020000);
+                __builtin_amdgcn_raw_buffer_store_b128(v, rs, (int)y_off, 0, 0);
+            } else {
+                const bf16x8_t v = *reinterpret_cast<const bf16x8_t *>(sx[from] + tid * 8);
+                const int r = tid >> 3, col = scan_chunk<8>(r, tid & 7) / 8 % 8 * 8;
+                bf16 *o = out + (int64_t)(t + r) * c.ld_out + x_at + col;
+                if (t + r < t1 && col + 8 <= np) *reinterpret_cast<u32x4_any *>(o) = __builtin_bit_cast(u32x4_t, v);
+                else if (t + r < t1)
+#pragma unroll
+                    for (int i = 0; i < 7; ++i)
+                        if (col + i < np) o[i] = v[i];
+            }
         }
     };
     // The sizes of the kScanAhead blocks from t on: a token in each lane of a wavefront's halves.
@@ -378,33 +427,20 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
 #pragma unroll
                 for (int i = 0; i < 4; ++i) y[tt][i] = fmaf(skip, (float)x[i], acc[tt][i]);
             }
-            if constexpr (WHOLE) {
-                if (c.z)
-#pragma unroll
-                    for (int tt = 0; tt < 2; ++tt) {
-                        const bf16x4_t z = *reinterpret_cast<const bf16x4_t *>(sg[now] + scan_chunk<8>(tt * 16 + l16, p >> 3) + (p & 4));
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) y[tt][i] *= silu((float)z[i]);
-                    }
+            if (c.z)
 #pragma unroll
                 for (int tt = 0; tt < 2; ++tt) {
-                    const bf16x2_t lo = __builtin_convertvector(f32x2_t{y[tt][0], y[tt][1]}, bf16x2_t), hi = __builtin_convertvector(f32x2_t{y[tt][2], y[tt][3]}, bf16x2_t);
-                    *reinterpret_cast<bf16x4_t *>(xs + scan_chunk<8>(tt * 16 + l16, p >> 3) + (p & 4)) = __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
-                }
-            } else {
+                    const bf16x4_t z = *reinterpret_cast<const bf16x4_t *>(sg[now] + scan_chunk<8>(tt * 16 + l16, p >> 3) + (p & 4));
 #pragma unroll
-                for (int tt = 0; tt < 2; ++tt) {
-                    const int64_t row = t + tt * 16 + l16;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (row < t1 && p + i < np) {
-                            float v = y[tt][i];
-                            if (c.z) v *= silu((float)static_cast<const bf16 *>(c.z)[row * c.ld_z + x_at + p + i]);
-                            out[row * c.ld_out + x_at + p + i] = (bf16)v;
-                        }
+                    for (int i = 0; i < 4; ++i) y[tt][i] *= silu((float)z[i]);
                 }
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+                const bf16x2_t lo = __builtin_convertvector(f32x2_t{y[tt][0], y[tt][1]}, bf16x2_t), hi = __builtin_convertvector(f32x2_t{y[tt][2], y[tt][3]}, bf16x2_t);
+                *reinterpret_cast<bf16x4_t *>(xs + scan_chunk<8>(tt * 16 + l16, p >> 3) + (p & 4)) = __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
             }
         }
+        if (t + Q < t1) put(t + Q, t1, std::integral_constant<int, 1 - now>{});
     };
 
     // Tokens [t0, t1) of one sequence.
@@ -412,6 +448,7 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
         __syncthreads();                             // (nobody reads what an earlier call has left)
         bring(t0, t1, std::integral_constant<int, 0>{});
         raw = raw_of(t0, t1);
+        put(t0, t1, std::integral_constant<int, 0>{});
         if constexpr (Y)                             // the tile above the diagonal
             if (tid < 32) *reinterpret_cast<bf16x8_t *>(sm + scan_chunk<4>(tid & 15, 2 + (tid >> 4))) = bf16x8_t{};
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
