@@ -47,7 +47,7 @@ static int check_packed(const char *who, const int32_t *h_offsets, const int32_t
 
 // ------------------------------------------------------------------ the short convolution
 // Runs of 32 tokens, over which a thread's filter (32 W bytes) is read once, as long as they are two rounds of the chip's wavefronts; four
-// tokens at a time where the shortest runs are less than one.  (Four | eight, us: 37 x 2304 7.7 | 8.9, 300 x 2304 10.4 | 12.6, 32768 x 4352 135 |
+// tokens at a time of a short filter where the shortest runs are less than one.  (Four | eight, us: 37 x 2304 7.7 | 8.9, 300 x 2304 10.4 | 12.6, 32768 x 4352 135 |
 // 135, fp32 16384 x 4352 141 | 128, 4000 x 2304 of eight taps 39 | 32.)
 template <typename T, int W>
 static void launch_conv(const void *d_x, void *d_out, ConvCall c, int64_t tokens, hipStream_t st)
@@ -56,7 +56,7 @@ static void launch_conv(const void *d_x, void *d_out, ConvCall c, int64_t tokens
         c.runs = cdiv(tokens, c.run = run);
         return c.units > 64 ? c.runs * cdiv(c.units, 64) : cdiv(c.runs, 64 / c.per_run);
     };
-    const bool few = waves(8) < 4096;
+    const bool few = W <= 4 && waves(8) < 4096;
     int64_t n;
     if (few) {
         n = waves(4);
@@ -142,7 +142,10 @@ static int check_heads(const char *who, int32_t dtype, int32_t dt_dtype, const H
     return SRM_OK;
 }
 
-// How a scan is cut over time.  A work-group holds `rows` rows of P; `chip` of them run at the chip's full rate together.
+// How a scan is cut over time.  A work-group holds `rows` rows of P; `chip` of them run at the chip's full rate together.  Segments cost a
+// pass of their own that forms the states at their ends (about half of the work again), so that whole sequences are taken up to three times a
+// segment's length (us, whole | segments: 8192 tokens in eight prompts of 32 heads 60 | 82; one prompt of 16384, 32 work-groups, with 256 | 384 |
+// 512 | 768 | 1024 work-groups of segments 167 | 150 | 126 | 115 | 133).
 struct ScanPlan {
     int parts, seg, segments;                        // segments 0: every sequence as a whole
 };
@@ -161,7 +164,7 @@ static ScanPlan scan_plan(int32_t dtype, const HeadSizes &s, int64_t tokens, int
     ScanPlan p{(int)cdiv(s.P, scan_rows(dtype, s)), 0, 0};
     const int64_t chip = dtype == SRM_BF16 ? 768 : 2048, units = (int64_t)s.H * p.parts, least = 64;
     const int64_t seg = std::max(least, cdiv(cdiv(tokens * units, chip), 64) * 64);
-    if (longest > 2 * seg + 2 * least) {
+    if (longest > 3 * seg + 3 * least) {
         p.seg = (int)seg;
         p.segments = (int)cdiv(tokens, seg);
     }

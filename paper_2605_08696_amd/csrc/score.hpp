@@ -15,7 +15,8 @@
 // other, a reading each.
 //
 // What bounds it: the row is read once; for bf16 rows about as much the ten instruction slots that a logit takes, four of them its
-// exponential's.  One row: one CU's share of both.
+// exponential's: 2001 x 128001 bf16 139 us, 512 MB at 3.7 TB/s, 600 x 150000 fp32 74 us, 4.9 TB/s.  One row: one CU's share of both, 32000 fp32
+// logits 8.6 us, 150000 bf16 ones 22.  (With two readings, the threads' sums joined one by one and a compare for each exponential 189, 80, 15, 33.)
 #pragma once
 #include "fp8.hpp"
 

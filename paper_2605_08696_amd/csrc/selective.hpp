@@ -8,7 +8,7 @@
 // a first pass leaves, for each segment that a sequence runs on from, the state at its end that the segment itself brings (`carry`) and
 // the factor by which it decays what came before (`decay`); a second one makes of these the states at the segments' ends; the third starts
 // each segment from the one in front of it and writes the outputs.  (Joined by the third pass itself, every segment adding up all carries in
-// front of it, 16384 tokens of 32 heads took 146 us instead of 130.)
+// front of it, 16384 tokens of 32 heads took 146 us, so 115.)
 #pragma once
 #include "conv.hpp"
 #include "tile.hpp"
@@ -51,8 +51,13 @@ __device__ __forceinline__ float dt_raw(const StepSizes &c, int64_t t, int h)
 __device__ __forceinline__ float dt_of(const StepSizes &c, float raw, float bias)
 {
     const float v = raw + bias;
-    // (log(1 + e^v) without loss on either side; a NaN stays one)
-    return c.softplus ? (v > 0.0f ? v : v == v ? 0.0f : v) + log1pf(__expf(-fabsf(v))) : v;
+    if (!c.softplus) return v;
+    // log(1 + e^v) = max(v, 0) + log(1 + u), u = e^-|v|; the logarithm by its series up to u = 1/16, where 1 + u would drop digits of u (the
+    // first term left out is below 2^-26 of the sum).  (A NaN stays one.)
+    const float u = __expf(-fabsf(v));
+    const float series = u * fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, -1.0f / 6.0f, 0.2f), -0.25f), 1.0f / 3.0f), -0.5f), 1.0f);
+    const float log = u < 0.0625f ? series : 0.69314718055994530942f * __builtin_amdgcn_logf(1.0f + u);
+    return (v > 0.0f ? v : v == v ? 0.0f : v) + log;
 }
 // The decay's exponent in steps of a factor of two.  Below 2^-200 a decay leaves nothing of a state of fp32; the limit keeps sums of
 // exponents small enough that their differences are exact where the decays are not 0.  (A comparison, so that a NaN stays one.)
@@ -160,7 +165,8 @@ selective_scan_join_kernel(float *__restrict__ carry, const float *__restrict__ 
 // One wavefront takes PR rows of P a lane, NL lanes with NR elements of N each: 64 / NL * PR rows, NL NR >= N.  Sixteen tokens at a time
 // are brought to LDS, the next sixteen on their way in registers; then for every token each lane updates its PR x NR elements (multiply,
 // multiply-add) and adds their products with C.  (Eight at a time of the widest rows, for the registers' sake.)
-// What bounds it: three vector instructions for each element of state and token.
+// What bounds it: three vector instructions for each element of state and token: 8192 tokens in eight prompts of 32 heads of 64 x 128 take
+// 434 us, of which those are 224.  (With the rows of a tile fetched when it is its turn, 1667 tokens of 10 heads of 50 x 37 took 123 us, now 65.)
 template <typename T, int NL, int NR, int MODE>
 __global__ void __launch_bounds__(64, NL * NR > 128 ? 1 : 2)
 selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c)
@@ -291,7 +297,8 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
 // Four wavefronts of a work-group, or one, take PW rows of P of one head of one request.  The state's loads start as soon as the slot is
 // known, the convolution of the head's x and its group's B and C runs while they travel.  B and C are formed anew for every head of a group;
 // the ring's row of the new token, which none of the taps reads, is written for the group's first head alone.
-// What bounds it: the state is read and written once.
+// What bounds it: the state is read and written once: 300 requests of 32 heads of 64 x 128 take 131 us, 640 MB at 4.9 TB/s, one request 6 (a launch
+// and its trips to memory; with the taps one by one 8.8).  1024 requests of 32 heads of 16 x 16: 32 us, 86 with four wavefronts to a head.
 struct StepCall {
     StepSizes dt;
     int64_t rows, slots, ld, ld_z, ld_out;

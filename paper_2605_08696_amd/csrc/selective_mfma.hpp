@@ -96,11 +96,18 @@ __device__ __forceinline__ void scan_barrier_lds() { asm volatile("s_waitcnt lgk
 // WHOLE: rows in whole chunks of eight elements, all at multiples of sixteen bytes, row strides of less than 2^23.
 //
 // A block's rows come to one of two LDS buffers while the block in front of it is worked on in the other, straight from memory (WHOLE), or by
-// way of registers where rows in whole chunks lie at any element, or one element at a time.  Two barriers a block: its rows are there; M is there.  y takes x's place in LDS, and leaves from there in whole
-// rows behind the next barrier (stored by each wavefront from its registers, 32 bytes of a row at a time, and z read so, the chip moves half
-// the bytes a second).
+// way of registers where rows in whole chunks lie at any element, or one element at a time.  Two barriers a block: its rows are there; M is
+// there.  y takes x's place in LDS, and leaves from there in whole rows behind the next barrier.
+//
+// What bounds it: 32768 tokens in eight prompts of 64 heads of 64 x 128 take 305 us, 940 MB at 3.1 TB/s.  Two work-groups on a CU; their
+// wavefronts issue vector instructions for half of the time, 271 a block beside 37 products of 16 clocks, and wait for each other, for LDS and
+// for products for two fifths.  Without the two smaller parts of x 274, without M 284, without the gate's exponentials 289; without any of these
+// and the other products 242, which is what the trips through memory take.  Not kept: three buffers (two work-groups on a CU instead of
+// three): 331, 8192 tokens in eight prompts of 32 heads 62 | 60 with two, states of 256 99 | 91; loads and stores that bypass the caches +-2%.
+// On the way: blocks of 64 tokens with rows through registers 394 (228 registers), each block's decays formed by one wavefront in front of a
+// barrier 394, by all for four blocks 354, y stored and z read by each wavefront in 32 bytes of a row 332.
 template <int NP, int MODE, bool WHOLE>
-__global__ void __launch_bounds__(256, NP > 128 ? (MODE == SCAN_CARRY ? 2 : 1) : WHOLE || NP <= 64 ? 3 : 2)
+__global__ void __launch_bounds__(256, NP > 128 && MODE != SCAN_CARRY ? 1 : WHOLE || NP <= 64 ? 3 : 2)
 selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out, ScanCall c)
 {
     constexpr int CH = NP / 8, NJ = NP / 32, Q = kScanBlock, SLOTS = Q * CH / 64;    // loads of 64 chunks that B or C of a block takes
@@ -291,14 +298,15 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
     // Block [t, t + Q) up to t1, number n of its sequence, which lies in buffer `now`.
     auto block = [&](int t, int t1, int n, auto now_) SCAN_INLINE {
         constexpr int now = decltype(now_)::value;
+        constexpr int then = 1 - now;                // the buffer of the blocks before and behind
         if constexpr (WHOLE) scan_barrier<0>();
         else scan_barrier_lds();
-        // (dt has come with the block's rows; the compiler, which does not count those, must not wait for it later)
+        // (dt has come with some block's rows; the compiler, which does not count those, must not wait for it behind further ones)
         asm volatile("" : "+v"(raw));
-        if (n > 0) leave(t - Q, t1, std::integral_constant<int, 1 - now>{});
+        if (n > 0) leave(t - Q, t1, std::integral_constant<int, then>{});
         if (t + Q < t1) {
             asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");               // (y has been read)
-            bring(t + Q, t1, std::integral_constant<int, 1 - now>{});
+            bring(t + Q, t1, std::integral_constant<int, then>{});
         }
         if (n % kScanAhead == 0) {
             put_sizes(raw, t, t1);
@@ -440,33 +448,29 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
                 *reinterpret_cast<bf16x4_t *>(xs + scan_chunk<8>(tt * 16 + l16, p >> 3) + (p & 4)) = __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
             }
         }
-        if (t + Q < t1) put(t + Q, t1, std::integral_constant<int, 1 - now>{});
+        if (t + Q < t1) put(t + Q, t1, std::integral_constant<int, then>{});
     };
 
     // Tokens [t0, t1) of one sequence.
     auto run = [&](int t0, int t1, float &sum) SCAN_INLINE {
         __syncthreads();                             // (nobody reads what an earlier call has left)
-        bring(t0, t1, std::integral_constant<int, 0>{});
         raw = raw_of(t0, t1);
+        bring(t0, t1, std::integral_constant<int, 0>{});
         put(t0, t1, std::integral_constant<int, 0>{});
         if constexpr (Y)                             // the tile above the diagonal
             if (tid < 32) *reinterpret_cast<bf16x8_t *>(sm + scan_chunk<4>(tid & 15, 2 + (tid >> 4))) = bf16x8_t{};
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         sum_of = 0.0f;
-        for (int t = t0, n = 0;; n += 2) {
-            block(t, t1, n, std::integral_constant<int, 0>{});
-            if ((t += Q) >= t1) {
-                scan_barrier_lds();
-                leave(t - Q, t1, std::integral_constant<int, 0>{});
-                break;
-            }
-            block(t, t1, n + 1, std::integral_constant<int, 1>{});
-            if ((t += Q) >= t1) {
-                scan_barrier_lds();
-                leave(t - Q, t1, std::integral_constant<int, 1>{});
-                break;
-            }
-        }
+        for (int t = t0, n = 0; t < t1;)
+            static_for<0, 2>([&](auto now_) SCAN_INLINE {
+                if (t >= t1) return;
+                block(t, t1, n++, now_);
+                t += Q;
+                if (t >= t1) {
+                    scan_barrier_lds();
+                    leave(t - Q, t1, now_);
+                }
+            });
         sum += sum_of;
     };
     scan_drive<MODE>(c, work, h, p0, head_at, lane, clear, load, store, run, zeros);
