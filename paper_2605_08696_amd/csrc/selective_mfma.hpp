@@ -100,7 +100,7 @@ __device__ __forceinline__ void scan_barrier_lds() { asm volatile("s_waitcnt lgk
 // there.  y takes x's place in LDS, and leaves from there in whole rows behind the next barrier.
 //
 // What bounds it: 32768 tokens in eight prompts of 64 heads of 64 x 128 take 305 us, 940 MB at 3.1 TB/s.  Two work-groups on a CU; their
-// wavefronts issue vector instructions for half of the time, 271 a block beside 37 products of 16 clocks, and wait for each other, for LDS and
+// wavefronts issue vector instructions for half of the time, 236 a block beside 37 products of 16 clocks, and wait for each other, for LDS and
 // for products for two fifths.  Without the two smaller parts of x 274, without M 284, without the gate's exponentials 289; without any of these
 // and the other products 242, which is what the trips through memory take.  Not kept: three buffers (two work-groups on a CU instead of
 // three): 331, 8192 tokens in eight prompts of 32 heads 62 | 60 with two, states of 256 99 | 91; loads and stores that bypass the caches +-2%.
