@@ -670,8 +670,8 @@ int srm_sample_rows(int32_t dtype, const void *d_logits, int64_t ld, int64_t row
  * d_pos [N] (device, int32; NULL: all 0) is the position of each sequence's first row in its conversation, for a prompt that comes in
  * several calls.  At position 0 nothing is read from the slot (it need not be cleared).  A negative position marks a sequence as idle: its
  * rows of the output become zeros, its slot stays.  d_slot [N] (device, int32; NULL: sequence n has slot n) is where what a sequence leaves
- * lies in a state of `slots` slots; outside [0, slots), or without a state, a sequence starts from zeros and leaves nothing.  Two sequences of
- * a call that share a slot leave it unspecified.  Buffers of a call must not overlap.  All calls may be made under stream capture.
+ * lies in a state of `slots` slots; outside [0, slots), or without a state, a sequence starts from zeros and leaves nothing.  Two sequences (or
+ * rows of a step) that share a slot leave it unspecified.  Buffers of a call must not overlap.  All calls may be made under stream capture.
  *
  * srm_causal_conv: out[t, c] = act(bias[c] + sum_k w[c, k] x[t - (width - 1) + k, c]), each channel by itself; act: 0 = none,
  * 1 = SiLU, v / (1 + e^-v).  d_x and d_out [rows][channels] of type dtype (SRM_FP32 | SRM_BF16), row strides ldx, ld_out; d_weight

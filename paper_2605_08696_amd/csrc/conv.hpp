@@ -109,7 +109,7 @@ causal_conv_kernel(const T *__restrict__ x, T *__restrict__ out, ConvCall c)
             const int64_t p = (int64_t)s.pos + at - s.begin;
             const bool old = at < s.begin;
             none[j] = old && (p < 0 || !ring);
-            hist[j] = raw8(none[j] || !old ? row_of(max(at, s.begin)) : ring + p % W * C, col, C);
+            hist[j] = raw8(!old ? row_of(at) : none[j] ? row_of(u) : ring + p % W * C, col, C);
         }
 #pragma unroll
         for (int j = 0; j < R; ++j) next[j] = raw8(row_of(min(u + j, until - 1)), col, C);

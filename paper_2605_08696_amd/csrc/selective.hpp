@@ -123,9 +123,9 @@ __device__ __forceinline__ void scan_drive(const ScanCall &c, int64_t work, int 
                 zeros(t, e);
             } else {
                 clear();
-                if (t == s.begin) {
+                if (t <= s.begin) {
                     if (s.slot >= 0 && s.pos > 0) load(s.end > t1 ? c.held + work * slot_size + head_at : slot_of(s));
-                } else {
+                } else if (work > 0) {               // (always, with the host's offsets)
                     load(c.carry + (work - 1) * slot_size + head_at);
                 }
                 run(t, e, sum);
