@@ -695,10 +695,13 @@ def _vector(t, n: int, dtype, name: str):
         raise ValueError(f"{name}: must be {n} contiguous {str(dtype)[6:]} values")
 
 
-def _vectors(n: int, dtype, **named):
-    for name, t in named.items():
+def _vectors(n: int, dtype, tensors, names):
+    for t, name in zip(tensors, names):
         if t is not None and (t.dtype is not dtype or t.numel() != n or not t.is_contiguous()):
             _vector(t, n, dtype, name)
+
+
+_INT_AT = C.c_int32.from_address
 
 
 def _offsets(offsets, d_offsets, rows: int):
@@ -713,7 +716,7 @@ def _offsets(offsets, d_offsets, rows: int):
         at, n = keep.ctypes.data, keep.size - 1
     if n < 1:
         raise ValueError("offsets: need at least two boundaries")
-    last = C.c_int32.from_address(at + 4 * n).value
+    last = _INT_AT(at + 4 * n).value
     if last > rows:
         raise ValueError(f"offsets: {last} rows, the operands have {rows}")
     _vector(d_offsets, n + 1, torch.int32, "d_offsets")
@@ -721,6 +724,10 @@ def _offsets(offsets, d_offsets, rows: int):
 
 
 def _same_rows(t, rows: int, cols: int, name: str, dtype=None):
+    if t.shape == (rows, cols) and (dtype is None or t.dtype is dtype):
+        ld, step = t.stride()
+        if step == 1 and (ld >= cols or rows <= 1):
+            return ld if ld >= cols else cols
     n, c, ld = _rows_of(t, name)
     if n != rows or c != cols:
         raise ValueError(f"{name}: shape {(n, c)}, expected {(rows, cols)}")
@@ -732,9 +739,10 @@ def _same_rows(t, rows: int, cols: int, name: str, dtype=None):
 def _slots_of(state, shape, dtype, name: str) -> int:
     if state is None:
         return 0
-    if state.dtype is not dtype or state.shape[1:] != shape or not state.is_contiguous():
+    size = state.shape
+    if state.dtype is not dtype or size[1:] != shape or not state.is_contiguous():
         raise ValueError(f"{name}: must be contiguous {str(dtype)[6:]} of shape (slots, {', '.join(map(str, shape))})")
-    return state.shape[0]
+    return size[0]
 
 
 def causal_conv(x, weight, bias, offsets, d_offsets, out, pos=None, slot=None, state=None, activation=True, stream=None):
@@ -750,7 +758,7 @@ def causal_conv(x, weight, bias, offsets, d_offsets, out, pos=None, slot=None, s
     _vector(weight, channels * width, torch.float32, "weight")
     if bias is not None:
         _vector(bias, channels, torch.float32, "bias")
-    _vectors(n, torch.int32, pos=pos, slot=slot)
+    _vectors(n, torch.int32, (pos, slot), ("pos", "slot"))
     slots = _slots_of(state, (width, channels), x.dtype, "state")
     ld_out = _same_rows(out, rows, channels, "out", x.dtype)
     _launch(lib().srm_causal_conv, (_row_dtype(x, "x"), x.data_ptr(), ldx, weight.data_ptr(), _ptr(bias), 1 if activation else 0, channels, width,
@@ -770,7 +778,7 @@ def _heads(xbc, dt, a, out, groups, dt_bias, skip, z):
     left = channels - inner
     if left <= 0 or left % (2 * groups):
         raise ValueError(f"xbc: {channels} columns are not {inner} + 2 x {groups} x state_dim")
-    _vectors(heads, _torch().float32, a=a, dt_bias=dt_bias, skip=skip)
+    _vectors(heads, _torch().float32, (a, dt_bias, skip), ("a", "dt_bias", "skip"))
     ld_z = 0 if z is None else _same_rows(z, rows, inner, "z", xbc.dtype)
     return rows, ld, _same_rows(dt, rows, heads, "dt"), ld_z, ld_out, heads, inner // heads, left // (2 * groups)
 
@@ -790,7 +798,7 @@ def selective_scan(xbc, dt, a, offsets, d_offsets, out, groups=1, dt_bias=None, 
     torch = _torch()
     rows, ld, ld_dt, ld_z, ld_out, heads, head_dim, state_dim = _heads(xbc, dt, a, out, groups, dt_bias, skip, z)
     h, n, keep = _offsets(offsets, d_offsets, rows)
-    _vectors(n, torch.int32, pos=pos, slot=slot)
+    _vectors(n, torch.int32, (pos, slot), ("pos", "slot"))
     slots = _slots_of(state, (heads, head_dim, state_dim), torch.float32, "state")
     code = _row_dtype(xbc, "xbc")
     if workspace is None:
@@ -815,9 +823,11 @@ def selective_step(xbc, dt, a, pos, state, out, groups=1, weight=None, bias=None
     causal_conv and selective_scan.  Without weight there is no convolution."""
     torch = _torch()
     rows, ld, ld_dt, ld_z, ld_out, heads, head_dim, state_dim = _heads(xbc, dt, a, out, groups, dt_bias, skip, z)
-    _vector(pos, rows, torch.int32, "pos")
-    if slot is not None:
-        _vector(slot, rows, torch.int32, "slot")
+    if pos is None:
+        raise ValueError("pos: must be given")
+    _vectors(rows, torch.int32, (pos, slot), ("pos", "slot"))
+    if state is None:
+        raise ValueError("state: must be given")
     slots = _slots_of(state, (heads, head_dim, state_dim), torch.float32, "state")
     width = 0
     if weight is not None:
@@ -831,9 +841,11 @@ def selective_step(xbc, dt, a, pos, state, out, groups=1, weight=None, bias=None
         if conv_state is not None and _slots_of(conv_state, (width, channels), xbc.dtype, "conv_state") != slots:
             raise ValueError(f"conv_state: {conv_state.shape[0]} slots, state has {slots}")
     _launch(lib().srm_selective_step,
-            (_row_dtype(xbc, "xbc"), xbc.data_ptr(), ld, _ptr(weight), _ptr(bias), 1 if activation else 0, width, _ptr(conv_state),
-             _row_dtype(dt, "dt"), dt.data_ptr(), ld_dt, a.data_ptr(), _ptr(dt_bias), _ptr(skip), 1 if softplus else 0, _ptr(z), ld_z, heads,
-             head_dim, groups, state_dim, rows, _ptr(pos), _ptr(slot), slots, _ptr(state), out.data_ptr(), ld_out),
+            (_row_dtype(xbc, "xbc"), xbc.data_ptr(), ld, None if weight is None else weight.data_ptr(), None if bias is None else bias.data_ptr(),
+             1 if activation else 0, width, None if conv_state is None else conv_state.data_ptr(), _row_dtype(dt, "dt"), dt.data_ptr(), ld_dt,
+             a.data_ptr(), None if dt_bias is None else dt_bias.data_ptr(), None if skip is None else skip.data_ptr(), 1 if softplus else 0,
+             None if z is None else z.data_ptr(), ld_z, heads, head_dim, groups, state_dim, rows, pos.data_ptr(),
+             None if slot is None else slot.data_ptr(), slots, state.data_ptr(), out.data_ptr(), ld_out),
             xbc, (dt, a, dt_bias, skip, z, pos, slot, state, weight, bias, conv_state, out), stream)
 
 
@@ -844,7 +856,7 @@ def token_logprobs(logits, token, logprob, temperature=None, entropy=None, top_t
     rows, vocab, ld = _rows_of(logits, "logits")
     if token is not None:
         _vector(token, rows, torch.int32, "token")
-    _vectors(rows, torch.float32, logprob=logprob, temperature=temperature, entropy=entropy)
+    _vectors(rows, torch.float32, (logprob, temperature, entropy), ("logprob", "temperature", "entropy"))
     top = 0
     if top_token is not None or top_logprob is not None:
         if top_token is None or top_logprob is None or top_token.dim() != 2:
