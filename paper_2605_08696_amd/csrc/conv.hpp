@@ -122,12 +122,18 @@ causal_conv_kernel(const T *__restrict__ x, T *__restrict__ out, ConvCall c)
                 for (int i = 0; i < 8; ++i) v[j][i] = 0.0f;
             }
         }
-        if (starts && ring)
-            for (int e = max(s.begin, s.end - W); e < s.end; ++e) {
+        if (starts && ring) {
+            Raw8<T> last[W];
+#pragma unroll
+            for (int j = 0; j < W; ++j) last[j] = raw8(row_of(max(s.end - W + j, s.begin)), col, C);
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                const int e = s.end - W + j;
                 float q[8];
-                values(raw8(row_of(e), col, C), q);
-                store8(ring + ((int64_t)s.pos + e - s.begin) % W * C + col, n_cols, q);
+                values(last[j], q);
+                if (e >= s.begin) store8(ring + ((int64_t)s.pos + e - s.begin) % W * C + col, n_cols, q);
             }
+        }
         for (; u < until; u += R) {
             Raw8<T> now[R];
 #pragma unroll

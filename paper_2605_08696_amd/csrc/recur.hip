@@ -48,7 +48,7 @@ static int check_packed(const char *who, const int32_t *h_offsets, const int32_t
 // ------------------------------------------------------------------ the short convolution
 // Runs of 32 tokens, over which a thread's filter (32 W bytes) is read once, as long as they are two rounds of the chip's wavefronts; four
 // tokens at a time of a short filter where the shortest runs are less than one.  (Four | eight, us: 37 x 2304 7.7 | 8.9, 300 x 2304 10.4 | 12.6, 32768 x 4352 135 |
-// 135, fp32 16384 x 4352 141 | 128, 4000 x 2304 of eight taps 39 | 32.)
+// 135, fp32 16384 x 4352 141 | 128, 4000 x 2304 of eight taps 39 | 32; 300 x 2304 in 300 sequences 17, in runs of one 10.)
 template <typename T, int W>
 static void launch_conv(const void *d_x, void *d_out, ConvCall c, int64_t tokens, hipStream_t st)
 {
@@ -58,13 +58,11 @@ static void launch_conv(const void *d_x, void *d_out, ConvCall c, int64_t tokens
     };
     const bool few = W <= 4 && waves(8) < 4096;
     int64_t n;
-    if (few) {
-        n = waves(4);
-    } else {
-        int run = 32;
-        while (run > 8 && waves(run) < 8192) run /= 2;
-        n = waves(run);
-    }
+    int run = few ? 4 : 32;
+    while (run > 8 && waves(run) < 8192) run /= 2;
+    // (the sequences of a run are worked on one after the other: shorter runs of sequences that are shorter still)
+    while (run > 1 && (int64_t)run * c.seqs.n > tokens && waves(run / 2) <= 16384) run /= 2;
+    n = waves(run);
     hipLaunchKernelGGL((few ? causal_conv_kernel<T, W, 4> : causal_conv_kernel<T, W, 8>), grid_of(cdiv(n, 4)), dim3(256), 0, st, static_cast<const T *>(d_x),
                        static_cast<T *>(d_out), c);
 }
@@ -100,7 +98,7 @@ extern "C" int srm_causal_conv(int32_t dtype, const void *d_x, int64_t ldx, cons
     if (misaligned(d_x, size) || misaligned(d_out, size) || misaligned(d_state, size) || misaligned(d_weight, 4) || misaligned(d_bias, 4))
         return fail(SRM_EINVAL, "%s: %s", who, kNotWhole);
     const int64_t tokens = c.seqs.hi - c.seqs.lo;
-    if (cdiv(tokens, 4) * cdiv(channels, 512) >= kMaxBlocks) return fail(SRM_EINVAL, "%s: sizes out of range", who);
+    if (tokens * cdiv(channels, 512) >= kMaxBlocks) return fail(SRM_EINVAL, "%s: sizes out of range", who);
     if (tokens == 0) return SRM_OK;
     c.ldx = ldx;
     c.ld_out = ld_out;
