@@ -9,7 +9,7 @@
 // holds the first of them, in which the same thread writes the ring behind them.
 // What bounds it: memory (x is read once, out written once) and, for bf16, the instructions of the activation (five for a value, two of them
 // at a quarter of the rate).  32768 x 4352 bf16, four taps 135 us, 571 MB at 4.2 TB/s, fp32 16384 x 4352 127 us, 4.5 TB/s; 37 x 2304, which is a
-// launch and three trips to memory, 7.6.  With runs of eight tokens, each of which reads its filter, and branches around the loads at a
+// launch and three trips to memory, 7.3.  With runs of eight tokens, each of which reads its filter, and branches around the loads at a
 // sequence's begin: 193 and 15.
 #pragma once
 #include "fp8.hpp"

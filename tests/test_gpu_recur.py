@@ -37,7 +37,7 @@ def _near(got, want, bound, what):
 
 
 # ------------------------------------------------------------------ convolution
-LENGTHS = [[1], [0, 1, 2, 0, 3, 4, 5], [8], [7, 9], [100], [1, 1, 1, 1, 1, 30, 1, 64], [65, 0, 17], [3] * 90]
+LENGTHS = [[1], [0, 1, 2, 0, 3, 4, 5], [8], [7, 9], [100], [1, 1, 1, 1, 1, 30, 1, 64], [65, 0, 17], [3] * 90, [1] * 70, [2, 1, 0] * 30]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
