@@ -688,8 +688,8 @@ int srm_sample_rows(int32_t dtype, const void *d_logits, int64_t ld, int64_t row
  * ld_xbc, and d_z [rows][heads * head_dim] (may be NULL: out = y) and d_out as x, row strides ld_z, ld_out, all of type dtype; d_dt
  * [rows][heads] of type dt_dtype; d_a, d_dt_bias, d_skip [heads] fp32 (the last two may be NULL).  a <= 0 is meant: with a > 0 the formula
  * holds as long as nothing overflows.  d_state [slots][heads][head_dim][state_dim] fp32 (may be NULL) is read (from position 1 on) and
- * updated.  state_dim up to 256.  The state, decays and all sums are fp32.  With bf16 operands, states and the weights of earlier tokens are
- * rounded to bf16 (2^-9 of their values) where they are multiplied on the matrix cores for y; what is kept is not.
+ * updated.  state_dim up to 256.  The state, decays and all sums are fp32.  With bf16 operands, what is multiplied on the matrix
+ * cores is cut into two bf16 numbers for y (2^-15 of a factor is lost at most) and into three for the state (nothing is).
  * d_workspace: a call with few sequences and heads is cut into segments of time, whose states lie there;
  * srm_selective_scan_workspace_bytes(the same arguments) is what the best cut takes (0: none), and with less, or NULL, there are fewer
  * segments or none.  Its content means nothing between calls; calls that may overlap in time need one each.  Results may differ in the

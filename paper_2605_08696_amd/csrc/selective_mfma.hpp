@@ -6,15 +6,17 @@
 // that is four products with 32 tokens as one side.  The running sum is formed in 64 bits, so that the exponents of S', which are small where
 // the weights are not, and of M lose nothing to what came before them.
 //
-// Roundings.  The state stays in fp32 in the accumulators of its own product.  What is rounded to bf16 is, for y alone, M and the copy of S
-// that meets C (2^-9 each, as much as y itself when it is stored).  x times its weight for S' is not rounded: it is cut into three bf16
-// numbers that add up to it, each of which is multiplied; with two the state would be 3e-6 off.
+// Roundings.  The state stays in fp32 in the accumulators of its own product.  M and the copy of S that meets C are cut into two bf16 numbers
+// each, which leave 2^-15 of a value at most (a hundredth of what y may lose when it is stored), and both are multiplied.  x times its
+// weight for S' is cut into three bf16 numbers that add up to it; with two the state would be 3e-6 off.
 //
 // Layout.  Four wavefronts with sixteen rows p of the head each.  A product's result D[i][j] lies as column j in lane j % 16, rows
 // 4 (lane / 16) .. + 3; an operand as row or column lane % 16, eight k from 8 (lane / 16) on.  S is formed as S^T (rows n), its rows n in
 // such an order that a lane's two tiles hold eight consecutive n: converted, they are the operand that meets C, without a way through LDS.
 // y is formed as y^T (rows p), four consecutive p of a token in a lane.  B^T and x^T come from LDS by the transposing reads.  M goes through
-// LDS, since the wavefronts share it: its ten tiles of sixteen by sixteen tokens are dealt to them.
+// LDS, since the wavefronts share it: three of them form one of its tiles of sixteen by sixteen tokens each.  The tile of the later sixteen tokens
+// with themselves, the one with the sixteen in front and their remainders make two operands of 32 tokens; the first sixteen's own tile and
+// its remainder are one, against those tokens of x twice.
 #pragma once
 #include "selective.hpp"
 
@@ -44,6 +46,17 @@ __device__ __forceinline__ bf16x8_t scan_pair(i16x4_t a, i16x4_t b)
     return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// Two values as pairs of bf16: their upper halves, and what these leave (less than 2^-7 of a value), rounded.
+struct ScanHalves {
+    uint32_t high, low;
+};
+__device__ __forceinline__ ScanHalves scan_halves(float a, float b)
+{
+    const uint32_t u = __float_as_uint(a), v = __float_as_uint(b);
+    const f32x2_t left = {a - __uint_as_float(u & 0xffff0000u), b - __uint_as_float(v & 0xffff0000u)};
+    return {__builtin_amdgcn_perm(v, u, 0x07060302u), __builtin_bit_cast(uint32_t, __builtin_convertvector(left, bf16x2_t))};
+}
+
 // Running sum over each half of the wavefront's lanes, this one's included.
 __device__ __forceinline__ double half_scan(double v)
 {
@@ -62,9 +75,8 @@ __device__ __forceinline__ double half_scan(double v)
     return v;
 }
 
-struct ScanBlockSizes {                              // of a block's tokens: running exponent, dt, weight in S', 2^exponent
-    float e[kScanBlock], dt[kScanBlock], w[kScanBlock], f[kScanBlock];
-    float total, factor;                             // the block's exponent and 2^it
+struct ScanBlockSizes {                              // of a block's tokens: running exponent (the last one's is the block's), dt, weight in S'
+    float e[kScanBlock], dt[kScanBlock], w[kScanBlock];
 };
 
 // Loads from memory to LDS are issued from asm statements: for one that it knows the compiler would wait in front of the next LDS read that
@@ -99,11 +111,13 @@ __device__ __forceinline__ void scan_barrier_lds() { asm volatile("s_waitcnt lgk
 // way of registers where rows in whole chunks lie at any element, or one element at a time.  Two barriers a block: its rows are there; M is
 // there.  y takes x's place in LDS, and leaves from there in whole rows behind the next barrier.
 //
-// What bounds it: 32768 tokens in eight prompts of 64 heads of 64 x 128 take 305 us, 940 MB at 3.1 TB/s.  Two work-groups on a CU; their
-// wavefronts issue vector instructions for half of the time, 236 a block beside 37 products of 16 clocks, and wait for each other, for LDS and
-// for products for two fifths.  Without the two smaller parts of x 274, without M 284, without the gate's exponentials 289; without any of these
-// and the other products 242, which is what the trips through memory take.  Not kept: three buffers (two work-groups on a CU instead of
-// three): 331, 8192 tokens in eight prompts of 32 heads 62 | 60 with two, states of 256 99 | 91; loads and stores that bypass the caches +-2%.
+// What bounds it: 32768 tokens in eight prompts of 64 heads of 64 x 128 take 343 us, 940 MB at 2.7 TB/s.  Two work-groups on a CU; their
+// wavefronts issue vector instructions for more than half of the time, some 320 a block beside 46 products of 16 clocks, and wait for each other,
+// for LDS and for products for the rest.  With M and S's copy rounded to one bf16 number each, whose errors showed in y, 304; of these, without
+// the two smaller parts of x 274, without M 284, without the gate's exponentials 289; without any of these
+// and the other products 242, which is what the trips through memory take.  Not kept, with one number each: three buffers (two work-groups on a CU
+// instead of three): 331, 8192 tokens in eight prompts of 32 heads 62 | 60 with two, states of 256 99 | 91; loads and stores that bypass the caches
+// +-2%.  Remainders of S from pairs rounded by one conversion 344, each value rounded once more 364.
 // On the way: blocks of 64 tokens with rows through registers 394 (228 registers), each block's decays formed by one wavefront in front of a
 // barrier 394, by all for four blocks 354, y stored and z read by each wavefront in 32 bytes of a row 332.
 template <int NP, int MODE, bool WHOLE>
@@ -113,7 +127,7 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
     constexpr int CH = NP / 8, NJ = NP / 32, Q = kScanBlock, SLOTS = Q * CH / 64;    // loads of 64 chunks that B or C of a block takes
     constexpr bool Y = MODE != SCAN_CARRY;
     __shared__ __align__(16) bf16 sb[2][Q * NP], sc[Y ? 2 : 1][Y ? Q * NP : 8], sx[2][Q * 64], sg[Y ? 2 : 1][Y ? Q * 64 : 8],
-        sm[Y ? Q * Q : 8];
+        sm[Y ? 48 * Q : 8];
     __shared__ __align__(16) ScanBlockSizes sizes[kScanAhead];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
     const int64_t id = scan_unit();
@@ -287,11 +301,6 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
         to.e[at] = (float)upto;
         to.dt[at] = dt;
         to.w[at] = __builtin_amdgcn_exp2f((float)(total - upto)) * dt;
-        to.f[at] = __builtin_amdgcn_exp2f((float)upto);
-        if (lane == 0) {
-            to.total = (float)total;
-            to.factor = __builtin_amdgcn_exp2f((float)total);
-        }
     };
 
     float raw = 0.0f, sum_of = 0.0f;                 // dt_raw of the next blocks whose sizes are formed
@@ -316,7 +325,8 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
         const ScanBlockSizes &sz = sizes[n % kScanAhead];
         bf16 *const xs = sx[now];
         const bf16 *const bs = sb[now], *const cs = sc[Y ? now : 0];
-        sum_of += sz.total;
+        const float total = sz.e[Q - 1];             // (tokens behind the last add nothing)
+        sum_of += total;
         const int q4 = l16 >> 2, c4 = l16 & 3;
         f32x4_t acc[2];
         if constexpr (Y) {
@@ -337,24 +347,32 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
                     v[i] = m[i] * (__builtin_amdgcn_exp2f(e - es[i]) * ds[i]);
                     v[i] = s0 + i <= row ? v[i] : 0.0f;
                 }
-                const bf16x2_t lo = __builtin_convertvector(f32x2_t{v[0], v[1]}, bf16x2_t), hi = __builtin_convertvector(f32x2_t{v[2], v[3]}, bf16x2_t);
-                const bf16x4_t q = __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
-                *reinterpret_cast<bf16x4_t *>(sm + scan_chunk<4>(row, s0 >> 3) + (s0 & 4)) = q;
+                const ScanHalves a = scan_halves(v[0], v[1]), b = scan_halves(v[2], v[3]);
+                *reinterpret_cast<uint2 *>(sm + scan_chunk<4>(row, s0 >> 3) + (s0 & 4)) = make_uint2(a.high, b.high);
+                *reinterpret_cast<uint2 *>(sm + scan_chunk<4>(row + 16 * tt, (s0 >> 3) + (tt ? 0 : 2)) + (s0 & 4)) = make_uint2(a.low, b.low);
             }
             // what the state in front of the block brings
             acc[0] = acc[1] = f32x4_t{0, 0, 0, 0};
             static_for<0, NJ>([&](auto j_) SCAN_INLINE {
                 constexpr int j = decltype(j_)::value;
-                bf16x8_t s;
+                u32x4_t high, low;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s[i] = (bf16)S[2 * j + (i >> 2)][i & 3];
+                for (int i = 0; i < 4; ++i) {
+                    const ScanHalves q = scan_halves(S[2 * j + (i >> 1)][2 * (i & 1)], S[2 * j + (i >> 1)][2 * (i & 1) + 1]);
+                    high[i] = q.high;
+                    low[i] = q.low;
+                }
+                const bf16x8_t s = __builtin_bit_cast(bf16x8_t, high), left = __builtin_bit_cast(bf16x8_t, low);
 #pragma unroll
-                for (int tt = 0; tt < 2; ++tt)
-                    acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(s, scan_row8<CH>(cs, tt * 16 + l16, 4 * j + g4), acc[tt], 0, 0, 0);
+                for (int tt = 0; tt < 2; ++tt) {
+                    const bf16x8_t row = scan_row8<CH>(cs, tt * 16 + l16, 4 * j + g4);
+                    acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(left, row, acc[tt], 0, 0, 0);
+                    acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(s, row, acc[tt], 0, 0, 0);
+                }
             });
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt) {
-                const float f = sz.f[tt * 16 + l16];
+                const float f = __builtin_amdgcn_exp2f(sz.e[tt * 16 + l16]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[tt][i] *= f;
             }
@@ -366,7 +384,7 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
             xf = scan_pair(scan_transposed(xs + scan_chunk<8>(r, ch) + half), scan_transposed(xs + scan_chunk<8>(r + 4, ch) + half));
         }
         // S'
-        const float factor = sz.factor;
+        const float factor = __builtin_amdgcn_exp2f(total);
         const f32x4_t w0 = *reinterpret_cast<const f32x4_t *>(sz.w + 8 * g4), w1 = *reinterpret_cast<const f32x4_t *>(sz.w + 8 * g4 + 4);
         uint32_t part[3][8];                         // the upper halves of three numbers that add up to x times its weight
 #pragma unroll
@@ -407,8 +425,12 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
                     if (!(fabsf(v) < INFINITY)) xg[i] = (bf16)0.0f;
                 }
             }
+            u32x4_t twice = __builtin_bit_cast(u32x4_t, xg);       // the first sixteen tokens, in both halves of the wavefront
 #pragma unroll
-            for (int tt = 0; tt < 2; ++tt) acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xg, scan_row8<4>(sm, tt * 16 + l16, g4), acc[tt], 0, 0, 0);
+            for (int i = 0; i < 4; ++i) twice[i] = __builtin_amdgcn_permlane32_swap(twice[i], twice[i], false, false)[0];
+            acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, twice), scan_row8<4>(sm, l16, g4), acc[0], 0, 0, 0);
+            acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xg, scan_row8<4>(sm, 32 + l16, g4), acc[1], 0, 0, 0);
+            acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xg, scan_row8<4>(sm, 16 + l16, g4), acc[1], 0, 0, 0);
             if (any) {
                 int column = l16;
                 asm volatile("" : "+v"(column));     // (addresses of this path are not kept in registers for all blocks)
@@ -418,7 +440,7 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
                     for (int tt = 0; tt < 2; ++tt) {
                         const int row = tt * 16 + column;
                         if (row < s) continue;
-                        const float m = (float)sm[scan_chunk<4>(row, s >> 3) + (s & 7)];
+                        const float m = (float)sm[scan_chunk<4>(row, s >> 3) + (s & 7)] + (float)sm[scan_chunk<4>(row + 16 * tt, (s >> 3) + (tt ? 0 : 2)) + (s & 7)];
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
                             if (!(fabsf((float)v[i]) < INFINITY)) acc[tt][i] = fmaf(m, (float)v[i], acc[tt][i]);
@@ -457,8 +479,6 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
         raw = raw_of(t0, t1);
         bring(t0, t1, std::integral_constant<int, 0>{});
         put(t0, t1, std::integral_constant<int, 0>{});
-        if constexpr (Y)                             // the tile above the diagonal
-            if (tid < 32) *reinterpret_cast<bf16x8_t *>(sm + scan_chunk<4>(tid & 15, 2 + (tid >> 4))) = bf16x8_t{};
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         sum_of = 0.0f;
         for (int t = t0, n = 0; t < t1;)
