@@ -2,6 +2,7 @@
 // memory and are clamped to the tokens that the host has validated, so that other values than the host's cannot lead outside the operands.
 #pragma once
 #include "common.hpp"
+#include "packed_spans.hpp"
 
 struct Packed {
     const int32_t *offsets, *pos, *slot;             // pos, slot: NULL = all 0, = the sequence's own number
@@ -19,8 +20,9 @@ __device__ __forceinline__ Sequence packed_sequence(const Packed &c, int n)
         s.begin = c.lo;
         s.end = c.hi;
     } else {
-        s.begin = min(max(c.offsets[n], c.lo), c.hi);
-        s.end = min(max(c.offsets[n + 1], s.begin), c.hi);
+        const Span span = packed_clamped(c.offsets[n], c.offsets[n + 1], c.lo, c.hi);
+        s.begin = span.begin;
+        s.end = span.end;
     }
     s.pos = c.pos ? c.pos[n] : 0;
     const int64_t slot = c.slot ? c.slot[n] : n;
@@ -31,14 +33,7 @@ __device__ __forceinline__ Sequence packed_sequence(const Packed &c, int n)
 // take two trips to memory (a search by halves takes one for each factor of two).
 __device__ __forceinline__ int packed_find(const Packed &c, int t, int lane)
 {
-    int first = 1, left = c.n - 1;                   // offsets[first .. first + left - 1] may still be at or before t
-    while (left > 0) {
-        const int step = (left + 63) >> 6, at = min((lane + 1) * step, left);
-        const int m = __popcll(__ballot(c.offsets[first + at - 1] <= t));
-        // (lanes behind the last offset look at the last one: all of them or none count)
-        const int gone = min(m * step, left);
-        first += gone;
-        left = step == 1 ? 0 : min(step - 1, left - gone);
-    }
-    return first - 1;
+    return packed_find_by(c.n, [&](int first, int step, int left) {
+        return __popcll(__ballot(c.offsets[first + min((lane + 1) * step, left) - 1] <= t));
+    });
 }

@@ -101,38 +101,31 @@ __device__ __forceinline__ void scan_drive(const ScanCall &c, int64_t work, int 
         const int t0 = c.seqs.lo + (int)work * c.seg, t1 = t0 + c.seg;
         if (t1 >= c.seqs.hi) return;
         const Sequence s = packed_sequence(c.seqs, packed_find(c.seqs, t1 - 1, lane));
-        if (s.end <= t1 || s.pos < 0) return;
+        const Span span = packed_carried({s.begin, s.end}, t0, t1);
+        if (span.begin == span.end || s.pos < 0) return;
         const int64_t at = work * slot_size + head_at;
         clear();
         if (s.begin >= t0 && s.slot >= 0 && s.pos > 0) {
             load(slot_of(s));
             store(c.held + at);                      // (the slot may be written before the second pass comes to read it)
         }
-        run(max(s.begin, t0), t1, sum);
+        run(span.begin, span.end, sum);
         store(c.carry + at);
         if (threadIdx.x == 0 && p0 == 0) c.decay[work * c.H + h] = s.begin >= t0 ? -1.0f : __builtin_amdgcn_exp2f(sum);
     } else {
         const int t0 = c.seqs.lo + (int)work * c.seg, t1 = min(t0 + c.seg, c.seqs.hi);
-        int n = packed_find(c.seqs, t0, lane);
-        for (int t = t0; t < t1;) {
-            Sequence s = packed_sequence(c.seqs, n);
-            while (t >= s.end && n + 1 < c.seqs.n) s = packed_sequence(c.seqs, ++n);
-            if (t >= s.end) break;                   // (offsets that are not the host's)
-            const int e = min(s.end, t1);
-            if (s.pos < 0) {
-                zeros(t, e);
-            } else {
-                clear();
-                if (t <= s.begin) {
-                    if (s.slot >= 0 && s.pos > 0) load(s.end > t1 ? c.held + work * slot_size + head_at : slot_of(s));
-                } else if (work > 0) {               // (always, with the host's offsets)
-                    load(c.carry + (work - 1) * slot_size + head_at);
-                }
-                run(t, e, sum);
-                if (e == s.end && s.slot >= 0) store(slot_of(s));
+        auto get = [&](int n) SCAN_INLINE { return packed_sequence(c.seqs, n); };
+        packed_pieces(t0, t1, packed_find(c.seqs, t0, lane), c.seqs.n, get, [&](const Sequence &s, int t, int e) SCAN_INLINE {
+            if (s.pos < 0) return zeros(t, e);
+            clear();
+            if (t <= s.begin) {
+                if (s.slot >= 0 && s.pos > 0) load(s.end > t1 ? c.held + work * slot_size + head_at : slot_of(s));
+            } else if (work > 0) {                   // (always, with the host's offsets)
+                load(c.carry + (work - 1) * slot_size + head_at);
             }
-            t = e;
-        }
+            run(t, e, sum);
+            if (e == s.end && s.slot >= 0) store(slot_of(s));
+        });
     }
 }
 
