@@ -552,6 +552,16 @@ def _row_dtype(t, name: str) -> int:
     return code
 
 
+def _scratch(n: int, dtype, device, stream):
+    """Memory that one call uses and leaves, from the pool of the call's stream: a block of another stream's pool may still be in use by work
+    that is queued there, behind which this stream does not wait."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(n, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(n, dtype=dtype, device=device)
+
+
 def _rows_of(t, name: str):
     """(rows, columns, row stride) of a matrix whose rows are contiguous."""
     shape = t.shape
@@ -804,9 +814,7 @@ def selective_scan(xbc, dt, a, offsets, d_offsets, out, groups=1, dt_bias=None, 
     if workspace is None:
         need = lib().srm_selective_scan_workspace_bytes(code, h, n, heads, head_dim, state_dim)
         if need and xbc.is_cuda:
-            workspace = torch.empty(need, dtype=torch.uint8, device=xbc.device)
-            if stream is not None:
-                workspace.record_stream(stream)
+            workspace = _scratch(need, torch.uint8, xbc.device, stream)
     elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
         raise ValueError("workspace: must be contiguous uint8")
     _launch(lib().srm_selective_scan,
