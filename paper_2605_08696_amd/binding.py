@@ -446,7 +446,7 @@ class Model:
         torch = _torch()
         n = B * self.d
         if slabs is None:
-            slabs = torch.empty((self.d // 128) * n, dtype=torch.float32, device=x.device)
+            slabs = _scratch((self.d // 128) * n, torch.float32, x.device, stream)
         p_x = _dev(x, torch.float32, n, "x")
         p_s = _dev(state_layer, self.state_torch_dtype, n, "state_layer")
         p_o = _dev(norm_out, self.act_dtype, n, "norm_out")

@@ -35,11 +35,12 @@ def watched(monkeypatch):
 
     def alloc(*args, **kw):
         log.append(("alloc", current[0]))
-        return empty(*args, **kw)
+        return empty(*args, **kw).as_subclass(Device)
 
     monkeypatch.setattr(torch.cuda, "stream", on)
     monkeypatch.setattr(torch, "empty", alloc)
     monkeypatch.setattr(torch.Tensor, "record_stream", lambda self, stream: None)
+    monkeypatch.setattr(binding, "_check", lambda rc: None)
     monkeypatch.setattr(binding, "_launch", lambda fn, args, first, others, stream: log.append(("launch", stream)))
     return binding, log
 
@@ -52,4 +53,23 @@ def test_the_scans_workspace(watched, stream):
     off = np.array([0, T], dtype=np.int32)
     assert binding.selective_scan_workspace_bytes(binding.SRM_BF16, off, H, P, N) > 0
     binding.selective_scan(xbc, dt, _on_gpu(H), off, torch.tensor([0, T], dtype=torch.int32), out, stream=stream)
+    assert log == [("alloc", stream), ("launch", stream)]
+
+
+@pytest.mark.parametrize("stream", [None, "another"])
+def test_a_mixer_blocks_slabs(watched, monkeypatch, stream):
+    binding, log = watched
+
+    class Library:
+        def srm_mixer_block(self, *args):
+            log.append(("launch", args[-1]))
+            return 0
+
+    monkeypatch.setattr(binding, "lib", Library)
+    monkeypatch.setattr(binding, "_stream", lambda s: s)
+    monkeypatch.setattr(binding.Model, "act_dtype", torch.bfloat16)
+    monkeypatch.setattr(binding.Model, "state_torch_dtype", torch.float32)
+    model = binding.Model.__new__(binding.Model)
+    model._h, model.d, model.sd = None, 256, 256
+    model.mixer_block(0, 3, 2, _on_gpu(2, 256), _on_gpu(2, 256), _on_gpu(2, 256, dtype=torch.bfloat16), stream=stream)
     assert log == [("alloc", stream), ("launch", stream)]
