@@ -94,18 +94,19 @@ token_logprobs_kernel(const T *__restrict__ logits, ScoreCall c)
             for (int i = 0; i < 8; ++i) v[i] = at + i < V ? v[i] : -INFINITY;
         }
     };
-    // The largest of eight, -infinity of none but NaN.  (Written out, as three at a time; the compiler would quiet each value first.  A NaN
-    // that signals, which the instruction makes a result of, is looked for.)
+    // The largest of eight, -infinity of none but NaN.  (Written out, as three at a time; the compiler would quiet each value first.  Of a NaN
+    // that signals the instruction makes a quiet one, which the next instruction drops with all that went into it: each one's result is
+    // looked at.)
     auto largest = [](const float (&v)[8]) __attribute__((always_inline)) {
-        float m;
-        asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(v[0]), "v"(v[1]), "v"(v[2]));
-        asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(m), "v"(v[3]), "v"(v[4]));
-        asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(m), "v"(v[5]), "v"(v[6]));
-        asm("v_max_f32 %0, %1, %2" : "=v"(m) : "v"(m), "v"(v[7]));
-        if (m != m) {
+        float a, b, d, m;
+        asm("v_max3_f32 %0, %1, %2, %3" : "=v"(a) : "v"(v[0]), "v"(v[1]), "v"(v[2]));
+        asm("v_max3_f32 %0, %1, %2, %3" : "=v"(b) : "v"(a), "v"(v[3]), "v"(v[4]));
+        asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(b), "v"(v[5]), "v"(v[6]));
+        asm("v_max_f32 %0, %1, %2" : "=v"(m) : "v"(d), "v"(v[7]));
+        if (__builtin_isunordered(a, b) || __builtin_isunordered(d, m)) {
             m = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m = fmaxf(m, v[i]);
+            for (int i = 0; i < 8; ++i) m = v[i] > m ? v[i] : m;
         }
         return m;
     };
