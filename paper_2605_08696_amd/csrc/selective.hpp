@@ -52,12 +52,21 @@ __device__ __forceinline__ float dt_of(const StepSizes &c, float raw, float bias
 {
     const float v = raw + bias;
     if (!c.softplus) return v;
-    // log(1 + e^v) = max(v, 0) + log(1 + u), u = e^-|v|; the logarithm by its series up to u = 1/16, where 1 + u would drop digits of u (the
-    // first term left out is below 2^-26 of the sum).  (A NaN stays one.)
-    const float u = __expf(-fabsf(v));
-    const float series = u * fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, -1.0f / 6.0f, 0.2f), -0.25f), 1.0f / 3.0f), -0.5f), 1.0f);
-    const float log = u < 0.0625f ? series : 0.69314718055994530942f * __builtin_amdgcn_logf(1.0f + u);
-    return (v > 0.0f ? v : v == v ? 0.0f : v) + log;
+    // log(1 + e^v) = max(v, 0) + log(1 + u), u = e^-|v|, to an ulp or two and in few registers, which the scans' widest forms do not have for
+    // expf and log1pf.  The exponential's argument in steps of a factor of two keeps what its product is rounded by (7 2^-24 of dt = 0.001
+    // otherwise).  The logarithm without the sum 1 + u, which would drop digits of u (2^-24 of a dt of 0.06): twice the area tangent of
+    // s = u / (2 + u), at most a third, by its series s (1 + s^2 / 3 + s^4 / 5 ..), whose first term left out is below 2^-29 of the sum.
+    // (A dt below 2^-126 is 0.  A NaN stays one.)
+    const float w = fminf(fabsf(v), 104.0f), at = w * -1.44269504f, left = fmaf(w, -1.92596299e-8f, fmaf(w, -1.44269504f, -at));
+    const float e = __builtin_amdgcn_exp2f(at), u = fmaf(e, left * 0.69314718f, e), s = u / (2.0f + u), q = s * s;
+    float p = 1.0f / 15.0f;
+    p = fmaf(p, q, 1.0f / 13.0f);
+    p = fmaf(p, q, 1.0f / 11.0f);
+    p = fmaf(p, q, 1.0f / 9.0f);
+    p = fmaf(p, q, 1.0f / 7.0f);
+    p = fmaf(p, q, 0.2f);
+    p = fmaf(p, q, 1.0f / 3.0f);
+    return (v > 0.0f ? v : v == v ? 0.0f : v) + 2.0f * fmaf(p * q, s, s);
 }
 // The decay's exponent in steps of a factor of two.  Below 2^-200 a decay leaves nothing of a state of fp32; the limit keeps sums of
 // exponents small enough that their differences are exact where the decays are not 0.  (A comparison, so that a NaN stays one.)

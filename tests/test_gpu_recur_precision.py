@@ -52,3 +52,29 @@ def test_a_scan_of_bf16_rounds_its_output_alone(srm, H, P, G, N, pad):
           f"{float((want.to(BF16).double() - want).norm() / want.norm()):.3e}; {many} outside", flush=True)
     assert many == 0, worst
     assert _over(state, after, of_state)[1] == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("entry", ["scan", "step"])
+def test_step_sizes_to_an_ulp_or_two(srm, entry, dtype):
+    """x = B = 1 from an empty state leave dt itself in the state.  The exponential loses an ulp at most (2^-23), the logarithm two, their sum with
+    v half of one; cut into three numbers of bf16 and added up in fp32, an ulp more.  (Of these three, one below 2^-126 is a subnormal number, which the matrix
+    cores take as 0: what is left of dt when the first one, or the first two, are taken off it is less than 2^-126 then, and so is the loss.
+    It shows at dt = 1e-37.)"""
+    H = 4096
+    v = torch.cat([torch.linspace(-85, 40, 3 * H), torch.linspace(-12, 0, 6 * H), torch.linspace(-3.2, -2.4, 2 * H), torch.linspace(-0.8, 0.8, H)]).float()
+    a, off = -torch.ones(H, device="cuda"), [0, 1]
+    ones = torch.ones(1, H + 2, dtype=dtype, device="cuda")
+    got = []
+    for part in v.view(-1, 1, H):
+        state, out = torch.full((1, H, 1, 1), 7.0, device="cuda"), torch.empty(1, H, dtype=dtype, device="cuda")
+        if entry == "scan":
+            srm.selective_scan(ones, part.cuda(), a, off, _i32(off), out, state=state)
+        else:
+            srm.selective_step(ones, part.cuda(), a, _i32([0]), state, out)
+        got.append(state.view(-1))
+    torch.cuda.synchronize()
+    got, want = torch.cat(got).double().cpu(), recur_ref.sizes(v, None, True)
+    wrong = ((got - want).abs() - (2.0 ** -126 if dtype is BF16 and entry == "scan" else 0.0)).clamp_min(0) / want
+    print(f"{entry} {dtype}: {float(wrong.max()):.2e} at {float(v[wrong.argmax()]):.4f}", flush=True)
+    assert wrong.max() <= 2.0 ** -23 + 2.0 ** -22 + 2.0 ** -24 + 2.0 ** -23
