@@ -58,7 +58,8 @@ __device__ __forceinline__ float dt_of(const StepSizes &c, float raw, float bias
     // s = u / (2 + u), at most a third, by its series s (1 + s^2 / 3 + s^4 / 5 ..), whose first term left out is below 2^-29 of the sum.
     // (A dt below 2^-126 is 0.  A NaN stays one.)
     const float w = fminf(fabsf(v), 104.0f), at = w * -1.44269504f, left = fmaf(w, -1.92596299e-8f, fmaf(w, -1.44269504f, -at));
-    const float e = __builtin_amdgcn_exp2f(at), u = fmaf(e, left * 0.69314718f, e), s = u / (2.0f + u), q = s * s;
+    const float e = __builtin_amdgcn_exp2f(at), u = fmaf(e, left * 0.69314718f, e);
+    const float d = 2.0f + u, r = __builtin_amdgcn_rcpf(d), s0 = u * r, s = fmaf(fmaf(-d, s0, u), r, s0), q = s * s;
     float p = 1.0f / 15.0f;
     p = fmaf(p, q, 1.0f / 13.0f);
     p = fmaf(p, q, 1.0f / 11.0f);
@@ -68,12 +69,26 @@ __device__ __forceinline__ float dt_of(const StepSizes &c, float raw, float bias
     p = fmaf(p, q, 1.0f / 3.0f);
     return (v > 0.0f ? v : v == v ? 0.0f : v) + 2.0f * fmaf(p * q, s, s);
 }
-// The decay's exponent in steps of a factor of two.  Below 2^-200 a decay leaves nothing of a state of fp32; the limit keeps sums of
-// exponents small enough that their differences are exact where the decays are not 0.  (A comparison, so that a NaN stays one.)
-__device__ __forceinline__ float decay_exponent(float dt, float a)
+// The decay's exponent in steps of a factor of two, in 64 bits: rounded to fp32, an exponent of -100 would lose 4e-6 of its decay, and a sum of
+// exponents what is behind a few large ones.  2^-200 is 0 in fp32 as every smaller decay is; the limit keeps sums of exponents in the range
+// of which 64 bits hold all that matters.  (Formed of products in fp32 with what they are rounded by: constants of 64 bits cost registers.
+// A comparison, so that a NaN stays one.)
+__device__ __forceinline__ double decay_exponent(float dt, float a)
 {
-    const float e = dt * a * 1.44269504088896340736f;
-    return e < -200.0f ? -200.0f : e;
+    const float p = dt * a, high = p * 1.44269504f;
+    const float low = fmaf(fmaf(dt, a, -p), 1.44269504f, fmaf(p, 1.92596299e-8f, fmaf(p, 1.44269504f, -high)));
+    return high < -200.0f ? -200.0 : (double)high + (double)low;
+}
+// 2^(high + low) of an exponent in two parts, low what fp32 leaves of it.
+__device__ __forceinline__ float exp2_of(float high, float low)
+{
+    const float f = __builtin_amdgcn_exp2f(high);
+    return fmaf(f, low * 0.69314718f, f);
+}
+__device__ __forceinline__ float exp2_of(double e)
+{
+    const float high = (float)e;
+    return exp2_of(high, (float)(e - high));
 }
 
 // Sum over groups of NL neighbouring lanes, in every lane of a group.
@@ -97,7 +112,7 @@ __device__ __forceinline__ void scan_drive(const ScanCall &c, int64_t work, int 
 {
     const int64_t slot_size = (int64_t)c.H * c.P * c.N;
     auto slot_of = [&](const Sequence &s) { return c.state + s.slot * slot_size + head_at; };
-    float sum = 0.0f;
+    double sum = 0.0;
     if constexpr (MODE == SCAN_WHOLE) {
         const Sequence s = packed_sequence(c.seqs, (int)work);
         if (s.begin == s.end) return;
@@ -120,7 +135,7 @@ __device__ __forceinline__ void scan_drive(const ScanCall &c, int64_t work, int 
         }
         run(span.begin, span.end, sum);
         store(c.carry + at);
-        if (threadIdx.x == 0 && p0 == 0) c.decay[work * c.H + h] = s.begin >= t0 ? -1.0f : __builtin_amdgcn_exp2f(sum);
+        if (threadIdx.x == 0 && p0 == 0) c.decay[work * c.H + h] = s.begin >= t0 ? -1.0f : exp2_of(sum);
     } else {
         const int t0 = c.seqs.lo + (int)work * c.seg, t1 = min(t0 + c.seg, c.seqs.hi);
         auto get = [&](int n) SCAN_INLINE { return packed_sequence(c.seqs, n); };
@@ -176,6 +191,7 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
     constexpr int PR = 4, PW = 64 / NL * PR, NP = NL * NR, TT = NP > 128 || PW > 128 ? 8 : 16;
     __shared__ __align__(16) float sb[TT][NP + 4], sc[TT][NP + 4], sx[TT][PW + 4], sy[TT][PW + 4];
     __shared__ float2 sd[TT];
+    __shared__ double se[MODE == SCAN_CARRY ? TT : 1];
     const int lane = threadIdx.x, ln = lane % NL, lp = lane / NL;
     const int64_t id = scan_unit();
     const int per = c.H * c.parts;
@@ -222,7 +238,7 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
         raw = dt_raw(c.dt, min(t + lane % TT, t1 - 1), h);
     };
     // Tokens [t0, t1) of one sequence; adds their decay exponents to `sum`.
-    auto run = [&](int t0, int t1, float &sum) SCAN_INLINE {
+    auto run = [&](int t0, int t1, double &sum) SCAN_INLINE {
         fetch(t0, t1);
         for (int t = t0; t < t1; t += TT) {
             const int nt = min(TT, t1 - t);
@@ -239,9 +255,10 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
                 sx[e / PW][e % PW] = e % PW < np ? rx[i] : 0.0f;
             });
             if (lane < TT) {
-                const float dt = dt_of(c.dt, raw, bias), ex = decay_exponent(dt, a);
-                sd[lane] = make_float2(__builtin_amdgcn_exp2f(ex), dt);
-                if (MODE == SCAN_CARRY) sb[lane][NP] = ex;
+                const float dt = dt_of(c.dt, raw, bias);
+                const double ex = decay_exponent(dt, a);
+                sd[lane] = make_float2(exp2_of(ex), dt);
+                if (MODE == SCAN_CARRY) se[lane] = ex;
             }
             if (t + TT < t1) fetch(t + TT, t1);
             float gate[MODE != SCAN_CARRY ? LX : 1]; // z of these tokens
@@ -254,7 +271,7 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
             __syncthreads();
             auto token = [&](int r) SCAN_INLINE {
                 const float2 d = sd[r];
-                if (MODE == SCAN_CARRY) sum += sb[r][NP];
+                if (MODE == SCAN_CARRY) sum += se[r];
                 float y[PR];
 #pragma unroll
                 for (int i = 0; i < PR; ++i) {
@@ -355,7 +372,7 @@ selective_step_kernel(const T *__restrict__ xbc, T *__restrict__ out, StepCall c
         }
     }
     const float dt = dt_of(c.dt, dt_raw(c.dt, r, h), c.dt.bias ? c.dt.bias[h] : 0.0f);
-    const float decay = __builtin_amdgcn_exp2f(decay_exponent(dt, c.a[h])), skip = c.skip ? c.skip[h] : 0.0f;
+    const float decay = exp2_of(decay_exponent(dt, c.a[h])), skip = c.skip ? c.skip[h] : 0.0f;
     const bool first = h % (c.H / c.G) == 0 && p0 == 0;
     const T *x = xbc + r * c.ld;
     T *ring = c.ring && kept ? static_cast<T *>(c.ring) + at * c.width * (int64_t)C : nullptr;

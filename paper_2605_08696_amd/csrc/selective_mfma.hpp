@@ -3,8 +3,8 @@
 // With e_t the decay exponents' running sum from the block's first token to token t, S the state in front of it:
 //   y_t = 2^e_t S C_t + sum_{s <= t} M_ts x_s      M_ts = (C_t . B_s) 2^(e_t - e_s) dt_s
 //   S' = 2^e_31 S + sum_s (2^(e_31 - e_s) dt_s x_s) B_s^T
-// that is four products with 32 tokens as one side.  The running sum is formed in 64 bits, so that the exponents of S', which are small where
-// the weights are not, and of M lose nothing to what came before them.
+// that is four products with 32 tokens as one side.  The running sum is formed in 64 bits and kept in two parts, so that the exponents of S' and
+// of M, which are small where the weights are not, lose nothing to what came before them.
 //
 // Roundings.  The state stays in fp32 in the accumulators of its own product.  M and the copy of S that meets C are cut into two bf16 numbers
 // each, which leave 2^-15 of a value at most (a hundredth of what y may lose when it is stored), and both are multiplied.  x times its
@@ -24,7 +24,7 @@ typedef __attribute__((ext_vector_type(4))) short i16x4_t;
 typedef __attribute__((ext_vector_type(8))) short i16x8_t;
 
 constexpr int kScanBlock = 32, kScanRows = 64;       // tokens of a block, rows of P of a work-group
-constexpr int kScanAhead = 4;                        // blocks whose sizes are formed together, one by each wavefront
+constexpr int kScanAhead = 3;                        // blocks whose sizes are formed together, one by a wavefront (a fourth's have no room in LDS)
 
 // LDS rows of CH chunks of sixteen bytes: chunk c of row r lies at c ^ f(r).  Sixteen rows' chunks c then lie on all banks, and so do the
 // sixteen chunks or halves of chunks that a transposing read takes from four rows.
@@ -76,7 +76,7 @@ __device__ __forceinline__ double half_scan(double v)
 }
 
 struct ScanBlockSizes {                              // of a block's tokens: running exponent (the last one's is the block's), dt, weight in S'
-    float e[kScanBlock], dt[kScanBlock], w[kScanBlock];
+    float e[kScanBlock], low[kScanBlock], dt[kScanBlock], w[kScanBlock];
 };
 
 // Loads from memory to LDS are issued from asm statements: for one that it knows the compiler would wait in front of the next LDS read that
@@ -111,9 +111,10 @@ __device__ __forceinline__ void scan_barrier_lds() { asm volatile("s_waitcnt lgk
 // way of registers where rows in whole chunks lie at any element, or one element at a time.  Two barriers a block: its rows are there; M is
 // there.  y takes x's place in LDS, and leaves from there in whole rows behind the next barrier.
 //
-// What bounds it: 32768 tokens in eight prompts of 64 heads of 64 x 128 take 343 us, 940 MB at 2.7 TB/s.  Two work-groups on a CU; their
+// What bounds it: 32768 tokens in eight prompts of 64 heads of 64 x 128 take 348 us, 940 MB at 2.7 TB/s.  Two work-groups on a CU; their
 // wavefronts issue vector instructions for more than half of the time, some 320 a block beside 46 products of 16 clocks, and wait for each other,
-// for LDS and for products for the rest.  With M and S's copy rounded to one bf16 number each, whose errors showed in y, 304; of these, without
+// for LDS and for products for the rest.  With exponents in one part of fp32 337 (sizes of four blocks together); with M and S's
+// copy rounded to one bf16 number each besides, whose errors showed in y, 304; of these, without
 // the two smaller parts of x 274, without M 284, without the gate's exponentials 289; without any of these
 // and the other products 242, which is what the trips through memory take.  Not kept, with one number each: three buffers (two work-groups on a CU
 // instead of three): 331, 8192 tokens in eight prompts of 32 heads 62 | 60 with two, states of 256 99 | 91; loads and stores that bypass the caches
@@ -292,18 +293,21 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
         const bool there = t + wave * Q + (lane & 31) < t1;
         float dt = dt_of(c.dt, raw, bias);
         dt = there ? dt : 0.0f;
-        const double upto = half_scan(there ? (double)decay_exponent(dt, a) : 0.0);
+        const double upto = half_scan(there ? decay_exponent(dt, a) : 0.0);
         const unsigned long long u = __builtin_bit_cast(unsigned long long, upto);
         const double total = __builtin_bit_cast(double, (unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), 31) << 32 |
                                                             (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, 31));
         ScanBlockSizes &to = sizes[wave];
         const int at = lane & 31;                    // (the halves of the wavefront write the same)
         to.e[at] = (float)upto;
-        to.dt[at] = dt;
-        to.w[at] = __builtin_amdgcn_exp2f((float)(total - upto)) * dt;
+        const float low = (float)(upto - (float)upto);
+        to.low[at] = low;
+        to.dt[at] = fmaf(dt, low * -0.69314718f, dt);
+        to.w[at] = exp2_of(total - upto) * dt;
     };
 
-    float raw = 0.0f, sum_of = 0.0f;                 // dt_raw of the next blocks whose sizes are formed
+    float raw = 0.0f;                                // dt_raw of the next blocks whose sizes are formed
+    double sum_of = 0.0;
     // Block [t, t + Q) up to t1, number n of its sequence, which lies in buffer `now`.
     auto block = [&](int t, int t1, int n, auto now_) SCAN_INLINE {
         constexpr int now = decltype(now_)::value;
@@ -318,15 +322,15 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
             bring(t + Q, t1, std::integral_constant<int, then>{});
         }
         if (n % kScanAhead == 0) {
-            put_sizes(raw, t, t1);
+            if (wave < kScanAhead) put_sizes(raw, t, t1);
             if (t + kScanAhead * Q < t1) raw = raw_of(t + kScanAhead * Q, t1);
             scan_barrier_lds();
         }
         const ScanBlockSizes &sz = sizes[n % kScanAhead];
         bf16 *const xs = sx[now];
         const bf16 *const bs = sb[now], *const cs = sc[Y ? now : 0];
-        const float total = sz.e[Q - 1];             // (tokens behind the last add nothing)
-        sum_of += total;
+        const float factor = exp2_of(sz.e[Q - 1], sz.low[Q - 1]);       // (tokens behind the last add nothing)
+        if (MODE == SCAN_CARRY) sum_of += (double)sz.e[Q - 1] + (double)sz.low[Q - 1];
         const int q4 = l16 >> 2, c4 = l16 & 3;
         f32x4_t acc[2];
         if constexpr (Y) {
@@ -339,12 +343,12 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
                     m = __builtin_amdgcn_mfma_f32_16x16x32_bf16(scan_row8<CH>(bs, ss * 16 + l16, 4 * j + g4), scan_row8<CH>(cs, tt * 16 + l16, 4 * j + g4), m, 0, 0, 0);
                 });
                 const int row = tt * 16 + l16, s0 = ss * 16 + 4 * g4;
-                const float e = sz.e[row];
+                const float e = sz.e[row], low = sz.low[row];
                 const f32x4_t es = *reinterpret_cast<const f32x4_t *>(sz.e + s0), ds = *reinterpret_cast<const f32x4_t *>(sz.dt + s0);
                 float v[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    v[i] = m[i] * (__builtin_amdgcn_exp2f(e - es[i]) * ds[i]);
+                    v[i] = m[i] * (__builtin_amdgcn_exp2f(e - es[i] + low) * ds[i]);
                     v[i] = s0 + i <= row ? v[i] : 0.0f;
                 }
                 const ScanHalves a = scan_halves(v[0], v[1]), b = scan_halves(v[2], v[3]);
@@ -384,7 +388,6 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
             xf = scan_pair(scan_transposed(xs + scan_chunk<8>(r, ch) + half), scan_transposed(xs + scan_chunk<8>(r + 4, ch) + half));
         }
         // S'
-        const float factor = __builtin_amdgcn_exp2f(total);
         const f32x4_t w0 = *reinterpret_cast<const f32x4_t *>(sz.w + 8 * g4), w1 = *reinterpret_cast<const f32x4_t *>(sz.w + 8 * g4 + 4);
         uint32_t part[3][8];                         // the upper halves of three numbers that add up to x times its weight
 #pragma unroll
@@ -474,13 +477,13 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
     };
 
     // Tokens [t0, t1) of one sequence.
-    auto run = [&](int t0, int t1, float &sum) SCAN_INLINE {
+    auto run = [&](int t0, int t1, double &sum) SCAN_INLINE {
         __syncthreads();                             // (nobody reads what an earlier call has left)
         raw = raw_of(t0, t1);
         bring(t0, t1, std::integral_constant<int, 0>{});
         put(t0, t1, std::integral_constant<int, 0>{});
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-        sum_of = 0.0f;
+        sum_of = 0.0;
         for (int t = t0, n = 0; t < t1;)
             static_for<0, 2>([&](auto now_) SCAN_INLINE {
                 if (t >= t1) return;

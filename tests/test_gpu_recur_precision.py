@@ -78,3 +78,54 @@ def test_step_sizes_to_an_ulp_or_two(srm, entry, dtype):
     wrong = ((got - want).abs() - (2.0 ** -126 if dtype is BF16 and entry == "scan" else 0.0)).clamp_min(0) / want
     print(f"{entry} {dtype}: {float(wrong.max()):.2e} at {float(v[wrong.argmax()]):.4f}", flush=True)
     assert wrong.max() <= 2.0 ** -23 + 2.0 ** -22 + 2.0 ** -24 + 2.0 ** -23
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("entry", ["scan", "step"])
+def test_decays_to_an_ulp_or_two(srm, entry, dtype):
+    """x = 0 leaves the decay itself in a state of ones.  The exponent is a product in 64 bits in two parts of fp32 (2^-48 of it is lost), the
+    exponential loses an ulp (2^-23), the second part's product and sum one between them, the state's product half of one."""
+    H = 4096
+    e = torch.cat([torch.linspace(-85, 0, 3 * H), torch.linspace(-2, 0, H)]).float()
+    gen = torch.Generator().manual_seed(1)
+    dt = torch.exp(torch.randn(e.numel(), generator=gen))
+    a = e / dt
+    got = []
+    for k in range(0, e.numel(), H):
+        part, factor = dt[None, k:k + H].cuda(), a[k:k + H].cuda()
+        zeros = torch.zeros(1, H + 2, dtype=dtype, device="cuda")
+        state, out = torch.ones(1, H, 1, 1, device="cuda"), torch.empty(1, H, dtype=dtype, device="cuda")
+        if entry == "scan":
+            srm.selective_scan(zeros, part, factor, [0, 1], _i32([0, 1]), out, softplus=False, pos=_i32([1]), state=state)
+        else:
+            srm.selective_step(zeros, part, factor, _i32([1]), state, out, softplus=False)
+        got.append(state.view(-1))
+    torch.cuda.synchronize()
+    got, want = torch.cat(got).double().cpu(), torch.exp(dt.double() * a.double())
+    wrong = (got - want).abs() / want
+    print(f"{entry} {dtype}: {float(wrong.max()):.2e} at {float(e[wrong.argmax()]):.4f}", flush=True)
+    assert wrong.max() <= 2.5 * 2.0 ** -23
+
+
+@pytest.mark.parametrize("many", [1, 12, 24, 30])
+def test_large_exponents_take_no_digits_of_the_weights_behind_them(srm, many):
+    """`many` tokens of a block whose decays are 0, then ordinary ones whose terms nearly cancel in y, so that an error of the weights shows
+    beside the output's rounding."""
+    gen = torch.Generator().manual_seed(many)
+    H, P, N, T = 4, 64, 8, 64
+    xbc = torch.zeros(T, H * P + 2 * N)
+    xbc[:, H * P:] = 1.0
+    sign = torch.where(torch.rand(H * P, generator=gen) < 0.5, -1.0, 1.0)
+    for t in range(many, T):
+        xbc[t, :H * P] = sign if (t - many) % 2 else -sign
+    dt = torch.ones(T, H)
+    dt[:many] = 1e6
+    a = -0.002 - 0.003 * torch.rand(H, generator=gen)
+    xbc, out = xbc.to(BF16), torch.empty(T, H * P, dtype=BF16, device="cuda")
+    state = torch.zeros(1, H, P, N, device="cuda")
+    srm.selective_scan(xbc.cuda(), dt.cuda(), a.cuda(), [0, T], _i32([0, T]), out, softplus=False, state=state)
+    torch.cuda.synchronize()
+    want, size, after, mag = recur_ref.scan(xbc, dt, a, [0, T], H, P, 1, N, softplus=False, state=torch.zeros(1, H, P, N))
+    bound, of_state = recur_ref.scan_bounds(want, size, mag, T - many, N, BF16, False)
+    assert _over(out, want, bound + 2.0 ** -15 * 1.02 * size)[1] == 0
+    assert _over(state, after, of_state)[1] == 0
