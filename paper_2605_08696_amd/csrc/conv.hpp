@@ -8,7 +8,7 @@
 // that begins inside a run is a piece of its own; its first W - 1 tokens, whose taps reach into the slot's ring, all belong to the run that
 // holds the first of them, in which the same thread writes the ring behind them.
 // What bounds it: memory (x is read once, out written once) and, for bf16, the instructions of the activation (five for a value, two of them
-// at a quarter of the rate).  32768 x 4352 bf16, four taps 135 us, 571 MB at 4.2 TB/s, fp32 16384 x 4352 127 us, 4.5 TB/s; 37 x 2304, which is a
+// at a quarter of the rate).  32768 x 4352 bf16, four taps 133 us, 571 MB at 4.3 TB/s, fp32 16384 x 4352 129 us, 4.4 TB/s (124 with the activation of bf16 outputs); 37 x 2304, which is a
 // launch and three trips to memory, 7.3.  With runs of eight tokens, each of which reads its filter, and branches around the loads at a
 // sequence's begin: 193 and 15.
 #pragma once
@@ -26,7 +26,27 @@ struct ConvCall {
     void *ring;
 };
 
-__device__ __forceinline__ float silu(float v) { return v * __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
+// e^-w for w >= 0, to an ulp: its argument in steps of a factor of two keeps what its product is rounded by, which the fast exponential drops
+// (w 2^-24 of the value).  Below 2^-126 it is 0.
+__device__ __forceinline__ float exp_minus(float w)
+{
+    w = fminf(w, 104.0f);                            // (a NaN's as well: what uses it keeps the NaN by another way)
+    const float at = w * -1.44269504f, left = fmaf(w, -1.92596299e-8f, fmaf(w, -1.44269504f, -at)), e = __builtin_amdgcn_exp2f(at);
+    return fmaf(e, left * 0.69314718f, e);
+}
+// v / (1 + e^-v) to a few ulp; what is below 2^-119 may be 0.  For values that stay in fp32.
+__device__ __forceinline__ float silu_f32(float v)
+{
+    const float u = exp_minus(fabsf(v)), d = 1.0f + u, r0 = __builtin_amdgcn_rcpf(d), r = fmaf(fmaf(-d, r0, 1.0f), r0, r0);
+    return (v < 0.0f ? v * u : v) * r;
+}
+// ... as an output of type T: five instructions and (|v| + 4) 2^-24 of the value for what is rounded to bf16 (2^-9 of it).
+template <typename T>
+__device__ __forceinline__ float silu(float v)
+{
+    if constexpr (sizeof(T) == 4) return silu_f32(v);
+    return v * __builtin_amdgcn_rcpf(1.0f + __expf(-v));
+}
 
 template <typename T, int W, int R>
 __global__ void __launch_bounds__(256)
@@ -154,7 +174,7 @@ causal_conv_kernel(const T *__restrict__ x, T *__restrict__ out, ConvCall c)
                 }
                 if (c.silu) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) acc[i] = silu(acc[i]);
+                    for (int i = 0; i < 8; ++i) acc[i] = silu<T>(acc[i]);
                 }
                 if (u + j < until) put(u + j, acc);
             }

@@ -53,13 +53,10 @@ __device__ __forceinline__ float dt_of(const StepSizes &c, float raw, float bias
     const float v = raw + bias;
     if (!c.softplus) return v;
     // log(1 + e^v) = max(v, 0) + log(1 + u), u = e^-|v|, to an ulp or two and in few registers, which the scans' widest forms do not have for
-    // expf and log1pf.  The exponential's argument in steps of a factor of two keeps what its product is rounded by (7 2^-24 of dt = 0.001
-    // otherwise).  The logarithm without the sum 1 + u, which would drop digits of u (2^-24 of a dt of 0.06): twice the area tangent of
+    // expf and log1pf.  The logarithm without the sum 1 + u, which would drop digits of u (2^-24 of a dt of 0.06): twice the area tangent of
     // s = u / (2 + u), at most a third, by its series s (1 + s^2 / 3 + s^4 / 5 ..), whose first term left out is below 2^-29 of the sum.
     // (A dt below 2^-126 is 0.  A NaN stays one.)
-    const float w = fminf(fabsf(v), 104.0f), at = w * -1.44269504f, left = fmaf(w, -1.92596299e-8f, fmaf(w, -1.44269504f, -at));
-    const float e = __builtin_amdgcn_exp2f(at), u = fmaf(e, left * 0.69314718f, e);
-    const float d = 2.0f + u, r = __builtin_amdgcn_rcpf(d), s0 = u * r, s = fmaf(fmaf(-d, s0, u), r, s0), q = s * s;
+    const float u = exp_minus(fabsf(v)), d = 2.0f + u, r = __builtin_amdgcn_rcpf(d), s0 = u * r, s = fmaf(fmaf(-d, s0, u), r, s0), q = s * s;
     float p = 1.0f / 15.0f;
     p = fmaf(p, q, 1.0f / 13.0f);
     p = fmaf(p, q, 1.0f / 11.0f);
@@ -297,7 +294,7 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
                     constexpr int i = decltype(i_)::value;
                     const int e = 64 * i + lane, r = e / PW, p = e % PW;
                     float y = fmaf(skip, sx[r][p], sy[r][p]);
-                    if (c.z) y *= silu(gate[i]);
+                    if (c.z) y *= silu<T>(gate[i]);
                     if (r < nt && p < np) store1(out + (int64_t)(t + r) * c.ld_out + (int64_t)h * P + p0 + p, y);
                 });
             }
@@ -399,7 +396,7 @@ selective_step_kernel(const T *__restrict__ xbc, T *__restrict__ out, StepCall c
             for (int k = TAPS - 1; k >= 0; --k) acc = fmaf(f[k], u[k], acc);
             acc = fmaf(last, q, acc);
             if (ring && there && (e < PW || first)) ring[(int64_t)(pos % c.width) * C + ch] = now;
-            q = c.silu ? silu(acc) : acc;
+            q = c.silu ? silu_f32(acc) : acc;                 // (not rounded to T: it goes into the state)
         }
         (e < PW ? sx + e : (which ? sc : sb) + n)[0] = there ? q : 0.0f;
     }
@@ -428,7 +425,7 @@ selective_step_kernel(const T *__restrict__ xbc, T *__restrict__ out, StepCall c
         if constexpr (NL > 32) y += __shfl_xor(y, 32);
         if (ln == 0 && p < np) {
             y = fmaf(skip, sx[p], y);
-            if (c.z) y *= silu((float)static_cast<const T *>(c.z)[r * c.ld_z + (int64_t)h * P + p0 + p]);
+            if (c.z) y *= silu<T>((float)static_cast<const T *>(c.z)[r * c.ld_z + (int64_t)h * P + p0 + p]);
             store1(o + p, y);
         }
     }

@@ -465,7 +465,7 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
                 for (int tt = 0; tt < 2; ++tt) {
                     const bf16x4_t z = *reinterpret_cast<const bf16x4_t *>(sg[now] + scan_chunk<8>(tt * 16 + l16, p >> 3) + (p & 4));
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) y[tt][i] *= silu((float)z[i]);
+                    for (int i = 0; i < 4; ++i) y[tt][i] *= silu<bf16>((float)z[i]);
                 }
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt) {

@@ -129,3 +129,47 @@ def test_large_exponents_take_no_digits_of_the_weights_behind_them(srm, many):
     bound, of_state = recur_ref.scan_bounds(want, size, mag, T - many, N, BF16, False)
     assert _over(out, want, bound + 2.0 ** -15 * 1.02 * size)[1] == 0
     assert _over(state, after, of_state)[1] == 0
+
+
+@pytest.mark.parametrize("entry", ["conv", "gate of the scan", "gate of the step", "step fp32", "step bf16"])
+def test_silu_of_what_stays_in_fp32_to_a_few_ulp(srm, entry):
+    """v / (1 + e^-v): the exponential loses an ulp (2^-23) and its product with v half of one, the sum half of one, the reciprocal one, the
+    last product half of one: 3.5 2^-23.  A gate's product with y = 1 is exact, the state is one product with dt = 1 and one with B = silu(40),
+    40 within half an ulp."""
+    H = 4096
+    v = torch.cat([torch.linspace(-80, 80, 3 * H), torch.linspace(-8, 8, H)]).float()
+    if entry == "step bf16":
+        v = v.to(BF16).float()
+    got = []
+    for k in range(0, v.numel(), H):
+        part = v[None, k:k + H].cuda()
+        out = torch.empty(1, H, device="cuda")
+        if entry == "conv":
+            srm.causal_conv(part, torch.ones(H, 1, device="cuda"), None, [0, 1], _i32([0, 1]), out)
+            got.append(out.view(-1))
+            continue
+        dtype = BF16 if entry == "step bf16" else F32
+        gate = entry.startswith("gate")
+        dt, a, state = torch.ones(1, H, device="cuda"), torch.zeros(H, device="cuda"), torch.zeros(1, H, 1, 1, device="cuda")
+        if gate:
+            xbc = torch.zeros(1, H + 2, device="cuda")
+            xbc[:, :H] = 1.0
+            kw = dict(skip=torch.ones(H, device="cuda"), z=part, softplus=False, state=state)
+            if entry == "gate of the scan":
+                srm.selective_scan(xbc, dt, a, [0, 1], _i32([0, 1]), out, **kw)
+            else:
+                srm.selective_step(xbc, dt, a, _i32([0]), out=out, **kw)
+            got.append(out.view(-1))
+            continue
+        xbc, bias = torch.zeros(1, H + 2, device="cuda"), torch.zeros(H + 2, device="cuda")
+        xbc[:, :H], bias[H] = part, 40.0
+        ring = torch.zeros(1, 1, H + 2, dtype=dtype, device="cuda")
+        srm.selective_step(xbc.to(dtype), dt, a, _i32([0]), state, out.to(dtype), weight=torch.ones(H + 2, 1, device="cuda"), bias=bias, conv_state=ring,
+                           softplus=False)
+        got.append(state.view(-1) / 40.0)
+    torch.cuda.synchronize()
+    got, v = torch.cat(got).double().cpu(), v.double()
+    want = v * recur_ref.sigmoid(v)
+    wrong = torch.where(want == 0, 0.0, (got - want).abs() / want.abs().clamp_min(1e-300))
+    print(f"{entry}: {float(wrong.max()):.2e} at {float(v[wrong.argmax()]):.4f}", flush=True)
+    assert wrong.max() <= (3.5 + (2.0 if entry.startswith("step") else 0.0)) * 2.0 ** -23
