@@ -180,12 +180,12 @@ selective_scan_join_kernel(float *__restrict__ carry, const float *__restrict__ 
 // are brought to LDS, the next sixteen on their way in registers; then for every token each lane updates its PR x NR elements (multiply,
 // multiply-add) and adds their products with C.  (Eight at a time of the widest rows, for the registers' sake.)
 // What bounds it: three vector instructions for each element of state and token: 8192 tokens in eight prompts of 32 heads of 64 x 128 take
-// 434 us, of which those are 224.  (With the rows of a tile fetched when it is its turn, 1667 tokens of 10 heads of 50 x 37 took 123 us, now 65.)
+// 447 us, of which those are 224.  (With the rows of a tile fetched when it is its turn, 1667 tokens of 10 heads of 50 x 37 took 123 us, now 65.)
 template <typename T, int NL, int NR, int MODE>
 __global__ void __launch_bounds__(64, NL * NR > 128 ? 1 : 2)
 selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c)
 {
-    constexpr int PR = 4, PW = 64 / NL * PR, NP = NL * NR, TT = NP > 128 || PW > 128 ? 8 : 16;
+    constexpr int PR = 4, PW = 64 / NL * PR, NP = NL * NR, TT = NP > 128 || PW > 64 ? 8 : 16;
     __shared__ __align__(16) float sb[TT][NP + 4], sc[TT][NP + 4], sx[TT][PW + 4], sy[TT][PW + 4];
     __shared__ float2 sd[TT];
     __shared__ double se[MODE == SCAN_CARRY ? TT : 1];
@@ -239,6 +239,7 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
         fetch(t0, t1);
         for (int t = t0; t < t1; t += TT) {
             const int nt = min(TT, t1 - t);
+            bool far = false;                        // dt x may be infinite, of which the zeros behind the last of N would make NaN of y
             __syncthreads();
             static_for<0, LB>([&](auto i_) SCAN_INLINE {
                 constexpr int i = decltype(i_)::value;
@@ -250,12 +251,14 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
                 constexpr int i = decltype(i_)::value;
                 const int e = 64 * i + lane;
                 sx[e / PW][e % PW] = e % PW < np ? rx[i] : 0.0f;
+                if (MODE != SCAN_CARRY) far |= !(fabsf(rx[i]) < 1e28f);
             });
             if (lane < TT) {
                 const float dt = dt_of(c.dt, raw, bias);
                 const double ex = decay_exponent(dt, a);
                 sd[lane] = make_float2(exp2_of(ex), dt);
                 if (MODE == SCAN_CARRY) se[lane] = ex;
+                else far |= !(fabsf(dt) < 1e10f);
             }
             if (t + TT < t1) fetch(t + TT, t1);
             float gate[MODE != SCAN_CARRY ? LX : 1]; // z of these tokens
@@ -266,7 +269,8 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
                     gate[i] = (float)static_cast<const T *>(c.z)[(int64_t)min(t + e / PW, t1 - 1) * c.ld_z + (int64_t)h * P + p0 + (p < np ? p : 0)];
                 });
             __syncthreads();
-            auto token = [&](int r) SCAN_INLINE {
+            auto token = [&](int r, auto far_) SCAN_INLINE {
+                constexpr bool far = decltype(far_)::value;
                 const float2 d = sd[r];
                 if (MODE == SCAN_CARRY) sum += se[r];
                 float y[PR];
@@ -277,6 +281,7 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
 #pragma unroll
                     for (int j = 0; j < NR; ++j) {
                         S[i][j] = fmaf(x, sb[r][ln * NR + j], d.x * S[i][j]);
+                        if (far && ln * NR + j >= N) S[i][j] = 0.0f;
                         if (MODE != SCAN_CARRY) y[i] = fmaf(S[i][j], sc[r][ln * NR + j], y[i]);
                     }
                 }
@@ -286,14 +291,20 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
                     if (ln == 0) *reinterpret_cast<f32x4_t *>(&sy[r][lp * PR]) = f32x4_t{y[0], y[1], y[2], y[3]};
                 }
             };
+            if (!__ballot(far)) {
 #pragma unroll 2
-            for (int r = 0; r < nt; ++r) token(r);
+                for (int r = 0; r < nt; ++r) token(r, std::false_type{});
+            } else {
+#pragma unroll 1
+                for (int r = 0; r < nt; ++r) token(r, std::true_type{});
+            }
             if (MODE != SCAN_CARRY) {
                 __syncthreads();
                 static_for<0, LX>([&](auto i_) SCAN_INLINE {
                     constexpr int i = decltype(i_)::value;
                     const int e = 64 * i + lane, r = e / PW, p = e % PW;
-                    float y = fmaf(skip, sx[r][p], sy[r][p]);
+                    float y = sy[r][p];
+                    if (c.skip) y = fmaf(skip, sx[r][p], y);      // (0 times an infinite x would be NaN)
                     if (c.z) y *= silu<T>(gate[i]);
                     if (r < nt && p < np) store1(out + (int64_t)(t + r) * c.ld_out + (int64_t)h * P + p0 + p, y);
                 });
@@ -411,7 +422,7 @@ selective_step_kernel(const T *__restrict__ xbc, T *__restrict__ out, StepCall c
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             v[u][i] = fmaf(xd, b[i], decay * v[u][i]);
-            y = fmaf(v[u][i], cc[i], y);
+            y = ln * 4 + i < N ? fmaf(v[u][i], cc[i], y) : y;         // (behind the last of N an infinite x leaves NaN, infinity times 0)
         }
         if (kept && p < np && ln * 4 < N) {
             float *to = S + (int64_t)p * N + ln * 4;
@@ -424,7 +435,7 @@ selective_step_kernel(const T *__restrict__ xbc, T *__restrict__ out, StepCall c
         if constexpr (NL > 16) y += __shfl_xor(y, 16);
         if constexpr (NL > 32) y += __shfl_xor(y, 32);
         if (ln == 0 && p < np) {
-            y = fmaf(skip, sx[p], y);
+            if (c.skip) y = fmaf(skip, sx[p], y);    // (0 times an infinite x would be NaN)
             if (c.z) y *= silu<T>((float)static_cast<const T *>(c.z)[r * c.ld_z + (int64_t)h * P + p0 + p]);
             store1(o + p, y);
         }

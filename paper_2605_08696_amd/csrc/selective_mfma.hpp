@@ -458,7 +458,7 @@ selective_scan_mfma_kernel(const bf16 *__restrict__ xbc, bf16 *__restrict__ out,
             for (int tt = 0; tt < 2; ++tt) {
                 const bf16x4_t x = *reinterpret_cast<const bf16x4_t *>(xs + scan_chunk<8>(tt * 16 + l16, p >> 3) + (p & 4));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) y[tt][i] = fmaf(skip, (float)x[i], acc[tt][i]);
+                for (int i = 0; i < 4; ++i) y[tt][i] = c.skip ? fmaf(skip, (float)x[i], acc[tt][i]) : acc[tt][i];
             }
             if (c.z)
 #pragma unroll

@@ -1,4 +1,6 @@
 """What the selective scan, the step and the convolution may lose, against the same in 64 bits, token by token (recur_ref)."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -173,3 +175,34 @@ def test_silu_of_what_stays_in_fp32_to_a_few_ulp(srm, entry):
     wrong = torch.where(want == 0, 0.0, (got - want).abs() / want.abs().clamp_min(1e-300))
     print(f"{entry}: {float(wrong.max()):.2e} at {float(v[wrong.argmax()]):.4f}", flush=True)
     assert wrong.max() <= (3.5 + (2.0 if entry.startswith("step") else 0.0)) * 2.0 ** -23
+
+
+@pytest.mark.parametrize("H,P,G,N", [(2, 4, 1, 1), (2, 70, 2, 3), (1, 64, 1, 5), (2, 20, 1, 13), (1, 40, 1, 27), (2, 50, 1, 37), (1, 64, 1, 100), (1, 33, 1, 200)])
+@pytest.mark.parametrize("entry", ["scan", "step fp32", "step bf16"])
+def test_an_infinite_x_is_an_infinity_in_y(srm, entry, H, P, G, N):
+    """B and C above 0, no skip: the state of the channel and y are infinite from the token on, whatever lies behind the last of state_dim's
+    lanes."""
+    gen = torch.Generator().manual_seed(N)
+    dtype, T = BF16 if entry == "step bf16" else F32, 40
+    xbc = torch.randn(T, H * P + 2 * G * N, generator=gen)
+    xbc[:, H * P:] = 0.5 + torch.rand(T, 2 * G * N, generator=gen)
+    xbc[19, 2], xbc[7, H * P - 1] = math.inf, -math.inf
+    xbc = xbc.to(dtype)
+    dt, a = 0.1 + torch.rand(T, H, generator=gen), -torch.rand(H, generator=gen)
+    state = torch.randn(1, H, P, N, generator=gen)
+    want, size, after, mag = recur_ref.scan(xbc, dt, a, [0, T], H, P, G, N, softplus=False, pos=[3], state=state)
+    out, held = torch.empty(T, H * P, dtype=dtype, device="cuda"), state.cuda()
+    if entry == "scan":
+        srm.selective_scan(xbc.cuda(), dt.cuda(), a.cuda(), [0, T], _i32([0, T]), out, groups=G, softplus=False, pos=_i32([3]), state=held)
+    else:
+        rows, sizes = xbc.cuda(), dt.cuda()
+        for t in range(T):
+            srm.selective_step(rows[t:t + 1], sizes[t:t + 1], a.cuda(), _i32([3 + t]), held, out[t:t + 1], groups=G, softplus=False)
+    torch.cuda.synchronize()
+    x = xbc[:, :H * P].double()
+    want = torch.where(torch.isinf(x), x, want)                # (the reference multiplies by the skip that is not there)
+    assert torch.isinf(want).sum() == 21 + 33 and not want.isnan().any()
+    for got, ref, bound in ((out, want, recur_ref.scan_bounds(want, size, mag, T, N, dtype, False)[0]), (held, after, (2 * T + 64) * 2.0 ** -24 * mag)):
+        got, far = got.double().cpu(), torch.isinf(ref)
+        assert torch.equal(got[far], ref[far])
+        assert ((got - ref).abs() <= bound)[~far].all()
