@@ -294,7 +294,13 @@ extern "C" int srm_selective_scan(int32_t dtype, const void *d_xbc, int64_t ld_x
 }
 
 // ------------------------------------------------------------------ single tokens
-// Four wavefronts of a work-group share a head of a request where its state takes them, else each has one of its own.
+// A head's state takes `need` rounds of a wavefront's 64 / NL rows of P.  Many heads: up to eight rounds are one wavefront's, further ones four
+// wavefronts' of a work-group, up to eight each.  Few: four wavefronts with as few rounds each as leave two work-groups a CU, so that the state's loads
+// start on as many CUs as there are.  (One wavefront | four with as many rounds | the best of other forms, us, four taps, bf16: 1024 requests of 32 heads
+// of 16 x 16 30 | 92, 64 x 16 63 | 110 | 63, 128 x 16 112 | 145, 64 x 32 108 | 140, 32 x 64 113 | 143, 16 x 128 127 | 168; from sixteen rounds on
+// 64 x 64 257 | 193, 128 x 32 201 | 194, 32 x 128 233 | 215, 64 x 128 449 | 378.  512 heads, as few rounds as leave two work-groups a CU | as many: 64 x 32
+// 5.9 | 8.0, 32 x 64 5.9 | 8.7, 128 x 16 5.8 | 8.9, 64 x 16 5.1 | 6.4; 2048 heads 11.5 | 9.6, 11.6 | 10.2, 11.9 | 10.9, 9.8 | 7.9; one request of 64 x 128
+// 4.9 | 7.8.  Over 119 sizes and numbers of requests the rule is 0.7 % off the best of eight forms in the mean, 12 % at most; fp32 0.9 and 16.)
 template <typename T, int NL, int U, int WAVES>
 static void launch_step(const void *d_xbc, void *d_out, StepCall c, hipStream_t st)
 {
@@ -302,16 +308,36 @@ static void launch_step(const void *d_xbc, void *d_out, StepCall c, hipStream_t 
     hipLaunchKernelGGL((selective_step_kernel<T, NL, U, WAVES>), grid_of(cdiv(c.rows * c.H * c.parts, 4 / WAVES)), dim3(256), 0, st,
                        static_cast<const T *>(d_xbc), static_cast<T *>(d_out), c);
 }
+template <typename T, int NL, int WAVES>
+static void step_rounds(int rounds, const void *d_xbc, void *d_out, const StepCall &c, hipStream_t st)
+{
+    if (rounds <= 1) return launch_step<T, NL, 1, WAVES>(d_xbc, d_out, c, st);
+    if (rounds <= 2) return launch_step<T, NL, 2, WAVES>(d_xbc, d_out, c, st);
+    if (rounds <= 4) return launch_step<T, NL, 4, WAVES>(d_xbc, d_out, c, st);
+    launch_step<T, NL, 8, WAVES>(d_xbc, d_out, c, st);
+}
+template <typename T, int NL>
+static void step_lanes(const void *d_xbc, void *d_out, const StepCall &c, hipStream_t st)
+{
+    const int64_t heads = c.rows * c.H, need = cdiv(c.P, 64 / NL), two_each = 2 * kChipCus;
+    if (heads <= two_each && need > 1) {
+        int rounds = 1;
+        while (rounds < 8 && heads * cdiv(need, 4 * rounds) > two_each) rounds *= 2;
+        step_rounds<T, NL, 4>(rounds, d_xbc, d_out, c, st);
+    } else if (need <= 8) {
+        step_rounds<T, NL, 1>((int)need, d_xbc, d_out, c, st);
+    } else {
+        step_rounds<T, NL, 4>((int)cdiv(need, 4), d_xbc, d_out, c, st);
+    }
+}
 template <typename T>
 static void step(const void *d_xbc, void *d_out, const StepCall &c, hipStream_t st)
 {
-    // (few work-groups: smaller ones)
-    const bool few = c.rows * c.H * cdiv(c.P, 64) < 2 * kChipCus;
-    if (c.N <= 16) return c.P > 32 ? launch_step<T, 4, 2, 4>(d_xbc, d_out, c, st) : c.P > 16 ? launch_step<T, 4, 2, 1>(d_xbc, d_out, c, st) : launch_step<T, 4, 1, 1>(d_xbc, d_out, c, st);
-    if (c.N <= 32) return c.P > 32 ? launch_step<T, 8, 2, 4>(d_xbc, d_out, c, st) : launch_step<T, 8, 4, 1>(d_xbc, d_out, c, st);
-    if (c.N <= 64) return c.P > 16 ? (few ? launch_step<T, 16, 1, 4>(d_xbc, d_out, c, st) : launch_step<T, 16, 4, 4>(d_xbc, d_out, c, st)) : launch_step<T, 16, 4, 1>(d_xbc, d_out, c, st);
-    if (c.N <= 128) return few ? launch_step<T, 32, 2, 4>(d_xbc, d_out, c, st) : launch_step<T, 32, 8, 4>(d_xbc, d_out, c, st);
-    return few ? launch_step<T, 64, 4, 4>(d_xbc, d_out, c, st) : launch_step<T, 64, 8, 4>(d_xbc, d_out, c, st);
+    if (c.N <= 16) return step_lanes<T, 4>(d_xbc, d_out, c, st);
+    if (c.N <= 32) return step_lanes<T, 8>(d_xbc, d_out, c, st);
+    if (c.N <= 64) return step_lanes<T, 16>(d_xbc, d_out, c, st);
+    if (c.N <= 128) return step_lanes<T, 32>(d_xbc, d_out, c, st);
+    step_lanes<T, 64>(d_xbc, d_out, c, st);
 }
 
 extern "C" int srm_selective_step(int32_t dtype, const void *d_xbc, int64_t ld_xbc, const float *d_weight, const float *d_bias, int32_t activation,

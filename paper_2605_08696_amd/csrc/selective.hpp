@@ -325,7 +325,7 @@ selective_scan_kernel(const T *__restrict__ xbc, T *__restrict__ out, ScanCall c
 // known, the convolution of the head's x and its group's B and C runs while they travel.  B and C are formed anew for every head of a group;
 // the ring's row of the new token, which none of the taps reads, is written for the group's first head alone.
 // What bounds it: the state is read and written once: 300 requests of 32 heads of 64 x 128 take 131 us, 640 MB at 4.9 TB/s, one request 6 (a launch
-// and its trips to memory; with the taps one by one 8.8).  1024 requests of 32 heads of 16 x 16: 32 us, 86 with four wavefronts to a head.
+// and its trips to memory; with the taps one by one 8.8).  1024 requests of 32 heads of 16 x 16: 30 us, 92 with four wavefronts to a head.
 struct StepCall {
     StepSizes dt;
     int64_t rows, slots, ld, ld_z, ld_out;
