@@ -147,15 +147,26 @@ static int check_heads(const char *who, int32_t dtype, int32_t dt_dtype, const H
 struct ScanPlan {
     int parts, seg, segments;                        // segments 0: every sequence as a whole
 };
+// The form of the fp32 kernel for heads of P x N, as form(lanes along N, elements of N in each): as few lanes along N, which share a row of P
+// and its sums, as leave none along P without rows.  (That form | the next with twice the lanes, us, 8192 tokens of 32 heads: in 64 prompts, as many
+// wavefronts as the chip takes, 64 x 16 73 | 73, 128 x 16 129 | 145, 64 x 32 92 | 102, 64 x 64 157 | 171, 64 x 128 315 | 438; in eight, with whole
+// sequences and few wavefronts, more lanes would be faster: 64 x 16 401 | 311, 64 x 32 498 | 351, 64 x 64 463 | 332, 64 x 128 455 | 427.)
+template <int NL, int NR>
+struct ScanForm {
+    static constexpr int lanes = NL, elements = NR, rows = 64 / NL * 4;
+};
+template <typename Form>
+static auto scan_f32_form(int P, int N, Form &&form)
+{
+    if (N <= 8) return P > 64 ? form(ScanForm<1, 8>{}) : form(ScanForm<4, 2>{});
+    if (N <= 16) return P > 64 ? form(ScanForm<2, 8>{}) : P > 32 ? form(ScanForm<4, 4>{}) : form(ScanForm<8, 2>{});
+    if (N <= 32) return P > 32 ? form(ScanForm<4, 8>{}) : form(ScanForm<8, 4>{});
+    if (N <= 64) return P > 16 ? form(ScanForm<8, 8>{}) : form(ScanForm<16, 4>{});
+    return N <= 128 ? form(ScanForm<16, 8>{}) : form(ScanForm<16, 16>{});
+}
 static int scan_rows(int32_t dtype, const HeadSizes &s)
 {
-    if (dtype == SRM_BF16) return kScanRows;
-    // (as the kernels that scan_f32 takes)
-    if (s.N <= 8) return s.P > 64 ? 256 : 64;
-    if (s.N <= 16) return s.P > 64 ? 128 : s.P > 32 ? 64 : 32;
-    if (s.N <= 32) return s.P > 32 ? 64 : 32;
-    if (s.N <= 64) return s.P > 16 ? 32 : 16;
-    return 16;
+    return dtype == SRM_BF16 ? kScanRows : scan_f32_form(s.P, s.N, [](auto form) { return decltype(form)::rows; });
 }
 static ScanPlan scan_plan(int32_t dtype, const HeadSizes &s, int64_t tokens, int32_t longest)
 {
@@ -202,30 +213,11 @@ static int launch_scan(const void *d_xbc, void *d_out, const ScanCall &c, const 
 }
 static int scan_f32(const void *d_xbc, void *d_out, const ScanCall &c, const ScanPlan &p, hipStream_t st)
 {
-#define SCAN_CASE(NL, NR)                                                                                                                     \
-    return launch_scan<float, selective_scan_kernel<float, NL, NR, SCAN_WHOLE>, selective_scan_kernel<float, NL, NR, SCAN_CARRY>,           \
-                       selective_scan_kernel<float, NL, NR, SCAN_SEGMENTS>>(d_xbc, d_out, c, p, 64, st)
-    // (as few lanes along N as leave none along P without rows)
-    if (c.N <= 8) {
-        if (c.P > 64) SCAN_CASE(1, 8);
-        SCAN_CASE(4, 2);
-    }
-    if (c.N <= 16) {
-        if (c.P > 64) SCAN_CASE(2, 8);
-        if (c.P > 32) SCAN_CASE(4, 4);
-        SCAN_CASE(8, 2);
-    }
-    if (c.N <= 32) {
-        if (c.P > 32) SCAN_CASE(4, 8);
-        SCAN_CASE(8, 4);
-    }
-    if (c.N <= 64) {
-        if (c.P > 16) SCAN_CASE(8, 8);
-        SCAN_CASE(16, 4);
-    }
-    if (c.N <= 128) SCAN_CASE(16, 8);
-    SCAN_CASE(16, 16);
-#undef SCAN_CASE
+    return scan_f32_form(c.P, c.N, [&](auto form) {
+        constexpr int NL = decltype(form)::lanes, NR = decltype(form)::elements;
+        return launch_scan<float, selective_scan_kernel<float, NL, NR, SCAN_WHOLE>, selective_scan_kernel<float, NL, NR, SCAN_CARRY>,
+                           selective_scan_kernel<float, NL, NR, SCAN_SEGMENTS>>(d_xbc, d_out, c, p, 64, st);
+    });
 }
 template <bool W>
 static int scan_bf16(const void *d_xbc, void *d_out, const ScanCall &c, const ScanPlan &p, hipStream_t st)

@@ -1,7 +1,7 @@
 // The selective recurrence: for each head a matrix of state S [P][N] whose decay and input depend on the token,
 //   dt = softplus(dt_raw + dt_bias[h])     S <- exp(dt A[h]) S + dt x[h] B[g]^T     y = S C[g] + D[h] x[h]     out = y silu(z)
-// with x [H][P] | B [G][N] | C [G][N] in a row and g = h / (H / G).  Here: what its kernels share, the kernel for operands in fp32 (and a
-// simple form for bf16), and the kernel of single tokens.
+// with x [H][P] | B [G][N] | C [G][N] in a row and g = h / (H / G).  Here: what its kernels share, the kernel for operands in fp32,
+// and the kernel of single tokens.
 //
 // Work over time.  A work-group takes one head (a part of its P rows) of one sequence from its first token to its last, the state in
 // registers.  Where there are too few of those, the packed tokens are cut into segments of equal length, whatever sequences they hold:
