@@ -210,7 +210,7 @@ def workspace_bytes_config(cfg, rows: int) -> int:
 
 def prefill_ragged_plan(cfg, offsets, workspace_bytes: int) -> dict:
     """srm_prefill_ragged_plan (host only): how a ragged prefill of these prompts would be cut and scanned."""
-    off = np.ascontiguousarray(offsets, dtype=np.int32)
+    off = _int32(offsets)
     c = c_config(cfg)
     plan = srm_prefill_plan()
     _check(lib().srm_prefill_ragged_plan(C.byref(c), off.ctypes.data_as(C.POINTER(C.c_int32)), len(off) - 1,
@@ -394,7 +394,7 @@ class Model:
         """Packed prompts of different lengths; offsets: host int32 sequence of N + 1 boundaries."""
         import numpy as np
         torch = _torch()
-        h_off = np.ascontiguousarray(offsets, dtype=np.int32)
+        h_off = _int32(offsets)
         N = h_off.size - 1
         if N < 1:
             raise ValueError("offsets: need at least two boundaries")
@@ -714,6 +714,16 @@ def _vectors(n: int, dtype, tensors, names):
 _INT_AT = C.c_int32.from_address
 
 
+def _int32(offsets):
+    """A contiguous int32 array of the offsets, whatever holds them; values that are none are refused, not wrapped or cut."""
+    given = np.asarray(offsets)
+    with np.errstate(invalid="ignore"):
+        whole = np.ascontiguousarray(given, dtype=np.int32)
+    if given.dtype != np.int32 and not np.array_equal(whole, given):
+        raise ValueError("offsets: must be 32-bit whole numbers")
+    return whole
+
+
 def _offsets(offsets, d_offsets, rows: int):
     """(address of the host's offsets, the number of sequences, what keeps the address alive)."""
     torch = _torch()
@@ -722,7 +732,7 @@ def _offsets(offsets, d_offsets, rows: int):
     else:
         if isinstance(offsets, torch.Tensor) and offsets.is_cuda:
             raise ValueError("offsets: must be host memory (d_offsets: the same values on the device)")
-        keep = np.ascontiguousarray(offsets, dtype=np.int32)
+        keep = _int32(offsets)
         at, n = keep.ctypes.data, keep.size - 1
     if n < 1:
         raise ValueError("offsets: need at least two boundaries")
@@ -795,7 +805,7 @@ def _heads(xbc, dt, a, out, groups, dt_bias, skip, z):
 
 def selective_scan_workspace_bytes(dtype: int, offsets, heads: int, head_dim: int, state_dim: int) -> int:
     """srm_selective_scan_workspace_bytes (host only); dtype SRM_FP32 | SRM_BF16, offsets host int32."""
-    h = np.ascontiguousarray(offsets, dtype=np.int32)
+    h = _int32(offsets)
     return lib().srm_selective_scan_workspace_bytes(dtype, h.ctypes.data, h.size - 1, heads, head_dim, state_dim)
 
 
