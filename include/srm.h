@@ -663,7 +663,8 @@ int srm_sample_rows(int32_t dtype, const void *d_logits, int64_t ld, int64_t row
  * tokens: operators that need no model.  Where the mixer of Eq. 2 / Eq. 3 keeps one value per channel with a decay of each head, this one
  * keeps a matrix for each head, whose decay and input depend on the token.
  *
- * Packed prompts: sequence n is rows offsets[n] .. offsets[n + 1] - 1 of every operand, which may be none.  The offsets (N + 1 values, int32,
+ * Packed prompts: sequence n is rows offsets[n] .. offsets[n + 1] - 1 of every operand, which may be none (a call without any rows does nothing;
+ * its arrays of rows may be NULL).  The offsets (N + 1 values, int32,
  * not falling, the first at least 0) are passed twice, as in srm_prefill_ragged: h_offsets in host memory, which the call validates and plans
  * by, and d_offsets, the same values in device memory (clamped to those of the host, so that a mismatch cannot cause an access outside the
  * operands; results are then unspecified).  Rows in front of the first sequence and behind the last are left as they are.

@@ -86,7 +86,7 @@ extern "C" int srm_causal_conv(int32_t dtype, const void *d_x, int64_t ldx, cons
                                const int32_t *d_slot, int64_t slots, void *d_state, void *d_out, int64_t ld_out, void *hip_stream)
 {
     const char *who = "srm_causal_conv";
-    if (!d_x || !d_weight || !d_out) return fail(SRM_EINVAL, "%s: null argument", who);
+    if (!d_weight) return fail(SRM_EINVAL, "%s: null argument", who);
     if (!known(dtype)) return fail(SRM_EINVAL, "%s: unknown dtype %d", who, dtype);
     if (channels <= 0 || channels > (1 << 24) || width <= 0 || width > kConvTaps) return fail(SRM_EINVAL, "%s: sizes out of range", who);
     if (activation != 0 && activation != 1) return fail(SRM_EINVAL, "%s: unknown activation %d", who, activation);
@@ -95,9 +95,10 @@ extern "C" int srm_causal_conv(int32_t dtype, const void *d_x, int64_t ldx, cons
     int32_t longest;
     SRM_TRY(check_packed(who, h_offsets, d_offsets, N, d_pos, d_slot, slots, d_state, c.seqs, longest));
     const unsigned size = size_of(dtype);
+    const int64_t tokens = c.seqs.hi - c.seqs.lo;
+    if (tokens > 0 && (!d_x || !d_out)) return fail(SRM_EINVAL, "%s: null argument", who);      // (arrays of no rows may lie nowhere)
     if (misaligned(d_x, size) || misaligned(d_out, size) || misaligned(d_state, size) || misaligned(d_weight, 4) || misaligned(d_bias, 4))
         return fail(SRM_EINVAL, "%s: %s", who, kNotWhole);
-    const int64_t tokens = c.seqs.hi - c.seqs.lo;
     if (tokens * cdiv(channels, 512) >= kMaxBlocks) return fail(SRM_EINVAL, "%s: sizes out of range", who);
     if (tokens == 0) return SRM_OK;
     c.ldx = ldx;
@@ -124,11 +125,11 @@ static bool fits(const HeadSizes &s)
     return s.H > 0 && s.H <= 65536 && s.P > 0 && s.P <= 4096 && s.N > 0 && s.N <= 256 && s.G > 0 && s.H % s.G == 0 &&
            (int64_t)s.H * s.P + 2ll * s.G * s.N < (1 << 30);
 }
-static int check_heads(const char *who, int32_t dtype, int32_t dt_dtype, const HeadSizes &s, const void *xbc, int64_t ld, const void *dt, int64_t ld_dt,
+static int check_heads(const char *who, int32_t dtype, int32_t dt_dtype, const HeadSizes &s, int64_t rows, const void *xbc, int64_t ld, const void *dt, int64_t ld_dt,
                        const float *a, const float *dt_bias, const float *skip, const void *z, int64_t ld_z, const void *out, int64_t ld_out,
                        const float *state)
 {
-    if (!xbc || !dt || !a || !out) return fail(SRM_EINVAL, "%s: null argument", who);
+    if (!a || (rows > 0 && (!xbc || !dt || !out))) return fail(SRM_EINVAL, "%s: null argument", who);        // (arrays of no rows may lie nowhere)
     if (!known(dtype) || !known(dt_dtype)) return fail(SRM_EINVAL, "%s: unknown dtype %d, %d", who, dtype, dt_dtype);
     if (!fits(s)) return fail(SRM_EINVAL, "%s: sizes out of range", who);
     const int64_t inner = (int64_t)s.H * s.P;
@@ -240,12 +241,12 @@ extern "C" int srm_selective_scan(int32_t dtype, const void *d_xbc, int64_t ld_x
 {
     const char *who = "srm_selective_scan";
     const HeadSizes s{heads, head_dim, groups, state_dim};
-    SRM_TRY(check_heads(who, dtype, dt_dtype, s, d_xbc, ld_xbc, d_dt, ld_dt, d_a, d_dt_bias, d_skip, d_z, ld_z, d_out, ld_out, d_state));
     ScanCall c{};
     int32_t longest;
     SRM_TRY(check_packed(who, h_offsets, d_offsets, N, d_pos, d_slot, slots, d_state, c.seqs, longest));
-    if (misaligned(d_workspace, 4)) return fail(SRM_EINVAL, "%s: %s", who, kNotWhole);
     const int64_t tokens = c.seqs.hi - c.seqs.lo;
+    SRM_TRY(check_heads(who, dtype, dt_dtype, s, tokens, d_xbc, ld_xbc, d_dt, ld_dt, d_a, d_dt_bias, d_skip, d_z, ld_z, d_out, ld_out, d_state));
+    if (misaligned(d_workspace, 4)) return fail(SRM_EINVAL, "%s: %s", who, kNotWhole);
     ScanPlan p = scan_plan(dtype, s, tokens, longest);
     const int64_t room = d_workspace ? (int64_t)(workspace_bytes / segment_bytes(s)) : 0;
     if (p.segments > room) {                         // fewer and longer segments, or none
@@ -340,7 +341,7 @@ extern "C" int srm_selective_step(int32_t dtype, const void *d_xbc, int64_t ld_x
 {
     const char *who = "srm_selective_step";
     const HeadSizes s{heads, head_dim, groups, state_dim};
-    SRM_TRY(check_heads(who, dtype, dt_dtype, s, d_xbc, ld_xbc, d_dt, ld_dt, d_a, d_dt_bias, d_skip, d_z, ld_z, d_out, ld_out, d_state));
+    SRM_TRY(check_heads(who, dtype, dt_dtype, s, 1, d_xbc, ld_xbc, d_dt, ld_dt, d_a, d_dt_bias, d_skip, d_z, ld_z, d_out, ld_out, d_state));
     if (!d_state || !d_pos) return fail(SRM_EINVAL, "%s: null argument", who);
     if (rows <= 0 || rows >= kMaxRows || slots <= 0) return fail(SRM_EINVAL, "%s: sizes out of range", who);
     if (d_weight) {

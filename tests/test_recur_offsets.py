@@ -43,3 +43,20 @@ def test_other_holders_of_whole_values_are_taken(srm, offsets):
 def test_plans_of_ragged_prompts_refuse_them_too(srm):
     with pytest.raises(ValueError, match="whole"):
         srm.prefill_ragged_plan(None, np.array([0, 2 ** 32 + 5]), 0)
+
+
+def test_no_rows_at_all_are_no_work(srm, monkeypatch):
+    """Arrays of no rows lie nowhere: not refused, nothing launched; what is wrong with the call otherwise still is."""
+    from paper_2605_08696_amd import binding
+    codes = []
+    monkeypatch.setattr(binding, "_launch", lambda fn, args, first, others, stream: codes.append(fn(*args, None)))
+    bf, off, d_off = torch.bfloat16, np.zeros(3, dtype=np.int32), torch.zeros(3, dtype=torch.int32)
+    x, w = torch.zeros(0, 24, dtype=bf), torch.zeros(24, 4)
+    assert x.data_ptr() == 0
+    srm.causal_conv(x, w, None, off, d_off, torch.zeros(0, 24, dtype=bf))
+    srm.selective_scan(x, torch.zeros(0, 2), torch.zeros(2), off, d_off, torch.zeros(0, 8, dtype=bf), state=torch.zeros(2, 2, 4, 8))
+    assert codes == [0, 0]
+    with pytest.raises(ValueError, match="rows"):
+        srm.causal_conv(x, w, None, [0, 0, 1], d_off, torch.zeros(0, 24, dtype=bf))
+    with pytest.raises(ValueError, match="weight"):
+        srm.causal_conv(x, w[:-1], None, off, d_off, torch.zeros(0, 24, dtype=bf))
