@@ -7,10 +7,11 @@
 // between them, while the R in front of them are worked on, and the filter's W - 1 rows in front of a row stay in registers.  A sequence
 // that begins inside a run is a piece of its own; its first W - 1 tokens, whose taps reach into the slot's ring, all belong to the run that
 // holds the first of them, in which the same thread writes the ring behind them.
-// What bounds it: memory (x is read once, out written once) and, for bf16, the instructions of the activation (five for a value, two of them
-// at a quarter of the rate).  32768 x 4352 bf16, four taps 133 us, 571 MB at 4.3 TB/s, fp32 16384 x 4352 129 us, 4.4 TB/s (124 with the activation of bf16 outputs); 37 x 2304, which is a
-// launch and three trips to memory, 7.3.  With runs of eight tokens, each of which reads its filter, and branches around the loads at a
-// sequence's begin: 193 and 15.
+// What bounds it: memory, x read once, out written once, and the way it is walked, a kilobyte of each of eight rows at a time: of 32768 x 4352
+// bf16 one tap without an activation takes 119 us (torch's copy 106, a copy in one stream of addresses 92), three more taps 9, the activation
+// 4; vector instructions issue for a fifth of the time.  With four taps 133 us, 571 MB at 4.3 TB/s, fp32 16384 x 4352 129 us, 4.4 TB/s (124
+// with the activation of bf16 outputs); 37 x 2304, which is a launch and three trips to memory, 6.3.  With runs of eight tokens, each of
+// which reads its filter, and branches around the loads at a sequence's begin: 193 and 15.
 #pragma once
 #include "fp8.hpp"
 #include "packed.hpp"

@@ -143,8 +143,8 @@ static int check_heads(const char *who, int32_t dtype, int32_t dt_dtype, const H
 
 // How a scan is cut over time.  A work-group holds `rows` rows of P; `chip` of them run at the chip's full rate together.  Segments cost a
 // pass of their own that forms the states at their ends (about half of the work again), so that whole sequences are taken up to three times a
-// segment's length (us, whole | segments: 8192 tokens in eight prompts of 32 heads 60 | 82; one prompt of 16384, 32 work-groups, with 256 | 384 |
-// 512 | 768 | 1024 work-groups of segments 167 | 150 | 126 | 115 | 133).
+// segment's length (us, whole | segments: 8192 tokens in eight prompts of 32 heads 59 | 80; one prompt of 16384, 32 work-groups, 799 as a whole, with
+// 256 | 384 | 512 | 768 | 1024 work-groups of segments 173 | 154 | 126 | 128 | 138).
 struct ScanPlan {
     int parts, seg, segments;                        // segments 0: every sequence as a whole
 };

@@ -8,7 +8,7 @@
 // a first pass leaves, for each segment that a sequence runs on from, the state at its end that the segment itself brings (`carry`) and
 // the factor by which it decays what came before (`decay`); a second one makes of these the states at the segments' ends; the third starts
 // each segment from the one in front of it and writes the outputs.  (Joined by the third pass itself, every segment adding up all carries in
-// front of it, 16384 tokens of 32 heads took 146 us, so 115.)
+// front of it, 16384 tokens of 32 heads took 146 us where this took 115.)
 #pragma once
 #include "conv.hpp"
 #include "tile.hpp"

@@ -111,14 +111,14 @@ __device__ __forceinline__ void scan_barrier_lds() { asm volatile("s_waitcnt lgk
 // way of registers where rows in whole chunks lie at any element, or one element at a time.  Two barriers a block: its rows are there; M is
 // there.  y takes x's place in LDS, and leaves from there in whole rows behind the next barrier.
 //
-// What bounds it: 32768 tokens in eight prompts of 64 heads of 64 x 128 take 348 us, 940 MB at 2.7 TB/s.  Two work-groups on a CU; their
-// wavefronts issue vector instructions for more than half of the time, some 320 a block beside 46 products of 16 clocks, and wait for each other,
-// for LDS and for products for the rest.  With exponents in one part of fp32 337 (sizes of four blocks together); with M and S's
-// copy rounded to one bf16 number each besides, whose errors showed in y, 304; of these, without
-// the two smaller parts of x 274, without M 284, without the gate's exponentials 289; without any of these
-// and the other products 242, which is what the trips through memory take.  Not kept, with one number each: three buffers (two work-groups on a CU
-// instead of three): 331, 8192 tokens in eight prompts of 32 heads 62 | 60 with two, states of 256 99 | 91; loads and stores that bypass the caches
-// +-2%.  Remainders of S from pairs rounded by one conversion 344, each value rounded once more 364.
+// What bounds it: 32768 tokens in eight prompts of 64 heads of 64 x 128 take 357 us, 940 MB at 2.6 TB/s.  Two work-groups on a CU; their
+// wavefronts issue vector instructions for two thirds of the time, 359 a block beside 46 products of 16 clocks, and wait for each other, for LDS
+// and for products for a third.  What the precision of y costs, measured in turn: exponents in one part of fp32 (and the sizes of four blocks
+// together) 346, M and S's copy rounded to one bf16 number each besides 306.  Remainders of S from pairs rounded by one conversion +0, each value
+// rounded once more for its remainder +6 %; four blocks' sizes, two work-groups on a CU instead of three, 16384 tokens in one prompt 144 | 128.
+// Of the 306: without the two smaller parts of x 274, without M 284, without the gate's exponentials 289; without any of these and the other
+// products 242, which is what the trips through memory take.  Not kept there: three buffers (two work-groups on a CU): 331, 8192 tokens in eight
+// prompts of 32 heads 62 | 60 with two, states of 256 99 | 91; loads and stores that bypass the caches +-2%.
 // On the way: blocks of 64 tokens with rows through registers 394 (228 registers), each block's decays formed by one wavefront in front of a
 // barrier 394, by all for four blocks 354, y stored and z read by each wavefront in 32 bytes of a row 332.
 template <int NP, int MODE, bool WHOLE>
