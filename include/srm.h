@@ -690,8 +690,9 @@ int srm_sample_rows(int32_t dtype, const void *d_logits, int64_t ld, int64_t row
  * [rows][heads] of type dt_dtype; d_a, d_dt_bias, d_skip [heads] fp32 (the last two may be NULL).  a <= 0 is meant: with a > 0 the formula
  * holds as long as nothing overflows.  d_state [slots][heads][head_dim][state_dim] fp32 (may be NULL) is read (from position 1 on) and
  * updated.  state_dim up to 256.  The state, decays and all sums are fp32.  With bf16 operands, what is multiplied on the matrix
- * cores is cut into two bf16 numbers for y (2^-15 of a factor is lost at most) and into three for the state (nothing is).  An x that is not
- * finite stays in its channel and behind its token; of bf16 operands an infinity may become NaN there, in the state as in y.
+ * cores is cut into two bf16 numbers for y (2^-15 of a factor is lost at most) and into three for the state (nothing is).  What is not
+ * finite changes nothing in front of its token, in x nothing outside its channel, in B or C nothing outside its group, and in C nothing behind
+ * its token; where it counts, an infinity of bf16 operands may become NaN, in the state as in y.
  * d_workspace: a call with few sequences and heads is cut into segments of time, whose states lie there;
  * srm_selective_scan_workspace_bytes(the same arguments) is what the best cut takes (0: none), and with less, or NULL, there are fewer
  * segments or none.  Its content means nothing between calls; calls that may overlap in time need one each.  Results may differ in the

@@ -206,3 +206,40 @@ def test_an_infinite_x_is_an_infinity_in_y(srm, entry, H, P, G, N):
         got, far = got.double().cpu(), torch.isinf(ref)
         assert torch.equal(got[far], ref[far])
         assert ((got - ref).abs() <= bound)[~far].all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,N", [(50, 64), (400, 64), (400, 37), (90, 128)])
+def test_what_is_not_finite_in_b_or_c_stays_in_its_group_and_behind_its_token(srm, dtype, T, N):
+    gen = torch.Generator().manual_seed(T + N)
+    H, P, G = 4, 40, 2
+    off, rows = [0, T, T + 40], T + 40
+    xbc = torch.randn(rows, H * P + 2 * G * N, generator=gen).to(dtype).cuda()
+    dt, a, z = torch.rand(rows, H, generator=gen).cuda(), -torch.rand(H, generator=gen).cuda(), torch.randn(rows, H * P, generator=gen).to(dtype).cuda()
+    b_at, c_at = H * P, H * P + G * N
+
+    def run(rows_of):
+        out, state = torch.empty(rows, H * P, dtype=dtype, device="cuda"), torch.zeros(2, H, P, N, device="cuda")
+        srm.selective_scan(rows_of, dt, a, off, _i32(off), out, groups=G, z=z, softplus=False, state=state)
+        torch.cuda.synchronize()
+        return out, state
+
+    clean, held = run(xbc)
+    for value in (math.inf, math.nan):
+        bad = xbc.clone()
+        bad[37, c_at + 5] = value                              # C of group 0: this token alone
+        out, state = run(bad)
+        touched = torch.zeros(rows, H * P, dtype=torch.bool, device="cuda")
+        touched[37, :2 * P] = True
+        assert torch.equal(out[~touched], clean[~touched]) and torch.equal(state, held)
+        assert not torch.isfinite(out[touched]).any()
+        bad = xbc.clone()
+        bad[21, b_at + N + 3] = value                          # B of group 1: from this token on
+        out, state = run(bad)
+        touched[37] = False
+        touched[21:T, 2 * P:] = True
+        assert torch.equal(out[~touched], clean[~touched])
+        assert not torch.isfinite(out[touched]).any()
+        far = torch.zeros_like(state, dtype=torch.bool)
+        far[0, 2:, :, 3] = True
+        assert torch.equal(state[~far], held[~far]) and not torch.isfinite(state[far]).any()
